@@ -211,7 +211,6 @@ def _prepare_adamw(case, seed):
         if case["states"] == 8:
             more.update(exp_avg_scale=scales(s["m_scale"]), exp_avg_sq_scale=scales(s["r_scale"]))
         s["table"] = P.adamw_table(views(s["w"]), views(s["grad"]), views(s["m"]), views(s["v" if case["states"] == 32 else "r"]), **more)
-        s["workspace"] = P.adamw_workspace(s["table"])
     return s
 
 
@@ -230,7 +229,7 @@ def _own(s):
         P.condensa_adapter_project_backward(s["dy"], s["x"], s["w"], s["table"], s["ids"], s["z"], dx=s["dx"], workspace=s["workspace"])
         return {"dx": s["dx"], "da": [a for a, _ in s["grads"]], "db": [b for _, b in s["grads"]]}
     P.condensa_lc_adamw_step(s["table"], LR, s["step"], betas=(BETA1, BETA2), eps=EPS, weight_decay=DECAY, mu=MU,
-                             seed=s["seed"] if s["stochastic"] else None, workspace=s["workspace"])
+                             seed=s["seed"] if s["stochastic"] else None)
     return _states(s)
 
 
