@@ -413,6 +413,77 @@ condensa_status condensa_thin(const float* w_dev, const int64_t* shape, int ndim
                               const int32_t* keep_in_dev, int64_t n_keep_in, int64_t keep_in_offset,
                               float* out_dev, void* stream);
 
+/*
+ * ---- Learning beside compressed weights: AdamW over lists of tensors, low-rank adapters ---------------------
+ *
+ * Element types of the calls below; 16-bit values are the bit patterns that condensa_quantize (F16) and
+ * condensa_quantize_bf16 (BF16) write.
+ */
+enum { CONDENSA_TYPE_F32 = 0, CONDENSA_TYPE_F16 = 1, CONDENSA_TYPE_BF16 = 2 };
+
+/*
+ * One AdamW update of the learning (L) step for a list of tensors in one launch, with the L-C penalty of
+ * condensa_lc_sgd_step folded in where a tensor has theta and lambda.  Per element, binary32, one rounding per operation, no
+ * fused multiply-add (the constants are evaluated in binary64 and rounded once):
+ *      g = grad * grad_scale;   g = (g + mu * (w - theta)) - lambda;
+ *      m = beta1 * m + (1 - beta1) * g;   v = beta2 * v + (1 - beta2) * (g * g);
+ *      w = (1 - lr * weight_decay) * w - [lr / (1 - beta1^step)] * (m / (sqrt(v) * [1 / sqrt(1 - beta2^step)] + eps)).
+ * States in 32 bits: exp_avg = m and exp_avg_sq = v.  States in 8 bits: exp_avg holds E4M3 codes (condensa_quantize_fp8) of
+ * m / scale and exp_avg_sq those of sqrt(v) / scale, one scale for every CONDENSA_STATE_BLOCK consecutive elements of a tensor:
+ * the largest finite magnitude of the new m (sqrt(v)) in the block / 448, or 0 where that magnitude is below 2^-100.  The step
+ * computes with the values before they are rounded.  Codes are rounded to the nearest (ties to even) or, with
+ * CONDENSA_ROUND_STOCHASTIC, up with the probability that keeps the mean: rounding to nearest leaves a state where it is when one
+ * step moves it by less than half the distance of two codes, which for beta2 near 1 is always.  The random bits are a hash of
+ * `seed` (another one for every step) and of the element's place in the list, so equal seeds give equal results.  A positive
+ * sqrt(v) never becomes 0, infinities saturate, a NaN stays the element's own.
+ */
+#define CONDENSA_STATE_BLOCK 256
+enum { CONDENSA_ROUND_NEAREST = 0, CONDENSA_ROUND_STOCHASTIC = 1 };
+
+typedef struct {
+    float*       w;                 /* n weights, updated in place                                            */
+    const void*  grad;              /* n gradients of the list's grad_type                                    */
+    void*        exp_avg;           /* n floats, or n E4M3 codes                                              */
+    void*        exp_avg_sq;        /* n floats, or n E4M3 codes of the square root                           */
+    float*       exp_avg_scale;     /* 8 bits: ceil(n / CONDENSA_STATE_BLOCK) scales; 32 bits: NULL           */
+    float*       exp_avg_sq_scale;
+    const float* theta;             /* both NULL: no penalty on this tensor                                   */
+    const float* lambda;
+    uint16_t*    codes;             /* NULL, or n codes of the updated weights in the list's code_type        */
+    uint64_t     n;                 /* 0 is valid, with NULL pointers                                         */
+} condensa_adamw_tensor;            /* device pointers, aligned for their types                               */
+
+/* A list that is ready for steps: made by condensa_adamw_list_init, read by the calls, kept by the caller. */
+typedef struct {
+    const void* table_dev;
+    const void* map_dev;
+    uint64_t    n_elems, n_chunks;
+    int32_t     n_tensors, state_bits, grad_type, code_type;
+} condensa_adamw_list;
+
+typedef struct {
+    double       lr, beta1, beta2, eps, weight_decay;   /* finite; beta in [0, 1); eps >= 0                   */
+    float        mu;                                    /* of the penalty: finite and >= 0                    */
+    int32_t      rounding;                              /* of 8-bit states                                    */
+    int64_t      step;                                  /* 1 for the first update                             */
+    uint64_t     seed;
+    const float* grad_scale_dev;                        /* NULL, or a device float that gradients are multiplied by */
+    int64_t      reserved;                              /* must be 0                                          */
+} condensa_adamw_settings;
+
+/*
+ * The same buffers take part in step after step, so their descriptors are laid out on the device once: `list_dev` is
+ * condensa_adamw_list_bytes(...) bytes of device memory, 256-byte aligned, that has to stay as it is while the list is in use
+ * (as have the buffers that it names).  `tensors` is host memory and may be freed after the call.  No written buffer may
+ * overlap another buffer of the list.  A step is one kernel without workspace; captured into a graph, the settings of that
+ * call are replayed.  Errors as for the other entry points: a step or rate that is no valid number is CONDENSA_ERR_DENSITY.
+ */
+size_t condensa_adamw_list_bytes(const condensa_adamw_tensor* tensors, int n_tensors);      /* 0: invalid arguments */
+condensa_status condensa_adamw_list_init(const condensa_adamw_tensor* tensors, int n_tensors, int state_bits, int grad_type,
+                                         int code_type, void* list_dev, size_t list_bytes, void* stream,
+                                         condensa_adamw_list* list);
+condensa_status condensa_lc_adamw_step(const condensa_adamw_list* list, const condensa_adamw_settings* settings, void* stream);
+
 /* ---- process-wide DEFAULTS of the knobs above: what a NULL config stands for ---------------------- */
 enum {
     CONDENSA_OPT_SELECT_PATH   = 0, /* condensa_config.select_path   */

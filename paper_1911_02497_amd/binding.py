@@ -43,7 +43,27 @@ class Tensor(ctypes.Structure):
                 ("reserved", ctypes.c_int32)]
 
 
+class AdamwTensor(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_void_p) for f in ("w", "grad", "exp_avg", "exp_avg_sq", "exp_avg_scale", "exp_avg_sq_scale", "theta",
+                                               "lambda_", "codes")] + [("n", ctypes.c_uint64)]
+
+
+class AdamwList(ctypes.Structure):
+    _fields_ = [("table_dev", ctypes.c_void_p), ("map_dev", ctypes.c_void_p), ("n_elems", ctypes.c_uint64), ("n_chunks", ctypes.c_uint64),
+                ("n_tensors", ctypes.c_int32), ("state_bits", ctypes.c_int32), ("grad_type", ctypes.c_int32), ("code_type", ctypes.c_int32)]
+
+
+class AdamwSettings(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("weight_decay", ctypes.c_double), ("mu", ctypes.c_float), ("rounding", ctypes.c_int32), ("step", ctypes.c_int64),
+                ("seed", ctypes.c_uint64), ("grad_scale_dev", ctypes.c_void_p), ("reserved", ctypes.c_int64)]
+
+
 _PROTOTYPES = {
+    "condensa_adamw_list_bytes": (ctypes.c_size_t, [ctypes.POINTER(AdamwTensor), ctypes.c_int]),
+    "condensa_adamw_list_init": (ctypes.c_int32, [ctypes.POINTER(AdamwTensor), ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int,
+                                                  ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p, ctypes.POINTER(AdamwList)]),
+    "condensa_lc_adamw_step": (ctypes.c_int32, [ctypes.POINTER(AdamwList), ctypes.POINTER(AdamwSettings), ctypes.c_void_p]),
     "condensa_workspace_bytes": (ctypes.c_size_t, [ctypes.c_int, ctypes.c_uint64, ctypes.c_uint64, ctypes.c_int,
                                                    ctypes.c_int, ctypes.c_int, ctypes.POINTER(Config)]),
     "condensa_config_init": (ctypes.c_int32, [ctypes.POINTER(Config)]),
@@ -583,6 +603,99 @@ def condensa_lc_sgd_step(tensors, grad_loss, theta, lambdas, momentum_buf, mu, l
     _check(lib.condensa_lc_sgd_step(tab, nt, p1, p2, p3, p4, float(mu), float(lr), float(momentum), ws.data_ptr(),
                                     ws.numel(), _stream(stream), None))
     return ws
+
+
+STATE_BLOCK = 256                   # elements of a tensor that share the scale of an 8-bit state
+TYPE_F32, TYPE_F16, TYPE_BF16 = 0, 1, 2
+ROUND_NEAREST, ROUND_STOCHASTIC = 0, 1
+
+
+def _type_of(dtype):
+    import torch
+    return {torch.float32: TYPE_F32, torch.float16: TYPE_F16, torch.bfloat16: TYPE_BF16}.get(dtype)
+
+
+def _stream_of(stream):
+    import torch
+    return torch.cuda.current_stream() if stream is None else stream
+
+
+def _wait_unless_captured(stream):
+    """A list on the device is read by calls on any stream later on: it is whole before the program goes on."""
+    import torch
+    if not torch.cuda.is_current_stream_capturing():
+        stream.synchronize()
+
+
+class AdamwTable:
+    """Weights, gradients and states of condensa_lc_adamw_step, laid out on the device once for many steps.  The tensors must
+    keep their storage.  See ``adamw_table``."""
+
+    def __init__(self, weights, grads, exp_avg, exp_avg_sq, exp_avg_scale=None, exp_avg_sq_scale=None, theta=None, lambdas=None,
+                 codes=None, stream=None):
+        import torch
+        n = len(weights)
+        lists = {"grad": grads, "exp_avg": exp_avg, "exp_avg_sq": exp_avg_sq, "exp_avg_scale": exp_avg_scale,
+                 "exp_avg_sq_scale": exp_avg_sq_scale, "theta": theta, "lambda_": lambdas, "codes": codes}
+        lists = {k: list(v) for k, v in lists.items() if v is not None}
+        if any(len(v) != n for v in lists.values()):
+            raise ValueError("every list holds one tensor for each weight")
+        bits = 8 if n and exp_avg[0].dtype == torch.uint8 else 32
+        state = torch.uint8 if bits == 8 else torch.float32
+        if bits == 8 and (exp_avg_scale is None or exp_avg_sq_scale is None):
+            raise ValueError("8-bit states come with their scales")
+        first = lambda k: next((t for t in lists.get(k, ()) if t is not None), None)  # noqa: E731
+        g0, c0 = first("grad"), first("codes")
+        grad_type = TYPE_F32 if g0 is None else _type_of(g0.dtype)
+        code_type = TYPE_F16 if c0 is None else _type_of(c0.dtype)
+        if grad_type is None or code_type in (None, TYPE_F32):
+            raise TypeError("gradients are float32, float16 or bfloat16 and codes are float16 or bfloat16")
+        want = {"exp_avg": state, "exp_avg_sq": state, "grad": None if g0 is None else g0.dtype, "codes": None if c0 is None else c0.dtype}
+        dev = weights[0].device if n else torch.device("cuda")
+        arr = (AdamwTensor * max(n, 1))()
+        for i, w in enumerate(weights):
+            if not (w.is_cuda and w.dtype == torch.float32 and w.is_contiguous()):
+                raise TypeError("weights must be contiguous float32 device tensors")
+            arr[i].w = w.data_ptr() or None
+            arr[i].n = w.numel()
+            for k, v in lists.items():
+                t = v[i]
+                if t is None and k in ("theta", "lambda_", "codes"):
+                    continue
+                elems = -(-w.numel() // STATE_BLOCK) if k.endswith("_scale") else w.numel()
+                if not (t.device == w.device and t.dtype == want.get(k, torch.float32) and t.is_contiguous() and t.numel() == elems):
+                    raise TypeError(f"{k.rstrip('_')} of tensor {i}: a contiguous tensor of {elems} elements beside the weights, one type for all")
+                setattr(arr[i], k, t.data_ptr() or None)
+        lib = library()
+        need = int(lib.condensa_adamw_list_bytes(arr, n))
+        self._memory = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+        self._keep = (list(weights), lists)
+        self.list = AdamwList()
+        st = _stream_of(stream)
+        with torch.cuda.device(dev):
+            _check(lib.condensa_adamw_list_init(arr, n, bits, grad_type, code_type, self._memory.data_ptr(), self._memory.numel(),
+                                                int(st.cuda_stream), ctypes.byref(self.list)))
+            _wait_unless_captured(st)
+
+
+def adamw_table(weights, grads, exp_avg, exp_avg_sq, **kw) -> AdamwTable:
+    """The buffers of an AdamW step.  States in 32 bits: float32 ``exp_avg`` and ``exp_avg_sq``.  States in 8 bits: uint8 E4M3 codes,
+    with ``exp_avg_scale`` and ``exp_avg_sq_scale`` (float32, one for every 256 elements of a tensor); zeros are a valid start.
+    ``theta`` and ``lambdas`` add the L-C penalty, ``codes`` (float16 or bfloat16) receive the updated weights in 16 bits; their
+    entries may be None."""
+    return AdamwTable(weights, grads, exp_avg, exp_avg_sq, **kw)
+
+
+def condensa_lc_adamw_step(table: AdamwTable, lr, step, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0, mu=0.0, seed=None,
+                           grad_scale=None, stream=None):
+    """Marshals condensa_lc_adamw_step: one update of everything in ``table``.  ``seed``: 8-bit states are rounded by random bits
+    made from it (another one for every step), None: to nearest.  ``grad_scale``: a float32 device scalar."""
+    import torch
+    if grad_scale is not None and not (grad_scale.is_cuda and grad_scale.dtype == torch.float32 and grad_scale.numel() == 1):
+        raise TypeError("grad_scale is one float32 on the device")
+    s = AdamwSettings(lr, betas[0], betas[1], eps, weight_decay, mu, ROUND_NEAREST if seed is None else ROUND_STOCHASTIC, step,
+                      0 if seed is None else seed & 0xFFFFFFFFFFFFFFFF, None if grad_scale is None else grad_scale.data_ptr(), 0)
+    _check(library().condensa_lc_adamw_step(ctypes.byref(table.list), ctypes.byref(s), _stream(stream)))
 
 
 def condensa_mu_schedule(mu0: float, a: float, j: int) -> float:
