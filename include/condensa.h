@@ -484,6 +484,62 @@ condensa_status condensa_adamw_list_init(const condensa_adamw_tensor* tensors, i
                                          condensa_adamw_list* list);
 condensa_status condensa_lc_adamw_step(const condensa_adamw_list* list, const condensa_adamw_settings* settings, void* stream);
 
+/*
+ * Low-rank adapters of many requests at once beside a shared projection.  The projection W [n_out, n_in] is what the compression
+ * left (16-bit codes, e.g. theta_f16 of condensa_prune or the codes of condensa_quantize_bf16); it is shared and not trained.  Adapter a adds a
+ * product of rank values, A_a [rank, n_in] and B_a [n_out, rank], with a scale s_a; every token names its adapter.
+ *   forward:   z[t] = s_a (x[t] A_a^T);   y[t] = x[t] W^T + z[t] B_a^T
+ *   backward:  dz[t] = s_a (dy[t] B_a);   dx[t] = dy[t] W + dz[t] A_a;
+ *              grad_A_a = sum of dz[t]^T x[t],  grad_B_a = sum of dy[t]^T z[t]  over the tokens of a
+ * All sums are binary32 in an order that depends on sizes and on the tokens' adapters alone, so equal calls give equal bits.  z and dz are
+ * rounded to the 16-bit type where they enter a product that is rounded to it anyway (y, dx); the gradients' product with dz keeps 16
+ * bits of it and more.  y, z and dx are rounded to nearest, ties to even; values outside the range of binary16 become infinite.
+ *
+ * A list names the adapters that the calls may use, laid out on the device once; it has to stay as it is while it is in use, as
+ * have the adapters' buffers (their values may change between calls).  list_dev: condensa_adapter_list_bytes(n) bytes, 256-byte
+ * aligned.  Rows of A and B are contiguous.  No written buffer may overlap another one of the list.
+ */
+#define CONDENSA_MAX_ADAPTERS 16384
+#define CONDENSA_MAX_RANK     256
+typedef struct {
+    const uint16_t* a;              /* device [rank, n_in]                                                    */
+    const uint16_t* b;              /* device [n_out, rank]                                                   */
+    float*          grad_a;         /* device [rank, n_in], [n_out, rank]; both NULL without a backward pass  */
+    float*          grad_b;
+    float           scale;          /* finite                                                                 */
+    int32_t         rank;           /* 1..CONDENSA_MAX_RANK                                                   */
+} condensa_adapter;
+typedef struct {
+    const void* table_dev;
+    int64_t     n_in, n_out;
+    int32_t     n_adapters, max_rank, type, flags;
+} condensa_adapter_list;
+size_t condensa_adapter_list_bytes(int n_adapters);
+condensa_status condensa_adapter_list_init(const condensa_adapter* adapters, int n_adapters, int type, int64_t n_in, int64_t n_out,
+                                           void* list_dev, size_t list_bytes, void* stream, condensa_adapter_list* list);
+/* Bytes of workspace (256-byte aligned device memory) of a call with n_tokens tokens; 0 for invalid arguments. */
+size_t condensa_adapter_workspace_bytes(const condensa_adapter_list* list, int64_t n_tokens, int backward);
+
+/*
+ * Forward pass.  n_tokens may be 0 (up to 2^24).  Strides count elements; the rows of x, W and y may be any distance apart and at any address
+ * (16-byte aligned rows of a multiple of eight values are fastest).  token_adapter_dev: device int32 [n_tokens], an index into
+ * the list; any other value means no adapter.  z_dev: NULL, or [n_tokens, z_stride] with z_stride >= the largest rank: receives z, zeros after
+ * the adapter's rank, which the backward pass wants.  No buffer may overlap y or z.
+ */
+condensa_status condensa_adapter_project(const condensa_adapter_list* list, const uint16_t* x_dev, int64_t x_stride, int64_t n_tokens,
+                                         const uint16_t* w_dev, int64_t w_stride, const int32_t* token_adapter_dev,
+                                         uint16_t* y_dev, int64_t y_stride, uint16_t* z_dev, int64_t z_stride,
+                                         void* workspace_dev, size_t workspace_bytes, void* stream);
+/*
+ * Backward pass: dx (NULL: not wanted) and the gradients of ALL adapters of the list, zeros for those without a token; every adapter
+ * needs its gradient buffers.  x, token_adapter and z as in the forward pass.  Gradients are written, not added to.
+ */
+condensa_status condensa_adapter_project_backward(const condensa_adapter_list* list, const uint16_t* dy_dev, int64_t dy_stride,
+                                                  const uint16_t* x_dev, int64_t x_stride, int64_t n_tokens,
+                                                  const uint16_t* w_dev, int64_t w_stride, const int32_t* token_adapter_dev,
+                                                  const uint16_t* z_dev, int64_t z_stride, uint16_t* dx_dev, int64_t dx_stride,
+                                                  void* workspace_dev, size_t workspace_bytes, void* stream);
+
 /* ---- process-wide DEFAULTS of the knobs above: what a NULL config stands for ---------------------- */
 enum {
     CONDENSA_OPT_SELECT_PATH   = 0, /* condensa_config.select_path   */

@@ -10,4 +10,5 @@ from .binding import (  # noqa: F401
     condensa_quantize, condensa_dequantize, condensa_quantize_bf16, condensa_dequantize_bf16, condensa_quantize_fp8, condensa_dequantize_fp8, FP8_E4M3, FP8_E5M2, condensa_lc_step, condensa_lc_step_pq, condensa_count_nonzero, condensa_thin, condensa_lc_sgd_step, condensa_mu_schedule, condensa_set_option, condensa_get_option,
     condensa_workspace_bytes, select_records, condensa_profile_read, condensa_profile_reset, condensa_launch_count,
     STATE_BLOCK, TYPE_F32, TYPE_F16, TYPE_BF16, ROUND_NEAREST, ROUND_STOCHASTIC, AdamwTable, adamw_table, condensa_lc_adamw_step,
+    AdapterTable, adapter_table, adapter_workspace, condensa_adapter_project, condensa_adapter_project_backward,
 )

@@ -59,7 +59,28 @@ class AdamwSettings(ctypes.Structure):
                 ("seed", ctypes.c_uint64), ("grad_scale_dev", ctypes.c_void_p), ("reserved", ctypes.c_int64)]
 
 
+class Adapter(ctypes.Structure):
+    _fields_ = [("a", ctypes.c_void_p), ("b", ctypes.c_void_p), ("grad_a", ctypes.c_void_p), ("grad_b", ctypes.c_void_p),
+                ("scale", ctypes.c_float), ("rank", ctypes.c_int32)]
+
+
+class AdapterList(ctypes.Structure):
+    _fields_ = [("table_dev", ctypes.c_void_p), ("n_in", ctypes.c_int64), ("n_out", ctypes.c_int64), ("n_adapters", ctypes.c_int32),
+                ("max_rank", ctypes.c_int32), ("type", ctypes.c_int32), ("flags", ctypes.c_int32)]
+
+
 _PROTOTYPES = {
+    "condensa_adapter_list_bytes": (ctypes.c_size_t, [ctypes.c_int]),
+    "condensa_adapter_list_init": (ctypes.c_int32, [ctypes.POINTER(Adapter), ctypes.c_int, ctypes.c_int, ctypes.c_int64, ctypes.c_int64,
+                                                    ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p, ctypes.POINTER(AdapterList)]),
+    "condensa_adapter_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(AdapterList), ctypes.c_int64, ctypes.c_int]),
+    "condensa_adapter_project": (ctypes.c_int32, [ctypes.POINTER(AdapterList), ctypes.c_void_p, ctypes.c_int64, ctypes.c_int64,
+                                                  ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64,
+                                                  ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    "condensa_adapter_project_backward": (ctypes.c_int32, [ctypes.POINTER(AdapterList), ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                                           ctypes.c_int64, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64,
+                                                           ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                                           ctypes.c_int64, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
     "condensa_adamw_list_bytes": (ctypes.c_size_t, [ctypes.POINTER(AdamwTensor), ctypes.c_int]),
     "condensa_adamw_list_init": (ctypes.c_int32, [ctypes.POINTER(AdamwTensor), ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int,
                                                   ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p, ctypes.POINTER(AdamwList)]),
@@ -696,6 +717,122 @@ def condensa_lc_adamw_step(table: AdamwTable, lr, step, betas=(0.9, 0.999), eps=
     s = AdamwSettings(lr, betas[0], betas[1], eps, weight_decay, mu, ROUND_NEAREST if seed is None else ROUND_STOCHASTIC, step,
                       0 if seed is None else seed & 0xFFFFFFFFFFFFFFFF, None if grad_scale is None else grad_scale.data_ptr(), 0)
     _check(library().condensa_lc_adamw_step(ctypes.byref(table.list), ctypes.byref(s), _stream(stream)))
+
+
+class AdapterTable:
+    """Adapters beside one shared projection, laid out on the device once for many calls.  The tensors must keep their storage.
+    See ``adapter_table``."""
+
+    def __init__(self, adapters, grads=None, n_in=None, n_out=None, dtype=None, stream=None):
+        import torch
+        adapters = [tuple(x) for x in adapters]
+        if adapters:
+            a0, b0, _ = adapters[0]
+            n_in, n_out, dtype = a0.shape[-1], b0.shape[0], a0.dtype
+        if grads is not None and len(grads) != len(adapters):
+            raise ValueError("gradients: one pair for each adapter")
+        if dtype not in (torch.float16, torch.bfloat16):
+            raise TypeError("adapters are float16 or bfloat16")
+        dev = adapters[0][0].device if adapters else torch.device("cuda", torch.cuda.current_device())
+        arr = (Adapter * max(len(adapters), 1))()
+        for i, (a, b, scale) in enumerate(adapters):
+            r = a.shape[0] if a.dim() == 2 else -1
+            for t, shape in ((a, (r, n_in)), (b, (n_out, r))):
+                if not (t.is_cuda and t.device == dev and t.dtype == dtype and t.is_contiguous() and tuple(t.shape) == shape):
+                    raise TypeError(f"adapter {i}: contiguous A [rank, {n_in}] and B [{n_out}, rank] on one device, one type for all")
+            arr[i].a, arr[i].b, arr[i].scale, arr[i].rank = a.data_ptr(), b.data_ptr(), float(scale), r
+            if grads is not None:
+                ga, gb = grads[i]
+                for t, shape in ((ga, (r, n_in)), (gb, (n_out, r))):
+                    if not (t.device == dev and t.dtype == torch.float32 and t.is_contiguous() and tuple(t.shape) == shape):
+                        raise TypeError(f"gradients of adapter {i}: contiguous float32 tensors shaped like A and B")
+                arr[i].grad_a, arr[i].grad_b = ga.data_ptr(), gb.data_ptr()
+        lib = library()
+        self.dtype, self.device, self.grads = dtype, dev, grads
+        self._keep = adapters
+        self._memory = torch.empty(max(int(lib.condensa_adapter_list_bytes(len(adapters))), 256), dtype=torch.uint8, device=dev)
+        self.list = AdapterList()
+        st = _stream_of(stream)
+        with torch.cuda.device(dev):
+            _check(lib.condensa_adapter_list_init(arr, len(adapters), _type_of(dtype), int(n_in or 0), int(n_out or 0), self._memory.data_ptr(),
+                                                  self._memory.numel(), int(st.cuda_stream), ctypes.byref(self.list)))
+            _wait_unless_captured(st)
+        self.n_in, self.n_out, self.max_rank = self.list.n_in, self.list.n_out, self.list.max_rank
+
+
+def adapter_table(adapters, grads=None, **kw) -> AdapterTable:
+    """``adapters``: (A [rank, n_in], B [n_out, rank], scale) each, float16 or bfloat16; ``grads``: float32 (grad_A, grad_B) each, which
+    condensa_adapter_project_backward writes.  Without any adapter, ``n_in``, ``n_out`` and ``dtype`` describe the projection."""
+    return AdapterTable(adapters, grads, **kw)
+
+
+def adapter_workspace(table: AdapterTable, n_tokens: int, backward: bool = False):
+    """Workspace of calls with ``n_tokens`` tokens, to be kept between them."""
+    import torch
+    need = int(library().condensa_adapter_workspace_bytes(ctypes.byref(table.list), int(n_tokens), int(backward)))
+    if need == 0:
+        raise ValueError("n_tokens is out of range")
+    return torch.empty(need, dtype=torch.uint8, device=table.device)
+
+
+def _rows(name, t, table, n_tokens, width):
+    """(address, row stride) of a two-dimensional operand whose rows are contiguous."""
+    if not (t.dim() == 2 and t.device == table.device and t.dtype == table.dtype and tuple(t.shape) == (n_tokens, width)
+            and (t.stride(1) == 1 or width == 1 or t.numel() == 0) and (n_tokens <= 1 or t.stride(0) >= width)):
+        raise TypeError(f"{name}: a {table.dtype} tensor [{n_tokens}, {width}] with contiguous rows, beside the adapters")
+    return t.data_ptr() or None, t.stride(0) if n_tokens > 1 else width
+
+
+def _token_ids(ids, table, n_tokens):
+    import torch
+    if not (ids.device == table.device and ids.dtype == torch.int32 and ids.is_contiguous() and ids.numel() == n_tokens):
+        raise TypeError(f"token_adapter: {n_tokens} contiguous int32 on the device")
+    return ids.data_ptr() or None
+
+
+def condensa_adapter_project(x, w, table: AdapterTable, token_adapter, y=None, z=False, workspace=None, stream=None):
+    """Marshals condensa_adapter_project.  ``z``: a tensor [tokens, >= largest rank] to receive x A^T scale, True to allocate one (the
+    backward pass wants it), False for none."""
+    import torch
+    T = x.shape[0]
+    px, ldx = _rows("x", x, table, T, table.n_in)
+    pw, ldw = _rows("w", w, table, table.n_out, table.n_in)
+    ids = _token_ids(token_adapter, table, T)
+    if y is None:
+        y = torch.empty((T, table.n_out), dtype=table.dtype, device=table.device)
+    py, ldy = _rows("y", y, table, T, table.n_out)
+    if z is True:
+        z = torch.empty((T, max(table.max_rank, 1)), dtype=table.dtype, device=table.device)
+    z = None if z is False else z
+    if z is not None and not (z.device == table.device and z.dtype == table.dtype and z.is_contiguous() and z.dim() == 2 and z.shape[0] == T):
+        raise TypeError(f"z: a contiguous {table.dtype} tensor with a row for each token")
+    if workspace is None:
+        workspace = adapter_workspace(table, T)
+    _check(library().condensa_adapter_project(ctypes.byref(table.list), px, ldx, T, pw, ldw, ids, py, ldy,
+                                              None if z is None else z.data_ptr() or None, 0 if z is None else z.shape[1],
+                                              workspace.data_ptr(), workspace.numel(), _stream(stream)))
+    return {"y": y, "z": z, "workspace": workspace}
+
+
+def condensa_adapter_project_backward(dy, x, w, table: AdapterTable, token_adapter, z, dx=True, workspace=None, stream=None):
+    """Marshals condensa_adapter_project_backward: writes the gradients that ``table`` names, and ``dx`` (a tensor, True to allocate
+    one, False for none)."""
+    import torch
+    T = x.shape[0]
+    pdy, lddy = _rows("dy", dy, table, T, table.n_out)
+    px, ldx = _rows("x", x, table, T, table.n_in)
+    pw, ldw = _rows("w", w, table, table.n_out, table.n_in)
+    ids = _token_ids(token_adapter, table, T)
+    if not (z.device == table.device and z.dtype == table.dtype and z.is_contiguous() and z.dim() == 2 and z.shape[0] == T):
+        raise TypeError(f"z: the contiguous {table.dtype} tensor of the forward pass")
+    if dx is True:
+        dx = torch.empty((T, table.n_in), dtype=table.dtype, device=table.device)
+    pdx, lddx = (None, 0) if dx is False else _rows("dx", dx, table, T, table.n_in)
+    if workspace is None:
+        workspace = adapter_workspace(table, T, backward=True)
+    _check(library().condensa_adapter_project_backward(ctypes.byref(table.list), pdy, lddy, px, ldx, T, pw, ldw, ids, z.data_ptr() or None,
+                                                       z.shape[1], pdx, lddx, workspace.data_ptr(), workspace.numel(), _stream(stream)))
+    return {"dx": None if dx is False else dx, "grads": table.grads, "workspace": workspace}
 
 
 def condensa_mu_schedule(mu0: float, a: float, j: int) -> float:

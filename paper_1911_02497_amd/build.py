@@ -6,7 +6,7 @@ import subprocess
 import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-SOURCES = [os.path.join(HERE, "csrc", name) for name in ("api.hip", "adamw.hip")]
+SOURCES = [os.path.join(HERE, "csrc", name) for name in ("api.hip", "adamw.hip", "adapter.hip")]
 LIB = os.path.join(HERE, "libcondensa.so")
 
 FLAGS = [

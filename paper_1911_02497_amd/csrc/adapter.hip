@@ -1,0 +1,339 @@
+// C-ABI entry points of the adapters beside a shared projection (include/condensa.h): checks, workspace, launches.
+#include <cmath>
+#include <memory>
+#include <new>
+
+#include "host_util.h"
+#include "k_adapter.h"
+
+namespace condensa {
+
+constexpr i64 kMaxSide = static_cast<i64>(1) << 20;
+constexpr i64 kMaxTokens = static_cast<i64>(1) << 24;
+enum : int32_t { kAlignedA = 1, kAlignedB = 2, kHasGrads = 4 };
+
+static bool aligned(const void* p, u64 bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+static u32 padded_rank(u32 r) { return (r + 31) / 32 * 32; }
+
+static bool list_ok(const condensa_adapter_list* l) {
+    return l && l->table_dev && l->n_adapters >= 0 && l->n_adapters <= CONDENSA_MAX_ADAPTERS && l->max_rank >= 0 && l->max_rank <= CONDENSA_MAX_RANK &&
+           (l->type == CONDENSA_TYPE_F16 || l->type == CONDENSA_TYPE_BF16) && l->n_in >= 1 && l->n_in <= kMaxSide && l->n_out >= 1 && l->n_out <= kMaxSide;
+}
+
+// Tokens of a run of the gradients: short enough that some 1024 workgroups share the columns of x and dy, long enough that the parts of
+// a run, binary32 and as wide as a gradient, are small beside the 16-bit rows that it reads.
+static u32 run_tokens(i64 n_tokens, i64 n_in, i64 n_out) {
+    const i64 tiles = (n_in + kGradCols - 1) / kGradCols + (n_out + kGradCols - 1) / kGradCols;
+    i64 run = n_tokens * tiles / 1024;
+    run = run < 512 ? 512 : run;
+    return static_cast<u32>((run + kGradStep - 1) / kGradStep * kGradStep);
+}
+
+struct Plan {
+    bool few = false;
+    u32 rp = 0, splits = 1, steps_each = 0, tiles_n = 0;
+    u32 run = 0, n_slots = 0, tiles = 0;
+    size_t zp = 0, z32 = 0, part = 0, row_max = 0, order = 0, seg = 0, slots = 0, total = 0;
+};
+
+// Up to this many tokens the weights are read straight into registers, by workgroups that share the sum.
+constexpr i64 kFewTokens = 64;
+
+static Plan make_plan(i64 T, i64 n_in, i64 n_out, u32 n_adapters, u32 max_rank, bool backward) {
+    Plan p;
+    size_t at = 0;
+    auto take = [&](u64 bytes) { const size_t o = at; at += align_up(bytes ? bytes : 1); return o; };
+    p.rp = padded_rank(max_rank ? max_rank : 1);
+    p.few = !backward && T <= kFewTokens;
+    if (p.few) {
+        const u32 steps = static_cast<u32>((n_in + 31) / 32);
+        p.tiles_n = static_cast<u32>((n_out + kFewCols - 1) / kFewCols);
+        // some 512 workgroups, and at least four steps for each of the four wavefronts that share a part of the sum
+        u32 s = (512 + p.tiles_n - 1) / p.tiles_n, most = steps / 16;
+        s = s > most ? most : s;
+        s = s > 8 ? 8 : (s < 1 ? 1 : s);
+        p.steps_each = (steps + s - 1) / s;
+        p.splits = (steps + p.steps_each - 1) / p.steps_each;
+        p.part = take(static_cast<u64>(p.splits) * T * n_out * 4);
+        p.z32 = take(static_cast<u64>(T) * (max_rank ? max_rank : 1) * 4);
+    } else {
+        p.zp = take(static_cast<u64>(T) * p.rp * 2);
+        if (backward) {
+            p.z32 = take(static_cast<u64>(T) * p.rp * 4);
+            p.row_max = take(static_cast<u64>(T) * 4);
+            p.run = run_tokens(T, n_in, n_out);
+            p.n_slots = static_cast<u32>(T / p.run) + n_adapters;
+            p.order = take(static_cast<u64>(T) * 4);
+            p.seg = take(static_cast<u64>(n_adapters) * sizeof(uint2));
+            p.slots = take(static_cast<u64>(p.n_slots) * 4);
+            if (T > p.run) p.part = take(static_cast<u64>(p.n_slots) * max_rank * (n_in + n_out) * 4);
+        }
+    }
+    p.total = at;
+    return p;
+}
+
+template <typename E, bool ALONG>
+static condensa_status launch_down(const DownArgs& a, u32 blocks, hipStream_t st) {
+    if (a.vec_x) hipLaunchKernelGGL((k_adapter_down<E, ALONG, true>), dim3(blocks), dim3(64 * kDownWaves), 0, st, a);
+    else         hipLaunchKernelGGL((k_adapter_down<E, ALONG, false>), dim3(blocks), dim3(64 * kDownWaves), 0, st, a);
+    CONDENSA_LAUNCH_CHECK();
+    return CONDENSA_OK;
+}
+
+template <typename E, int BM, int BN, int WM, int WN, bool ALONG, bool VEC>
+static void launch_wide_tile(const WideArgs& a, hipStream_t st) {
+    const u64 tiles = (static_cast<u64>(a.n_tokens) + BM - 1) / BM * ((static_cast<u64>(a.n_out) + BN - 1) / BN);
+    hipLaunchKernelGGL((k_adapter_wide<E, BM, BN, WM, WN, ALONG, VEC>), dim3(static_cast<unsigned>(tiles)), dim3(64 * WM * WN), 0, st, a);
+}
+
+template <typename E, bool ALONG>
+static condensa_status launch_wide(const WideArgs& a, bool vec, hipStream_t st) {
+    const auto tiles = [&](u64 m, u64 n) { return (a.n_tokens + m - 1) / m * ((a.n_out + n - 1) / n); };
+    if (vec && tiles(256, 256) >= 192) launch_wide_tile<E, 256, 256, 2, 4, ALONG, true>(a, st);
+    else if (tiles(128, 128) >= 192) {
+        if (vec) launch_wide_tile<E, 128, 128, 2, 2, ALONG, true>(a, st);
+        else     launch_wide_tile<E, 128, 128, 2, 2, ALONG, false>(a, st);
+    } else {
+        if (vec) launch_wide_tile<E, 64, 64, 2, 2, ALONG, true>(a, st);
+        else     launch_wide_tile<E, 64, 64, 2, 2, ALONG, false>(a, st);
+    }
+    CONDENSA_LAUNCH_CHECK();
+    return CONDENSA_OK;
+}
+
+template <typename E, u32 FM>
+static void launch_few_tile(const FewArgs& f, bool vec, u32 blocks, hipStream_t st) {
+    if (vec) hipLaunchKernelGGL((k_adapter_few<E, FM, true>), dim3(blocks), dim3(64 * kFewWaves), 0, st, f);
+    else     hipLaunchKernelGGL((k_adapter_few<E, FM, false>), dim3(blocks), dim3(64 * kFewWaves), 0, st, f);
+}
+
+template <typename E>
+static condensa_status launch_few(const FewArgs& f, bool vec, hipStream_t st) {
+    const u32 T = f.wide.n_tokens, blocks = f.tiles_n * f.splits + T;
+    if (T <= 16)      launch_few_tile<E, 1>(f, vec, blocks, st);
+    else if (T <= 32) launch_few_tile<E, 2>(f, vec, blocks, st);
+    else              launch_few_tile<E, 4>(f, vec, blocks, st);
+    CONDENSA_LAUNCH_CHECK();
+    hipLaunchKernelGGL((k_adapter_few_join<E>), dim3((f.wide.n_out + 255) / 256, T), dim3(256), 0, st, f);
+    CONDENSA_LAUNCH_CHECK();
+    return CONDENSA_OK;
+}
+
+// Checks that both directions share; `used`: the call has work to do.
+static condensa_status check_call(bool used, i64 n_tokens, const void* ids, const void* workspace_dev, size_t workspace_bytes, const Plan& p) {
+    if (n_tokens > 0 && !ids) return CONDENSA_ERR_NULL;
+    if (!aligned(ids, 4)) return CONDENSA_ERR_ARG;
+    if (used && (!workspace_dev || !aligned(workspace_dev, 256) || workspace_bytes < p.total)) return CONDENSA_ERR_WORKSPACE;
+    return CONDENSA_OK;
+}
+
+static u64 rows_bytes(i64 rows, i64 ld, i64 cols, u64 elem) { return rows > 0 ? (static_cast<u64>(rows - 1) * ld + cols) * elem : 0; }
+
+}  // namespace condensa
+
+using namespace condensa;
+
+template <typename T>
+static T* at(void* ws, size_t off) { return reinterpret_cast<T*>(static_cast<char*>(ws) + off); }
+
+extern "C" {
+
+size_t condensa_adapter_list_bytes(int n_adapters) {
+    if (n_adapters < 0 || n_adapters > CONDENSA_MAX_ADAPTERS) return 0;
+    return align_up((n_adapters ? static_cast<size_t>(n_adapters) : 1) * sizeof(AdapterDesc));
+}
+
+condensa_status condensa_adapter_list_init(const condensa_adapter* adapters, int n_adapters, int type, int64_t n_in, int64_t n_out,
+                                           void* list_dev, size_t list_bytes, void* stream, condensa_adapter_list* list) {
+    if (list == nullptr) return CONDENSA_ERR_NULL;
+    if (n_adapters < 0 || n_adapters > CONDENSA_MAX_ADAPTERS) return CONDENSA_ERR_SIZE;
+    if (n_adapters > 0 && adapters == nullptr) return CONDENSA_ERR_NULL;
+    if (type != CONDENSA_TYPE_F16 && type != CONDENSA_TYPE_BF16) return CONDENSA_ERR_ARG;
+    if (n_in < 1 || n_out < 1 || n_in > kMaxSide || n_out > kMaxSide) return CONDENSA_ERR_SHAPE;
+    const size_t need = condensa_adapter_list_bytes(n_adapters);
+    if (!list_dev || !aligned(list_dev, 256) || list_bytes < need) return CONDENSA_ERR_WORKSPACE;
+    std::unique_ptr<ByteRange[]> ranges(new (std::nothrow) ByteRange[static_cast<size_t>(n_adapters) * 4 + 1]);
+    if (!ranges) return CONDENSA_ERR_SIZE;
+    size_t nr = 0;
+    int32_t max_rank = 0, flags = kAlignedA | kAlignedB | kHasGrads;
+    for (int i = 0; i < n_adapters; ++i) {
+        const condensa_adapter& s = adapters[i];
+        if (s.rank < 1 || s.rank > CONDENSA_MAX_RANK) return CONDENSA_ERR_SHAPE;
+        if (!s.a || !s.b || (s.grad_a == nullptr) != (s.grad_b == nullptr)) return CONDENSA_ERR_NULL;
+        if (!aligned(s.a, 2) || !aligned(s.b, 2) || !aligned(s.grad_a, 4) || !aligned(s.grad_b, 4)) return CONDENSA_ERR_ARG;
+        if (!std::isfinite(s.scale)) return CONDENSA_ERR_DENSITY;
+        max_rank = s.rank > max_rank ? s.rank : max_rank;
+        if (!aligned(s.a, 16) || n_in % 8) flags &= ~kAlignedA;
+        if (!aligned(s.b, 16) || s.rank % 8) flags &= ~kAlignedB;
+        if (!s.grad_a) flags &= ~kHasGrads;
+        ranges[nr++] = byte_range(s.a, static_cast<u64>(s.rank) * n_in * 2, false);
+        ranges[nr++] = byte_range(s.b, static_cast<u64>(s.rank) * n_out * 2, false);
+        ranges[nr++] = byte_range(s.grad_a, static_cast<u64>(s.rank) * n_in * 4, true);
+        ranges[nr++] = byte_range(s.grad_b, static_cast<u64>(s.rank) * n_out * 4, true);
+    }
+    ranges[nr++] = byte_range(list_dev, need, true);
+    if (ranges_conflict(ranges.get(), nr)) return CONDENSA_ERR_ARG;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    for (int first = 0; first < n_adapters; first += kAdapterPoke) {
+        AdapterPoke p{};
+        const int k = n_adapters - first < kAdapterPoke ? n_adapters - first : kAdapterPoke;
+        for (int i = 0; i < k; ++i) {
+            const condensa_adapter& s = adapters[first + i];
+            p.d[i].a = s.a; p.d[i].b = s.b; p.d[i].grad_a = s.grad_a; p.d[i].grad_b = s.grad_b;
+            p.d[i].scale = s.scale; p.d[i].rank = static_cast<u32>(s.rank);
+        }
+        hipLaunchKernelGGL(k_adapter_list, dim3(1), dim3(256), 0, st, static_cast<AdapterDesc*>(list_dev), p, static_cast<u32>(first), static_cast<u32>(k));
+        CONDENSA_LAUNCH_CHECK();
+    }
+    list->table_dev = list_dev;
+    list->n_in = n_in;
+    list->n_out = n_out;
+    list->n_adapters = n_adapters;
+    list->max_rank = max_rank;
+    list->type = type;
+    list->flags = flags;
+    return CONDENSA_OK;
+}
+
+size_t condensa_adapter_workspace_bytes(const condensa_adapter_list* list, int64_t n_tokens, int backward) {
+    if (!list_ok(list) || n_tokens < 0 || n_tokens > kMaxTokens) return 0;
+    const size_t b = make_plan(n_tokens, list->n_in, list->n_out, static_cast<u32>(list->n_adapters), static_cast<u32>(list->max_rank), backward != 0).total;
+    return b ? b : 256;
+}
+
+condensa_status condensa_adapter_project(const condensa_adapter_list* list, const uint16_t* x_dev, int64_t x_stride, int64_t n_tokens,
+                                         const uint16_t* w_dev, int64_t w_stride, const int32_t* token_adapter_dev,
+                                         uint16_t* y_dev, int64_t y_stride, uint16_t* z_dev, int64_t z_stride,
+                                         void* workspace_dev, size_t workspace_bytes, void* stream) {
+    if (!list) return CONDENSA_ERR_NULL;
+    if (!list_ok(list)) return CONDENSA_ERR_ARG;
+    if (n_tokens < 0 || n_tokens > kMaxTokens) return CONDENSA_ERR_SIZE;
+    if (n_tokens > 0 && (!x_dev || !w_dev || !y_dev)) return CONDENSA_ERR_NULL;
+    if (x_stride < list->n_in || w_stride < list->n_in || y_stride < list->n_out || x_stride > kMaxSide * 16 || w_stride > kMaxSide * 16 || y_stride > kMaxSide * 16 ||
+        (z_dev && (z_stride < list->max_rank || z_stride > kMaxSide)))
+        return CONDENSA_ERR_SHAPE;
+    if (!aligned(x_dev, 2) || !aligned(w_dev, 2) || !aligned(y_dev, 2) || !aligned(z_dev, 2)) return CONDENSA_ERR_ARG;
+    const Plan p = make_plan(n_tokens, list->n_in, list->n_out, static_cast<u32>(list->n_adapters), static_cast<u32>(list->max_rank), false);
+    const condensa_status rc = check_call(n_tokens > 0, n_tokens, token_adapter_dev, workspace_dev, workspace_bytes, p);
+    if (rc != CONDENSA_OK) return rc;
+    if (n_tokens == 0) return CONDENSA_OK;
+    ByteRange r[] = {byte_range(x_dev, rows_bytes(n_tokens, x_stride, list->n_in, 2), false), byte_range(w_dev, rows_bytes(list->n_out, w_stride, list->n_in, 2), false),
+                     byte_range(token_adapter_dev, static_cast<u64>(n_tokens) * 4, false), byte_range(y_dev, rows_bytes(n_tokens, y_stride, list->n_out, 2), true),
+                     byte_range(z_dev, static_cast<u64>(n_tokens) * z_stride * 2, true), byte_range(workspace_dev, p.total, true),
+                     byte_range(list->table_dev, condensa_adapter_list_bytes(list->n_adapters), false)};
+    if (ranges_conflict(r, sizeof(r) / sizeof(r[0]))) return CONDENSA_ERR_ARG;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const bool f16 = list->type == CONDENSA_TYPE_F16;
+    const bool vec_x = aligned(x_dev, 16) && x_stride % 8 == 0 && list->n_in % 8 == 0;
+    const bool vec = vec_x && aligned(w_dev, 16) && w_stride % 8 == 0;
+    WideArgs g{};
+    g.x = x_dev; g.ldx = x_stride; g.w = w_dev; g.ldw = w_stride; g.y = y_dev; g.ldy = y_stride;
+    g.n_tokens = static_cast<u32>(n_tokens); g.n_out = static_cast<u32>(list->n_out); g.n_sum = static_cast<u32>(list->n_in);
+    g.rp = p.rp; g.ids = token_adapter_dev; g.ad = static_cast<const AdapterDesc*>(list->table_dev);
+    g.n_adapters = static_cast<u32>(list->n_adapters); g.max_rank = static_cast<u32>(list->max_rank);
+    g.vec_m = (list->flags & kAlignedB) != 0;
+    g.vec_y = aligned(y_dev, 8) && y_stride % 4 == 0;
+    if (p.few) {
+        FewArgs f{};
+        f.wide = g;
+        f.part = at<float>(workspace_dev, p.part);
+        f.z32 = at<float>(workspace_dev, p.z32);
+        f.z = z_dev; f.ldz = z_stride;
+        f.tiles_n = p.tiles_n; f.splits = p.splits; f.steps_each = p.steps_each;
+        f.vec_a = (list->flags & kAlignedA) != 0;
+        return f16 ? launch_few<ElemF16>(f, vec, st) : launch_few<ElemBF16>(f, vec, st);
+    }
+    g.zp = at<u16>(workspace_dev, p.zp);
+    DownArgs d{};
+    d.x = x_dev; d.ldx = x_stride; d.n_tokens = g.n_tokens; d.n_sum = g.n_sum; d.ids = g.ids; d.ad = g.ad; d.n_adapters = g.n_adapters; d.max_rank = g.max_rank;
+    d.zp = at<u16>(workspace_dev, p.zp); d.rp = p.rp; d.z = z_dev; d.ldz = z_stride;
+    d.vec_x = vec_x; d.vec_m = (list->flags & kAlignedA) != 0;
+    d.tiles = (g.n_tokens + kDownTokens - 1) / kDownTokens;
+    condensa_status s = f16 ? launch_down<ElemF16, true>(d, d.tiles, st) : launch_down<ElemBF16, true>(d, d.tiles, st);
+    if (s != CONDENSA_OK) return s;
+    return f16 ? launch_wide<ElemF16, true>(g, vec, st) : launch_wide<ElemBF16, true>(g, vec, st);
+}
+
+condensa_status condensa_adapter_project_backward(const condensa_adapter_list* list, const uint16_t* dy_dev, int64_t dy_stride,
+                                                  const uint16_t* x_dev, int64_t x_stride, int64_t n_tokens,
+                                                  const uint16_t* w_dev, int64_t w_stride, const int32_t* token_adapter_dev,
+                                                  const uint16_t* z_dev, int64_t z_stride, uint16_t* dx_dev, int64_t dx_stride,
+                                                  void* workspace_dev, size_t workspace_bytes, void* stream) {
+    if (!list) return CONDENSA_ERR_NULL;
+    if (!list_ok(list)) return CONDENSA_ERR_ARG;
+    if (!(list->flags & kHasGrads)) return CONDENSA_ERR_NULL;
+    if (n_tokens < 0 || n_tokens > kMaxTokens) return CONDENSA_ERR_SIZE;
+    if (n_tokens > 0 && (!dy_dev || !x_dev || !w_dev || !z_dev)) return CONDENSA_ERR_NULL;
+    if (x_stride < list->n_in || w_stride < list->n_in || dy_stride < list->n_out || x_stride > kMaxSide * 16 || w_stride > kMaxSide * 16 || dy_stride > kMaxSide * 16 ||
+        z_stride < list->max_rank || z_stride > kMaxSide || (dx_dev && (dx_stride < list->n_in || dx_stride > kMaxSide * 16)))
+        return CONDENSA_ERR_SHAPE;
+    if (!aligned(dy_dev, 2) || !aligned(x_dev, 2) || !aligned(w_dev, 2) || !aligned(z_dev, 2) || !aligned(dx_dev, 2)) return CONDENSA_ERR_ARG;
+    const Plan p = make_plan(n_tokens, list->n_in, list->n_out, static_cast<u32>(list->n_adapters), static_cast<u32>(list->max_rank), true);
+    const condensa_status rc = check_call(n_tokens > 0 || list->n_adapters > 0, n_tokens, token_adapter_dev, workspace_dev, workspace_bytes, p);
+    if (rc != CONDENSA_OK) return rc;
+    ByteRange r[] = {byte_range(dy_dev, rows_bytes(n_tokens, dy_stride, list->n_out, 2), false), byte_range(x_dev, rows_bytes(n_tokens, x_stride, list->n_in, 2), false),
+                     byte_range(w_dev, rows_bytes(list->n_out, w_stride, list->n_in, 2), false), byte_range(token_adapter_dev, static_cast<u64>(n_tokens) * 4, false),
+                     byte_range(z_dev, static_cast<u64>(n_tokens) * z_stride * 2, false), byte_range(dx_dev, rows_bytes(n_tokens, dx_stride, list->n_in, 2), true),
+                     byte_range(workspace_dev, p.total, true), byte_range(list->table_dev, condensa_adapter_list_bytes(list->n_adapters), false)};
+    if (ranges_conflict(r, sizeof(r) / sizeof(r[0]))) return CONDENSA_ERR_ARG;
+    const u64 grad_blocks = static_cast<u64>(p.n_slots) * ((list->n_in + kGradCols - 1) / kGradCols + (list->n_out + kGradCols - 1) / kGradCols);
+    if (grad_blocks >= (static_cast<u64>(1) << 24)) return CONDENSA_ERR_SIZE;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const bool f16 = list->type == CONDENSA_TYPE_F16;
+    const bool vec_dy = aligned(dy_dev, 16) && dy_stride % 8 == 0 && list->n_out % 8 == 0;
+    const bool vec_x = aligned(x_dev, 16) && x_stride % 8 == 0 && list->n_in % 8 == 0;
+    const bool vec_w = aligned(w_dev, 16) && w_stride % 8 == 0 && list->n_in % 8 == 0;
+    const u32 T = static_cast<u32>(n_tokens), n = static_cast<u32>(list->n_adapters);
+    const AdapterDesc* ad = static_cast<const AdapterDesc*>(list->table_dev);
+    DownArgs d{};
+    d.x = dy_dev; d.ldx = dy_stride; d.n_tokens = T; d.n_sum = static_cast<u32>(list->n_out); d.ids = token_adapter_dev; d.ad = ad; d.n_adapters = n;
+    d.max_rank = static_cast<u32>(list->max_rank);
+    d.zp = at<u16>(workspace_dev, p.zp); d.rp = p.rp; d.z32 = at<float>(workspace_dev, p.z32); d.row_max = at<u32>(workspace_dev, p.row_max);
+    d.vec_x = vec_dy; d.vec_m = (list->flags & kAlignedB) != 0;
+    d.tiles = (T + kDownTokens - 1) / kDownTokens;
+    d.order = at<u32>(workspace_dev, p.order); d.seg = at<uint2>(workspace_dev, p.seg); d.slots = at<u32>(workspace_dev, p.slots);
+    d.n_slots = p.n_slots; d.run = p.run;
+    const u32 blocks = d.tiles + (n + kDownWaves - 1) / kDownWaves;
+    if (blocks == 0) return CONDENSA_OK;
+    condensa_status s = f16 ? launch_down<ElemF16, false>(d, blocks, st) : launch_down<ElemBF16, false>(d, blocks, st);
+    if (s != CONDENSA_OK) return s;
+    if (dx_dev && T > 0) {
+        WideArgs g{};
+        g.x = dy_dev; g.ldx = dy_stride; g.w = w_dev; g.ldw = w_stride; g.y = dx_dev; g.ldy = dx_stride;
+        g.n_tokens = T; g.n_out = static_cast<u32>(list->n_in); g.n_sum = static_cast<u32>(list->n_out);
+        g.zp = d.zp; g.rp = p.rp; g.ids = token_adapter_dev; g.ad = ad; g.n_adapters = n; g.max_rank = d.max_rank;
+        g.vec_m = (list->flags & kAlignedA) != 0;
+        g.vec_y = aligned(dx_dev, 8) && dx_stride % 4 == 0;
+        s = f16 ? launch_wide<ElemF16, false>(g, vec_dy && vec_w, st) : launch_wide<ElemBF16, false>(g, vec_dy && vec_w, st);
+        if (s != CONDENSA_OK) return s;
+    }
+    if (n == 0) return CONDENSA_OK;
+    GradArgs q{};
+    q.x = x_dev; q.ldx = x_stride; q.n_in = static_cast<u32>(list->n_in); q.dy = dy_dev; q.ldy = dy_stride; q.n_out = static_cast<u32>(list->n_out);
+    q.dz = d.z32; q.rp = p.rp; q.z = z_dev; q.ldz = z_stride; q.row_max = d.row_max; q.order = d.order; q.seg = d.seg; q.slots = d.slots; q.ad = ad;
+    q.max_rank = d.max_rank; q.run = p.run;
+    q.tiles_in = (q.n_in + kGradCols - 1) / kGradCols;
+    q.tiles = q.tiles_in + (q.n_out + kGradCols - 1) / kGradCols;
+    q.part = n_tokens > p.run ? at<float>(workspace_dev, p.part) : nullptr;
+    const dim3 grid(p.n_slots * q.tiles, (q.max_rank + 63) / 64);
+    const bool vec = vec_x && vec_dy;
+    if (f16) {
+        if (vec) hipLaunchKernelGGL((k_adapter_grads<ElemF16, true>), grid, dim3(256), 0, st, q);
+        else     hipLaunchKernelGGL((k_adapter_grads<ElemF16, false>), grid, dim3(256), 0, st, q);
+    } else {
+        if (vec) hipLaunchKernelGGL((k_adapter_grads<ElemBF16, true>), grid, dim3(256), 0, st, q);
+        else     hipLaunchKernelGGL((k_adapter_grads<ElemBF16, false>), grid, dim3(256), 0, st, q);
+    }
+    CONDENSA_LAUNCH_CHECK();
+    if (n_tokens > p.run) {
+        const u64 elems = static_cast<u64>(q.max_rank) * (list->n_in + list->n_out);
+        u64 each = (elems + 1023) / 1024;
+        each = each > 512 ? 512 : each;
+        hipLaunchKernelGGL(k_adapter_join, dim3(static_cast<unsigned>(each * n)), dim3(256), 0, st, q, static_cast<u32>(each));
+        CONDENSA_LAUNCH_CHECK();
+    }
+    return CONDENSA_OK;
+}
+
+}  // extern "C"
