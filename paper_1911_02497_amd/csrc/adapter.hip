@@ -10,6 +10,7 @@ namespace condensa {
 
 constexpr i64 kMaxSide = static_cast<i64>(1) << 20;
 constexpr i64 kMaxTokens = static_cast<i64>(1) << 24;
+constexpr i64 kMaxStride = static_cast<i64>(1) << 22;       // 256 rows of a tile are less than 2^32 bytes apart
 enum : int32_t { kAlignedA = 1, kAlignedB = 2, kHasGrads = 4 };
 
 static bool aligned(const void* p, u64 bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
@@ -25,7 +26,7 @@ static bool list_ok(const condensa_adapter_list* l) {
 static u32 run_tokens(i64 n_tokens, i64 n_in, i64 n_out) {
     const i64 tiles = (n_in + kGradCols - 1) / kGradCols + (n_out + kGradCols - 1) / kGradCols;
     i64 run = n_tokens * tiles / 1024;
-    run = run < 512 ? 512 : run;
+    run = run < 256 ? 256 : run;
     return static_cast<u32>((run + kGradStep - 1) / kGradStep * kGradStep);
 }
 
@@ -81,22 +82,29 @@ static condensa_status launch_down(const DownArgs& a, u32 blocks, hipStream_t st
     return CONDENSA_OK;
 }
 
-template <typename E, int BM, int BN, int WM, int WN, bool ALONG, bool VEC>
+template <typename E, int BM, int BN, int WM, int WN, u32 NB, bool ALONG, bool VEC>
 static void launch_wide_tile(const WideArgs& a, hipStream_t st) {
     const u64 tiles = (static_cast<u64>(a.n_tokens) + BM - 1) / BM * ((static_cast<u64>(a.n_out) + BN - 1) / BN);
-    hipLaunchKernelGGL((k_adapter_wide<E, BM, BN, WM, WN, ALONG, VEC>), dim3(static_cast<unsigned>(tiles)), dim3(64 * WM * WN), 0, st, a);
+    hipLaunchKernelGGL((k_adapter_wide<E, BM, BN, WM, WN, NB, ALONG, VEC>), dim3(static_cast<unsigned>(tiles * a.splits)), dim3(64 * WM * WN), 0, st, a);
 }
 
 template <typename E, bool ALONG>
-static condensa_status launch_wide(const WideArgs& a, bool vec, hipStream_t st) {
+static condensa_status launch_wide(WideArgs a, bool vec, hipStream_t st) {
+    a.splits = 1;
+    a.steps_each = (a.n_sum + 63) / 64;
     const auto tiles = [&](u64 m, u64 n) { return (a.n_tokens + m - 1) / m * ((a.n_out + n - 1) / n); };
-    if (vec && tiles(256, 256) >= 192) launch_wide_tile<E, 256, 256, 2, 4, ALONG, true>(a, st);
-    else if (tiles(128, 128) >= 192) {
-        if (vec) launch_wide_tile<E, 128, 128, 2, 2, ALONG, true>(a, st);
-        else     launch_wide_tile<E, 128, 128, 2, 2, ALONG, false>(a, st);
+    // A tile of 256 rows fills a compute unit.  The one whose rounds over the 256 of them cost less is taken: 8192 x 4608 outputs are 2.25 rounds
+    // of 256 x 256, which take as long as three, and three of 256 x 192.
+    const auto cost = [&](u64 n) { return (tiles(256, n) + 255) / 256 * n; };
+    if (vec && tiles(256, 256) >= 192) {
+        if (cost(192) < cost(256)) launch_wide_tile<E, 256, 192, 2, 4, 2, ALONG, true>(a, st);
+        else                       launch_wide_tile<E, 256, 256, 2, 4, 2, ALONG, true>(a, st);
+    } else if (tiles(128, 128) >= 192) {
+        if (vec) launch_wide_tile<E, 128, 128, 2, 2, 2, ALONG, true>(a, st);
+        else     launch_wide_tile<E, 128, 128, 2, 2, 2, ALONG, false>(a, st);
     } else {
-        if (vec) launch_wide_tile<E, 64, 64, 2, 2, ALONG, true>(a, st);
-        else     launch_wide_tile<E, 64, 64, 2, 2, ALONG, false>(a, st);
+        if (vec) launch_wide_tile<E, 64, 64, 2, 2, 4, ALONG, true>(a, st);
+        else     launch_wide_tile<E, 64, 64, 2, 2, 2, ALONG, false>(a, st);
     }
     CONDENSA_LAUNCH_CHECK();
     return CONDENSA_OK;
@@ -210,7 +218,7 @@ condensa_status condensa_adapter_project(const condensa_adapter_list* list, cons
     if (!list_ok(list)) return CONDENSA_ERR_ARG;
     if (n_tokens < 0 || n_tokens > kMaxTokens) return CONDENSA_ERR_SIZE;
     if (n_tokens > 0 && (!x_dev || !w_dev || !y_dev)) return CONDENSA_ERR_NULL;
-    if (x_stride < list->n_in || w_stride < list->n_in || y_stride < list->n_out || x_stride > kMaxSide * 16 || w_stride > kMaxSide * 16 || y_stride > kMaxSide * 16 ||
+    if (x_stride < list->n_in || w_stride < list->n_in || y_stride < list->n_out || x_stride > kMaxStride || w_stride > kMaxStride || y_stride > kMaxStride ||
         (z_dev && (z_stride < list->max_rank || z_stride > kMaxSide)))
         return CONDENSA_ERR_SHAPE;
     if (!aligned(x_dev, 2) || !aligned(w_dev, 2) || !aligned(y_dev, 2) || !aligned(z_dev, 2)) return CONDENSA_ERR_ARG;
@@ -265,8 +273,8 @@ condensa_status condensa_adapter_project_backward(const condensa_adapter_list* l
     if (!(list->flags & kHasGrads)) return CONDENSA_ERR_NULL;
     if (n_tokens < 0 || n_tokens > kMaxTokens) return CONDENSA_ERR_SIZE;
     if (n_tokens > 0 && (!dy_dev || !x_dev || !w_dev || !z_dev)) return CONDENSA_ERR_NULL;
-    if (x_stride < list->n_in || w_stride < list->n_in || dy_stride < list->n_out || x_stride > kMaxSide * 16 || w_stride > kMaxSide * 16 || dy_stride > kMaxSide * 16 ||
-        z_stride < list->max_rank || z_stride > kMaxSide || (dx_dev && (dx_stride < list->n_in || dx_stride > kMaxSide * 16)))
+    if (x_stride < list->n_in || w_stride < list->n_in || dy_stride < list->n_out || x_stride > kMaxStride || w_stride > kMaxStride || dy_stride > kMaxStride ||
+        z_stride < list->max_rank || z_stride > kMaxSide || (dx_dev && (dx_stride < list->n_in || dx_stride > kMaxStride)))
         return CONDENSA_ERR_SHAPE;
     if (!aligned(dy_dev, 2) || !aligned(x_dev, 2) || !aligned(w_dev, 2) || !aligned(z_dev, 2) || !aligned(dx_dev, 2)) return CONDENSA_ERR_ARG;
     const Plan p = make_plan(n_tokens, list->n_in, list->n_out, static_cast<u32>(list->n_adapters), static_cast<u32>(list->max_rank), true);

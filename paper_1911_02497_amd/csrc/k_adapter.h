@@ -59,12 +59,8 @@ __device__ inline u32x4 load8(const u16* __restrict__ p, i64 k, i64 n) {
     u32x4 v = {0u, 0u, 0u, 0u};
     if (VEC) {
         if (k < n) v = *reinterpret_cast<const u32x4*>(p + k);
-    } else if ((reinterpret_cast<u64>(p + k) & 3u) == 0) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (k + 2 * i + 2 <= n) v[i] = *reinterpret_cast<const u32*>(p + k + 2 * i);
-            else if (k + 2 * i < n) v[i] = p[k + 2 * i];
-        }
+    } else if (k + 8 <= n) {
+        __builtin_memcpy(&v, p + k, 16);                    // one load: the hardware takes any address
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -77,7 +73,7 @@ typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef __attribute__((address_space(3))) void lds_void;
 typedef const __attribute__((address_space(1))) void global_void;
 
-// Tiles with the summed axis along their rows: [rows][64], 16-byte pieces of a row at piece ^ (row & 7), so that the 16 rows of a
+// Tiles with the summed axis along their rows: [rows][64], 16-byte pieces of a row at piece ^ (row & 7), so that eight rows of a
 // fragment lie in different banks although rows are 128 bytes apart.
 __device__ inline u32 along_at(u32 row, u32 piece) { return row * 64 + ((piece ^ (row & 7u)) << 3); }
 __device__ inline u32x4 along_frag(const u16* tile, u32 row0, u32 sub) {        // sub: which 32 of the 64
@@ -91,7 +87,7 @@ __device__ inline u32x4 along_frag(const u16* tile, u32 row0, u32 sub) {        
 template <u32 COLS>
 __device__ inline u32 across_at(u32 k, u32 piece) {
     constexpr u32 kPieces = COLS / 8;
-    const u32 slot = kPieces >= 16 ? ((k & 3u) | ((k >> 1) & 4u)) << 1 : (kPieces >= 8 ? (k & 3u) << 1 : 0u);
+    const u32 slot = kPieces % 16 == 0 ? ((k & 3u) | ((k >> 1) & 4u)) << 1 : (kPieces % 8 == 0 ? (k & 3u) << 1 : (kPieces == 4 ? k & 2u : 0u));
     return k * COLS + ((piece ^ slot) << 3);
 }
 template <u32 COLS>
@@ -110,10 +106,25 @@ __device__ inline u32x4 across_frag(const u16* tile, u32 col0, u32 sub) {
 
 __device__ __align__(256) const u16 g_zeros[64] = {};        // where pieces outside a matrix are read from
 
-// Ends a step whose next tile is on its way into LDS: a barrier alone orders LDS accesses, but loads into LDS count as loads from memory.
-__device__ inline void sync_staged() {
-    __builtin_amdgcn_s_waitcnt(0x0F70);          // vmcnt(0)
-    __syncthreads();
+// Every wavefront's loads into LDS but the last N and all its LDS reads are done, then the workgroup meets.  (A barrier alone orders LDS
+// accesses, but loads into LDS count as loads from memory, and waiting for all of them would wait for tiles that are wanted later.)
+// Nothing is moved across it.
+template <u32 N>
+__device__ inline void meet_loads() {
+    static_assert(N < 64, "the counter has six bits");
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((N & 15u) | (N >> 4 << 14) | 0x0070);      // vmcnt(N), lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// Sixteen bytes a lane from `base` (the same in all lanes) + `offset` straight into LDS, at byte `lds` + 16 * lane.  Written out because the
+// compiler, which cannot tell the tiles of one array apart, would wait for every such load before any LDS read; here meet_loads says
+// what has come.  There is no output register that could be reused while the load is under way.
+__device__ inline void load_lds(u32 offset, const void* base, u32 lds) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(lds) : "memory");
 }
 
 // The adapter of a token; -1 for none and for values outside the list.
@@ -192,13 +203,70 @@ __device__ inline void sort_tokens(const DownArgs& p, u32 a) {
     }
 }
 
+// Sums of 32 tokens and 16 G ranks from r0 on, over the steps of 64 values that are this wavefront's.  ALONG: the narrow matrix is [rank, n_sum]
+// and its fragments come from memory as they are.  Else it is [n_sum, rank]: 64 rows of it go through this wavefront's part of LDS, whose
+// transposing load makes fragments of them.
+template <typename E, bool ALONG, bool VECX, u32 G>
+__device__ inline void down_sums(const DownArgs& p, const u16* xa, const u16* xb, const u16* m, u32 rank, u32 r0, u16* own, f32x4 (&acc)[2][4]) {
+    const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, sub = (lane >> 4) * 8;
+    const u32 steps = (p.n_sum + 63) / 64;
+    constexpr u32 kPieces = ALONG ? 1 : 2 * G;             // 16-byte pieces of 64 rows of 16 G ranks, for each lane
+    auto rows = [&](u32 s, u32x4 (&v)[kPieces]) {
+#pragma unroll
+        for (u32 i = 0; i < kPieces; ++i) {
+            const u32 at = i * 64 + lane, k = at / (2 * G), piece = at % (2 * G);
+            const i64 n = static_cast<i64>(s) * 64 + k;
+            const u16* src = m + n * rank;
+            const i64 end = n < p.n_sum ? rank : 0;
+            v[i] = p.vec_m ? load8<true>(src, r0 + piece * 8, end) : load8<false>(src, r0 + piece * 8, end);
+        }
+    };
+    u32x4 next[kPieces];
+    if (!ALONG && wave < steps) rows(wave, next);
+#pragma unroll 2
+    for (u32 s = wave; s < steps; s += kDownWaves) {
+        const i64 k = static_cast<i64>(s) * 64 + sub;
+        u32x4 fa[2], fb[2], fm[2][G];
+#pragma unroll
+        for (u32 h = 0; h < 2; ++h) { fa[h] = load8<VECX>(xa, k + h * 32, p.n_sum); fb[h] = load8<VECX>(xb, k + h * 32, p.n_sum); }
+        if (ALONG) {
+#pragma unroll
+            for (u32 h = 0; h < 2; ++h)
+#pragma unroll
+                for (u32 g = 0; g < G; ++g) {
+                    const u32 j = r0 + g * 16 + row;           // rows past the rank: the last one again, their sums are not stored
+                    const u16* src = m + static_cast<i64>(j < rank ? j : rank - 1) * p.n_sum;
+                    fm[h][g] = p.vec_m ? load8<true>(src, k + h * 32, p.n_sum) : load8<false>(src, k + h * 32, p.n_sum);
+                }
+        } else {
+#pragma unroll
+            for (u32 i = 0; i < kPieces; ++i) {
+                const u32 at = i * 64 + lane;
+                *reinterpret_cast<u32x4*>(own + across_at<16 * G>(at / (2 * G), at % (2 * G))) = next[i];
+            }
+            if (s + kDownWaves < steps) rows(s + kDownWaves, next);
+#pragma unroll
+            for (u32 h = 0; h < 2; ++h)
+#pragma unroll
+                for (u32 g = 0; g < G; ++g) fm[h][g] = across_frag<16 * G>(own, g * 16, h);
+        }
+#pragma unroll
+        for (u32 h = 0; h < 2; ++h)
+#pragma unroll
+            for (u32 g = 0; g < G; ++g) {
+                acc[0][g] = E::mfma(fa[h], fm[h][g], acc[0][g]);
+                acc[1][g] = E::mfma(fb[h], fm[h][g], acc[1][g]);
+            }
+    }
+}
+
 // z = s x M_a^T for 32 tokens a workgroup, where M_a is the adapter's A [rank, n_sum] (ALONG), or its B [n_sum, rank] in the backward
-// pass.  Reading x bounds it: each row is read once, by eight wavefronts that take every eighth piece of 32 values of it straight into
-// operand registers (nothing of x is shared between wavefronts, so LDS would only add a trip) and add their sums up at the end.
+// pass.  Reading x bounds it: each row is read once, in whole cache lines, by eight wavefronts that take every eighth 64 values of it straight
+// into operand registers (nothing of x is shared between wavefronts, so LDS would only add a trip) and add their sums up at the end.
 // Thirty-two tokens share what is read of M_a.  Tokens of several adapters in one tile are done one adapter after the other.
 template <typename E, bool ALONG, bool VECX>
 __global__ __launch_bounds__(64 * kDownWaves) void k_adapter_down(DownArgs p) {
-    __shared__ __align__(16) float sums[kDownWaves][kDownTokens][kDownRanks];
+    __shared__ __align__(16) float sums[kDownWaves][kDownTokens][kDownRanks];       // or, before, 8 KB of M_a for each wavefront
     const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     if (blockIdx.x >= p.tiles) {                             // uniform
         const u32 a = (blockIdx.x - p.tiles) * kDownWaves + wave;
@@ -213,44 +281,26 @@ __global__ __launch_bounds__(64 * kDownWaves) void k_adapter_down(DownArgs p) {
         const u32 t = t0 + i;
         if (t >= p.n_tokens || __shfl(my_id, static_cast<int>(i), 64) >= 0) continue;
         for (u32 j = lane; j < width; j += 64) {
-            if (j < p.rp) { p.zp[static_cast<u64>(t) * p.rp + j] = 0; if (p.z32) p.z32[static_cast<u64>(t) * p.rp + j] = 0.0f; }
+            if (j < p.rp) { if (p.zp) p.zp[static_cast<u64>(t) * p.rp + j] = 0; if (p.z32) p.z32[static_cast<u64>(t) * p.rp + j] = 0.0f; }
             if (p.z && j < p.ldz) p.z[static_cast<u64>(t) * p.ldz + j] = 0;
         }
     }
-    const u32 steps = (p.n_sum + 31) / 32, row = lane & 15, sub = (lane >> 4) * 8;
-    u32 ta = t0 + row, tb = t0 + 16 + row;
-    if (ta >= p.n_tokens) ta = p.n_tokens - 1;               // their sums are not stored
-    if (tb >= p.n_tokens) tb = p.n_tokens - 1;
-    const u16* xa = p.x + static_cast<i64>(ta) * p.ldx;
+    const u32 row = lane & 15;
+    const u32 ta = t0 + row < p.n_tokens ? t0 + row : p.n_tokens - 1, tb = t0 + 16 + row < p.n_tokens ? t0 + 16 + row : p.n_tokens - 1;
+    const u16* xa = p.x + static_cast<i64>(ta) * p.ldx;      // sums of tokens past the last are not stored
     const u16* xb = p.x + static_cast<i64>(tb) * p.ldx;
+    u16* own = reinterpret_cast<u16*>(&sums[wave][0][0]);
     for (int a = next_adapter(my_id, -1); a != 0x7FFFFFFF; a = next_adapter(my_id, a)) {       // uniform over the workgroup
         const AdapterDesc& d = p.ad[a];
         const u32 rank = d.rank < p.max_rank ? d.rank : p.max_rank;
         const u16* m = ALONG ? d.a : d.b;
-        for (u32 r0 = 0; r0 == 0 || r0 < rank; r0 += kDownRanks) {
+        for (u32 r0 = 0; r0 < rank; r0 += kDownRanks) {
             const u32 ranks = rank - r0 < static_cast<u32>(kDownRanks) ? rank - r0 : static_cast<u32>(kDownRanks);
-            const u32 groups = (ranks + 15) / 16;
+            const u32 groups = ranks <= 16 ? 1 : (ranks <= 32 ? 2 : 4);
             f32x4 acc[2][4] = {};
-            for (u32 s = wave; s < steps; s += kDownWaves) {
-                const i64 k = static_cast<i64>(s) * 32 + sub;
-                const u32x4 fa = load8<VECX>(xa, k, p.n_sum), fb = load8<VECX>(xb, k, p.n_sum);
-#pragma unroll
-                for (u32 g = 0; g < 4; ++g) {
-                    if (g >= groups) continue;               // uniform
-                    const u32 j = r0 + g * 16 + row;
-                    u32x4 fm = {0u, 0u, 0u, 0u};
-                    if (ALONG) {
-                        if (j < rank) fm = p.vec_m ? load8<true>(m + static_cast<i64>(j) * p.n_sum, k, p.n_sum) : load8<false>(m + static_cast<i64>(j) * p.n_sum, k, p.n_sum);
-                    } else if (j < rank) {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            if (k + i < p.n_sum) fm[i >> 1] |= static_cast<u32>(m[(k + i) * rank + j]) << (16 * (i & 1));
-                    }
-                    acc[0][g] = E::mfma(fa, fm, acc[0][g]);
-                    acc[1][g] = E::mfma(fb, fm, acc[1][g]);
-                }
-            }
-            __syncthreads();                                 // the sums of the round before are read
+            if (groups == 1)      down_sums<E, ALONG, VECX, 1>(p, xa, xb, m, rank, r0, own, acc);
+            else if (groups == 2) down_sums<E, ALONG, VECX, 2>(p, xa, xb, m, rank, r0, own, acc);
+            else                  down_sums<E, ALONG, VECX, 4>(p, xa, xb, m, rank, r0, own, acc);
 #pragma unroll
             for (u32 h = 0; h < 2; ++h)
 #pragma unroll
@@ -274,7 +324,7 @@ __global__ __launch_bounds__(64 * kDownWaves) void k_adapter_down(DownArgs p) {
                         v *= d.scale;
                     }
                     const u16 h = E::enc(v);
-                    if (j < p.rp) { p.zp[t * p.rp + j] = h; if (p.z32) p.z32[t * p.rp + j] = v; }
+                    if (j < p.rp) { if (p.zp) p.zp[t * p.rp + j] = h; if (p.z32) p.z32[t * p.rp + j] = v; }
                     if (p.z && j < p.ldz) p.z[t * p.ldz + j] = h;
                     const u32 u = __float_as_uint(v) & 0x7FFFFFFFu;
                     if (u < 0x7F800000u) most = most > u ? most : u;
@@ -291,6 +341,7 @@ __global__ __launch_bounds__(64 * kDownWaves) void k_adapter_down(DownArgs p) {
                     }
                 }
             }
+            __syncthreads();                                 // before the sums are overwritten
         }
     }
 }
@@ -308,6 +359,8 @@ struct WideArgs {
     u32 n_adapters, max_rank;
     u32 vec_m;                           // 16-byte aligned rows of the adapters' matrix
     u32 vec_y;                           // 8-byte aligned groups of four outputs
+    u32 splits, steps_each;              // steps of 64 values that a split sums
+    float* part;                         // splits > 1: [splits][n_tokens][n_out]
 };
 
 // Workgroups go round the eight dies one by one; this gives each die a run of neighbouring tiles, whose rows its cache keeps.
@@ -316,199 +369,256 @@ __device__ inline u32 die_order(u32 i, u32 n) {
     return die * each + (die < more ? die : more) + k;
 }
 
-// Tiles of BM tokens by BN outputs, summed 64 values a step.
-template <typename E, int BM, int BN, int WM, int WN, bool ALONG, bool VEC>
-__global__ __launch_bounds__(64 * WM * WN) void k_adapter_wide(WideArgs p) {
+// Tiles of BM tokens by BN outputs, summed 64 values a step (whole cache lines of x), NB steps in LDS.  VEC: loads go straight into LDS, up to
+// NB steps ahead of their use.  A fragment register is read again as soon as its last product has begun, half a step ahead, so that the
+// matrix instructions wait for neither LDS nor memory; wavefronts meet once a step, in its middle, where the next step has come and the
+// last read of this one is done.  Otherwise (rows that are not 16-byte aligned) steps go through registers.
+// splits > 1: a workgroup sums a part of the steps and stores it in binary32; the adapters' share is then added with the parts.
+template <typename E, int BM, int BN, int WM, int WN, u32 NB, bool ALONG, bool VEC>
+__global__ __launch_bounds__(64 * WM * WN, 2) void k_adapter_wide(WideArgs p) {
     constexpr u32 kThreads = 64 * WM * WN;
     constexpr u32 TM = BM / WM, TN = BN / WN, FM = TM / 16, FN = TN / 16;
-    constexpr u32 kXPieces = BM * 8 / kThreads, kWPieces = BN * 8 / kThreads;
-    __shared__ __align__(16) u16 sx0[BM * 64], sw0[BN * 64], sx1[BM * 64], sw1[BN * 64];
+    constexpr u32 kXPieces = BM * 8 / kThreads, kWPieces = BN * 8 / kThreads, kLoads = kXPieces + kWPieces;
+    constexpr u32 kTile = (BM + BN) * 64, kEarly = FN < FM ? FN : FN / 2, kEach = FN / kEarly;
+    __shared__ __align__(16) u16 tiles[NB * kTile];
     __shared__ int s_ids[BM];
-    const u32 tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const u32 tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const u32 wm = wave / WN, wn = wave % WN;
-    const u32 tiles_n = (p.n_out + BN - 1) / BN;
-    const u32 tile = die_order(blockIdx.x, gridDim.x);
-    const u32 t0 = tile / tiles_n * BM, n0 = tile % tiles_n * BN;
+    const u32 tiles_m = (p.n_tokens + BM - 1) / BM, tiles_n = (p.n_out + BN - 1) / BN;
+    const u32 block = die_order(blockIdx.x, gridDim.x);
+    const u32 tile = block / p.splits, split = block % p.splits;
+    // four rows of tiles at a time: tiles that run together share rows of x and of W
+    const u32 band = tile / (4 * tiles_n), in_band = tile % (4 * tiles_n), high = tiles_m - band * 4 < 4 ? tiles_m - band * 4 : 4;
+    const u32 t0 = (band * 4 + in_band % high) * BM, n0 = in_band / high * BN;
+    const u32 all_steps = (p.n_sum + 63) / 64;
+    const u32 begin = split * p.steps_each, end = begin + p.steps_each < all_steps ? begin + p.steps_each : all_steps;
+    const u32 steps = end > begin ? end - begin : 0;
     f32x4 acc[FN][FM] = {};
+    u32x4 fx[FM], fw[FN];
 
-    auto x_src = [&](u32 i, u32 k0) -> const u16* {            // piece i of this thread in step k0, or nullptr outside
-        const u32 at = i * kThreads + tid, row = at >> 3, piece = (at & 7u) ^ (row & 7u);
-        u32 t = t0 + row;
-        if (t >= p.n_tokens) t = p.n_tokens - 1;
-        return p.x + static_cast<i64>(t) * p.ldx + k0 + piece * 8;
+    auto frag_x = [&](const u16* sx, u32 j, u32 sub) { return along_frag(sx, wm * TM + j * 16, sub); };
+    auto frag_w = [&](const u16* sx, u32 i, u32 sub) {
+        return ALONG ? along_frag(sx + BM * 64, wn * TN + i * 16, sub) : across_frag<BN>(sx + BM * 64, wn * TN + i * 16, sub);
     };
-    auto stage = [&](u16* sx, u16* sw, u32 k0) {               // VEC: straight into LDS, 16 bytes a lane
+
+    for (u32 i = tid; i < BM; i += kThreads) s_ids[i] = adapter_of(p.ids, t0 + i, p.n_tokens, p.n_adapters);
+    bool rest = false;                                             // a last step that ends past the sum is left
+    if (VEC) {
+        u32 xo[kXPieces], wo[kWPieces];                            // byte offsets of this lane's pieces
 #pragma unroll
         for (u32 i = 0; i < kXPieces; ++i) {
-            const u32 at = i * kThreads + tid, piece = (at & 7u) ^ ((at >> 3) & 7u);
-            const u16* src = k0 + piece * 8 < p.n_sum ? x_src(i, k0) : g_zeros;
-            __builtin_amdgcn_global_load_lds((global_void*)src, (lds_void*)(sx + (i * kThreads + wave * 64) * 8), 16, 0, 0);
+            const u32 at = i * kThreads + tid, row = at >> 3, piece = (at & 7u) ^ (row & 7u);
+            const u32 r = t0 + row < p.n_tokens ? row : p.n_tokens - 1 - t0;
+            xo[i] = (r * static_cast<u32>(p.ldx) + piece * 8) * 2;
         }
 #pragma unroll
         for (u32 i = 0; i < kWPieces; ++i) {
             const u32 at = i * kThreads + tid;
-            const u16* src;
             if (ALONG) {
                 const u32 row = at >> 3, piece = (at & 7u) ^ (row & 7u);
-                u32 n = n0 + row;
-                if (n >= p.n_out) n = p.n_out - 1;
-                src = k0 + piece * 8 < p.n_sum ? p.w + static_cast<i64>(n) * p.ldw + k0 + piece * 8 : g_zeros;
-            } else {
-                constexpr u32 kRow = BN / 8;
-                const u32 k = at / kRow, piece = ((across_at<BN>(k, at % kRow) - k * BN) >> 3);
-                src = k0 + k < p.n_sum && n0 + piece * 8 < p.n_out ? p.w + static_cast<i64>(k0 + k) * p.ldw + n0 + piece * 8 : g_zeros;
-            }
-            __builtin_amdgcn_global_load_lds((global_void*)src, (lds_void*)(sw + (i * kThreads + wave * 64) * 8), 16, 0, 0);
-        }
-    };
-    u32x4 rx[VEC ? 1 : kXPieces], rw[VEC ? 1 : kWPieces];
-    auto fetch = [&](u32 k0) {                                 // not VEC: through registers
-#pragma unroll
-        for (u32 i = 0; i < kXPieces; ++i) {
-            const u32 at = i * kThreads + tid, row = at >> 3, piece = at & 7u;
-            u32 t = t0 + row;
-            if (t >= p.n_tokens) t = p.n_tokens - 1;
-            rx[VEC ? 0 : i] = load8<false>(p.x + static_cast<i64>(t) * p.ldx, k0 + piece * 8, p.n_sum);
-        }
-#pragma unroll
-        for (u32 i = 0; i < kWPieces; ++i) {
-            const u32 at = i * kThreads + tid;
-            if (ALONG) {
-                u32 n = n0 + (at >> 3);
-                if (n >= p.n_out) n = p.n_out - 1;
-                rw[VEC ? 0 : i] = load8<false>(p.w + static_cast<i64>(n) * p.ldw, k0 + (at & 7u) * 8, p.n_sum);
+                const u32 r = n0 + row < p.n_out ? row : p.n_out - 1 - n0;
+                wo[i] = (r * static_cast<u32>(p.ldw) + piece * 8) * 2;
             } else {
                 constexpr u32 kRow = BN / 8;
                 const u32 k = at / kRow;
-                rw[VEC ? 0 : i] = k0 + k < p.n_sum ? load8<false>(p.w + static_cast<i64>(k0 + k) * p.ldw, n0 + (at % kRow) * 8, p.n_out) : u32x4{0u, 0u, 0u, 0u};
+                u32 col = across_at<BN>(k, at % kRow) - k * BN;
+                if (n0 + col >= p.n_out) col = p.n_out - 8 - n0;
+                wo[i] = (k * static_cast<u32>(p.ldw) + col) * 2;
             }
         }
-    };
-    auto put = [&](u16* sx, u16* sw) {
+        const u32 full = begin + steps == all_steps && (p.n_sum & 63u) ? steps - 1 : steps;
+        rest = full < steps;
+        const char* xs = reinterpret_cast<const char*>(p.x + static_cast<i64>(t0) * p.ldx + begin * 64);
+        const char* ws = reinterpret_cast<const char*>(ALONG ? p.w + static_cast<i64>(n0) * p.ldw + begin * 64 : p.w + static_cast<i64>(begin) * 64 * p.ldw + n0);
+        const i64 w_step = (ALONG ? 64 : 64 * p.ldw) * 2;
+        const u32 lds0 = static_cast<u32>(reinterpret_cast<uintptr_t>((lds_void*)tiles)) + wave * 1024;
+        u32 loaded = 0, to = 0;
+        auto load = [&]() {                                        // the next step, or the last one again
 #pragma unroll
-        for (u32 i = 0; i < kXPieces; ++i) {
-            const u32 at = i * kThreads + tid;
-            *reinterpret_cast<u32x4*>(sx + along_at(at >> 3, at & 7u)) = rx[VEC ? 0 : i];
-        }
+            for (u32 i = 0; i < kXPieces; ++i) load_lds(xo[i], xs, lds0 + to + i * kThreads * 16);
 #pragma unroll
-        for (u32 i = 0; i < kWPieces; ++i) {
-            const u32 at = i * kThreads + tid;
-            const u32 to = ALONG ? along_at(at >> 3, at & 7u) : across_at<BN>(at / (BN / 8), at % (BN / 8));
-            *reinterpret_cast<u32x4*>(sw + to) = rw[VEC ? 0 : i];
-        }
-    };
-    auto multiply = [&](const u16* sx, const u16* sw) {
-#pragma unroll
-        for (u32 sub = 0; sub < 2; ++sub) {
-            u32x4 fx[FM], fw[FN];
-#pragma unroll
-            for (u32 i = 0; i < FM; ++i) fx[i] = along_frag(sx, wm * TM + i * 16, sub);
-#pragma unroll
-            for (u32 i = 0; i < FN; ++i) fw[i] = ALONG ? along_frag(sw, wn * TN + i * 16, sub) : across_frag<BN>(sw, wn * TN + i * 16, sub);
-#pragma unroll
-            for (u32 i = 0; i < FN; ++i)
-#pragma unroll
-                for (u32 j = 0; j < FM; ++j) acc[i][j] = E::mfma(fw[i], fx[j], acc[i][j]);
-        }
-    };
-
-    // The adapter's product is added where the token is the adapter's and nowhere else: zeros in its place would spread infinities and
-    // NaN of one request's adapter to its neighbours.
-    auto multiply_own = [&](const u16* sx, const u16* sw, u32 subs, int a) {
-#pragma unroll
-        for (u32 sub = 0; sub < 2; ++sub) {
-            if (sub >= subs) continue;
-            u32x4 fw[FN];
-#pragma unroll
-            for (u32 i = 0; i < FN; ++i) fw[i] = ALONG ? along_frag(sw, wn * TN + i * 16, sub) : across_frag<BN>(sw, wn * TN + i * 16, sub);
+            for (u32 i = 0; i < kWPieces; ++i) load_lds(wo[i], ws, lds0 + to + BM * 128 + i * kThreads * 16);
+            ++loaded;
+            const bool more = loaded < full;
+            xs += more ? 128 : 0;
+            ws += more ? w_step : 0;
+            to = to + kTile * 2 == NB * kTile * 2 ? 0 : to + kTile * 2;
+        };
+        // products of the fragments in registers, which are replaced by those of half `sub` of the tile at `sx`
+        auto half = [&](const u16* sx, u32 sub) {
+            u32x4 next[FN];
 #pragma unroll
             for (u32 j = 0; j < FM; ++j) {
-                const bool mine = s_ids[wm * TM + j * 16 + (lane & 15)] == a;
-                const u32x4 fx = along_frag(sx, wm * TM + j * 16, sub);
+#pragma unroll
+                for (u32 i = 0; i < FN; ++i) acc[i][j] = E::mfma(fw[i], fx[j], acc[i][j]);
+                fx[j] = frag_x(sx, j, sub);
+                if (j < kEarly) {                                  // what the next half's first product waits for comes first
+#pragma unroll
+                    for (u32 i = j * kEach; i < (j + 1) * kEach; ++i) next[i] = frag_w(sx, i, sub);
+                    __builtin_amdgcn_sched_group_barrier(0x008, FN, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1 + kEach * (ALONG ? 1 : 2), 0);
+                } else {
+                    __builtin_amdgcn_sched_group_barrier(0x008, FN, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                }
+            }
+#pragma unroll
+            for (u32 i = 0; i < FN; ++i) fw[i] = next[i];
+        };
+        if (full > 0) {
+#pragma unroll
+            for (u32 i = 0; i < NB; ++i) load();
+            meet_loads<(NB - 1) * kLoads>();
+#pragma unroll
+            for (u32 i = 0; i < FN; ++i) fw[i] = frag_w(tiles, i, 0);
+#pragma unroll
+            for (u32 j = 0; j < FM; ++j) fx[j] = frag_x(tiles, j, 0);
+            u32 from = 0;
+            for (u32 s = 0; s < full; ++s) {
+                half(tiles + from, 1);
+                meet_loads<(NB - 2) * kLoads>();
+                load();                                            // where this step was
+                from = from + kTile == NB * kTile ? 0 : from + kTile;
+                half(tiles + from, 0);
+            }
+            meet_loads<0>();
+        }
+    } else {
+        u32x4 rx[kXPieces], rw[kWPieces];
+        auto fetch = [&](u32 s) {
+            const i64 k0 = static_cast<i64>(s) * 64;
+#pragma unroll
+            for (u32 i = 0; i < kXPieces; ++i) {
+                const u32 at = i * kThreads + tid, t = t0 + (at >> 3) < p.n_tokens ? t0 + (at >> 3) : p.n_tokens - 1;
+                rx[i] = load8<false>(p.x + static_cast<i64>(t) * p.ldx, k0 + (at & 7u) * 8, p.n_sum);
+            }
+#pragma unroll
+            for (u32 i = 0; i < kWPieces; ++i) {
+                const u32 at = i * kThreads + tid;
+                if (ALONG) {
+                    const u32 n = n0 + (at >> 3) < p.n_out ? n0 + (at >> 3) : p.n_out - 1;
+                    rw[i] = load8<false>(p.w + static_cast<i64>(n) * p.ldw, k0 + (at & 7u) * 8, p.n_sum);
+                } else {
+                    constexpr u32 kRow = BN / 8;
+                    const i64 k = k0 + at / kRow;
+                    rw[i] = load8<false>(p.w + k * p.ldw, n0 + (at % kRow) * 8, k < p.n_sum ? p.n_out : 0);
+                }
+            }
+        };
+        if (steps > 0) fetch(begin);
+        u32 to = 0;
+        for (u32 s = begin; s < end; ++s) {
+            u16* sx = tiles + to;
+#pragma unroll
+            for (u32 i = 0; i < kXPieces; ++i) {
+                const u32 at = i * kThreads + tid;
+                *reinterpret_cast<u32x4*>(sx + along_at(at >> 3, at & 7u)) = rx[i];
+            }
+#pragma unroll
+            for (u32 i = 0; i < kWPieces; ++i) {
+                const u32 at = i * kThreads + tid;
+                const u32 w_at = ALONG ? along_at(at >> 3, at & 7u) : across_at<BN>(at / (BN / 8), at % (BN / 8));
+                *reinterpret_cast<u32x4*>(sx + BM * 64 + w_at) = rw[i];
+            }
+            __syncthreads();
+            if (s + 1 < end) fetch(s + 1);
+#pragma unroll
+            for (u32 sub = 0; sub < 2; ++sub) {
+#pragma unroll
+                for (u32 i = 0; i < FN; ++i) fw[i] = frag_w(sx, i, sub);
+#pragma unroll
+                for (u32 j = 0; j < FM; ++j) fx[j] = frag_x(sx, j, sub);
+#pragma unroll
+                for (u32 j = 0; j < FM; ++j)
+#pragma unroll
+                    for (u32 i = 0; i < FN; ++i) acc[i][j] = E::mfma(fw[i], fx[j], acc[i][j]);
+            }
+            to = to == 0 ? kTile : 0;                              // the one that all have read since the barrier before this one
+        }
+    }
+    __syncthreads();
+
+    // What is left of the sum, then the adapters' share: 64 values of rank for each adapter that the tile's tokens have.  A product is added
+    // where the token is the adapter's and nowhere else: zeros in its place would spread infinities and NaN of one request's adapter to its
+    // neighbours.
+    int a = -1;
+    u32 r0 = 0, rank = 0;
+    const u16* m = nullptr;
+    for (;;) {                                                     // uniform
+        if (!rest) {
+            if (p.splits > 1) break;                               // added with the parts
+            r0 += 64;
+            if (r0 >= rank) {
+                int next = 0x7FFFFFFF;
+                for (u32 i = lane; i < BM; i += 64) {
+                    const int id = s_ids[i];
+                    if (id > a && id < next) next = id;
+                }
+                a = next_adapter(next, -1);                        // the same in every wavefront
+                if (a == 0x7FFFFFFF) break;
+                const AdapterDesc& d = p.ad[a];
+                rank = d.rank < p.max_rank ? d.rank : p.max_rank;
+                m = ALONG ? d.b : d.a;
+                r0 = 0;
+            }
+        }
+        const i64 k0 = rest ? static_cast<i64>(all_steps - 1) * 64 : r0;
+        const i64 k_end = rest ? p.n_sum : rank;
+        const u32 subs = k_end - k0 > 32 ? 2 : 1;
+        const u16* x = rest ? p.x : p.zp;
+        const i64 ldx = rest ? p.ldx : static_cast<i64>(p.rp), x_end = rest ? p.n_sum : p.rp;
+        for (u32 at = tid; at < BM * 8; at += kThreads) {
+            const u32 row = at >> 3, piece = at & 7u, t = t0 + row < p.n_tokens ? t0 + row : p.n_tokens - 1;
+            if (piece < subs * 4) *reinterpret_cast<u32x4*>(tiles + along_at(row, piece)) = load8<true>(x + static_cast<i64>(t) * ldx, k0 + piece * 8, x_end);
+        }
+        const u16* w = rest ? p.w : m;
+        const i64 ldw = rest ? p.ldw : (ALONG ? static_cast<i64>(rank) : static_cast<i64>(p.n_out));
+        const bool vec_w = rest || p.vec_m;
+        for (u32 at = tid; at < BN * 8; at += kThreads) {
+            const u32 row = ALONG ? at >> 3 : at / (BN / 8), piece = ALONG ? at & 7u : at % (BN / 8);
+            if ((ALONG ? piece >> 2 : row >> 5) >= subs) continue;
+            const u16* src = ALONG ? w + static_cast<i64>(n0 + row < p.n_out ? n0 + row : p.n_out - 1) * ldw : w + (k0 + row) * ldw;
+            const i64 from = ALONG ? k0 + piece * 8 : n0 + piece * 8, end_at = ALONG ? k_end : (k0 + row < k_end ? p.n_out : 0);
+            const u32x4 v = vec_w ? load8<true>(src, from, end_at) : load8<false>(src, from, end_at);
+            *reinterpret_cast<u32x4*>(tiles + BM * 64 + (ALONG ? along_at(row, piece) : across_at<BN>(row, piece))) = v;
+        }
+        __syncthreads();
+        for (u32 sub = 0; sub < subs; ++sub) {
+#pragma unroll
+            for (u32 i = 0; i < FN; ++i) fw[i] = frag_w(tiles, i, sub);
+#pragma unroll
+            for (u32 j = 0; j < FM; ++j) {
+                fx[0] = frag_x(tiles, j, sub);
+                const bool mine = rest || s_ids[wm * TM + j * 16 + (lane & 15)] == a;
 #pragma unroll
                 for (u32 i = 0; i < FN; ++i) {
-                    const f32x4 v = E::mfma(fw[i], fx, f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+                    const f32x4 v = E::mfma(fw[i], fx[0], f32x4{0.0f, 0.0f, 0.0f, 0.0f});
 #pragma unroll
                     for (u32 k = 0; k < 4; ++k) acc[i][j][k] = mine ? acc[i][j][k] + v[k] : acc[i][j][k];
                 }
             }
         }
-    };
-
-    for (u32 i = tid; i < BM; i += kThreads) s_ids[i] = adapter_of(p.ids, t0 + i, p.n_tokens, p.n_adapters);
-    if (VEC) {
-        stage(sx0, sw0, 0);
-        sync_staged();
-        for (u32 k0 = 0; k0 < p.n_sum; k0 += 128) {
-            if (k0 + 64 < p.n_sum) stage(sx1, sw1, k0 + 64);
-            multiply(sx0, sw0);
-            sync_staged();
-            if (k0 + 64 < p.n_sum) {
-                if (k0 + 128 < p.n_sum) stage(sx0, sw0, k0 + 128);
-                multiply(sx1, sw1);
-                sync_staged();
-            }
-        }
-    } else {
-        fetch(0);
-        for (u32 k0 = 0; k0 < p.n_sum; k0 += 64) {
-            put(sx0, sw0);
-            __syncthreads();
-            if (k0 + 64 < p.n_sum) fetch(k0 + 64);
-            multiply(sx0, sw0);
-            __syncthreads();
-        }
+        __syncthreads();
+        rest = false;
     }
 
-    // the adapters' share: one more step of the sum for each adapter that the tile's tokens have
-    __syncthreads();
-    int last = -1;
-    for (;;) {
-        int a = 0x7FFFFFFF;
-        for (u32 i = lane; i < BM; i += 64) {
-            const int id = s_ids[i];
-            if (id > last && id < a) a = id;
-        }
-        a = next_adapter(a, -1);                               // the same in every wavefront
-        if (a == 0x7FFFFFFF) break;
-        last = a;
-        const AdapterDesc& d = p.ad[a];
-        const u32 rank = d.rank < p.max_rank ? d.rank : p.max_rank;
-        const u16* m = ALONG ? d.b : d.a;
-        for (u32 r0 = 0; r0 < rank; r0 += 64) {
-            const u32 subs = rank - r0 > 32 ? 2 : 1;
-            for (u32 at = tid; at < BM * 8; at += kThreads) {
-                const u32 row = at >> 3, piece = at & 7u;
-                if (piece >= subs * 4) continue;
-                u32x4 v = {0u, 0u, 0u, 0u};
-                if (s_ids[row] == a) v = load8<true>(p.zp + static_cast<u64>(t0 + row) * p.rp, r0 + piece * 8, p.rp);
-                *reinterpret_cast<u32x4*>(sx0 + along_at(row, piece)) = v;
+    if (p.splits > 1) {                                            // uniform
+        float* part = p.part + static_cast<u64>(split) * p.n_tokens * p.n_out;
+#pragma unroll
+        for (u32 j = 0; j < FM; ++j) {
+            const u32 t = t0 + wm * TM + j * 16 + (lane & 15);
+            if (t >= p.n_tokens) continue;
+            float* out = part + static_cast<u64>(t) * p.n_out;
+#pragma unroll
+            for (u32 i = 0; i < FN; ++i) {
+                const u32 n = n0 + wn * TN + i * 16 + (lane >> 4) * 4;
+                if ((p.n_out & 3u) == 0 && n + 4 <= p.n_out) *reinterpret_cast<f32x4*>(out + n) = acc[i][j];
+                else
+#pragma unroll
+                    for (u32 k = 0; k < 4; ++k) if (n + k < p.n_out) out[n + k] = acc[i][j][k];
             }
-            for (u32 at = tid; at < BN * 8; at += kThreads) {
-                u32x4 v = {0u, 0u, 0u, 0u};
-                if (ALONG) {
-                    const u32 row = at >> 3, piece = at & 7u;
-                    if (piece >= subs * 4) continue;
-                    if (n0 + row < p.n_out) {
-                        const u16* src = m + static_cast<i64>(n0 + row) * rank;
-                        v = p.vec_m ? load8<true>(src, r0 + piece * 8, rank) : load8<false>(src, r0 + piece * 8, rank);
-                    }
-                    *reinterpret_cast<u32x4*>(sw0 + along_at(row, piece)) = v;
-                } else {
-                    constexpr u32 kRow = BN / 8;
-                    const u32 k = at / kRow, piece = at % kRow;
-                    if (k >= subs * 32) continue;
-                    if (r0 + k < rank) {
-                        const u16* src = m + static_cast<i64>(r0 + k) * p.n_out;
-                        v = p.vec_m ? load8<true>(src, n0 + piece * 8, p.n_out) : load8<false>(src, n0 + piece * 8, p.n_out);
-                    }
-                    *reinterpret_cast<u32x4*>(sw0 + across_at<BN>(k, piece)) = v;
-                }
-            }
-            __syncthreads();
-            multiply_own(sx0, sw0, subs, a);
-            __syncthreads();
         }
+        return;
     }
 
 #pragma unroll
@@ -680,15 +790,19 @@ struct GradArgs {
     float* part;                         // [n_slots][max_rank (n_in + n_out)]
 };
 
-constexpr u32 kGradCols = 128, kGradStep = 64;
+constexpr u32 kGradCols = 128, kGradStep = 64, kGradTokens = 1024;
 
-// One run of one adapter's tokens times 128 columns of x or of dy: 64 tokens a step, both operands across the rows of their tiles.
-// dz enters as the sum of two 16-bit values, so that a binary32 gradient keeps 16 bits of it (22 with float16) and not 8; runs of
-// float16 are scaled by a power of two first, so that the largest dz of the run sits near the top of the type's range.
+// One run of one adapter's tokens times 128 columns of x or of dy: 64 tokens a step, both operands across the rows of their tiles, the next
+// step's rows on their way while this one's are multiplied.  Reading x and dy once more bounds it; the columns are split and not the ranks,
+// so that they are read by one workgroup only (up to 64 ranks).  dz enters as a sum of 16-bit values, three of bfloat16 or two of
+// float16, since a binary32 gradient would keep no more than 8 or 11 bits of one; runs of float16 are scaled by a power of two first, so that the
+// largest dz of the run sits near the top of the type's range.
 template <typename E, bool VEC>
 __global__ __launch_bounds__(256) void k_adapter_grads(GradArgs p) {
-    __shared__ __align__(16) u16 sv[kGradStep * kGradCols], su[kGradStep * 64], sl[kGradStep * 64];
-    __shared__ u32 s_tok[kGradStep];
+    constexpr u32 kTerms = E::kNarrow ? 2 : 3;
+    constexpr u32 kVPieces = kGradStep * kGradCols / 8 / 256, kUPieces = kGradStep * 8 / 256;
+    __shared__ __align__(16) u16 sv[kGradStep * kGradCols], su[kTerms][kGradStep * 64];
+    __shared__ u32 s_tok[kGradTokens];
     __shared__ u32 s_max;
     const u32 tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const u32 slot = blockIdx.x / p.tiles, col_tile = blockIdx.x % p.tiles, r0 = blockIdx.y * 64;
@@ -705,6 +819,7 @@ __global__ __launch_bounds__(256) void k_adapter_grads(GradArgs p) {
     const u32 n_cols = of_a ? p.n_in : p.n_out;
     const u16* v_src = of_a ? p.x : p.dy;
     const i64 ldv = of_a ? p.ldx : p.ldy;
+    const u32 pieces = (rank - r0 < 64 ? rank - r0 + 7 : 64) / 8;             // of eight ranks
     float up = 1.0f, down = 1.0f;
     if (E::kNarrow && of_a) {
         if (tid == 0) s_max = 0;
@@ -719,58 +834,89 @@ __global__ __launch_bounds__(256) void k_adapter_grads(GradArgs p) {
         down = __uint_as_float(static_cast<u32>(127 - e) << 23);
     }
     f32x4 acc[2][4] = {};
-    for (u32 s = 0; s < count; s += kGradStep) {
+    for (u32 c = 0; c < count; c += kGradTokens) {
+        const u32 here = count - c < kGradTokens ? count - c : kGradTokens;
         __syncthreads();
-        if (tid < kGradStep) s_tok[tid] = s + tid < count ? p.order[first + s + tid] : ~0u;
+        for (u32 i = tid; i < here; i += 256) s_tok[i] = p.order[first + c + i];
         __syncthreads();
+        u32x4 rv[kVPieces], ru[2 * kUPieces];
+        auto fetch = [&](u32 s) {
 #pragma unroll
-        for (u32 i = 0; i < kGradStep * kGradCols / 8 / 256; ++i) {
-            const u32 at = i * 256 + tid, k = at / (kGradCols / 8), piece = at % (kGradCols / 8), t = s_tok[k];
-            u32x4 v = {0u, 0u, 0u, 0u};
-            if (t != ~0u) v = load8<VEC>(v_src + static_cast<i64>(t) * ldv, c0 + piece * 8, n_cols);
-            *reinterpret_cast<u32x4*>(sv + across_at<kGradCols>(k, piece)) = v;
-        }
-        for (u32 at = tid; at < kGradStep * 8; at += 256) {
-            const u32 k = at >> 3, piece = at & 7u, t = s_tok[k], c = r0 + piece * 8;
-            u32x4 hi = {0u, 0u, 0u, 0u}, lo = {0u, 0u, 0u, 0u};
-            if (t != ~0u && c < rank) {
-                if (of_a) {
-                    const float* src = p.dz + static_cast<u64>(t) * p.rp + c;        // zeros past the rank
+            for (u32 i = 0; i < kVPieces; ++i) {
+                const u32 at = i * 256 + tid, k = s + at / (kGradCols / 8), piece = at % (kGradCols / 8);
+                rv[i] = u32x4{0u, 0u, 0u, 0u};
+                if (k < here) rv[i] = load8<VEC>(v_src + static_cast<i64>(s_tok[k]) * ldv, c0 + piece * 8, n_cols);
+            }
 #pragma unroll
-                    for (u32 i = 0; i < 8; ++i) {
-                        const float f = src[i] * up;
-                        const u16 h = E::enc(f);
-                        const float rest = f - E::dec(h);
-                        const u16 l = __builtin_fabsf(rest) < INFINITY ? E::enc(rest) : static_cast<u16>(0);
-                        hi[i >> 1] |= static_cast<u32>(h) << (16 * (i & 1));
-                        lo[i >> 1] |= static_cast<u32>(l) << (16 * (i & 1));
+            for (u32 i = 0; i < kUPieces; ++i) {
+                const u32 at = i * 256 + tid, k = s + (at >> 3), piece = at & 7u;
+                ru[2 * i] = ru[2 * i + 1] = u32x4{0u, 0u, 0u, 0u};
+                if (k < here && piece < pieces) {
+                    if (of_a) {                                // rows of rp values, zeros past the rank
+                        const u32x4* src = reinterpret_cast<const u32x4*>(p.dz + static_cast<u64>(s_tok[k]) * p.rp + r0 + piece * 8);
+                        ru[2 * i] = src[0];
+                        ru[2 * i + 1] = src[1];
+                    } else {
+                        ru[2 * i] = load8<false>(p.z + static_cast<i64>(s_tok[k]) * p.ldz, r0 + piece * 8, rank);
                     }
-                } else {
-                    hi = load8<false>(p.z + static_cast<i64>(t) * p.ldz, c, rank);
                 }
             }
-            *reinterpret_cast<u32x4*>(su + across_at<64>(k, piece)) = hi;
-            if (of_a) *reinterpret_cast<u32x4*>(sl + across_at<64>(k, piece)) = lo;
-        }
-        __syncthreads();
+        };
+        fetch(0);
+        for (u32 s = 0; s < here; s += kGradStep) {
 #pragma unroll
-        for (u32 sub = 0; sub < 2; ++sub) {
-            u32x4 fv[2];
+            for (u32 i = 0; i < kVPieces; ++i) {
+                const u32 at = i * 256 + tid;
+                *reinterpret_cast<u32x4*>(sv + across_at<kGradCols>(at / (kGradCols / 8), at % (kGradCols / 8))) = rv[i];
+            }
 #pragma unroll
-            for (u32 i = 0; i < 2; ++i) fv[i] = across_frag<kGradCols>(sv, wave * 32 + i * 16, sub);
-#pragma unroll
-            for (u32 g = 0; g < 4; ++g) {
-                if (r0 + g * 16 >= rank) continue;
-                const u32x4 fu = across_frag<64>(su, g * 16, sub);
+            for (u32 i = 0; i < kUPieces; ++i) {
+                const u32 at = i * 256 + tid, to = across_at<64>(at >> 3, at & 7u);
+                if ((at & 7u) >= ((pieces + 1) & ~1u)) continue;       // no fragment reads it
                 if (of_a) {
-                    const u32x4 fl = across_frag<64>(sl, g * 16, sub);
+                    u32x4 term[kTerms] = {};
 #pragma unroll
-                    for (u32 i = 0; i < 2; ++i) acc[i][g] = E::mfma(fv[i], fl, E::mfma(fv[i], fu, acc[i][g]));
+                    for (u32 q = 0; q < 8; ++q) {
+                        float f = __uint_as_float(ru[2 * i + (q >> 2)][q & 3u]) * up;
+#pragma unroll
+                        for (u32 t = 0; t < kTerms; ++t) {
+                            const u16 h = E::enc(f);
+                            term[t][q >> 1] |= static_cast<u32>(h) << (16 * (q & 1u));
+                            f -= E::dec(h);
+                            f = __builtin_fabsf(f) < INFINITY ? f : 0.0f;
+                        }
+                    }
+#pragma unroll
+                    for (u32 t = 0; t < kTerms; ++t) *reinterpret_cast<u32x4*>(su[t] + to) = term[t];
                 } else {
-#pragma unroll
-                    for (u32 i = 0; i < 2; ++i) acc[i][g] = E::mfma(fu, fv[i], acc[i][g]);
+                    *reinterpret_cast<u32x4*>(su[0] + to) = ru[2 * i];
                 }
             }
+            __syncthreads();
+            if (s + kGradStep < here) fetch(s + kGradStep);
+#pragma unroll
+            for (u32 sub = 0; sub < 2; ++sub) {
+                u32x4 fv[2];
+#pragma unroll
+                for (u32 i = 0; i < 2; ++i) fv[i] = across_frag<kGradCols>(sv, wave * 32 + i * 16, sub);
+#pragma unroll
+                for (u32 g = 0; g < 4; ++g) {
+                    if (r0 + g * 16 >= rank) continue;
+                    if (of_a) {
+#pragma unroll
+                        for (u32 t = kTerms; t-- > 0;) {
+                            const u32x4 fu = across_frag<64>(su[t], g * 16, sub);
+#pragma unroll
+                            for (u32 i = 0; i < 2; ++i) acc[i][g] = E::mfma(fv[i], fu, acc[i][g]);
+                        }
+                    } else {
+                        const u32x4 fu = across_frag<64>(su[0], g * 16, sub);
+#pragma unroll
+                        for (u32 i = 0; i < 2; ++i) acc[i][g] = E::mfma(fu, fv[i], acc[i][g]);
+                    }
+                }
+            }
+            __syncthreads();
         }
     }
     const bool whole = seg.y <= p.run;
