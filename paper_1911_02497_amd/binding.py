@@ -6,6 +6,7 @@ from __future__ import annotations
 
 import array
 import ctypes
+import functools
 import os
 from typing import Dict, List, Optional, Sequence
 
@@ -181,7 +182,7 @@ def library() -> ctypes.CDLL:
 
 
 def _check(code: int) -> None:
-    if code != 0:
+    if code:
         lib = library()
         msg = lib.condensa_status_string(code).decode()
         if code == -7:
@@ -191,8 +192,9 @@ def _check(code: int) -> None:
 
 def _stream(stream) -> int:
     import torch
-    s = torch.cuda.current_stream() if stream is None else stream
-    return int(s.cuda_stream)
+    if stream is None:                       # the current stream of the current device, without a Stream object made for it
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    return int(stream.cuda_stream)
 
 
 class TensorTable(list):
@@ -697,6 +699,7 @@ class AdamwTable:
             _check(lib.condensa_adamw_list_init(arr, n, bits, grad_type, code_type, self._memory.data_ptr(), self._memory.numel(),
                                                 int(st.cuda_stream), ctypes.byref(self.list)))
             _wait_unless_captured(st)
+        self.ref = ctypes.byref(self.list)
 
 
 def adamw_table(weights, grads, exp_avg, exp_avg_sq, **kw) -> AdamwTable:
@@ -711,12 +714,15 @@ def condensa_lc_adamw_step(table: AdamwTable, lr, step, betas=(0.9, 0.999), eps=
                            grad_scale=None, stream=None):
     """Marshals condensa_lc_adamw_step: one update of everything in ``table``.  ``seed``: 8-bit states are rounded by random bits
     made from it (another one for every step), None: to nearest.  ``grad_scale``: a float32 device scalar."""
-    import torch
-    if grad_scale is not None and not (grad_scale.is_cuda and grad_scale.dtype == torch.float32 and grad_scale.numel() == 1):
-        raise TypeError("grad_scale is one float32 on the device")
+    scale = None
+    if grad_scale is not None:
+        import torch
+        if not (grad_scale.is_cuda and grad_scale.dtype == torch.float32 and grad_scale.numel() == 1):
+            raise TypeError("grad_scale is one float32 on the device")
+        scale = grad_scale.data_ptr()
     s = AdamwSettings(lr, betas[0], betas[1], eps, weight_decay, mu, ROUND_NEAREST if seed is None else ROUND_STOCHASTIC, step,
-                      0 if seed is None else seed & 0xFFFFFFFFFFFFFFFF, None if grad_scale is None else grad_scale.data_ptr(), 0)
-    _check(library().condensa_lc_adamw_step(ctypes.byref(table.list), ctypes.byref(s), _stream(stream)))
+                      0 if seed is None else seed & 0xFFFFFFFFFFFFFFFF, scale, 0)
+    _check(library().condensa_lc_adamw_step(table.ref, ctypes.byref(s), _stream(stream)))
 
 
 class AdapterTable:
@@ -758,6 +764,11 @@ class AdapterTable:
                                                   self._memory.numel(), int(st.cuda_stream), ctypes.byref(self.list)))
             _wait_unless_captured(st)
         self.n_in, self.n_out, self.max_rank = self.list.n_in, self.list.n_out, self.list.max_rank
+        self.ref, self.index = ctypes.byref(self.list), dev.index
+
+    def empty(self, rows, cols):
+        import torch
+        return torch.empty((rows, cols), dtype=self.dtype, device=self.device)
 
 
 def adapter_table(adapters, grads=None, **kw) -> AdapterTable:
@@ -777,61 +788,69 @@ def adapter_workspace(table: AdapterTable, n_tokens: int, backward: bool = False
 
 def _rows(name, t, table, n_tokens, width):
     """(address, row stride) of a two-dimensional operand whose rows are contiguous."""
-    if not (t.dim() == 2 and t.device == table.device and t.dtype == table.dtype and tuple(t.shape) == (n_tokens, width)
-            and (t.stride(1) == 1 or width == 1 or t.numel() == 0) and (n_tokens <= 1 or t.stride(0) >= width)):
+    shape, stride = t.shape, t.stride()
+    if not (len(shape) == 2 and shape[0] == n_tokens and shape[1] == width and t.dtype is table.dtype and t.get_device() == table.index
+            and (stride[1] == 1 or width == 1 or n_tokens == 0) and (n_tokens <= 1 or stride[0] >= width)):
         raise TypeError(f"{name}: a {table.dtype} tensor [{n_tokens}, {width}] with contiguous rows, beside the adapters")
-    return t.data_ptr() or None, t.stride(0) if n_tokens > 1 else width
+    return t.data_ptr(), (stride[0] if n_tokens > 1 else width)      # the address of a tensor without elements is 0
 
 
 def _token_ids(ids, table, n_tokens):
-    import torch
-    if not (ids.device == table.device and ids.dtype == torch.int32 and ids.is_contiguous() and ids.numel() == n_tokens):
+    if not (ids.dtype is _int32() and ids.get_device() == table.index and ids.is_contiguous() and ids.numel() == n_tokens):
         raise TypeError(f"token_adapter: {n_tokens} contiguous int32 on the device")
-    return ids.data_ptr() or None
+    return ids.data_ptr()
+
+
+@functools.lru_cache(None)
+def _int32():
+    import torch
+    return torch.int32
+
+
+def _kept_z(z, table, n_tokens):
+    shape = z.shape
+    if not (len(shape) == 2 and shape[0] == n_tokens and z.dtype is table.dtype and z.get_device() == table.index and z.is_contiguous()):
+        raise TypeError(f"z: a contiguous {table.dtype} tensor with a row for each token")
+    return z.data_ptr(), shape[1]
 
 
 def condensa_adapter_project(x, w, table: AdapterTable, token_adapter, y=None, z=False, workspace=None, stream=None):
     """Marshals condensa_adapter_project.  ``z``: a tensor [tokens, >= largest rank] to receive x A^T scale, True to allocate one (the
     backward pass wants it), False for none."""
-    import torch
     T = x.shape[0]
     px, ldx = _rows("x", x, table, T, table.n_in)
     pw, ldw = _rows("w", w, table, table.n_out, table.n_in)
     ids = _token_ids(token_adapter, table, T)
     if y is None:
-        y = torch.empty((T, table.n_out), dtype=table.dtype, device=table.device)
+        y = table.empty(T, table.n_out)
     py, ldy = _rows("y", y, table, T, table.n_out)
     if z is True:
-        z = torch.empty((T, max(table.max_rank, 1)), dtype=table.dtype, device=table.device)
+        z = table.empty(T, max(table.max_rank, 1))
     z = None if z is False else z
-    if z is not None and not (z.device == table.device and z.dtype == table.dtype and z.is_contiguous() and z.dim() == 2 and z.shape[0] == T):
-        raise TypeError(f"z: a contiguous {table.dtype} tensor with a row for each token")
+    pz, ldz = (None, 0) if z is None else _kept_z(z, table, T)
     if workspace is None:
         workspace = adapter_workspace(table, T)
-    _check(library().condensa_adapter_project(ctypes.byref(table.list), px, ldx, T, pw, ldw, ids, py, ldy,
-                                              None if z is None else z.data_ptr() or None, 0 if z is None else z.shape[1],
-                                              workspace.data_ptr(), workspace.numel(), _stream(stream)))
+    _check(library().condensa_adapter_project(table.ref, px, ldx, T, pw, ldw, ids, py, ldy, pz, ldz, workspace.data_ptr(),
+                                              workspace.numel(), _stream(stream)))
     return {"y": y, "z": z, "workspace": workspace}
 
 
 def condensa_adapter_project_backward(dy, x, w, table: AdapterTable, token_adapter, z, dx=True, workspace=None, stream=None):
     """Marshals condensa_adapter_project_backward: writes the gradients that ``table`` names, and ``dx`` (a tensor, True to allocate
     one, False for none)."""
-    import torch
     T = x.shape[0]
     pdy, lddy = _rows("dy", dy, table, T, table.n_out)
     px, ldx = _rows("x", x, table, T, table.n_in)
     pw, ldw = _rows("w", w, table, table.n_out, table.n_in)
     ids = _token_ids(token_adapter, table, T)
-    if not (z.device == table.device and z.dtype == table.dtype and z.is_contiguous() and z.dim() == 2 and z.shape[0] == T):
-        raise TypeError(f"z: the contiguous {table.dtype} tensor of the forward pass")
+    pz, ldz = _kept_z(z, table, T)
     if dx is True:
-        dx = torch.empty((T, table.n_in), dtype=table.dtype, device=table.device)
+        dx = table.empty(T, table.n_in)
     pdx, lddx = (None, 0) if dx is False else _rows("dx", dx, table, T, table.n_in)
     if workspace is None:
         workspace = adapter_workspace(table, T, backward=True)
-    _check(library().condensa_adapter_project_backward(ctypes.byref(table.list), pdy, lddy, px, ldx, T, pw, ldw, ids, z.data_ptr() or None,
-                                                       z.shape[1], pdx, lddx, workspace.data_ptr(), workspace.numel(), _stream(stream)))
+    _check(library().condensa_adapter_project_backward(table.ref, pdy, lddy, px, ldx, T, pw, ldw, ids, pz, ldz, pdx, lddx,
+                                                       workspace.data_ptr(), workspace.numel(), _stream(stream)))
     return {"dx": None if dx is False else dx, "grads": table.grads, "workspace": workspace}
 
 

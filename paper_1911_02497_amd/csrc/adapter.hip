@@ -11,7 +11,7 @@ namespace condensa {
 constexpr i64 kMaxSide = static_cast<i64>(1) << 20;
 constexpr i64 kMaxTokens = static_cast<i64>(1) << 24;
 constexpr i64 kMaxStride = static_cast<i64>(1) << 22;       // 256 rows of a tile are less than 2^32 bytes apart
-enum : int32_t { kAlignedA = 1, kAlignedB = 2, kHasGrads = 4 };
+enum : int32_t { kHasGrads = 4 };
 
 static bool aligned(const void* p, u64 bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 static u32 padded_rank(u32 r) { return (r + 31) / 32 * 32; }
@@ -31,10 +31,10 @@ static u32 run_tokens(i64 n_tokens, i64 n_in, i64 n_out) {
 }
 
 struct Plan {
-    bool few = false;
+    bool few = false, split = false;
     u32 rp = 0, splits = 1, steps_each = 0, tiles_n = 0;
     u32 run = 0, n_slots = 0, tiles = 0;
-    size_t zp = 0, z32 = 0, part = 0, row_max = 0, order = 0, seg = 0, slots = 0, total = 0;
+    size_t zp = 0, z32 = 0, part = 0, part_wide = 0, row_max = 0, order = 0, seg = 0, slots = 0, total = 0;
 };
 
 // Up to this many tokens the weights are read straight into registers, by workgroups that share the sum.
@@ -47,26 +47,39 @@ static Plan make_plan(i64 T, i64 n_in, i64 n_out, u32 n_adapters, u32 max_rank, 
     p.rp = padded_rank(max_rank ? max_rank : 1);
     p.few = !backward && T <= kFewTokens;
     if (p.few) {
-        const u32 steps = static_cast<u32>((n_in + 31) / 32);
+        const u32 steps = static_cast<u32>((n_in + 63) / 64);
         p.tiles_n = static_cast<u32>((n_out + kFewCols - 1) / kFewCols);
-        // some 512 workgroups, and at least four steps for each of the four wavefronts that share a part of the sum
-        u32 s = (512 + p.tiles_n - 1) / p.tiles_n, most = steps / 16;
+        // some 320 workgroups, and at least a step for each of the eight wavefronts of one
+        u32 s = (320 + p.tiles_n / 2) / p.tiles_n, most = steps / kFewWaves;
         s = s > most ? most : s;
         s = s > 8 ? 8 : (s < 1 ? 1 : s);
         p.steps_each = (steps + s - 1) / s;
         p.splits = (steps + p.steps_each - 1) / p.steps_each;
-        p.part = take(static_cast<u64>(p.splits) * T * n_out * 4);
+        p.part_wide = take(static_cast<u64>(p.splits) * T * n_out * 4);
         p.z32 = take(static_cast<u64>(T) * (max_rank ? max_rank : 1) * 4);
     } else {
-        p.zp = take(static_cast<u64>(T) * p.rp * 2);
+        // the wide product: tiles of 64 x 64 outputs that would leave compute units without one are split along the sum
+        const i64 n_wide = backward ? n_in : n_out, n_sum = backward ? n_out : n_in;
+        const u64 tiles = static_cast<u64>((T + 63) / 64) * ((n_wide + 63) / 64);
+        const u32 steps = static_cast<u32>((n_sum + 63) / 64);
+        if (T > 0 && tiles < 512 && steps >= 4) {
+            u32 s = static_cast<u32>((1024 + tiles - 1) / tiles), most = steps / 2;
+            s = s > most ? most : s;
+            s = s > 16 ? 16 : s;
+            p.split = s > 1;
+            p.steps_each = (steps + s - 1) / s;
+            p.splits = (steps + p.steps_each - 1) / p.steps_each;
+            if (p.split) p.part_wide = take(static_cast<u64>(p.splits) * T * n_wide * 4);
+        }
+        if (!p.split) p.zp = take(static_cast<u64>(T) * p.rp * 2);
+        if (p.split || backward) p.z32 = take(static_cast<u64>(T) * p.rp * 4);
         if (backward) {
-            p.z32 = take(static_cast<u64>(T) * p.rp * 4);
             p.row_max = take(static_cast<u64>(T) * 4);
             p.run = run_tokens(T, n_in, n_out);
             p.n_slots = static_cast<u32>(T / p.run) + n_adapters;
             p.order = take(static_cast<u64>(T) * 4);
             p.seg = take(static_cast<u64>(n_adapters) * sizeof(uint2));
-            p.slots = take(static_cast<u64>(p.n_slots) * 4);
+            p.slots = take(static_cast<u64>(p.n_slots) * sizeof(uint4));
             if (T > p.run) p.part = take(static_cast<u64>(p.n_slots) * max_rank * (n_in + n_out) * 4);
         }
     }
@@ -99,13 +112,22 @@ static condensa_status launch_wide(WideArgs a, bool vec, hipStream_t st) {
     if (vec && tiles(256, 256) >= 192) {
         if (cost(192) < cost(256)) launch_wide_tile<E, 256, 192, 2, 4, 2, ALONG, true>(a, st);
         else                       launch_wide_tile<E, 256, 256, 2, 4, 2, ALONG, true>(a, st);
-    } else if (tiles(128, 128) >= 192) {
-        if (vec) launch_wide_tile<E, 128, 128, 2, 2, 2, ALONG, true>(a, st);
-        else     launch_wide_tile<E, 128, 128, 2, 2, 2, ALONG, false>(a, st);
+    } else if (vec && tiles(128, 128) >= 192) {
+        launch_wide_tile<E, 128, 128, 2, 2, 2, ALONG, true>(a, st);
     } else {
         if (vec) launch_wide_tile<E, 64, 64, 2, 2, 4, ALONG, true>(a, st);
         else     launch_wide_tile<E, 64, 64, 2, 2, 2, ALONG, false>(a, st);
     }
+    CONDENSA_LAUNCH_CHECK();
+    return CONDENSA_OK;
+}
+
+template <typename E, bool ALONG>
+static condensa_status launch_split(const DownArgs& d, const WideArgs& w, u32 down_blocks, bool vec, hipStream_t st) {
+    const u32 blocks = down_blocks + (w.n_tokens + 63) / 64 * ((w.n_out + 63) / 64) * w.splits;
+    if (vec)          hipLaunchKernelGGL((k_adapter_split<E, ALONG, true, true>), dim3(blocks), dim3(256), 0, st, d, w, down_blocks);
+    else if (d.vec_x) hipLaunchKernelGGL((k_adapter_split<E, ALONG, true, false>), dim3(blocks), dim3(256), 0, st, d, w, down_blocks);
+    else              hipLaunchKernelGGL((k_adapter_split<E, ALONG, false, false>), dim3(blocks), dim3(256), 0, st, d, w, down_blocks);
     CONDENSA_LAUNCH_CHECK();
     return CONDENSA_OK;
 }
@@ -118,7 +140,7 @@ static void launch_few_tile(const FewArgs& f, bool vec, u32 blocks, hipStream_t 
 
 template <typename E>
 static condensa_status launch_few(const FewArgs& f, bool vec, hipStream_t st) {
-    const u32 T = f.wide.n_tokens, blocks = f.tiles_n * f.splits + T;
+    const u32 T = f.wide.n_tokens, blocks = f.tiles_n * f.wide.splits + T;
     if (T <= 16)      launch_few_tile<E, 1>(f, vec, blocks, st);
     else if (T <= 32) launch_few_tile<E, 2>(f, vec, blocks, st);
     else              launch_few_tile<E, 4>(f, vec, blocks, st);
@@ -164,7 +186,7 @@ condensa_status condensa_adapter_list_init(const condensa_adapter* adapters, int
     std::unique_ptr<ByteRange[]> ranges(new (std::nothrow) ByteRange[static_cast<size_t>(n_adapters) * 4 + 1]);
     if (!ranges) return CONDENSA_ERR_SIZE;
     size_t nr = 0;
-    int32_t max_rank = 0, flags = kAlignedA | kAlignedB | kHasGrads;
+    int32_t max_rank = 0, flags = kHasGrads;
     for (int i = 0; i < n_adapters; ++i) {
         const condensa_adapter& s = adapters[i];
         if (s.rank < 1 || s.rank > CONDENSA_MAX_RANK) return CONDENSA_ERR_SHAPE;
@@ -172,8 +194,6 @@ condensa_status condensa_adapter_list_init(const condensa_adapter* adapters, int
         if (!aligned(s.a, 2) || !aligned(s.b, 2) || !aligned(s.grad_a, 4) || !aligned(s.grad_b, 4)) return CONDENSA_ERR_ARG;
         if (!std::isfinite(s.scale)) return CONDENSA_ERR_DENSITY;
         max_rank = s.rank > max_rank ? s.rank : max_rank;
-        if (!aligned(s.a, 16) || n_in % 8) flags &= ~kAlignedA;
-        if (!aligned(s.b, 16) || s.rank % 8) flags &= ~kAlignedB;
         if (!s.grad_a) flags &= ~kHasGrads;
         ranges[nr++] = byte_range(s.a, static_cast<u64>(s.rank) * n_in * 2, false);
         ranges[nr++] = byte_range(s.b, static_cast<u64>(s.rank) * n_out * 2, false);
@@ -190,6 +210,8 @@ condensa_status condensa_adapter_list_init(const condensa_adapter* adapters, int
             const condensa_adapter& s = adapters[first + i];
             p.d[i].a = s.a; p.d[i].b = s.b; p.d[i].grad_a = s.grad_a; p.d[i].grad_b = s.grad_b;
             p.d[i].scale = s.scale; p.d[i].rank = static_cast<u32>(s.rank);
+            p.d[i].vec_a = aligned(s.a, 16) && n_in % 8 == 0;
+            p.d[i].vec_b = aligned(s.b, 16) && s.rank % 8 == 0;
         }
         hipLaunchKernelGGL(k_adapter_list, dim3(1), dim3(256), 0, st, static_cast<AdapterDesc*>(list_dev), p, static_cast<u32>(first), static_cast<u32>(k));
         CONDENSA_LAUNCH_CHECK();
@@ -240,24 +262,33 @@ condensa_status condensa_adapter_project(const condensa_adapter_list* list, cons
     g.n_tokens = static_cast<u32>(n_tokens); g.n_out = static_cast<u32>(list->n_out); g.n_sum = static_cast<u32>(list->n_in);
     g.rp = p.rp; g.ids = token_adapter_dev; g.ad = static_cast<const AdapterDesc*>(list->table_dev);
     g.n_adapters = static_cast<u32>(list->n_adapters); g.max_rank = static_cast<u32>(list->max_rank);
-    g.vec_m = (list->flags & kAlignedB) != 0;
     g.vec_y = aligned(y_dev, 8) && y_stride % 4 == 0;
+    g.splits = p.splits; g.steps_each = p.steps_each;
+    g.part = at<float>(workspace_dev, p.part_wide);
     if (p.few) {
         FewArgs f{};
         f.wide = g;
-        f.part = at<float>(workspace_dev, p.part);
         f.z32 = at<float>(workspace_dev, p.z32);
         f.z = z_dev; f.ldz = z_stride;
-        f.tiles_n = p.tiles_n; f.splits = p.splits; f.steps_each = p.steps_each;
-        f.vec_a = (list->flags & kAlignedA) != 0;
+        f.tiles_n = p.tiles_n;
         return f16 ? launch_few<ElemF16>(f, vec, st) : launch_few<ElemBF16>(f, vec, st);
     }
-    g.zp = at<u16>(workspace_dev, p.zp);
+    g.zp = p.split ? nullptr : at<u16>(workspace_dev, p.zp);
     DownArgs d{};
     d.x = x_dev; d.ldx = x_stride; d.n_tokens = g.n_tokens; d.n_sum = g.n_sum; d.ids = g.ids; d.ad = g.ad; d.n_adapters = g.n_adapters; d.max_rank = g.max_rank;
-    d.zp = at<u16>(workspace_dev, p.zp); d.rp = p.rp; d.z = z_dev; d.ldz = z_stride;
-    d.vec_x = vec_x; d.vec_m = (list->flags & kAlignedA) != 0;
+    d.zp = p.split ? nullptr : at<u16>(workspace_dev, p.zp); d.rp = p.rp; d.z = z_dev; d.ldz = z_stride;
+    d.z32 = p.split ? at<float>(workspace_dev, p.z32) : nullptr;
+    d.vec_x = vec_x;
     d.tiles = (g.n_tokens + kDownTokens - 1) / kDownTokens;
+    if (p.split) {
+        condensa_status s = f16 ? launch_split<ElemF16, true>(d, g, d.tiles, vec, st) : launch_split<ElemBF16, true>(d, g, d.tiles, vec, st);
+        if (s != CONDENSA_OK) return s;
+        const dim3 grid((g.n_out + 255) / 256, g.n_tokens);
+        if (f16) hipLaunchKernelGGL((k_adapter_split_join<ElemF16, true>), grid, dim3(256), 0, st, g, static_cast<const float*>(d.z32), p.rp);
+        else     hipLaunchKernelGGL((k_adapter_split_join<ElemBF16, true>), grid, dim3(256), 0, st, g, static_cast<const float*>(d.z32), p.rp);
+        CONDENSA_LAUNCH_CHECK();
+        return CONDENSA_OK;
+    }
     condensa_status s = f16 ? launch_down<ElemF16, true>(d, d.tiles, st) : launch_down<ElemBF16, true>(d, d.tiles, st);
     if (s != CONDENSA_OK) return s;
     return f16 ? launch_wide<ElemF16, true>(g, vec, st) : launch_wide<ElemBF16, true>(g, vec, st);
@@ -285,7 +316,7 @@ condensa_status condensa_adapter_project_backward(const condensa_adapter_list* l
                      byte_range(z_dev, static_cast<u64>(n_tokens) * z_stride * 2, false), byte_range(dx_dev, rows_bytes(n_tokens, dx_stride, list->n_in, 2), true),
                      byte_range(workspace_dev, p.total, true), byte_range(list->table_dev, condensa_adapter_list_bytes(list->n_adapters), false)};
     if (ranges_conflict(r, sizeof(r) / sizeof(r[0]))) return CONDENSA_ERR_ARG;
-    const u64 grad_blocks = static_cast<u64>(p.n_slots) * ((list->n_in + kGradCols - 1) / kGradCols + (list->n_out + kGradCols - 1) / kGradCols);
+    const u64 grad_blocks = static_cast<u64>((list->max_rank + 63) / 64) * p.n_slots * ((list->n_in + kGradCols - 1) / kGradCols + (list->n_out + kGradCols - 1) / kGradCols);
     if (grad_blocks >= (static_cast<u64>(1) << 24)) return CONDENSA_ERR_SIZE;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const bool f16 = list->type == CONDENSA_TYPE_F16;
@@ -297,26 +328,34 @@ condensa_status condensa_adapter_project_backward(const condensa_adapter_list* l
     DownArgs d{};
     d.x = dy_dev; d.ldx = dy_stride; d.n_tokens = T; d.n_sum = static_cast<u32>(list->n_out); d.ids = token_adapter_dev; d.ad = ad; d.n_adapters = n;
     d.max_rank = static_cast<u32>(list->max_rank);
-    d.zp = at<u16>(workspace_dev, p.zp); d.rp = p.rp; d.z32 = at<float>(workspace_dev, p.z32); d.row_max = at<u32>(workspace_dev, p.row_max);
-    d.vec_x = vec_dy; d.vec_m = (list->flags & kAlignedB) != 0;
+    const bool wide = dx_dev && T > 0, split = wide && p.split;
+    d.zp = p.split || !wide ? nullptr : at<u16>(workspace_dev, p.zp); d.rp = p.rp; d.z32 = at<float>(workspace_dev, p.z32); d.row_max = at<u32>(workspace_dev, p.row_max);
+    d.vec_x = vec_dy;
     d.tiles = (T + kDownTokens - 1) / kDownTokens;
-    d.order = at<u32>(workspace_dev, p.order); d.seg = at<uint2>(workspace_dev, p.seg); d.slots = at<u32>(workspace_dev, p.slots);
+    d.order = at<u32>(workspace_dev, p.order); d.seg = at<uint2>(workspace_dev, p.seg); d.slots = at<uint4>(workspace_dev, p.slots);
     d.n_slots = p.n_slots; d.run = p.run;
-    const u32 blocks = d.tiles + (n + kDownWaves - 1) / kDownWaves;
+    const u32 waves = split ? 4 : kDownWaves, blocks = d.tiles + (n + waves - 1) / waves;
     if (blocks == 0) return CONDENSA_OK;
-    condensa_status s = f16 ? launch_down<ElemF16, false>(d, blocks, st) : launch_down<ElemBF16, false>(d, blocks, st);
-    if (s != CONDENSA_OK) return s;
-    if (dx_dev && T > 0) {
-        WideArgs g{};
-        g.x = dy_dev; g.ldx = dy_stride; g.w = w_dev; g.ldw = w_stride; g.y = dx_dev; g.ldy = dx_stride;
-        g.n_tokens = T; g.n_out = static_cast<u32>(list->n_in); g.n_sum = static_cast<u32>(list->n_out);
-        g.zp = d.zp; g.rp = p.rp; g.ids = token_adapter_dev; g.ad = ad; g.n_adapters = n; g.max_rank = d.max_rank;
-        g.vec_m = (list->flags & kAlignedA) != 0;
-        g.vec_y = aligned(dx_dev, 8) && dx_stride % 4 == 0;
-        s = f16 ? launch_wide<ElemF16, false>(g, vec_dy && vec_w, st) : launch_wide<ElemBF16, false>(g, vec_dy && vec_w, st);
+    WideArgs g{};
+    g.x = dy_dev; g.ldx = dy_stride; g.w = w_dev; g.ldw = w_stride; g.y = dx_dev; g.ldy = dx_stride;
+    g.n_tokens = T; g.n_out = static_cast<u32>(list->n_in); g.n_sum = static_cast<u32>(list->n_out);
+    g.zp = d.zp; g.rp = p.rp; g.ids = token_adapter_dev; g.ad = ad; g.n_adapters = n; g.max_rank = d.max_rank;
+    g.vec_y = aligned(dx_dev, 8) && dx_stride % 4 == 0;
+    g.splits = p.splits; g.steps_each = p.steps_each;
+    g.part = at<float>(workspace_dev, p.part_wide);
+    const bool vec_wide = vec_dy && vec_w;
+    condensa_status s;
+    if (split) {
+        s = f16 ? launch_split<ElemF16, false>(d, g, blocks, vec_wide, st) : launch_split<ElemBF16, false>(d, g, blocks, vec_wide, st);
+        if (s != CONDENSA_OK) return s;
+    } else {
+        s = f16 ? launch_down<ElemF16, false>(d, blocks, st) : launch_down<ElemBF16, false>(d, blocks, st);
+        if (s != CONDENSA_OK) return s;
+        if (wide) s = f16 ? launch_wide<ElemF16, false>(g, vec_wide, st) : launch_wide<ElemBF16, false>(g, vec_wide, st);
         if (s != CONDENSA_OK) return s;
     }
-    if (n == 0) return CONDENSA_OK;
+    const u32 joins = split ? (g.n_out + 255) / 256 * T : 0;
+    if (n == 0 && joins == 0) return CONDENSA_OK;
     GradArgs q{};
     q.x = x_dev; q.ldx = x_stride; q.n_in = static_cast<u32>(list->n_in); q.dy = dy_dev; q.ldy = dy_stride; q.n_out = static_cast<u32>(list->n_out);
     q.dz = d.z32; q.rp = p.rp; q.z = z_dev; q.ldz = z_stride; q.row_max = d.row_max; q.order = d.order; q.seg = d.seg; q.slots = d.slots; q.ad = ad;
@@ -324,17 +363,18 @@ condensa_status condensa_adapter_project_backward(const condensa_adapter_list* l
     q.tiles_in = (q.n_in + kGradCols - 1) / kGradCols;
     q.tiles = q.tiles_in + (q.n_out + kGradCols - 1) / kGradCols;
     q.part = n_tokens > p.run ? at<float>(workspace_dev, p.part) : nullptr;
-    const dim3 grid(p.n_slots * q.tiles, (q.max_rank + 63) / 64);
+    q.rank_groups = (q.max_rank + 63) / 64;
+    const dim3 grid(joins + static_cast<u32>(n > 0 ? p.n_slots * q.tiles * q.rank_groups : 0));
     const bool vec = vec_x && vec_dy;
     if (f16) {
-        if (vec) hipLaunchKernelGGL((k_adapter_grads<ElemF16, true>), grid, dim3(256), 0, st, q);
-        else     hipLaunchKernelGGL((k_adapter_grads<ElemF16, false>), grid, dim3(256), 0, st, q);
+        if (vec) hipLaunchKernelGGL((k_adapter_grads<ElemF16, true>), grid, dim3(256), 0, st, q, g, joins);
+        else     hipLaunchKernelGGL((k_adapter_grads<ElemF16, false>), grid, dim3(256), 0, st, q, g, joins);
     } else {
-        if (vec) hipLaunchKernelGGL((k_adapter_grads<ElemBF16, true>), grid, dim3(256), 0, st, q);
-        else     hipLaunchKernelGGL((k_adapter_grads<ElemBF16, false>), grid, dim3(256), 0, st, q);
+        if (vec) hipLaunchKernelGGL((k_adapter_grads<ElemBF16, true>), grid, dim3(256), 0, st, q, g, joins);
+        else     hipLaunchKernelGGL((k_adapter_grads<ElemBF16, false>), grid, dim3(256), 0, st, q, g, joins);
     }
     CONDENSA_LAUNCH_CHECK();
-    if (n_tokens > p.run) {
+    if (n > 0 && n_tokens > p.run) {
         const u64 elems = static_cast<u64>(q.max_rank) * (list->n_in + list->n_out);
         u64 each = (elems + 1023) / 1024;
         each = each > 512 ? 512 : each;

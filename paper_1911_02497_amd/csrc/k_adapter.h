@@ -5,6 +5,8 @@
 // the rows of a matrix in memory, tiles of it lie in LDS as they are and the transposing LDS load collects the fragment.  A result
 // tile puts its column in lane l % 16 and its rows 4 (l / 16) .. + 3 in four registers.
 #pragma once
+#include <type_traits>
+
 #include "common.h"
 
 typedef int64_t i64;
@@ -39,7 +41,7 @@ struct AdapterDesc {
     float* grad_b;
     float scale;
     u32 rank;
-    u64 reserved;
+    u32 vec_a, vec_b;          // rows are 16-byte aligned and a multiple of eight long
 };
 static_assert(sizeof(AdapterDesc) == 48, "AdapterDesc layout");
 
@@ -52,22 +54,40 @@ __global__ __launch_bounds__(256) void k_adapter_list(AdapterDesc* __restrict__ 
 
 // ---- operand access ---------------------------------------------------------------------------------------------
 
+// Sixteen bytes from global memory; of the second form at any address that a 16-bit value may have.  The address space is given because
+// pointers that come out of the device list would otherwise be taken for pointers to any memory.
+typedef u32 u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+__device__ inline u32x4 load16(const u16* p) { return *reinterpret_cast<const __attribute__((address_space(1))) u32x4*>((u64)p); }
+__device__ inline u32x4 load16_any(const u16* p) { return *reinterpret_cast<const __attribute__((address_space(1))) u32x4_any*>((u64)p); }
+__device__ inline u16 load2(const u16* p) { return *reinterpret_cast<const __attribute__((address_space(1))) u16*>((u64)p); }
+
 // Eight consecutive 16-bit values p[k .. k+7] of a row of n, zeros past its end.  VEC: rows are 16-byte aligned and n and k are
 // multiples of eight.
 template <bool VEC>
-__device__ inline u32x4 load8(const u16* __restrict__ p, i64 k, i64 n) {
+__device__ inline u32x4 load8(const u16* p, i64 k, i64 n) {
     u32x4 v = {0u, 0u, 0u, 0u};
     if (VEC) {
-        if (k < n) v = *reinterpret_cast<const u32x4*>(p + k);
+        if (k < n) v = load16(p + k);
     } else if (k + 8 <= n) {
-        __builtin_memcpy(&v, p + k, 16);                    // one load: the hardware takes any address
-    } else {
+        v = load16_any(p + k);
+    } else if (k < n) {
+        if (n >= 8) {                                        // the row's last eight, moved down
+            const u32x4 t = load16_any(p + n - 8);
+            u64 lo = static_cast<u64>(t.y) << 32 | t.x, hi = static_cast<u64>(t.w) << 32 | t.z;
+            u32 drop = static_cast<u32>(k + 8 - n) * 16;     // 16 .. 112 bits
+            if (drop >= 64) { lo = hi; hi = 0; drop -= 64; }
+            if (drop) { lo = lo >> drop | hi << (64 - drop); hi >>= drop; }
+            v = u32x4{static_cast<u32>(lo), static_cast<u32>(lo >> 32), static_cast<u32>(hi), static_cast<u32>(hi >> 32)};
+        } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (k + i < n) v[i >> 1] |= static_cast<u32>(p[k + i]) << (16 * (i & 1));
+            for (int i = 0; i < 7; ++i)
+                if (k + i < n) v[i >> 1] |= static_cast<u32>(load2(p + k + i)) << (16 * (i & 1));
+        }
     }
     return v;
 }
+template <bool VEC>
+__device__ inline u32x4 load8_inside(const u16* p) { return VEC ? load16(p) : load16_any(p); }           // all eight are there
 
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef __attribute__((address_space(3))) void lds_void;
@@ -140,7 +160,7 @@ __device__ inline int next_adapter(int id, int last) {
         const int y = __shfl_xor(x, d, 64);
         x = x < y ? x : y;
     }
-    return x;
+    return __builtin_amdgcn_readfirstlane(x);          // known to be the same in all lanes: what it selects comes in scalar registers
 }
 
 // ---- down: the product with the narrow matrix -------------------------------------------------------------------
@@ -155,16 +175,17 @@ struct DownArgs {
     u16* z; i64 ldz;                     // the caller's copy, or NULL; all ldz columns are written
     float* z32;                          // [n_tokens, rp] before rounding, or NULL
     u32* row_max;                        // largest finite magnitude of each token's z (bits), or NULL
-    u32 vec_x, vec_m;                    // 16-byte aligned rows of x / of the narrow matrix
+    u32 vec_x;                           // 16-byte aligned rows of x
     // blocks past the tiles sort the tokens by adapter (backward)
     u32 tiles;
     u32* order;                          // tokens of adapter 0, 1, ... in ascending order
-    uint2* seg;                          // [n_adapters] first place in `order`, count
-    u32* slots;                          // [n_slots] adapter of a run of tokens, or ~0
+    uint4* slots;                        // [n_slots] of a run of tokens: adapter or ~0, first place in `order`, tokens, tokens of the adapter
+    uint2* seg;                          // [n_adapters] first slot, slots
     u32 n_slots, run;                    // tokens of a run
 };
 
-constexpr int kDownTokens = 32, kDownWaves = 8, kDownRanks = 64;
+constexpr int kDownTokens = 32, kDownRanks = 64;
+constexpr u32 down_lds(u32 waves) { return waves * kDownTokens * kDownRanks * 4; }
 
 // Places of the runs of an adapter whose tokens begin at `first`: run j of it is slot first / run + a + j.  (One slot at least for
 // each adapter; the slots of different adapters never meet, since ceil(n / run) <= floor((first + n) / run) - floor(first / run) + 1.)
@@ -184,10 +205,13 @@ __device__ inline void sort_tokens(const DownArgs& p, u32 a) {
             mine += static_cast<u32>(__popcll(__ballot(id[i] == static_cast<int>(a))));
         }
     }
-    if (lane == 0) p.seg[a] = make_uint2(less, mine);
     const u32 s0 = first_slot(less, p.run, a), s1 = a + 1 < p.n_adapters ? first_slot(less + mine, p.run, a + 1) : p.n_slots;
     const u32 runs = mine == 0 ? 1 : (mine + p.run - 1) / p.run;
-    for (u32 s = s0 + lane; s < s1; s += 64) p.slots[s] = s - s0 < runs ? a : ~0u;
+    if (lane == 0) p.seg[a] = make_uint2(s0, runs);
+    for (u32 s = s0 + lane; s < s1; s += 64) {
+        const u32 done = (s - s0) * p.run;
+        p.slots[s] = make_uint4(s - s0 < runs ? a : ~0u, less + done, mine - done < p.run ? mine - done : p.run, mine);
+    }
     u32 at = less;
     if (mine == 0) return;                                   // uniform
     for (u32 t = 0; t < p.n_tokens; t += 256) {
@@ -206,57 +230,86 @@ __device__ inline void sort_tokens(const DownArgs& p, u32 a) {
 // Sums of 32 tokens and 16 G ranks from r0 on, over the steps of 64 values that are this wavefront's.  ALONG: the narrow matrix is [rank, n_sum]
 // and its fragments come from memory as they are.  Else it is [n_sum, rank]: 64 rows of it go through this wavefront's part of LDS, whose
 // transposing load makes fragments of them.
-template <typename E, bool ALONG, bool VECX, u32 G>
+template <typename E, bool ALONG, bool VECX, bool VECM, u32 WAVES, u32 G>
 __device__ inline void down_sums(const DownArgs& p, const u16* xa, const u16* xb, const u16* m, u32 rank, u32 r0, u16* own, f32x4 (&acc)[2][4]) {
-    const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, sub = (lane >> 4) * 8;
-    const u32 steps = (p.n_sum + 63) / 64;
-    constexpr u32 kPieces = ALONG ? 1 : 2 * G;             // 16-byte pieces of 64 rows of 16 G ranks, for each lane
-    auto rows = [&](u32 s, u32x4 (&v)[kPieces]) {
+    u32 lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));                         // keeps the places of each form out of the registers of the others
+    const u32 wave = threadIdx.x >> 6, row = lane & 15, sub = (lane >> 4) * 8;
+    const u32 full = p.n_sum / 64;
+    constexpr u32 kPieces = 2 * G;                         // 16-byte pieces of the narrow matrix for each lane and step
+    constexpr bool kRolled = !ALONG && !VECM && G == 4;    // many ranks, a number that eight does not divide: a few pieces at a time, registers are short
+    const u16* mj[G];
 #pragma unroll
-        for (u32 i = 0; i < kPieces; ++i) {
-            const u32 at = i * 64 + lane, k = at / (2 * G), piece = at % (2 * G);
-            const i64 n = static_cast<i64>(s) * 64 + k;
-            const u16* src = m + n * rank;
-            const i64 end = n < p.n_sum ? rank : 0;
-            v[i] = p.vec_m ? load8<true>(src, r0 + piece * 8, end) : load8<false>(src, r0 + piece * 8, end);
-        }
-    };
-    u32x4 next[kPieces];
-    if (!ALONG && wave < steps) rows(wave, next);
-#pragma unroll 2
-    for (u32 s = wave; s < steps; s += kDownWaves) {
+    for (u32 g = 0; g < G; ++g) {                          // rows past the rank: the last one again, their sums are not stored
+        const u32 j = r0 + g * 16 + row;
+        mj[g] = ALONG ? m + static_cast<i64>(j < rank ? j : rank - 1) * p.n_sum : m;
+    }
+    // GUARD: the step that ends past the sum
+    auto fetch = [&](auto guard, u32 s, u32x4 (&x)[4], u32x4 (&v)[kPieces]) {
+        constexpr bool GUARD = decltype(guard)::value;
         const i64 k = static_cast<i64>(s) * 64 + sub;
-        u32x4 fa[2], fb[2], fm[2][G];
 #pragma unroll
-        for (u32 h = 0; h < 2; ++h) { fa[h] = load8<VECX>(xa, k + h * 32, p.n_sum); fb[h] = load8<VECX>(xb, k + h * 32, p.n_sum); }
+        for (u32 h = 0; h < 2; ++h) {
+            x[2 * h] = GUARD ? load8<VECX>(xa, k + h * 32, p.n_sum) : load8_inside<VECX>(xa + k + h * 32);
+            x[2 * h + 1] = GUARD ? load8<VECX>(xb, k + h * 32, p.n_sum) : load8_inside<VECX>(xb + k + h * 32);
+        }
         if (ALONG) {
 #pragma unroll
             for (u32 h = 0; h < 2; ++h)
 #pragma unroll
-                for (u32 g = 0; g < G; ++g) {
-                    const u32 j = r0 + g * 16 + row;           // rows past the rank: the last one again, their sums are not stored
-                    const u16* src = m + static_cast<i64>(j < rank ? j : rank - 1) * p.n_sum;
-                    fm[h][g] = p.vec_m ? load8<true>(src, k + h * 32, p.n_sum) : load8<false>(src, k + h * 32, p.n_sum);
-                }
+                for (u32 g = 0; g < G; ++g)
+                    v[h * G + g] = GUARD ? load8<VECM>(mj[g], k + h * 32, p.n_sum) : load8_inside<VECM>(mj[g] + k + h * 32);
+        } else if (!kRolled) {
+#pragma unroll
+            for (u32 i = 0; i < kPieces; ++i) {
+                const u32 at = i * 64 + lane, piece = at % (2 * G);
+                const i64 n = static_cast<i64>(s) * 64 + at / (2 * G);
+                v[i] = load8<VECM>(m + n * rank, r0 + piece * 8, !GUARD || n < p.n_sum ? rank : 0);
+            }
         } else {
+#pragma unroll 2
+            for (u32 i = 0; i < kPieces; ++i) {
+                const u32 at = i * 64 + lane, piece = at % (2 * G);
+                const i64 n = static_cast<i64>(s) * 64 + at / (2 * G);
+                *reinterpret_cast<u32x4*>(own + across_at<16 * G>(at / (2 * G), piece)) = load8<VECM>(m + n * rank, r0 + piece * 8, !GUARD || n < p.n_sum ? rank : 0);
+            }
+        }
+    };
+    auto add = [&](const u32x4 (&x)[4], const u32x4 (&v)[kPieces]) {
+        if (!ALONG && !kRolled) {
 #pragma unroll
             for (u32 i = 0; i < kPieces; ++i) {
                 const u32 at = i * 64 + lane;
-                *reinterpret_cast<u32x4*>(own + across_at<16 * G>(at / (2 * G), at % (2 * G))) = next[i];
+                *reinterpret_cast<u32x4*>(own + across_at<16 * G>(at / (2 * G), at % (2 * G))) = v[i];
             }
-            if (s + kDownWaves < steps) rows(s + kDownWaves, next);
-#pragma unroll
-            for (u32 h = 0; h < 2; ++h)
-#pragma unroll
-                for (u32 g = 0; g < G; ++g) fm[h][g] = across_frag<16 * G>(own, g * 16, h);
         }
 #pragma unroll
         for (u32 h = 0; h < 2; ++h)
 #pragma unroll
             for (u32 g = 0; g < G; ++g) {
-                acc[0][g] = E::mfma(fa[h], fm[h][g], acc[0][g]);
-                acc[1][g] = E::mfma(fb[h], fm[h][g], acc[1][g]);
+                const u32x4 fm = ALONG ? v[h * G + g] : across_frag<16 * G>(own, g * 16, h);
+                acc[0][g] = E::mfma(x[2 * h], fm, acc[0][g]);
+                acc[1][g] = E::mfma(x[2 * h + 1], fm, acc[1][g]);
             }
+    };
+    constexpr u32 kAhead = G == 1 ? 3 : (ALONG || G == 2 ? 2 : 1);      // steps whose loads are under way at once
+    u32x4 x[kAhead][4], v[kAhead][kPieces];
+    u32 s = wave;
+    for (; s + (kAhead - 1) * WAVES < full; s += kAhead * WAVES) {
+#pragma unroll
+        for (u32 i = 0; i < kAhead; ++i) fetch(std::false_type{}, s + i * WAVES, x[i], v[i]);
+        __builtin_amdgcn_sched_barrier(0);                 // all of them before the first product
+#pragma unroll
+        for (u32 i = 0; i < kAhead; ++i) add(x[i], v[i]);
+    }
+#pragma unroll 1
+    for (; s < full; s += WAVES) {
+        fetch(std::false_type{}, s, x[0], v[0]);
+        add(x[0], v[0]);
+    }
+    if (s == full && (p.n_sum & 63u)) {
+        fetch(std::true_type{}, s, x[0], v[0]);
+        add(x[0], v[0]);
     }
 }
 
@@ -264,20 +317,21 @@ __device__ inline void down_sums(const DownArgs& p, const u16* xa, const u16* xb
 // pass.  Reading x bounds it: each row is read once, in whole cache lines, by eight wavefronts that take every eighth 64 values of it straight
 // into operand registers (nothing of x is shared between wavefronts, so LDS would only add a trip) and add their sums up at the end.
 // Thirty-two tokens share what is read of M_a.  Tokens of several adapters in one tile are done one adapter after the other.
-template <typename E, bool ALONG, bool VECX>
-__global__ __launch_bounds__(64 * kDownWaves) void k_adapter_down(DownArgs p) {
-    __shared__ __align__(16) float sums[kDownWaves][kDownTokens][kDownRanks];       // or, before, 8 KB of M_a for each wavefront
+// Workgroups past the tiles sort the tokens.
+template <typename E, bool ALONG, bool VECX, u32 WAVES>
+__device__ inline void down_tile(const DownArgs& p, u32 block, void* lds) {
+    float (*sums)[kDownTokens][kDownRanks] = reinterpret_cast<float (*)[kDownTokens][kDownRanks]>(lds);       // or, before, 8 KB of M_a for each wavefront
     const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    if (blockIdx.x >= p.tiles) {                             // uniform
-        const u32 a = (blockIdx.x - p.tiles) * kDownWaves + wave;
+    if (block >= p.tiles) {                                  // uniform
+        const u32 a = (block - p.tiles) * WAVES + wave;
         if (a < p.n_adapters) sort_tokens(p, a);
         return;
     }
-    const u32 t0 = blockIdx.x * kDownTokens;
+    const u32 t0 = block * kDownTokens;
     const int my_id = lane < kDownTokens ? adapter_of(p.ids, t0 + lane, p.n_tokens, p.n_adapters) : -1;
     const u32 width = p.z && p.ldz > p.rp ? static_cast<u32>(p.ldz) : p.rp;
     // tokens without an adapter
-    for (u32 i = wave; i < kDownTokens; i += kDownWaves) {
+    for (u32 i = wave; i < kDownTokens; i += WAVES) {
         const u32 t = t0 + i;
         if (t >= p.n_tokens || __shfl(my_id, static_cast<int>(i), 64) >= 0) continue;
         for (u32 j = lane; j < width; j += 64) {
@@ -291,16 +345,23 @@ __global__ __launch_bounds__(64 * kDownWaves) void k_adapter_down(DownArgs p) {
     const u16* xb = p.x + static_cast<i64>(tb) * p.ldx;
     u16* own = reinterpret_cast<u16*>(&sums[wave][0][0]);
     for (int a = next_adapter(my_id, -1); a != 0x7FFFFFFF; a = next_adapter(my_id, a)) {       // uniform over the workgroup
-        const AdapterDesc& d = p.ad[a];
+        const AdapterDesc d = p.ad[a];
         const u32 rank = d.rank < p.max_rank ? d.rank : p.max_rank;
         const u16* m = ALONG ? d.a : d.b;
+        const bool vec_m = ALONG ? d.vec_a : d.vec_b;
         for (u32 r0 = 0; r0 < rank; r0 += kDownRanks) {
             const u32 ranks = rank - r0 < static_cast<u32>(kDownRanks) ? rank - r0 : static_cast<u32>(kDownRanks);
             const u32 groups = ranks <= 16 ? 1 : (ranks <= 32 ? 2 : 4);
             f32x4 acc[2][4] = {};
-            if (groups == 1)      down_sums<E, ALONG, VECX, 1>(p, xa, xb, m, rank, r0, own, acc);
-            else if (groups == 2) down_sums<E, ALONG, VECX, 2>(p, xa, xb, m, rank, r0, own, acc);
-            else                  down_sums<E, ALONG, VECX, 4>(p, xa, xb, m, rank, r0, own, acc);
+            if (vec_m) {
+                if (groups == 1)      down_sums<E, ALONG, VECX, true, WAVES, 1>(p, xa, xb, m, rank, r0, own, acc);
+                else if (groups == 2) down_sums<E, ALONG, VECX, true, WAVES, 2>(p, xa, xb, m, rank, r0, own, acc);
+                else                  down_sums<E, ALONG, VECX, true, WAVES, 4>(p, xa, xb, m, rank, r0, own, acc);
+            } else {
+                if (groups == 1)      down_sums<E, ALONG, VECX, false, WAVES, 1>(p, xa, xb, m, rank, r0, own, acc);
+                else if (groups == 2) down_sums<E, ALONG, VECX, false, WAVES, 2>(p, xa, xb, m, rank, r0, own, acc);
+                else                  down_sums<E, ALONG, VECX, false, WAVES, 4>(p, xa, xb, m, rank, r0, own, acc);
+            }
 #pragma unroll
             for (u32 h = 0; h < 2; ++h)
 #pragma unroll
@@ -312,7 +373,7 @@ __global__ __launch_bounds__(64 * kDownWaves) void k_adapter_down(DownArgs p) {
             __syncthreads();
             const bool last = r0 + kDownRanks >= rank;
             const u32 end = last ? width : r0 + kDownRanks;
-            for (u32 i = wave; i < kDownTokens; i += kDownWaves) {
+            for (u32 i = wave; i < kDownTokens; i += WAVES) {
                 if (__shfl(my_id, static_cast<int>(i), 64) != a) continue;       // uniform
                 const u64 t = t0 + i;
                 u32 most = 0;
@@ -320,7 +381,7 @@ __global__ __launch_bounds__(64 * kDownWaves) void k_adapter_down(DownArgs p) {
                     float v = 0.0f;
                     if (j < rank) {
 #pragma unroll
-                        for (int w = 0; w < kDownWaves; ++w) v += sums[w][i][j - r0];
+                        for (u32 w = 0; w < WAVES; ++w) v += sums[w][i][j - r0];
                         v *= d.scale;
                     }
                     const u16 h = E::enc(v);
@@ -346,6 +407,13 @@ __global__ __launch_bounds__(64 * kDownWaves) void k_adapter_down(DownArgs p) {
     }
 }
 
+constexpr u32 kDownWaves = 8;
+template <typename E, bool ALONG, bool VECX>
+__global__ __launch_bounds__(64 * kDownWaves) void k_adapter_down(DownArgs p) {
+    __shared__ __align__(16) char lds[down_lds(kDownWaves)];
+    down_tile<E, ALONG, VECX, kDownWaves>(p, blockIdx.x, lds);
+}
+
 // ---- the wide product with the adapters' share added ------------------------------------------------------------
 
 struct WideArgs {
@@ -357,7 +425,6 @@ struct WideArgs {
     const int* ids;
     const AdapterDesc* ad;
     u32 n_adapters, max_rank;
-    u32 vec_m;                           // 16-byte aligned rows of the adapters' matrix
     u32 vec_y;                           // 8-byte aligned groups of four outputs
     u32 splits, steps_each;              // steps of 64 values that a split sums
     float* part;                         // splits > 1: [splits][n_tokens][n_out]
@@ -374,18 +441,19 @@ __device__ inline u32 die_order(u32 i, u32 n) {
 // matrix instructions wait for neither LDS nor memory; wavefronts meet once a step, in its middle, where the next step has come and the
 // last read of this one is done.  Otherwise (rows that are not 16-byte aligned) steps go through registers.
 // splits > 1: a workgroup sums a part of the steps and stores it in binary32; the adapters' share is then added with the parts.
+constexpr u32 wide_lds(u32 bm, u32 bn, u32 nb) { return nb * (bm + bn) * 128 + bm * 4; }
 template <typename E, int BM, int BN, int WM, int WN, u32 NB, bool ALONG, bool VEC>
-__global__ __launch_bounds__(64 * WM * WN, 2) void k_adapter_wide(WideArgs p) {
+__device__ inline void wide_tile(const WideArgs& p, u32 block_id, u32 n_blocks, char* lds) {
     constexpr u32 kThreads = 64 * WM * WN;
     constexpr u32 TM = BM / WM, TN = BN / WN, FM = TM / 16, FN = TN / 16;
     constexpr u32 kXPieces = BM * 8 / kThreads, kWPieces = BN * 8 / kThreads, kLoads = kXPieces + kWPieces;
     constexpr u32 kTile = (BM + BN) * 64, kEarly = FN < FM ? FN : FN / 2, kEach = FN / kEarly;
-    __shared__ __align__(16) u16 tiles[NB * kTile];
-    __shared__ int s_ids[BM];
+    u16* tiles = reinterpret_cast<u16*>(lds);
+    int* s_ids = reinterpret_cast<int*>(lds + NB * kTile * 2);
     const u32 tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const u32 wm = wave / WN, wn = wave % WN;
     const u32 tiles_m = (p.n_tokens + BM - 1) / BM, tiles_n = (p.n_out + BN - 1) / BN;
-    const u32 block = die_order(blockIdx.x, gridDim.x);
+    const u32 block = die_order(block_id, n_blocks);
     const u32 tile = block / p.splits, split = block % p.splits;
     // four rows of tiles at a time: tiles that run together share rows of x and of W
     const u32 band = tile / (4 * tiles_n), in_band = tile % (4 * tiles_n), high = tiles_m - band * 4 < 4 ? tiles_m - band * 4 : 4;
@@ -484,56 +552,64 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_adapter_wide(WideArgs p) {
             meet_loads<0>();
         }
     } else {
-        u32x4 rx[kXPieces], rw[kWPieces];
-        auto fetch = [&](u32 s) {
+        constexpr u32 kAhead = 3;                                  // steps whose rows are under way
+        u32x4 rx[kAhead][kXPieces], rw[kAhead][kWPieces];
+        const i64 sum_end = static_cast<i64>(end) * 64 < p.n_sum ? static_cast<i64>(end) * 64 : p.n_sum;       // zeros from there on
+        auto fetch = [&](u32 set, u32 s) {
             const i64 k0 = static_cast<i64>(s) * 64;
 #pragma unroll
             for (u32 i = 0; i < kXPieces; ++i) {
                 const u32 at = i * kThreads + tid, t = t0 + (at >> 3) < p.n_tokens ? t0 + (at >> 3) : p.n_tokens - 1;
-                rx[i] = load8<false>(p.x + static_cast<i64>(t) * p.ldx, k0 + (at & 7u) * 8, p.n_sum);
+                rx[set][i] = load8<false>(p.x + static_cast<i64>(t) * p.ldx, k0 + (at & 7u) * 8, sum_end);
             }
 #pragma unroll
             for (u32 i = 0; i < kWPieces; ++i) {
                 const u32 at = i * kThreads + tid;
                 if (ALONG) {
                     const u32 n = n0 + (at >> 3) < p.n_out ? n0 + (at >> 3) : p.n_out - 1;
-                    rw[i] = load8<false>(p.w + static_cast<i64>(n) * p.ldw, k0 + (at & 7u) * 8, p.n_sum);
+                    rw[set][i] = load8<false>(p.w + static_cast<i64>(n) * p.ldw, k0 + (at & 7u) * 8, sum_end);
                 } else {
                     constexpr u32 kRow = BN / 8;
                     const i64 k = k0 + at / kRow;
-                    rw[i] = load8<false>(p.w + k * p.ldw, n0 + (at % kRow) * 8, k < p.n_sum ? p.n_out : 0);
+                    rw[set][i] = load8<false>(p.w + k * p.ldw, n0 + (at % kRow) * 8, k < sum_end ? p.n_out : 0);
                 }
             }
         };
-        if (steps > 0) fetch(begin);
+        if (steps > 0) {
+#pragma unroll
+            for (u32 q = 0; q < kAhead; ++q) fetch(q, begin + q);
+        }
         u32 to = 0;
-        for (u32 s = begin; s < end; ++s) {
-            u16* sx = tiles + to;
+        for (u32 s = begin; s < end; s += kAhead) {
 #pragma unroll
-            for (u32 i = 0; i < kXPieces; ++i) {
-                const u32 at = i * kThreads + tid;
-                *reinterpret_cast<u32x4*>(sx + along_at(at >> 3, at & 7u)) = rx[i];
+            for (u32 q = 0; q < kAhead; ++q) {                     // past the end: zeros
+                u16* sx = tiles + to;
+#pragma unroll
+                for (u32 i = 0; i < kXPieces; ++i) {
+                    const u32 at = i * kThreads + tid;
+                    *reinterpret_cast<u32x4*>(sx + along_at(at >> 3, at & 7u)) = rx[q][i];
+                }
+#pragma unroll
+                for (u32 i = 0; i < kWPieces; ++i) {
+                    const u32 at = i * kThreads + tid;
+                    const u32 w_at = ALONG ? along_at(at >> 3, at & 7u) : across_at<BN>(at / (BN / 8), at % (BN / 8));
+                    *reinterpret_cast<u32x4*>(sx + BM * 64 + w_at) = rw[q][i];
+                }
+                __syncthreads();
+                fetch(q, s + q + kAhead);
+#pragma unroll
+                for (u32 sub = 0; sub < 2; ++sub) {
+#pragma unroll
+                    for (u32 i = 0; i < FN; ++i) fw[i] = frag_w(sx, i, sub);
+#pragma unroll
+                    for (u32 j = 0; j < FM; ++j) fx[j] = frag_x(sx, j, sub);
+#pragma unroll
+                    for (u32 j = 0; j < FM; ++j)
+#pragma unroll
+                        for (u32 i = 0; i < FN; ++i) acc[i][j] = E::mfma(fw[i], fx[j], acc[i][j]);
+                }
+                to = to == 0 ? kTile : 0;                          // the one that all have read since the barrier before this one
             }
-#pragma unroll
-            for (u32 i = 0; i < kWPieces; ++i) {
-                const u32 at = i * kThreads + tid;
-                const u32 w_at = ALONG ? along_at(at >> 3, at & 7u) : across_at<BN>(at / (BN / 8), at % (BN / 8));
-                *reinterpret_cast<u32x4*>(sx + BM * 64 + w_at) = rw[i];
-            }
-            __syncthreads();
-            if (s + 1 < end) fetch(s + 1);
-#pragma unroll
-            for (u32 sub = 0; sub < 2; ++sub) {
-#pragma unroll
-                for (u32 i = 0; i < FN; ++i) fw[i] = frag_w(sx, i, sub);
-#pragma unroll
-                for (u32 j = 0; j < FM; ++j) fx[j] = frag_x(sx, j, sub);
-#pragma unroll
-                for (u32 j = 0; j < FM; ++j)
-#pragma unroll
-                    for (u32 i = 0; i < FN; ++i) acc[i][j] = E::mfma(fw[i], fx[j], acc[i][j]);
-            }
-            to = to == 0 ? kTile : 0;                              // the one that all have read since the barrier before this one
         }
     }
     __syncthreads();
@@ -541,24 +617,28 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_adapter_wide(WideArgs p) {
     // What is left of the sum, then the adapters' share: 64 values of rank for each adapter that the tile's tokens have.  A product is added
     // where the token is the adapter's and nowhere else: zeros in its place would spread infinities and NaN of one request's adapter to its
     // neighbours.
+    u32 me = tid;
+    asm volatile("" : "+v"(me));                                  // keeps the places below out of registers while the sum runs
     int a = -1;
     u32 r0 = 0, rank = 0;
     const u16* m = nullptr;
+    bool vec_m = false;
     for (;;) {                                                     // uniform
         if (!rest) {
             if (p.splits > 1) break;                               // added with the parts
             r0 += 64;
             if (r0 >= rank) {
                 int next = 0x7FFFFFFF;
-                for (u32 i = lane; i < BM; i += 64) {
+                for (u32 i = me & 63u; i < BM; i += 64) {
                     const int id = s_ids[i];
                     if (id > a && id < next) next = id;
                 }
                 a = next_adapter(next, -1);                        // the same in every wavefront
                 if (a == 0x7FFFFFFF) break;
-                const AdapterDesc& d = p.ad[a];
+                const AdapterDesc d = p.ad[a];
                 rank = d.rank < p.max_rank ? d.rank : p.max_rank;
                 m = ALONG ? d.b : d.a;
+                vec_m = ALONG ? d.vec_b : d.vec_a;
                 r0 = 0;
             }
         }
@@ -567,14 +647,14 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_adapter_wide(WideArgs p) {
         const u32 subs = k_end - k0 > 32 ? 2 : 1;
         const u16* x = rest ? p.x : p.zp;
         const i64 ldx = rest ? p.ldx : static_cast<i64>(p.rp), x_end = rest ? p.n_sum : p.rp;
-        for (u32 at = tid; at < BM * 8; at += kThreads) {
+        for (u32 at = me; at < BM * 8; at += kThreads) {
             const u32 row = at >> 3, piece = at & 7u, t = t0 + row < p.n_tokens ? t0 + row : p.n_tokens - 1;
             if (piece < subs * 4) *reinterpret_cast<u32x4*>(tiles + along_at(row, piece)) = load8<true>(x + static_cast<i64>(t) * ldx, k0 + piece * 8, x_end);
         }
         const u16* w = rest ? p.w : m;
         const i64 ldw = rest ? p.ldw : (ALONG ? static_cast<i64>(rank) : static_cast<i64>(p.n_out));
-        const bool vec_w = rest || p.vec_m;
-        for (u32 at = tid; at < BN * 8; at += kThreads) {
+        const bool vec_w = rest || vec_m;
+        for (u32 at = me; at < BN * 8; at += kThreads) {
             const u32 row = ALONG ? at >> 3 : at / (BN / 8), piece = ALONG ? at & 7u : at % (BN / 8);
             if ((ALONG ? piece >> 2 : row >> 5) >= subs) continue;
             const u16* src = ALONG ? w + static_cast<i64>(n0 + row < p.n_out ? n0 + row : p.n_out - 1) * ldw : w + (k0 + row) * ldw;
@@ -589,7 +669,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_adapter_wide(WideArgs p) {
 #pragma unroll
             for (u32 j = 0; j < FM; ++j) {
                 fx[0] = frag_x(tiles, j, sub);
-                const bool mine = rest || s_ids[wm * TM + j * 16 + (lane & 15)] == a;
+                const bool mine = rest || s_ids[wm * TM + j * 16 + (me & 15u)] == a;
 #pragma unroll
                 for (u32 i = 0; i < FN; ++i) {
                     const f32x4 v = E::mfma(fw[i], fx[0], f32x4{0.0f, 0.0f, 0.0f, 0.0f});
@@ -645,102 +725,201 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_adapter_wide(WideArgs p) {
     }
 }
 
+template <typename E, int BM, int BN, int WM, int WN, u32 NB, bool ALONG, bool VEC>
+__global__ __launch_bounds__(64 * WM * WN, 2) void k_adapter_wide(WideArgs p) {
+    __shared__ __align__(16) char lds[wide_lds(BM, BN, NB)];
+    wide_tile<E, BM, BN, WM, WN, NB, ALONG, VEC>(p, blockIdx.x, gridDim.x, lds);
+}
+
+// Where the tiles of 64 x 64 outputs are few, the sum is split and z is made in the same launch: nothing in it waits for anything.
+template <typename E, bool ALONG, bool VECX, bool VEC>
+__global__ __launch_bounds__(256, 2) void k_adapter_split(DownArgs d, WideArgs w, u32 down_blocks) {
+    constexpr u32 NB = VEC ? 4 : 2;
+    __shared__ __align__(16) char lds[wide_lds(64, 64, NB) > down_lds(4) ? wide_lds(64, 64, NB) : down_lds(4)];
+    if (blockIdx.x < down_blocks) down_tile<E, ALONG, VECX, 4>(d, blockIdx.x, lds);
+    else wide_tile<E, 64, 64, 2, 2, NB, ALONG, VEC>(w, blockIdx.x - down_blocks, gridDim.x - down_blocks, lds);
+}
+
+// out = the parts added in order + z M_a (M_a: B^T or A), one output a thread; z in binary32.
+template <typename E, bool ALONG>
+__device__ inline void join_parts(const WideArgs& g, const float* z32, u32 ldz32, u32 t, u32 n) {
+    const int a = __builtin_amdgcn_readfirstlane(adapter_of(g.ids, t, g.n_tokens, g.n_adapters));
+    if (n >= g.n_out) return;
+    const float* part = g.part + static_cast<u64>(t) * g.n_out + n;
+    const u64 each = static_cast<u64>(g.n_tokens) * g.n_out;
+    float v = 0.0f;
+#pragma unroll 4
+    for (u32 s = 0; s < g.splits; ++s) v += part[s * each];
+    if (a >= 0) {
+        const AdapterDesc d = g.ad[a];
+        const u32 rank = d.rank < g.max_rank ? d.rank : g.max_rank;
+        const float* z = z32 + static_cast<u64>(t) * ldz32;
+        float u = 0.0f;
+        if (ALONG) {
+            const u16* b = d.b + static_cast<i64>(n) * rank;
+            for (u32 j = 0; j < rank; j += 8) {
+                const u32x4 h = d.vec_b ? load8<true>(b, j, rank) : load8<false>(b, j, rank);
+#pragma unroll
+                for (u32 i = 0; i < 8; ++i) if (j + i < rank) u = __builtin_fmaf(z[j + i], E::dec(static_cast<u16>(h[i >> 1] >> (16 * (i & 1)))), u);
+            }
+        } else {
+            const u16* m = d.a + n;
+#pragma unroll 8
+            for (u32 j = 0; j < rank; ++j) u = __builtin_fmaf(z[j], E::dec(load2(m + static_cast<i64>(j) * g.n_out)), u);
+        }
+        v += u;
+    }
+    g.y[static_cast<i64>(t) * g.ldy + n] = E::enc(v);
+}
+
+template <typename E, bool ALONG>
+__global__ __launch_bounds__(256) void k_adapter_split_join(WideArgs w, const float* z32, u32 ldz32) {
+    join_parts<E, ALONG>(w, z32, ldz32, blockIdx.y, blockIdx.x * 256 + threadIdx.x);
+}
+
 // ---- few tokens -------------------------------------------------------------------------------------------------
 
 struct FewArgs {
     WideArgs wide;
-    float* part;                         // [splits][n_tokens][n_out]
     float* z32;                          // [n_tokens][max_rank]
     u16* z; i64 ldz;
-    u32 tiles_n, splits, steps_each;     // steps of 32 values that a split sums
-    u32 vec_a;
+    u32 tiles_n;
 };
 
-constexpr u32 kFewCols = 64, kFewWaves = 8;
+constexpr u32 kFewCols = 32, kFewWaves = 8;
 
-// Up to 64 tokens: reading the weights once bounds it.  One launch reads everything that does not wait for anything: workgroups of
-// 64 outputs and a part of the sum (two times 32 outputs by four interleaved quarters of it, added up in LDS) and one workgroup a token that
-// makes z; the next launch adds the parts and z B^T.  Weights go from memory straight to operand registers; FM tiles of 16 tokens use
-// them at once.
-template <typename E, u32 FM, bool VEC>
-__global__ __launch_bounds__(64 * kFewWaves) void k_adapter_few(FewArgs p) {
-    __shared__ __align__(16) float sums[4 * 2 * 2 * FM * 256];
+// z of one token: eight wavefronts share its sum, 16 G ranks at a time.
+template <typename E, bool VEC, bool VECM, u32 G>
+__device__ inline void few_z(const FewArgs& p, const AdapterDesc& d, u32 rank, u32 t, float* sums) {
     const WideArgs& g = p.wide;
     const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, sub = (lane >> 4) * 8;
-    const u32 steps = (g.n_sum + 31) / 32;
-    if (blockIdx.x >= p.tiles_n * p.splits) {                  // z of one token: all eight wavefronts share its sum
-        const u32 t = blockIdx.x - p.tiles_n * p.splits;
-        const int a = adapter_of(g.ids, t, g.n_tokens, g.n_adapters);
-        const u32 rank = a < 0 ? 0 : (g.ad[a].rank < g.max_rank ? g.ad[a].rank : g.max_rank);
-        const u16* x = g.x + static_cast<i64>(t) * g.ldx;
-        for (u32 r0 = 0; r0 < rank; r0 += 16) {
-            f32x4 acc = {};
-            const u32 j = r0 + row;
-            const u16* m = g.ad[a].a + static_cast<i64>(j < rank ? j : 0) * g.n_sum;
-#pragma unroll 4
-            for (u32 s = wave; s < steps; s += kFewWaves) {
-                const i64 k = static_cast<i64>(s) * 32 + sub;
-                const u32x4 fm = p.vec_a ? load8<true>(m, k, g.n_sum) : load8<false>(m, k, g.n_sum);
-                acc = E::mfma(fm, load8<VEC>(x, k, g.n_sum), acc);       // the token in every column
-            }
-            __syncthreads();
-            if (row == 0)
+    const u16* x = g.x + static_cast<i64>(t) * g.ldx;
+    for (u32 r0 = 0; r0 < rank; r0 += 16 * G) {
+        f32x4 acc[G] = {};
+        const u16* m[G];
 #pragma unroll
-                for (u32 i = 0; i < 4; ++i) sums[wave * 16 + (lane >> 4) * 4 + i] = acc[i];
-            __syncthreads();
-            if (threadIdx.x < 16 && r0 + threadIdx.x < rank) {
-                float v = 0.0f;
+        for (u32 q = 0; q < G; ++q) {
+            const u32 j = r0 + q * 16 + row;
+            m[q] = d.a + static_cast<i64>(j < rank ? j : rank - 1) * g.n_sum;
+        }
+        auto step = [&](auto guard, u32 s) {
+            const i64 k = static_cast<i64>(s) * 64 + sub;
+            u32x4 fx[2], fm[2][G];
 #pragma unroll
-                for (u32 w = 0; w < kFewWaves; ++w) v += sums[w * 16 + threadIdx.x];
-                p.z32[static_cast<u64>(t) * g.max_rank + r0 + threadIdx.x] = v * g.ad[a].scale;
+            for (u32 h = 0; h < 2; ++h) {
+                fx[h] = decltype(guard)::value ? load8<VEC>(x, k + h * 32, g.n_sum) : load8_inside<VEC>(x + k + h * 32);
+#pragma unroll
+                for (u32 q = 0; q < G; ++q) fm[h][q] = decltype(guard)::value ? load8<VECM>(m[q], k + h * 32, g.n_sum) : load8_inside<VECM>(m[q] + k + h * 32);
             }
+#pragma unroll
+            for (u32 h = 0; h < 2; ++h)
+#pragma unroll
+                for (u32 q = 0; q < G; ++q) acc[q] = E::mfma(fm[h][q], fx[h], acc[q]);       // the token in every column
+        };
+        const u32 full = g.n_sum / 64;
+        u32 s = wave;
+#pragma unroll 3
+        for (; s < full; s += kFewWaves) step(std::false_type{}, s);
+        if (s == full && (g.n_sum & 63u)) step(std::true_type{}, s);
+        __syncthreads();
+        if (row == 0)
+#pragma unroll
+            for (u32 q = 0; q < G; ++q)
+#pragma unroll
+                for (u32 i = 0; i < 4; ++i) sums[(wave * G + q) * 16 + (lane >> 4) * 4 + i] = acc[q][i];
+        __syncthreads();
+        if (threadIdx.x < 16 * G && r0 + threadIdx.x < rank) {
+            float v = 0.0f;
+#pragma unroll
+            for (u32 w = 0; w < kFewWaves; ++w) v += sums[w * G * 16 + threadIdx.x];
+            p.z32[static_cast<u64>(t) * g.max_rank + r0 + threadIdx.x] = v * d.scale;
+        }
+    }
+}
+
+// Up to 64 tokens: reading the weights once bounds it.  One launch reads everything that does not wait for anything: one workgroup a token
+// that makes z (they come first, theirs is the longest chain), and workgroups of 32 outputs and a part of the sum, of which eight wavefronts
+// take every eighth 64 values; the next launch adds the parts and z B^T.  Weights and tokens go from memory straight to operand
+// registers, and FM tiles of 16 tokens use the weights at once.
+template <typename E, u32 FM, bool VEC>
+__global__ __launch_bounds__(64 * kFewWaves, 4) void k_adapter_few(FewArgs p) {
+    __shared__ __align__(16) float sums[4 * 2 * FM * 256];
+    const WideArgs& g = p.wide;
+    const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, sub = (lane >> 4) * 8;
+    if (blockIdx.x < g.n_tokens) {
+        const int a = __builtin_amdgcn_readfirstlane(adapter_of(g.ids, blockIdx.x, g.n_tokens, g.n_adapters));
+        if (a < 0) return;
+        const AdapterDesc d = g.ad[a];
+        const u32 rank = d.rank < g.max_rank ? d.rank : g.max_rank;
+        if (d.vec_a) {
+            if (rank <= 16) few_z<E, VEC, true, 1>(p, d, rank, blockIdx.x, sums);
+            else            few_z<E, VEC, true, 4>(p, d, rank, blockIdx.x, sums);
+        } else {
+            if (rank <= 16) few_z<E, VEC, false, 1>(p, d, rank, blockIdx.x, sums);
+            else            few_z<E, VEC, false, 4>(p, d, rank, blockIdx.x, sums);
         }
         return;
     }
-    const u32 tile = blockIdx.x % p.tiles_n, split = blockIdx.x / p.tiles_n;
-    const u32 part = wave >> 1, n0 = tile * kFewCols + (wave & 1) * 32;
-    const u32 begin = split * p.steps_each, end = begin + p.steps_each < steps ? begin + p.steps_each : steps;
+    const u32 block = blockIdx.x - g.n_tokens, tile = block % p.tiles_n, split = block / p.tiles_n;
+    const u32 steps = (g.n_sum + 63) / 64, n0 = tile * kFewCols;
+    const u32 begin = split * g.steps_each, end = begin + g.steps_each < steps ? begin + g.steps_each : steps;
     const u16* w[2];
     const u16* x[FM];
 #pragma unroll
     for (u32 i = 0; i < 2; ++i) {
-        u32 n = n0 + i * 16 + row;
-        if (n >= g.n_out) n = g.n_out - 1;
-        w[i] = g.w + static_cast<i64>(n) * g.ldw;
+        const u32 n = n0 + i * 16 + row;
+        w[i] = g.w + static_cast<i64>(n < g.n_out ? n : g.n_out - 1) * g.ldw;
     }
 #pragma unroll
     for (u32 i = 0; i < FM; ++i) {
-        u32 t = i * 16 + row;
-        if (t >= g.n_tokens) t = g.n_tokens - 1;
-        x[i] = g.x + static_cast<i64>(t) * g.ldx;
+        const u32 t = i * 16 + row;
+        x[i] = g.x + static_cast<i64>(t < g.n_tokens ? t : g.n_tokens - 1) * g.ldx;
     }
     f32x4 acc[2][FM] = {};
-#pragma unroll 2
-    for (u32 s = begin + part; s < end; s += 4) {
-        const i64 k = static_cast<i64>(s) * 32 + sub;
-        u32x4 fw[2], fx[FM];
+    auto step = [&](auto guard, u32 s) {
+        const i64 k = static_cast<i64>(s) * 64 + sub;
+        u32x4 fw[2][2], fx[2][FM];
 #pragma unroll
-        for (u32 i = 0; i < 2; ++i) fw[i] = load8<VEC>(w[i], k, g.n_sum);
+        for (u32 h = 0; h < 2; ++h) {
 #pragma unroll
-        for (u32 i = 0; i < FM; ++i) fx[i] = load8<VEC>(x[i], k, g.n_sum);
+            for (u32 i = 0; i < 2; ++i) fw[h][i] = decltype(guard)::value ? load8<VEC>(w[i], k + h * 32, g.n_sum) : load8_inside<VEC>(w[i] + k + h * 32);
+#pragma unroll
+            for (u32 i = 0; i < FM; ++i) fx[h][i] = decltype(guard)::value ? load8<VEC>(x[i], k + h * 32, g.n_sum) : load8_inside<VEC>(x[i] + k + h * 32);
+        }
+        __builtin_amdgcn_sched_barrier(0);                     // all loads before the first product
+#pragma unroll
+        for (u32 h = 0; h < 2; ++h)
+#pragma unroll
+            for (u32 i = 0; i < 2; ++i)
+#pragma unroll
+                for (u32 j = 0; j < FM; ++j) acc[i][j] = E::mfma(fw[h][i], fx[h][j], acc[i][j]);
+    };
+    const u32 full = (g.n_sum & 63u) && end == steps && end > begin ? end - 1 : end;
+    u32 s = begin + wave;
+    for (; s < full; s += kFewWaves) step(std::false_type{}, s);
+    if (s == full && full < end) step(std::true_type{}, s);
+    // eight sums: the upper four are added to the lower ones, then those in LDS
+    f32x4* mine = reinterpret_cast<f32x4*>(sums) + (wave & 3u) * 2 * FM * 64 + lane;
+    if (wave >= 4)
 #pragma unroll
         for (u32 i = 0; i < 2; ++i)
 #pragma unroll
-            for (u32 j = 0; j < FM; ++j) acc[i][j] = E::mfma(fw[i], fx[j], acc[i][j]);
-    }
-#pragma unroll
-    for (u32 i = 0; i < 2; ++i)
-#pragma unroll
-        for (u32 j = 0; j < FM; ++j) *reinterpret_cast<f32x4*>(&sums[((((part * 2 + (wave & 1)) * 2 + i) * FM + j) * 64 + lane) * 4]) = acc[i][j];
+            for (u32 j = 0; j < FM; ++j) mine[(i * FM + j) * 64] = acc[i][j];
     __syncthreads();
-    for (u32 at = threadIdx.x; at < 2 * 2 * FM * 64; at += 64 * kFewWaves) {
-        f32x4 v = *reinterpret_cast<const f32x4*>(&sums[at * 4]);
+    if (wave < 4)
 #pragma unroll
-        for (u32 q = 1; q < 4; ++q) v += *reinterpret_cast<const f32x4*>(&sums[(q * 2 * 2 * FM * 64 + at) * 4]);
-        const u32 l = at & 63, j = at / 64 % FM, i = at / 64 / FM % 2, half = at / 64 / FM / 2;
-        const u32 t = j * 16 + (l & 15), n = tile * kFewCols + half * 32 + i * 16 + (l >> 4) * 4;
+        for (u32 i = 0; i < 2; ++i)
+#pragma unroll
+            for (u32 j = 0; j < FM; ++j) mine[(i * FM + j) * 64] += acc[i][j];
+    __syncthreads();
+    for (u32 at = threadIdx.x; at < 2 * FM * 64; at += 64 * kFewWaves) {
+        f32x4 v = reinterpret_cast<const f32x4*>(sums)[at];
+#pragma unroll
+        for (u32 q = 1; q < 4; ++q) v += reinterpret_cast<const f32x4*>(sums)[q * 2 * FM * 64 + at];
+        const u32 l = at & 63, j = at / 64 % FM, i = at / 64 / FM;
+        const u32 t = j * 16 + (l & 15), n = n0 + i * 16 + (l >> 4) * 4;
         if (t >= g.n_tokens) continue;
-        float* out = p.part + (static_cast<u64>(split) * g.n_tokens + t) * g.n_out + n;
+        float* out = g.part + (static_cast<u64>(split) * g.n_tokens + t) * g.n_out + n;
         if ((g.n_out & 3u) == 0 && n + 4 <= g.n_out) *reinterpret_cast<f32x4*>(out) = v;
         else
 #pragma unroll
@@ -748,30 +927,16 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_adapter_few(FewArgs p) {
     }
 }
 
-// y = the parts added in order + z B^T, one output a thread; z is kept in binary32 here.
 template <typename E>
 __global__ __launch_bounds__(256) void k_adapter_few_join(FewArgs p) {
     const WideArgs& g = p.wide;
-    const u32 t = blockIdx.y, n = blockIdx.x * 256 + threadIdx.x;
-    const int a = adapter_of(g.ids, t, g.n_tokens, g.n_adapters);
-    const u32 rank = a < 0 ? 0 : (g.ad[a].rank < g.max_rank ? g.ad[a].rank : g.max_rank);
-    const float* z = p.z32 + static_cast<u64>(t) * g.max_rank;
-    if (p.z && blockIdx.x == 0)
-        for (u32 j = threadIdx.x; j < p.ldz; j += 256) p.z[static_cast<u64>(t) * p.ldz + j] = j < rank ? E::enc(z[j]) : static_cast<u16>(0);
-    if (n >= g.n_out) return;
-    float v = 0.0f;
-    for (u32 s = 0; s < p.splits; ++s) v += p.part[(static_cast<u64>(s) * g.n_tokens + t) * g.n_out + n];
-    if (rank) {
-        const u16* b = g.ad[a].b + static_cast<i64>(n) * rank;
-        float u = 0.0f;
-        for (u32 j = 0; j < rank; j += 8) {
-            const u32x4 h = g.vec_m ? load8<true>(b, j, rank) : load8<false>(b, j, rank);
-#pragma unroll
-            for (u32 i = 0; i < 8; ++i) if (j + i < rank) u = __builtin_fmaf(z[j + i], E::dec(static_cast<u16>(h[i >> 1] >> (16 * (i & 1)))), u);
-        }
-        v += u;
+    const u32 t = blockIdx.y;
+    if (p.z && blockIdx.x == 0) {
+        const int a = adapter_of(g.ids, t, g.n_tokens, g.n_adapters);
+        const u32 rank = a < 0 ? 0 : (g.ad[a].rank < g.max_rank ? g.ad[a].rank : g.max_rank);
+        for (u32 j = threadIdx.x; j < p.ldz; j += 256) p.z[static_cast<u64>(t) * p.ldz + j] = j < rank ? E::enc(p.z32[static_cast<u64>(t) * g.max_rank + j]) : static_cast<u16>(0);
     }
-    g.y[static_cast<i64>(t) * g.ldy + n] = E::enc(v);
+    join_parts<E, true>(g, p.z32, g.max_rank, t, blockIdx.x * 256 + threadIdx.x);
 }
 
 // ---- gradients of the adapters ----------------------------------------------------------------------------------
@@ -783,10 +948,10 @@ struct GradArgs {
     const u16* z; i64 ldz;
     const u32* row_max;
     const u32* order;
+    const uint4* slots;
     const uint2* seg;
-    const u32* slots;
     const AdapterDesc* ad;
-    u32 max_rank, run, tiles_in, tiles, vec;
+    u32 max_rank, run, tiles_in, tiles, rank_groups;
     float* part;                         // [n_slots][max_rank (n_in + n_out)]
 };
 
@@ -797,23 +962,29 @@ constexpr u32 kGradCols = 128, kGradStep = 64, kGradTokens = 1024;
 // so that they are read by one workgroup only (up to 64 ranks).  dz enters as a sum of 16-bit values, three of bfloat16 or two of
 // float16, since a binary32 gradient would keep no more than 8 or 11 bits of one; runs of float16 are scaled by a power of two first, so that the
 // largest dz of the run sits near the top of the type's range.
+// Workgroups before `joins` add the parts of dx.
 template <typename E, bool VEC>
-__global__ __launch_bounds__(256) void k_adapter_grads(GradArgs p) {
+__global__ __launch_bounds__(256) void k_adapter_grads(GradArgs p, WideArgs dx, u32 joins) {
     constexpr u32 kTerms = E::kNarrow ? 2 : 3;
     constexpr u32 kVPieces = kGradStep * kGradCols / 8 / 256, kUPieces = kGradStep * 8 / 256;
     __shared__ __align__(16) u16 sv[kGradStep * kGradCols], su[kTerms][kGradStep * 64];
     __shared__ u32 s_tok[kGradTokens];
     __shared__ u32 s_max;
     const u32 tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const u32 slot = blockIdx.x / p.tiles, col_tile = blockIdx.x % p.tiles, r0 = blockIdx.y * 64;
-    const u32 a = p.slots[slot];
+    const u32 grads = gridDim.x - joins;
+    if (blockIdx.x >= grads) {                                 // uniform
+        const u32 cols = (dx.n_out + 255) / 256, block = blockIdx.x - grads;
+        join_parts<E, false>(dx, p.dz, p.rp, block / cols, block % cols * 256 + tid);
+        return;
+    }
+    const u32 col_tile = blockIdx.x % p.tiles, r0 = blockIdx.x / p.tiles % p.rank_groups * 64, slot = blockIdx.x / p.tiles / p.rank_groups;
+    const uint4 of = p.slots[slot];
+    const u32 a = __builtin_amdgcn_readfirstlane(of.x), first = __builtin_amdgcn_readfirstlane(of.y), count = __builtin_amdgcn_readfirstlane(of.z);
+    const bool whole = of.w <= p.run;
     if (a == ~0u) return;                                      // uniform, as all that follow
-    const AdapterDesc& d = p.ad[a];
+    const AdapterDesc d = p.ad[a];
     const u32 rank = d.rank < p.max_rank ? d.rank : p.max_rank;
     if (r0 >= rank) return;
-    const uint2 seg = p.seg[a];
-    const u32 j = slot - first_slot(seg.x, p.run, a);
-    const u32 first = seg.x + j * p.run, count = seg.y < j * p.run ? 0 : (seg.y - j * p.run < p.run ? seg.y - j * p.run : p.run);
     const bool of_a = col_tile < p.tiles_in;
     const u32 c0 = (of_a ? col_tile : col_tile - p.tiles_in) * kGradCols;
     const u32 n_cols = of_a ? p.n_in : p.n_out;
@@ -821,22 +992,11 @@ __global__ __launch_bounds__(256) void k_adapter_grads(GradArgs p) {
     const i64 ldv = of_a ? p.ldx : p.ldy;
     const u32 pieces = (rank - r0 < 64 ? rank - r0 + 7 : 64) / 8;             // of eight ranks
     float up = 1.0f, down = 1.0f;
-    if (E::kNarrow && of_a) {
-        if (tid == 0) s_max = 0;
-        __syncthreads();
-        u32 most = 0;
-        for (u32 i = tid; i < count; i += 256) { const u32 m = p.row_max[p.order[first + i]]; most = most > m ? most : m; }
-        atomicMax(&s_max, most);
-        __syncthreads();
-        int e = 14 - (static_cast<int>(s_max >> 23) - 127);    // the largest becomes 2^14 .. 2^15
-        e = e > 120 ? 120 : (e < -100 ? -100 : e);
-        up = __uint_as_float(static_cast<u32>(127 + e) << 23);
-        down = __uint_as_float(static_cast<u32>(127 - e) << 23);
-    }
     f32x4 acc[2][4] = {};
     for (u32 c = 0; c < count; c += kGradTokens) {
         const u32 here = count - c < kGradTokens ? count - c : kGradTokens;
         __syncthreads();
+        if (tid == 0 && c == 0) s_max = 0;
         for (u32 i = tid; i < here; i += 256) s_tok[i] = p.order[first + c + i];
         __syncthreads();
         u32x4 rv[kVPieces], ru[2 * kUPieces];
@@ -863,6 +1023,19 @@ __global__ __launch_bounds__(256) void k_adapter_grads(GradArgs p) {
             }
         };
         fetch(0);
+        if (E::kNarrow && of_a && c == 0) {
+            u32 most = 0;
+            for (u32 i = tid; i < count; i += 256) {
+                const u32 m = p.row_max[i < here ? s_tok[i] : p.order[first + i]];
+                most = most > m ? most : m;
+            }
+            atomicMax(&s_max, most);
+            __syncthreads();
+            int e = 14 - (static_cast<int>(s_max >> 23) - 127);                // the largest becomes 2^14 .. 2^15
+            e = e > 120 ? 120 : (e < -100 ? -100 : e);
+            up = __uint_as_float(static_cast<u32>(127 + e) << 23);
+            down = __uint_as_float(static_cast<u32>(127 - e) << 23);
+        }
         for (u32 s = 0; s < here; s += kGradStep) {
 #pragma unroll
             for (u32 i = 0; i < kVPieces; ++i) {
@@ -919,7 +1092,6 @@ __global__ __launch_bounds__(256) void k_adapter_grads(GradArgs p) {
             __syncthreads();
         }
     }
-    const bool whole = seg.y <= p.run;
     float* out = whole ? (of_a ? d.grad_a : d.grad_b)
                        : p.part + static_cast<u64>(slot) * p.max_rank * (static_cast<u64>(p.n_in) + p.n_out) + (of_a ? 0 : static_cast<u64>(rank) * p.n_in);
 #pragma unroll
@@ -943,14 +1115,15 @@ __global__ __launch_bounds__(256) void k_adapter_grads(GradArgs p) {
 __global__ __launch_bounds__(256) void k_adapter_join(GradArgs p, u32 blocks_each) {
     const u32 a = blockIdx.x / blocks_each;
     const uint2 seg = p.seg[a];
-    if (seg.y <= p.run) return;                                // uniform
-    const AdapterDesc& d = p.ad[a];
+    if (seg.y <= 1) return;                                    // uniform
+    const AdapterDesc d = p.ad[a];
     const u32 rank = d.rank < p.max_rank ? d.rank : p.max_rank;
     const u64 na = static_cast<u64>(rank) * p.n_in, n = na + static_cast<u64>(rank) * p.n_out;
     const u64 each = static_cast<u64>(p.max_rank) * (static_cast<u64>(p.n_in) + p.n_out);
-    const u32 s0 = first_slot(seg.x, p.run, a), runs = (seg.y + p.run - 1) / p.run;
+    const u32 s0 = seg.x, runs = seg.y;
     for (u64 i = static_cast<u64>(blockIdx.x % blocks_each) * 256 + threadIdx.x; i < n; i += static_cast<u64>(blocks_each) * 256) {
         float v = p.part[s0 * each + i];
+#pragma unroll 4
         for (u32 r = 1; r < runs; ++r) v += p.part[(s0 + r) * each + i];
         if (i < na) d.grad_a[i] = v;
         else d.grad_b[i - na] = v;
