@@ -31,42 +31,31 @@ static u32 run_tokens(i64 n_tokens, i64 n_in, i64 n_out) {
 }
 
 struct Plan {
-    bool few = false, split = false;
-    u32 rp = 0, splits = 1, steps_each = 0, tiles_n = 0;
+    bool split = false;
+    u32 rp = 0, splits = 1, steps_each = 0, bm = 64;
     u32 run = 0, n_slots = 0, tiles = 0;
     size_t zp = 0, z32 = 0, part = 0, part_wide = 0, row_max = 0, order = 0, seg = 0, slots = 0, total = 0;
 };
 
-// Up to this many tokens the weights are read straight into registers, by workgroups that share the sum.
-constexpr i64 kFewTokens = 64;
+// Forward passes of up to this many tokens make z token by token.
+constexpr i64 kTokenwise = 256;
 
 static Plan make_plan(i64 T, i64 n_in, i64 n_out, u32 n_adapters, u32 max_rank, bool backward) {
     Plan p;
     size_t at = 0;
     auto take = [&](u64 bytes) { const size_t o = at; at += align_up(bytes ? bytes : 1); return o; };
     p.rp = padded_rank(max_rank ? max_rank : 1);
-    p.few = !backward && T <= kFewTokens;
-    if (p.few) {
-        const u32 steps = static_cast<u32>((n_in + 63) / 64);
-        p.tiles_n = static_cast<u32>((n_out + kFewCols - 1) / kFewCols);
-        // some 320 workgroups, and at least a step for each of the eight wavefronts of one
-        u32 s = (320 + p.tiles_n / 2) / p.tiles_n, most = steps / kFewWaves;
-        s = s > most ? most : s;
-        s = s > 8 ? 8 : (s < 1 ? 1 : s);
-        p.steps_each = (steps + s - 1) / s;
-        p.splits = (steps + p.steps_each - 1) / p.steps_each;
-        p.part_wide = take(static_cast<u64>(p.splits) * T * n_out * 4);
-        p.z32 = take(static_cast<u64>(T) * (max_rank ? max_rank : 1) * 4);
-    } else {
-        // the wide product: tiles of 64 x 64 outputs that would leave compute units without one are split along the sum
+    {
+        // The wide product: where tiles of 32 or 64 tokens by 64 outputs would leave compute units without work, several share a sum.
         const i64 n_wide = backward ? n_in : n_out, n_sum = backward ? n_out : n_in;
-        const u64 tiles = static_cast<u64>((T + 63) / 64) * ((n_wide + 63) / 64);
+        p.bm = T <= 32 ? 32 : 64;
+        const u64 tiles = static_cast<u64>((T + p.bm - 1) / p.bm) * ((n_wide + 63) / 64);
         const u32 steps = static_cast<u32>((n_sum + 63) / 64);
-        if (T > 0 && tiles < 512 && steps >= 4) {
-            u32 s = static_cast<u32>((1024 + tiles - 1) / tiles), most = steps / 2;
+        if (T > 0 && tiles < 512) {
+            u32 s = static_cast<u32>((512 + tiles - 1) / tiles), most = steps / 2;
             s = s > most ? most : s;
-            s = s > 16 ? 16 : s;
-            p.split = s > 1;
+            s = s > 16 ? 16 : (s < 1 ? 1 : s);
+            p.split = s > 1 || T <= kTokenwise;
             p.steps_each = (steps + s - 1) / s;
             p.splits = (steps + p.steps_each - 1) / p.steps_each;
             if (p.split) p.part_wide = take(static_cast<u64>(p.splits) * T * n_wide * 4);
@@ -104,6 +93,7 @@ static void launch_wide_tile(const WideArgs& a, hipStream_t st) {
 template <typename E, bool ALONG>
 static condensa_status launch_wide(WideArgs a, bool vec, hipStream_t st) {
     a.splits = 1;
+    a.part = nullptr;
     a.steps_each = (a.n_sum + 63) / 64;
     const auto tiles = [&](u64 m, u64 n) { return (a.n_tokens + m - 1) / m * ((a.n_out + n - 1) / n); };
     // A tile of 256 rows fills a compute unit.  The one whose rounds over the 256 of them cost less is taken: 8192 x 4608 outputs are 2.25 rounds
@@ -122,30 +112,18 @@ static condensa_status launch_wide(WideArgs a, bool vec, hipStream_t st) {
     return CONDENSA_OK;
 }
 
+template <typename E, bool ALONG, int BM>
+static void launch_split_tile(const DownArgs& d, const WideArgs& w, u32 down_blocks, bool by_token, bool vec, hipStream_t st) {
+    const u32 blocks = down_blocks + (w.n_tokens + BM - 1) / BM * ((w.n_out + 63) / 64) * w.splits;
+    if (vec)          hipLaunchKernelGGL((k_adapter_split<E, ALONG, true, true, BM>), dim3(blocks), dim3(256), 0, st, d, w, down_blocks, by_token);
+    else if (d.vec_x) hipLaunchKernelGGL((k_adapter_split<E, ALONG, true, false, BM>), dim3(blocks), dim3(256), 0, st, d, w, down_blocks, by_token);
+    else              hipLaunchKernelGGL((k_adapter_split<E, ALONG, false, false, BM>), dim3(blocks), dim3(256), 0, st, d, w, down_blocks, by_token);
+}
+
 template <typename E, bool ALONG>
-static condensa_status launch_split(const DownArgs& d, const WideArgs& w, u32 down_blocks, bool vec, hipStream_t st) {
-    const u32 blocks = down_blocks + (w.n_tokens + 63) / 64 * ((w.n_out + 63) / 64) * w.splits;
-    if (vec)          hipLaunchKernelGGL((k_adapter_split<E, ALONG, true, true>), dim3(blocks), dim3(256), 0, st, d, w, down_blocks);
-    else if (d.vec_x) hipLaunchKernelGGL((k_adapter_split<E, ALONG, true, false>), dim3(blocks), dim3(256), 0, st, d, w, down_blocks);
-    else              hipLaunchKernelGGL((k_adapter_split<E, ALONG, false, false>), dim3(blocks), dim3(256), 0, st, d, w, down_blocks);
-    CONDENSA_LAUNCH_CHECK();
-    return CONDENSA_OK;
-}
-
-template <typename E, u32 FM>
-static void launch_few_tile(const FewArgs& f, bool vec, u32 blocks, hipStream_t st) {
-    if (vec) hipLaunchKernelGGL((k_adapter_few<E, FM, true>), dim3(blocks), dim3(64 * kFewWaves), 0, st, f);
-    else     hipLaunchKernelGGL((k_adapter_few<E, FM, false>), dim3(blocks), dim3(64 * kFewWaves), 0, st, f);
-}
-
-template <typename E>
-static condensa_status launch_few(const FewArgs& f, bool vec, hipStream_t st) {
-    const u32 T = f.wide.n_tokens, blocks = f.tiles_n * f.wide.splits + T;
-    if (T <= 16)      launch_few_tile<E, 1>(f, vec, blocks, st);
-    else if (T <= 32) launch_few_tile<E, 2>(f, vec, blocks, st);
-    else              launch_few_tile<E, 4>(f, vec, blocks, st);
-    CONDENSA_LAUNCH_CHECK();
-    hipLaunchKernelGGL((k_adapter_few_join<E>), dim3((f.wide.n_out + 255) / 256, T), dim3(256), 0, st, f);
+static condensa_status launch_split(const DownArgs& d, const WideArgs& w, u32 bm, u32 down_blocks, bool by_token, bool vec, hipStream_t st) {
+    if (bm == 32) launch_split_tile<E, ALONG, 32>(d, w, down_blocks, by_token, vec, st);
+    else          launch_split_tile<E, ALONG, 64>(d, w, down_blocks, by_token, vec, st);
     CONDENSA_LAUNCH_CHECK();
     return CONDENSA_OK;
 }
@@ -264,15 +242,7 @@ condensa_status condensa_adapter_project(const condensa_adapter_list* list, cons
     g.n_adapters = static_cast<u32>(list->n_adapters); g.max_rank = static_cast<u32>(list->max_rank);
     g.vec_y = aligned(y_dev, 8) && y_stride % 4 == 0;
     g.splits = p.splits; g.steps_each = p.steps_each;
-    g.part = at<float>(workspace_dev, p.part_wide);
-    if (p.few) {
-        FewArgs f{};
-        f.wide = g;
-        f.z32 = at<float>(workspace_dev, p.z32);
-        f.z = z_dev; f.ldz = z_stride;
-        f.tiles_n = p.tiles_n;
-        return f16 ? launch_few<ElemF16>(f, vec, st) : launch_few<ElemBF16>(f, vec, st);
-    }
+    g.part = p.split ? at<float>(workspace_dev, p.part_wide) : nullptr;
     g.zp = p.split ? nullptr : at<u16>(workspace_dev, p.zp);
     DownArgs d{};
     d.x = x_dev; d.ldx = x_stride; d.n_tokens = g.n_tokens; d.n_sum = g.n_sum; d.ids = g.ids; d.ad = g.ad; d.n_adapters = g.n_adapters; d.max_rank = g.max_rank;
@@ -281,7 +251,9 @@ condensa_status condensa_adapter_project(const condensa_adapter_list* list, cons
     d.vec_x = vec_x;
     d.tiles = (g.n_tokens + kDownTokens - 1) / kDownTokens;
     if (p.split) {
-        condensa_status s = f16 ? launch_split<ElemF16, true>(d, g, d.tiles, vec, st) : launch_split<ElemBF16, true>(d, g, d.tiles, vec, st);
+        const bool by_token = n_tokens <= kTokenwise;
+        const u32 down = by_token ? g.n_tokens : d.tiles * kDownShare;
+        condensa_status s = f16 ? launch_split<ElemF16, true>(d, g, p.bm, down, by_token, vec, st) : launch_split<ElemBF16, true>(d, g, p.bm, down, by_token, vec, st);
         if (s != CONDENSA_OK) return s;
         const dim3 grid((g.n_out + 255) / 256, g.n_tokens);
         if (f16) hipLaunchKernelGGL((k_adapter_split_join<ElemF16, true>), grid, dim3(256), 0, st, g, static_cast<const float*>(d.z32), p.rp);
@@ -289,7 +261,7 @@ condensa_status condensa_adapter_project(const condensa_adapter_list* list, cons
         CONDENSA_LAUNCH_CHECK();
         return CONDENSA_OK;
     }
-    condensa_status s = f16 ? launch_down<ElemF16, true>(d, d.tiles, st) : launch_down<ElemBF16, true>(d, d.tiles, st);
+    condensa_status s = f16 ? launch_down<ElemF16, true>(d, d.tiles * kDownShare, st) : launch_down<ElemBF16, true>(d, d.tiles * kDownShare, st);
     if (s != CONDENSA_OK) return s;
     return f16 ? launch_wide<ElemF16, true>(g, vec, st) : launch_wide<ElemBF16, true>(g, vec, st);
 }
@@ -334,7 +306,7 @@ condensa_status condensa_adapter_project_backward(const condensa_adapter_list* l
     d.tiles = (T + kDownTokens - 1) / kDownTokens;
     d.order = at<u32>(workspace_dev, p.order); d.seg = at<uint2>(workspace_dev, p.seg); d.slots = at<uint4>(workspace_dev, p.slots);
     d.n_slots = p.n_slots; d.run = p.run;
-    const u32 waves = split ? 4 : kDownWaves, blocks = d.tiles + (n + waves - 1) / waves;
+    const u32 waves = split ? 4 : kDownWaves, blocks = d.tiles * kDownShare + (n + waves - 1) / waves;
     if (blocks == 0) return CONDENSA_OK;
     WideArgs g{};
     g.x = dy_dev; g.ldx = dy_stride; g.w = w_dev; g.ldw = w_stride; g.y = dx_dev; g.ldy = dx_stride;
@@ -342,11 +314,11 @@ condensa_status condensa_adapter_project_backward(const condensa_adapter_list* l
     g.zp = d.zp; g.rp = p.rp; g.ids = token_adapter_dev; g.ad = ad; g.n_adapters = n; g.max_rank = d.max_rank;
     g.vec_y = aligned(dx_dev, 8) && dx_stride % 4 == 0;
     g.splits = p.splits; g.steps_each = p.steps_each;
-    g.part = at<float>(workspace_dev, p.part_wide);
+    g.part = p.split ? at<float>(workspace_dev, p.part_wide) : nullptr;
     const bool vec_wide = vec_dy && vec_w;
     condensa_status s;
     if (split) {
-        s = f16 ? launch_split<ElemF16, false>(d, g, blocks, vec_wide, st) : launch_split<ElemBF16, false>(d, g, blocks, vec_wide, st);
+        s = f16 ? launch_split<ElemF16, false>(d, g, p.bm, blocks, false, vec_wide, st) : launch_split<ElemBF16, false>(d, g, p.bm, blocks, false, vec_wide, st);
         if (s != CONDENSA_OK) return s;
     } else {
         s = f16 ? launch_down<ElemF16, false>(d, blocks, st) : launch_down<ElemBF16, false>(d, blocks, st);

@@ -184,8 +184,9 @@ struct DownArgs {
     u32 n_slots, run;                    // tokens of a run
 };
 
-constexpr int kDownTokens = 32, kDownRanks = 64;
-constexpr u32 down_lds(u32 waves) { return waves * kDownTokens * kDownRanks * 4; }
+constexpr int kDownTokens = 32, kDownRanks = 32;
+constexpr u32 kDownShare = 4;                                // workgroups that share the adapters of a tile
+constexpr u32 down_lds(u32 waves) { return waves * 8192; }
 
 // Places of the runs of an adapter whose tokens begin at `first`: run j of it is slot first / run + a + j.  (One slot at least for
 // each adapter; the slots of different adapters never meet, since ceil(n / run) <= floor((first + n) / run) - floor(first / run) + 1.)
@@ -227,72 +228,67 @@ __device__ inline void sort_tokens(const DownArgs& p, u32 a) {
     }
 }
 
-// Sums of 32 tokens and 16 G ranks from r0 on, over the steps of 64 values that are this wavefront's.  ALONG: the narrow matrix is [rank, n_sum]
-// and its fragments come from memory as they are.  Else it is [n_sum, rank]: 64 rows of it go through this wavefront's part of LDS, whose
-// transposing load makes fragments of them.
+// Sums of 32 tokens and 16 G ranks from r0 on, over the steps of 64 values that are this wavefront's.  Loads take whole cache lines, eight
+// lanes to a line (a lane each from sixteen rows, as the operands want them, costs the address unit four times as long), and this
+// wavefront's 8 KB of LDS turn them into fragments.  ALONG: the narrow matrix is [rank, n_sum]; else it is [n_sum, rank], and the
+// transposing LDS load makes its fragments.
 template <typename E, bool ALONG, bool VECX, bool VECM, u32 WAVES, u32 G>
-__device__ inline void down_sums(const DownArgs& p, const u16* xa, const u16* xb, const u16* m, u32 rank, u32 r0, u16* own, f32x4 (&acc)[2][4]) {
+__device__ inline void down_sums(const DownArgs& p, u32 t0, const u16* m, u32 rank, u32 r0, u16* own, f32x4 (&acc)[2][2]) {
     u32 lane = threadIdx.x & 63;
     asm volatile("" : "+v"(lane));                         // keeps the places of each form out of the registers of the others
-    const u32 wave = threadIdx.x >> 6, row = lane & 15, sub = (lane >> 4) * 8;
+    const u32 wave = threadIdx.x >> 6, piece = lane & 7u;
     const u32 full = p.n_sum / 64;
     constexpr u32 kPieces = 2 * G;                         // 16-byte pieces of the narrow matrix for each lane and step
-    constexpr bool kRolled = !ALONG && !VECM && G == 4;    // many ranks, a number that eight does not divide: a few pieces at a time, registers are short
-    const u16* mj[G];
+    u16* own_m = own + kDownTokens * 64;
+    const u16* xr[4];
+    const u16* mr[kPieces];
 #pragma unroll
-    for (u32 g = 0; g < G; ++g) {                          // rows past the rank: the last one again, their sums are not stored
-        const u32 j = r0 + g * 16 + row;
-        mj[g] = ALONG ? m + static_cast<i64>(j < rank ? j : rank - 1) * p.n_sum : m;
+    for (u32 i = 0; i < 4; ++i) {                          // sums of tokens past the last are not stored
+        const u32 t = t0 + i * 8 + (lane >> 3);
+        xr[i] = p.x + static_cast<i64>(t < p.n_tokens ? t : p.n_tokens - 1) * p.ldx;
+    }
+#pragma unroll
+    for (u32 i = 0; i < kPieces; ++i) {                    // nor are those of rows past the rank
+        const u32 j = r0 + i * 8 + (lane >> 3);
+        mr[i] = ALONG ? m + static_cast<i64>(j < rank ? j : rank - 1) * p.n_sum : m;
     }
     // GUARD: the step that ends past the sum
     auto fetch = [&](auto guard, u32 s, u32x4 (&x)[4], u32x4 (&v)[kPieces]) {
         constexpr bool GUARD = decltype(guard)::value;
-        const i64 k = static_cast<i64>(s) * 64 + sub;
+        const i64 k = static_cast<i64>(s) * 64 + piece * 8;
 #pragma unroll
-        for (u32 h = 0; h < 2; ++h) {
-            x[2 * h] = GUARD ? load8<VECX>(xa, k + h * 32, p.n_sum) : load8_inside<VECX>(xa + k + h * 32);
-            x[2 * h + 1] = GUARD ? load8<VECX>(xb, k + h * 32, p.n_sum) : load8_inside<VECX>(xb + k + h * 32);
-        }
-        if (ALONG) {
+        for (u32 i = 0; i < 4; ++i) x[i] = GUARD ? load8<VECX>(xr[i], k, p.n_sum) : load8_inside<VECX>(xr[i] + k);
 #pragma unroll
-            for (u32 h = 0; h < 2; ++h)
-#pragma unroll
-                for (u32 g = 0; g < G; ++g)
-                    v[h * G + g] = GUARD ? load8<VECM>(mj[g], k + h * 32, p.n_sum) : load8_inside<VECM>(mj[g] + k + h * 32);
-        } else if (!kRolled) {
-#pragma unroll
-            for (u32 i = 0; i < kPieces; ++i) {
-                const u32 at = i * 64 + lane, piece = at % (2 * G);
+        for (u32 i = 0; i < kPieces; ++i) {
+            if (ALONG) {
+                v[i] = GUARD ? load8<VECM>(mr[i], k, p.n_sum) : load8_inside<VECM>(mr[i] + k);
+            } else {
+                const u32 at = i * 64 + lane;
                 const i64 n = static_cast<i64>(s) * 64 + at / (2 * G);
-                v[i] = load8<VECM>(m + n * rank, r0 + piece * 8, !GUARD || n < p.n_sum ? rank : 0);
-            }
-        } else {
-#pragma unroll 2
-            for (u32 i = 0; i < kPieces; ++i) {
-                const u32 at = i * 64 + lane, piece = at % (2 * G);
-                const i64 n = static_cast<i64>(s) * 64 + at / (2 * G);
-                *reinterpret_cast<u32x4*>(own + across_at<16 * G>(at / (2 * G), piece)) = load8<VECM>(m + n * rank, r0 + piece * 8, !GUARD || n < p.n_sum ? rank : 0);
+                v[i] = load8<VECM>(m + n * rank, r0 + at % (2 * G) * 8, !GUARD || n < p.n_sum ? rank : 0);
             }
         }
     };
     auto add = [&](const u32x4 (&x)[4], const u32x4 (&v)[kPieces]) {
-        if (!ALONG && !kRolled) {
 #pragma unroll
-            for (u32 i = 0; i < kPieces; ++i) {
-                const u32 at = i * 64 + lane;
-                *reinterpret_cast<u32x4*>(own + across_at<16 * G>(at / (2 * G), at % (2 * G))) = v[i];
-            }
+        for (u32 i = 0; i < 4; ++i) *reinterpret_cast<u32x4*>(own + along_at(i * 8 + (lane >> 3), piece)) = x[i];
+#pragma unroll
+        for (u32 i = 0; i < kPieces; ++i) {
+            const u32 at = i * 64 + lane;
+            *reinterpret_cast<u32x4*>(own_m + (ALONG ? along_at(i * 8 + (lane >> 3), piece) : across_at<16 * G>(at / (2 * G), at % (2 * G)))) = v[i];
         }
 #pragma unroll
-        for (u32 h = 0; h < 2; ++h)
+        for (u32 h = 0; h < 2; ++h) {
+            const u32x4 fa = along_frag(own, 0, h), fb = along_frag(own, 16, h);
 #pragma unroll
             for (u32 g = 0; g < G; ++g) {
-                const u32x4 fm = ALONG ? v[h * G + g] : across_frag<16 * G>(own, g * 16, h);
-                acc[0][g] = E::mfma(x[2 * h], fm, acc[0][g]);
-                acc[1][g] = E::mfma(x[2 * h + 1], fm, acc[1][g]);
+                const u32x4 fm = ALONG ? along_frag(own_m, g * 16, h) : across_frag<16 * G>(own_m, g * 16, h);
+                acc[0][g] = E::mfma(fa, fm, acc[0][g]);
+                acc[1][g] = E::mfma(fb, fm, acc[1][g]);
             }
+        }
     };
-    constexpr u32 kAhead = G == 1 ? 3 : (ALONG || G == 2 ? 2 : 1);      // steps whose loads are under way at once
+    constexpr u32 kAhead = G == 1 ? 3 : 2;                 // steps whose loads are under way at once
     u32x4 x[kAhead][4], v[kAhead][kPieces];
     u32 s = wave;
     for (; s + (kAhead - 1) * WAVES < full; s += kAhead * WAVES) {
@@ -313,80 +309,76 @@ __device__ inline void down_sums(const DownArgs& p, const u16* xa, const u16* xb
     }
 }
 
-// z = s x M_a^T for 32 tokens a workgroup, where M_a is the adapter's A [rank, n_sum] (ALONG), or its B [n_sum, rank] in the backward
-// pass.  Reading x bounds it: each row is read once, in whole cache lines, by eight wavefronts that take every eighth 64 values of it straight
-// into operand registers (nothing of x is shared between wavefronts, so LDS would only add a trip) and add their sums up at the end.
-// Thirty-two tokens share what is read of M_a.  Tokens of several adapters in one tile are done one adapter after the other.
-// Workgroups past the tiles sort the tokens.
+// z = s x M_a^T for 32 tokens, where M_a is the adapter's A [rank, n_sum] (ALONG), or its B [n_sum, rank] in the backward pass.  Reading x
+// bounds it: wavefronts take every WAVES-th 64 values of its rows (nothing of x is shared between them) and add their sums up at the
+// end; thirty-two tokens share what is read of M_a.  Four workgroups have the same tile and take its tokens' adapters in turn: most find
+// none, and a tile where one request ends and the next begins takes no longer than the others.  Workgroups past the tiles sort the tokens.
 template <typename E, bool ALONG, bool VECX, u32 WAVES>
-__device__ inline void down_tile(const DownArgs& p, u32 block, void* lds) {
-    float (*sums)[kDownTokens][kDownRanks] = reinterpret_cast<float (*)[kDownTokens][kDownRanks]>(lds);       // or, before, 8 KB of M_a for each wavefront
+__device__ inline void down_tile(const DownArgs& p, u32 block, char* lds) {
     const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    if (block >= p.tiles) {                                  // uniform
-        const u32 a = (block - p.tiles) * WAVES + wave;
+    if (block >= p.tiles * kDownShare) {                     // uniform
+        const u32 a = (block - p.tiles * kDownShare) * WAVES + wave;
         if (a < p.n_adapters) sort_tokens(p, a);
         return;
     }
-    const u32 t0 = block * kDownTokens;
+    const u32 share = block / p.tiles, t0 = block % p.tiles * kDownTokens;
     const int my_id = lane < kDownTokens ? adapter_of(p.ids, t0 + lane, p.n_tokens, p.n_adapters) : -1;
     const u32 width = p.z && p.ldz > p.rp ? static_cast<u32>(p.ldz) : p.rp;
-    // tokens without an adapter
-    for (u32 i = wave; i < kDownTokens; i += WAVES) {
-        const u32 t = t0 + i;
-        if (t >= p.n_tokens || __shfl(my_id, static_cast<int>(i), 64) >= 0) continue;
-        for (u32 j = lane; j < width; j += 64) {
-            if (j < p.rp) { if (p.zp) p.zp[static_cast<u64>(t) * p.rp + j] = 0; if (p.z32) p.z32[static_cast<u64>(t) * p.rp + j] = 0.0f; }
-            if (p.z && j < p.ldz) p.z[static_cast<u64>(t) * p.ldz + j] = 0;
+    auto put = [&](u64 t, u32 j, float v) {
+        const u16 h = E::enc(v);
+        if (j < p.rp) {
+            if (p.zp) p.zp[t * p.rp + j] = h;
+            if (p.z32) p.z32[t * p.rp + j] = v;
         }
-    }
-    const u32 row = lane & 15;
-    const u32 ta = t0 + row < p.n_tokens ? t0 + row : p.n_tokens - 1, tb = t0 + 16 + row < p.n_tokens ? t0 + 16 + row : p.n_tokens - 1;
-    const u16* xa = p.x + static_cast<i64>(ta) * p.ldx;      // sums of tokens past the last are not stored
-    const u16* xb = p.x + static_cast<i64>(tb) * p.ldx;
-    u16* own = reinterpret_cast<u16*>(&sums[wave][0][0]);
-    for (int a = next_adapter(my_id, -1); a != 0x7FFFFFFF; a = next_adapter(my_id, a)) {       // uniform over the workgroup
+        if (p.z && j < p.ldz) p.z[t * p.ldz + j] = h;
+    };
+    if (share == 0)                                          // tokens without an adapter
+        for (u32 i = wave; i < kDownTokens; i += WAVES) {
+            if (t0 + i >= p.n_tokens || __shfl(my_id, static_cast<int>(i), 64) >= 0) continue;
+            for (u32 j = lane; j < width; j += 64) put(t0 + i, j, 0.0f);
+        }
+    float (*sums)[kDownTokens][kDownRanks] = reinterpret_cast<float (*)[kDownTokens][kDownRanks]>(lds);
+    u16* own = reinterpret_cast<u16*>(lds) + wave * 4096;
+    u32 turn = 0;
+    for (int a = next_adapter(my_id, -1); a != 0x7FFFFFFF; a = next_adapter(my_id, a), ++turn) {       // uniform over the workgroup
+        if (turn % kDownShare != share) continue;
         const AdapterDesc d = p.ad[a];
         const u32 rank = d.rank < p.max_rank ? d.rank : p.max_rank;
         const u16* m = ALONG ? d.a : d.b;
         const bool vec_m = ALONG ? d.vec_a : d.vec_b;
         for (u32 r0 = 0; r0 < rank; r0 += kDownRanks) {
-            const u32 ranks = rank - r0 < static_cast<u32>(kDownRanks) ? rank - r0 : static_cast<u32>(kDownRanks);
-            const u32 groups = ranks <= 16 ? 1 : (ranks <= 32 ? 2 : 4);
-            f32x4 acc[2][4] = {};
+            const u32 groups = rank - r0 <= 16 ? 1 : 2;
+            f32x4 acc[2][2] = {};
             if (vec_m) {
-                if (groups == 1)      down_sums<E, ALONG, VECX, true, WAVES, 1>(p, xa, xb, m, rank, r0, own, acc);
-                else if (groups == 2) down_sums<E, ALONG, VECX, true, WAVES, 2>(p, xa, xb, m, rank, r0, own, acc);
-                else                  down_sums<E, ALONG, VECX, true, WAVES, 4>(p, xa, xb, m, rank, r0, own, acc);
+                if (groups == 1) down_sums<E, ALONG, VECX, true, WAVES, 1>(p, t0, m, rank, r0, own, acc);
+                else             down_sums<E, ALONG, VECX, true, WAVES, 2>(p, t0, m, rank, r0, own, acc);
             } else {
-                if (groups == 1)      down_sums<E, ALONG, VECX, false, WAVES, 1>(p, xa, xb, m, rank, r0, own, acc);
-                else if (groups == 2) down_sums<E, ALONG, VECX, false, WAVES, 2>(p, xa, xb, m, rank, r0, own, acc);
-                else                  down_sums<E, ALONG, VECX, false, WAVES, 4>(p, xa, xb, m, rank, r0, own, acc);
+                if (groups == 1) down_sums<E, ALONG, VECX, false, WAVES, 1>(p, t0, m, rank, r0, own, acc);
+                else             down_sums<E, ALONG, VECX, false, WAVES, 2>(p, t0, m, rank, r0, own, acc);
             }
+            __syncthreads();                                 // sums take the place of the others' tiles
 #pragma unroll
             for (u32 h = 0; h < 2; ++h)
 #pragma unroll
-                for (u32 g = 0; g < 4; ++g) {
+                for (u32 g = 0; g < 2; ++g) {
                     if (g >= groups) continue;
 #pragma unroll
-                    for (u32 i = 0; i < 4; ++i) sums[wave][h * 16 + (lane >> 4) * 4 + i][g * 16 + row] = acc[h][g][i];
+                    for (u32 i = 0; i < 4; ++i) sums[wave][h * 16 + (lane >> 4) * 4 + i][g * 16 + (lane & 15)] = acc[h][g][i];
                 }
             __syncthreads();
-            const bool last = r0 + kDownRanks >= rank;
-            const u32 end = last ? width : r0 + kDownRanks;
+            const u32 end = r0 + kDownRanks >= rank ? width : r0 + kDownRanks;
             for (u32 i = wave; i < kDownTokens; i += WAVES) {
                 if (__shfl(my_id, static_cast<int>(i), 64) != a) continue;       // uniform
                 const u64 t = t0 + i;
                 u32 most = 0;
                 for (u32 j = r0 + lane; j < end; j += 64) {
                     float v = 0.0f;
-                    if (j < rank) {
+                    if (j < rank && j < r0 + kDownRanks) {
 #pragma unroll
                         for (u32 w = 0; w < WAVES; ++w) v += sums[w][i][j - r0];
                         v *= d.scale;
                     }
-                    const u16 h = E::enc(v);
-                    if (j < p.rp) { if (p.zp) p.zp[t * p.rp + j] = h; if (p.z32) p.z32[t * p.rp + j] = v; }
-                    if (p.z && j < p.ldz) p.z[t * p.ldz + j] = h;
+                    put(t, j, v);
                     const u32 u = __float_as_uint(v) & 0x7FFFFFFFu;
                     if (u < 0x7F800000u) most = most > u ? most : u;
                 }
@@ -402,7 +394,54 @@ __device__ inline void down_tile(const DownArgs& p, u32 block, void* lds) {
                     }
                 }
             }
-            __syncthreads();                                 // before the sums are overwritten
+            __syncthreads();                                 // before tiles take the place of the sums
+        }
+    }
+}
+
+// z of one token, for batches where tokens that follow each other have adapters of their own: a wavefront takes every WAVES-th four rows of A,
+// whose values meet x in order, 512 a load, and adds up its lanes.
+template <typename E, bool VECX, u32 WAVES>
+__device__ inline void down_token(const DownArgs& p, u32 t) {
+    const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int a = __builtin_amdgcn_readfirstlane(adapter_of(p.ids, t, p.n_tokens, p.n_adapters));
+    AdapterDesc d{};
+    if (a >= 0) d = p.ad[a];
+    const u32 rank = d.rank < p.max_rank ? d.rank : p.max_rank;
+    const u32 width = p.z && p.ldz > p.rp ? static_cast<u32>(p.ldz) : p.rp;
+    for (u32 j = rank + threadIdx.x; j < width; j += 64 * WAVES) {
+        if (j < p.rp) p.z32[static_cast<u64>(t) * p.rp + j] = 0.0f;
+        if (p.z && j < p.ldz) p.z[static_cast<u64>(t) * p.ldz + j] = 0;
+    }
+    const u16* x = p.x + static_cast<i64>(t) * p.ldx;
+    for (u32 r0 = wave * 4; r0 < rank; r0 += 4 * WAVES) {
+        float sum[4] = {};
+        const u16* m[4];
+#pragma unroll
+        for (u32 r = 0; r < 4; ++r) m[r] = d.a + static_cast<i64>(r0 + r < rank ? r0 + r : rank - 1) * p.n_sum;
+#pragma unroll 3
+        for (u32 k0 = 0; k0 < p.n_sum; k0 += 512) {
+            const i64 k = k0 + lane * 8;
+            u32x4 vm[4];
+            const u32x4 vx = load8<VECX>(x, k, p.n_sum);
+#pragma unroll
+            for (u32 r = 0; r < 4; ++r) vm[r] = d.vec_a ? load8<true>(m[r], k, p.n_sum) : load8<false>(m[r], k, p.n_sum);
+#pragma unroll
+            for (u32 i = 0; i < 8; ++i) {
+                const float fx = E::dec(static_cast<u16>(vx[i >> 1] >> (16 * (i & 1))));
+#pragma unroll
+                for (u32 r = 0; r < 4; ++r) sum[r] = __builtin_fmaf(fx, E::dec(static_cast<u16>(vm[r][i >> 1] >> (16 * (i & 1)))), sum[r]);
+            }
+        }
+#pragma unroll
+        for (u32 r = 0; r < 4; ++r) {
+#pragma unroll
+            for (int w = 32; w >= 1; w >>= 1) sum[r] += __shfl_xor(sum[r], w, 64);
+            if (lane == r && r0 + r < rank) {
+                const float v = sum[r] * d.scale;
+                p.z32[static_cast<u64>(t) * p.rp + r0 + r] = v;
+                if (p.z) p.z[static_cast<u64>(t) * p.ldz + r0 + r] = E::enc(v);
+            }
         }
     }
 }
@@ -427,7 +466,7 @@ struct WideArgs {
     u32 n_adapters, max_rank;
     u32 vec_y;                           // 8-byte aligned groups of four outputs
     u32 splits, steps_each;              // steps of 64 values that a split sums
-    float* part;                         // splits > 1: [splits][n_tokens][n_out]
+    float* part;                         // [splits][n_tokens][n_out], or NULL: y is written
 };
 
 // Workgroups go round the eight dies one by one; this gives each die a run of neighbouring tiles, whose rows its cache keeps.
@@ -440,7 +479,7 @@ __device__ inline u32 die_order(u32 i, u32 n) {
 // NB steps ahead of their use.  A fragment register is read again as soon as its last product has begun, half a step ahead, so that the
 // matrix instructions wait for neither LDS nor memory; wavefronts meet once a step, in its middle, where the next step has come and the
 // last read of this one is done.  Otherwise (rows that are not 16-byte aligned) steps go through registers.
-// splits > 1: a workgroup sums a part of the steps and stores it in binary32; the adapters' share is then added with the parts.
+// With `part` a workgroup sums a part of the steps and stores it in binary32; the adapters' share is then added with the parts.
 constexpr u32 wide_lds(u32 bm, u32 bn, u32 nb) { return nb * (bm + bn) * 128 + bm * 4; }
 template <typename E, int BM, int BN, int WM, int WN, u32 NB, bool ALONG, bool VEC>
 __device__ inline void wide_tile(const WideArgs& p, u32 block_id, u32 n_blocks, char* lds) {
@@ -625,7 +664,7 @@ __device__ inline void wide_tile(const WideArgs& p, u32 block_id, u32 n_blocks, 
     bool vec_m = false;
     for (;;) {                                                     // uniform
         if (!rest) {
-            if (p.splits > 1) break;                               // added with the parts
+            if (p.part) break;                                     // added with the parts
             r0 += 64;
             if (r0 >= rank) {
                 int next = 0x7FFFFFFF;
@@ -682,7 +721,7 @@ __device__ inline void wide_tile(const WideArgs& p, u32 block_id, u32 n_blocks, 
         rest = false;
     }
 
-    if (p.splits > 1) {                                            // uniform
+    if (p.part) {                                                  // uniform
         float* part = p.part + static_cast<u64>(split) * p.n_tokens * p.n_out;
 #pragma unroll
         for (u32 j = 0; j < FM; ++j) {
@@ -731,13 +770,15 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_adapter_wide(WideArgs p) {
     wide_tile<E, BM, BN, WM, WN, NB, ALONG, VEC>(p, blockIdx.x, gridDim.x, lds);
 }
 
-// Where the tiles of 64 x 64 outputs are few, the sum is split and z is made in the same launch: nothing in it waits for anything.
-template <typename E, bool ALONG, bool VECX, bool VEC>
-__global__ __launch_bounds__(256, 2) void k_adapter_split(DownArgs d, WideArgs w, u32 down_blocks) {
+// Where tiles of 64 outputs are few, the sum is split and z is made in the same launch: nothing in it waits for anything.  z comes first, its
+// chain of loads is the longest.
+template <typename E, bool ALONG, bool VECX, bool VEC, int BM>
+__global__ __launch_bounds__(256, 2) void k_adapter_split(DownArgs d, WideArgs w, u32 down_blocks, u32 by_token) {
     constexpr u32 NB = VEC ? 4 : 2;
-    __shared__ __align__(16) char lds[wide_lds(64, 64, NB) > down_lds(4) ? wide_lds(64, 64, NB) : down_lds(4)];
-    if (blockIdx.x < down_blocks) down_tile<E, ALONG, VECX, 4>(d, blockIdx.x, lds);
-    else wide_tile<E, 64, 64, 2, 2, NB, ALONG, VEC>(w, blockIdx.x - down_blocks, gridDim.x - down_blocks, lds);
+    __shared__ __align__(16) char lds[wide_lds(BM, 64, NB) > down_lds(4) ? wide_lds(BM, 64, NB) : down_lds(4)];
+    if (blockIdx.x >= down_blocks) wide_tile<E, BM, 64, BM / 32, 128 / BM, NB, ALONG, VEC>(w, blockIdx.x - down_blocks, gridDim.x - down_blocks, lds);
+    else if (ALONG && by_token) down_token<E, VECX, 4>(d, blockIdx.x);
+    else down_tile<E, ALONG, VECX, 4>(d, blockIdx.x, lds);
 }
 
 // out = the parts added in order + z M_a (M_a: B^T or A), one output a thread; z in binary32.
@@ -775,168 +816,6 @@ __device__ inline void join_parts(const WideArgs& g, const float* z32, u32 ldz32
 template <typename E, bool ALONG>
 __global__ __launch_bounds__(256) void k_adapter_split_join(WideArgs w, const float* z32, u32 ldz32) {
     join_parts<E, ALONG>(w, z32, ldz32, blockIdx.y, blockIdx.x * 256 + threadIdx.x);
-}
-
-// ---- few tokens -------------------------------------------------------------------------------------------------
-
-struct FewArgs {
-    WideArgs wide;
-    float* z32;                          // [n_tokens][max_rank]
-    u16* z; i64 ldz;
-    u32 tiles_n;
-};
-
-constexpr u32 kFewCols = 32, kFewWaves = 8;
-
-// z of one token: eight wavefronts share its sum, 16 G ranks at a time.
-template <typename E, bool VEC, bool VECM, u32 G>
-__device__ inline void few_z(const FewArgs& p, const AdapterDesc& d, u32 rank, u32 t, float* sums) {
-    const WideArgs& g = p.wide;
-    const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, sub = (lane >> 4) * 8;
-    const u16* x = g.x + static_cast<i64>(t) * g.ldx;
-    for (u32 r0 = 0; r0 < rank; r0 += 16 * G) {
-        f32x4 acc[G] = {};
-        const u16* m[G];
-#pragma unroll
-        for (u32 q = 0; q < G; ++q) {
-            const u32 j = r0 + q * 16 + row;
-            m[q] = d.a + static_cast<i64>(j < rank ? j : rank - 1) * g.n_sum;
-        }
-        auto step = [&](auto guard, u32 s) {
-            const i64 k = static_cast<i64>(s) * 64 + sub;
-            u32x4 fx[2], fm[2][G];
-#pragma unroll
-            for (u32 h = 0; h < 2; ++h) {
-                fx[h] = decltype(guard)::value ? load8<VEC>(x, k + h * 32, g.n_sum) : load8_inside<VEC>(x + k + h * 32);
-#pragma unroll
-                for (u32 q = 0; q < G; ++q) fm[h][q] = decltype(guard)::value ? load8<VECM>(m[q], k + h * 32, g.n_sum) : load8_inside<VECM>(m[q] + k + h * 32);
-            }
-#pragma unroll
-            for (u32 h = 0; h < 2; ++h)
-#pragma unroll
-                for (u32 q = 0; q < G; ++q) acc[q] = E::mfma(fm[h][q], fx[h], acc[q]);       // the token in every column
-        };
-        const u32 full = g.n_sum / 64;
-        u32 s = wave;
-#pragma unroll 3
-        for (; s < full; s += kFewWaves) step(std::false_type{}, s);
-        if (s == full && (g.n_sum & 63u)) step(std::true_type{}, s);
-        __syncthreads();
-        if (row == 0)
-#pragma unroll
-            for (u32 q = 0; q < G; ++q)
-#pragma unroll
-                for (u32 i = 0; i < 4; ++i) sums[(wave * G + q) * 16 + (lane >> 4) * 4 + i] = acc[q][i];
-        __syncthreads();
-        if (threadIdx.x < 16 * G && r0 + threadIdx.x < rank) {
-            float v = 0.0f;
-#pragma unroll
-            for (u32 w = 0; w < kFewWaves; ++w) v += sums[w * G * 16 + threadIdx.x];
-            p.z32[static_cast<u64>(t) * g.max_rank + r0 + threadIdx.x] = v * d.scale;
-        }
-    }
-}
-
-// Up to 64 tokens: reading the weights once bounds it.  One launch reads everything that does not wait for anything: one workgroup a token
-// that makes z (they come first, theirs is the longest chain), and workgroups of 32 outputs and a part of the sum, of which eight wavefronts
-// take every eighth 64 values; the next launch adds the parts and z B^T.  Weights and tokens go from memory straight to operand
-// registers, and FM tiles of 16 tokens use the weights at once.
-template <typename E, u32 FM, bool VEC>
-__global__ __launch_bounds__(64 * kFewWaves, 4) void k_adapter_few(FewArgs p) {
-    __shared__ __align__(16) float sums[4 * 2 * FM * 256];
-    const WideArgs& g = p.wide;
-    const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, sub = (lane >> 4) * 8;
-    if (blockIdx.x < g.n_tokens) {
-        const int a = __builtin_amdgcn_readfirstlane(adapter_of(g.ids, blockIdx.x, g.n_tokens, g.n_adapters));
-        if (a < 0) return;
-        const AdapterDesc d = g.ad[a];
-        const u32 rank = d.rank < g.max_rank ? d.rank : g.max_rank;
-        if (d.vec_a) {
-            if (rank <= 16) few_z<E, VEC, true, 1>(p, d, rank, blockIdx.x, sums);
-            else            few_z<E, VEC, true, 4>(p, d, rank, blockIdx.x, sums);
-        } else {
-            if (rank <= 16) few_z<E, VEC, false, 1>(p, d, rank, blockIdx.x, sums);
-            else            few_z<E, VEC, false, 4>(p, d, rank, blockIdx.x, sums);
-        }
-        return;
-    }
-    const u32 block = blockIdx.x - g.n_tokens, tile = block % p.tiles_n, split = block / p.tiles_n;
-    const u32 steps = (g.n_sum + 63) / 64, n0 = tile * kFewCols;
-    const u32 begin = split * g.steps_each, end = begin + g.steps_each < steps ? begin + g.steps_each : steps;
-    const u16* w[2];
-    const u16* x[FM];
-#pragma unroll
-    for (u32 i = 0; i < 2; ++i) {
-        const u32 n = n0 + i * 16 + row;
-        w[i] = g.w + static_cast<i64>(n < g.n_out ? n : g.n_out - 1) * g.ldw;
-    }
-#pragma unroll
-    for (u32 i = 0; i < FM; ++i) {
-        const u32 t = i * 16 + row;
-        x[i] = g.x + static_cast<i64>(t < g.n_tokens ? t : g.n_tokens - 1) * g.ldx;
-    }
-    f32x4 acc[2][FM] = {};
-    auto step = [&](auto guard, u32 s) {
-        const i64 k = static_cast<i64>(s) * 64 + sub;
-        u32x4 fw[2][2], fx[2][FM];
-#pragma unroll
-        for (u32 h = 0; h < 2; ++h) {
-#pragma unroll
-            for (u32 i = 0; i < 2; ++i) fw[h][i] = decltype(guard)::value ? load8<VEC>(w[i], k + h * 32, g.n_sum) : load8_inside<VEC>(w[i] + k + h * 32);
-#pragma unroll
-            for (u32 i = 0; i < FM; ++i) fx[h][i] = decltype(guard)::value ? load8<VEC>(x[i], k + h * 32, g.n_sum) : load8_inside<VEC>(x[i] + k + h * 32);
-        }
-        __builtin_amdgcn_sched_barrier(0);                     // all loads before the first product
-#pragma unroll
-        for (u32 h = 0; h < 2; ++h)
-#pragma unroll
-            for (u32 i = 0; i < 2; ++i)
-#pragma unroll
-                for (u32 j = 0; j < FM; ++j) acc[i][j] = E::mfma(fw[h][i], fx[h][j], acc[i][j]);
-    };
-    const u32 full = (g.n_sum & 63u) && end == steps && end > begin ? end - 1 : end;
-    u32 s = begin + wave;
-    for (; s < full; s += kFewWaves) step(std::false_type{}, s);
-    if (s == full && full < end) step(std::true_type{}, s);
-    // eight sums: the upper four are added to the lower ones, then those in LDS
-    f32x4* mine = reinterpret_cast<f32x4*>(sums) + (wave & 3u) * 2 * FM * 64 + lane;
-    if (wave >= 4)
-#pragma unroll
-        for (u32 i = 0; i < 2; ++i)
-#pragma unroll
-            for (u32 j = 0; j < FM; ++j) mine[(i * FM + j) * 64] = acc[i][j];
-    __syncthreads();
-    if (wave < 4)
-#pragma unroll
-        for (u32 i = 0; i < 2; ++i)
-#pragma unroll
-            for (u32 j = 0; j < FM; ++j) mine[(i * FM + j) * 64] += acc[i][j];
-    __syncthreads();
-    for (u32 at = threadIdx.x; at < 2 * FM * 64; at += 64 * kFewWaves) {
-        f32x4 v = reinterpret_cast<const f32x4*>(sums)[at];
-#pragma unroll
-        for (u32 q = 1; q < 4; ++q) v += reinterpret_cast<const f32x4*>(sums)[q * 2 * FM * 64 + at];
-        const u32 l = at & 63, j = at / 64 % FM, i = at / 64 / FM;
-        const u32 t = j * 16 + (l & 15), n = n0 + i * 16 + (l >> 4) * 4;
-        if (t >= g.n_tokens) continue;
-        float* out = g.part + (static_cast<u64>(split) * g.n_tokens + t) * g.n_out + n;
-        if ((g.n_out & 3u) == 0 && n + 4 <= g.n_out) *reinterpret_cast<f32x4*>(out) = v;
-        else
-#pragma unroll
-            for (u32 q = 0; q < 4; ++q) if (n + q < g.n_out) out[q] = v[q];
-    }
-}
-
-template <typename E>
-__global__ __launch_bounds__(256) void k_adapter_few_join(FewArgs p) {
-    const WideArgs& g = p.wide;
-    const u32 t = blockIdx.y;
-    if (p.z && blockIdx.x == 0) {
-        const int a = adapter_of(g.ids, t, g.n_tokens, g.n_adapters);
-        const u32 rank = a < 0 ? 0 : (g.ad[a].rank < g.max_rank ? g.ad[a].rank : g.max_rank);
-        for (u32 j = threadIdx.x; j < p.ldz; j += 256) p.z[static_cast<u64>(t) * p.ldz + j] = j < rank ? E::enc(p.z32[static_cast<u64>(t) * g.max_rank + j]) : static_cast<u16>(0);
-    }
-    join_parts<E, true>(g, p.z32, g.max_rank, t, blockIdx.x * 256 + threadIdx.x);
 }
 
 // ---- gradients of the adapters ----------------------------------------------------------------------------------
