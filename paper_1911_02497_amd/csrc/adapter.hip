@@ -52,7 +52,9 @@ static Plan make_plan(i64 T, i64 n_in, i64 n_out, u32 n_adapters, u32 max_rank, 
         const u64 tiles = static_cast<u64>((T + p.bm - 1) / p.bm) * ((n_wide + 63) / 64);
         const u32 steps = static_cast<u32>((n_sum + 63) / 64);
         if (T > 0 && tiles < 512) {
-            u32 s = static_cast<u32>((512 + tiles - 1) / tiles), most = steps / 2;
+            // three workgroups of a unit at once, those that make z among them
+            const u64 others = backward || T > kTokenwise ? 128 : static_cast<u64>(T), room = 768 - others;
+            u32 s = static_cast<u32>(room / tiles), most = steps / 2;
             s = s > most ? most : s;
             s = s > 16 ? 16 : (s < 1 ? 1 : s);
             p.split = s > 1 || T <= kTokenwise;
@@ -84,14 +86,14 @@ static condensa_status launch_down(const DownArgs& a, u32 blocks, hipStream_t st
     return CONDENSA_OK;
 }
 
-template <typename E, int BM, int BN, int WM, int WN, u32 NB, bool ALONG, bool VEC>
+template <typename E, int BM, int BN, int WM, int WN, u32 NB, bool ALONG, int ROWS>
 static void launch_wide_tile(const WideArgs& a, hipStream_t st) {
     const u64 tiles = (static_cast<u64>(a.n_tokens) + BM - 1) / BM * ((static_cast<u64>(a.n_out) + BN - 1) / BN);
-    hipLaunchKernelGGL((k_adapter_wide<E, BM, BN, WM, WN, NB, ALONG, VEC>), dim3(static_cast<unsigned>(tiles * a.splits)), dim3(64 * WM * WN), 0, st, a);
+    hipLaunchKernelGGL((k_adapter_wide<E, BM, BN, WM, WN, NB, ALONG, ROWS>), dim3(static_cast<unsigned>(tiles * a.splits)), dim3(64 * WM * WN), 0, st, a);
 }
 
 template <typename E, bool ALONG>
-static condensa_status launch_wide(WideArgs a, bool vec, hipStream_t st) {
+static condensa_status launch_wide(WideArgs a, int rows, hipStream_t st) {
     a.splits = 1;
     a.part = nullptr;
     a.steps_each = (a.n_sum + 63) / 64;
@@ -99,33 +101,42 @@ static condensa_status launch_wide(WideArgs a, bool vec, hipStream_t st) {
     // A tile of 256 rows fills a compute unit.  The one whose rounds over the 256 of them cost less is taken: 8192 x 4608 outputs are 2.25 rounds
     // of 256 x 256, which take as long as three, and three of 256 x 192.
     const auto cost = [&](u64 n) { return (tiles(256, n) + 255) / 256 * n; };
-    if (vec && tiles(256, 256) >= 192) {
-        if (cost(192) < cost(256)) launch_wide_tile<E, 256, 192, 2, 4, 2, ALONG, true>(a, st);
-        else                       launch_wide_tile<E, 256, 256, 2, 4, 2, ALONG, true>(a, st);
-    } else if (vec && tiles(128, 128) >= 192) {
-        launch_wide_tile<E, 128, 128, 2, 2, 2, ALONG, true>(a, st);
+    if (rows == kRows16 && tiles(256, 256) >= 192) {
+        if (cost(192) < cost(256)) launch_wide_tile<E, 256, 192, 2, 4, 2, ALONG, kRows16>(a, st);
+        else                       launch_wide_tile<E, 256, 256, 2, 4, 2, ALONG, kRows16>(a, st);
+    } else if (rows != kRowsAny && tiles(128, 128) >= (rows == kRows16 ? 192 : 512)) {
+        if (rows == kRows16) launch_wide_tile<E, 128, 128, 2, 2, 2, ALONG, kRows16>(a, st);
+        else                 launch_wide_tile<E, 128, 128, 2, 2, 2, ALONG, kRows4>(a, st);
     } else {
-        if (vec) launch_wide_tile<E, 64, 64, 2, 2, 4, ALONG, true>(a, st);
-        else     launch_wide_tile<E, 64, 64, 2, 2, 2, ALONG, false>(a, st);
+        if (rows == kRows16)     launch_wide_tile<E, 64, 64, 2, 2, 3, ALONG, kRows16>(a, st);
+        else if (rows == kRows4) launch_wide_tile<E, 64, 64, 2, 2, 3, ALONG, kRows4>(a, st);
+        else                     launch_wide_tile<E, 64, 64, 2, 2, 2, ALONG, kRowsAny>(a, st);
     }
     CONDENSA_LAUNCH_CHECK();
     return CONDENSA_OK;
 }
 
 template <typename E, bool ALONG, int BM>
-static void launch_split_tile(const DownArgs& d, const WideArgs& w, u32 down_blocks, bool by_token, bool vec, hipStream_t st) {
-    const u32 blocks = down_blocks + (w.n_tokens + BM - 1) / BM * ((w.n_out + 63) / 64) * w.splits;
-    if (vec)          hipLaunchKernelGGL((k_adapter_split<E, ALONG, true, true, BM>), dim3(blocks), dim3(256), 0, st, d, w, down_blocks, by_token);
-    else if (d.vec_x) hipLaunchKernelGGL((k_adapter_split<E, ALONG, true, false, BM>), dim3(blocks), dim3(256), 0, st, d, w, down_blocks, by_token);
-    else              hipLaunchKernelGGL((k_adapter_split<E, ALONG, false, false, BM>), dim3(blocks), dim3(256), 0, st, d, w, down_blocks, by_token);
+static void launch_split_tile(const DownArgs& d, const WideArgs& w, u32 down_blocks, bool by_token, int rows, hipStream_t st) {
+    const dim3 blocks(down_blocks + (w.n_tokens + BM - 1) / BM * ((w.n_out + 63) / 64) * w.splits);
+    if (rows == kRows16)     hipLaunchKernelGGL((k_adapter_split<E, ALONG, kRows16, BM>), blocks, dim3(256), 0, st, d, w, down_blocks, by_token);
+    else if (rows == kRows4) hipLaunchKernelGGL((k_adapter_split<E, ALONG, kRows4, BM>), blocks, dim3(256), 0, st, d, w, down_blocks, by_token);
+    else                     hipLaunchKernelGGL((k_adapter_split<E, ALONG, kRowsAny, BM>), blocks, dim3(256), 0, st, d, w, down_blocks, by_token);
 }
 
 template <typename E, bool ALONG>
-static condensa_status launch_split(const DownArgs& d, const WideArgs& w, u32 bm, u32 down_blocks, bool by_token, bool vec, hipStream_t st) {
-    if (bm == 32) launch_split_tile<E, ALONG, 32>(d, w, down_blocks, by_token, vec, st);
-    else          launch_split_tile<E, ALONG, 64>(d, w, down_blocks, by_token, vec, st);
+static condensa_status launch_split(const DownArgs& d, const WideArgs& w, u32 bm, u32 down_blocks, bool by_token, int rows, hipStream_t st) {
+    if (bm == 32) launch_split_tile<E, ALONG, 32>(d, w, down_blocks, by_token, rows, st);
+    else          launch_split_tile<E, ALONG, 64>(d, w, down_blocks, by_token, rows, st);
     CONDENSA_LAUNCH_CHECK();
     return CONDENSA_OK;
+}
+
+// How rows lie that a sum runs along (x, W forward, dy) or across (W in the backward pass).
+static int rows_of(const void* p, i64 stride, i64 cols, bool across) {
+    if (aligned(p, 16) && stride % 8 == 0 && cols % 8 == 0) return kRows16;
+    if (aligned(p, 4) && stride % 2 == 0 && (!across || cols % 2 == 0)) return kRows4;
+    return kRowsAny;
 }
 
 // Checks that both directions share; `used`: the call has work to do.
@@ -234,7 +245,7 @@ condensa_status condensa_adapter_project(const condensa_adapter_list* list, cons
     hipStream_t st = static_cast<hipStream_t>(stream);
     const bool f16 = list->type == CONDENSA_TYPE_F16;
     const bool vec_x = aligned(x_dev, 16) && x_stride % 8 == 0 && list->n_in % 8 == 0;
-    const bool vec = vec_x && aligned(w_dev, 16) && w_stride % 8 == 0;
+    const int rows = std::min(rows_of(x_dev, x_stride, list->n_in, false), rows_of(w_dev, w_stride, list->n_in, false));
     WideArgs g{};
     g.x = x_dev; g.ldx = x_stride; g.w = w_dev; g.ldw = w_stride; g.y = y_dev; g.ldy = y_stride;
     g.n_tokens = static_cast<u32>(n_tokens); g.n_out = static_cast<u32>(list->n_out); g.n_sum = static_cast<u32>(list->n_in);
@@ -253,7 +264,7 @@ condensa_status condensa_adapter_project(const condensa_adapter_list* list, cons
     if (p.split) {
         const bool by_token = n_tokens <= kTokenwise;
         const u32 down = by_token ? g.n_tokens : d.tiles * kDownShare;
-        condensa_status s = f16 ? launch_split<ElemF16, true>(d, g, p.bm, down, by_token, vec, st) : launch_split<ElemBF16, true>(d, g, p.bm, down, by_token, vec, st);
+        condensa_status s = f16 ? launch_split<ElemF16, true>(d, g, p.bm, down, by_token, rows, st) : launch_split<ElemBF16, true>(d, g, p.bm, down, by_token, rows, st);
         if (s != CONDENSA_OK) return s;
         const dim3 grid((g.n_out + 255) / 256, g.n_tokens);
         if (f16) hipLaunchKernelGGL((k_adapter_split_join<ElemF16, true>), grid, dim3(256), 0, st, g, static_cast<const float*>(d.z32), p.rp);
@@ -263,7 +274,7 @@ condensa_status condensa_adapter_project(const condensa_adapter_list* list, cons
     }
     condensa_status s = f16 ? launch_down<ElemF16, true>(d, d.tiles * kDownShare, st) : launch_down<ElemBF16, true>(d, d.tiles * kDownShare, st);
     if (s != CONDENSA_OK) return s;
-    return f16 ? launch_wide<ElemF16, true>(g, vec, st) : launch_wide<ElemBF16, true>(g, vec, st);
+    return f16 ? launch_wide<ElemF16, true>(g, rows, st) : launch_wide<ElemBF16, true>(g, rows, st);
 }
 
 condensa_status condensa_adapter_project_backward(const condensa_adapter_list* list, const uint16_t* dy_dev, int64_t dy_stride,
@@ -294,7 +305,6 @@ condensa_status condensa_adapter_project_backward(const condensa_adapter_list* l
     const bool f16 = list->type == CONDENSA_TYPE_F16;
     const bool vec_dy = aligned(dy_dev, 16) && dy_stride % 8 == 0 && list->n_out % 8 == 0;
     const bool vec_x = aligned(x_dev, 16) && x_stride % 8 == 0 && list->n_in % 8 == 0;
-    const bool vec_w = aligned(w_dev, 16) && w_stride % 8 == 0 && list->n_in % 8 == 0;
     const u32 T = static_cast<u32>(n_tokens), n = static_cast<u32>(list->n_adapters);
     const AdapterDesc* ad = static_cast<const AdapterDesc*>(list->table_dev);
     DownArgs d{};
@@ -306,7 +316,9 @@ condensa_status condensa_adapter_project_backward(const condensa_adapter_list* l
     d.tiles = (T + kDownTokens - 1) / kDownTokens;
     d.order = at<u32>(workspace_dev, p.order); d.seg = at<uint2>(workspace_dev, p.seg); d.slots = at<uint4>(workspace_dev, p.slots);
     d.n_slots = p.n_slots; d.run = p.run;
-    const u32 waves = split ? 4 : kDownWaves, blocks = d.tiles * kDownShare + (n + waves - 1) / waves;
+    const u32 waves = split ? 4 : kDownWaves;
+    d.sorters = (n + waves - 1) / waves;
+    const u32 blocks = d.tiles * kDownShare + d.sorters;
     if (blocks == 0) return CONDENSA_OK;
     WideArgs g{};
     g.x = dy_dev; g.ldx = dy_stride; g.w = w_dev; g.ldw = w_stride; g.y = dx_dev; g.ldy = dx_stride;
@@ -315,15 +327,15 @@ condensa_status condensa_adapter_project_backward(const condensa_adapter_list* l
     g.vec_y = aligned(dx_dev, 8) && dx_stride % 4 == 0;
     g.splits = p.splits; g.steps_each = p.steps_each;
     g.part = p.split ? at<float>(workspace_dev, p.part_wide) : nullptr;
-    const bool vec_wide = vec_dy && vec_w;
+    const int rows = std::min(rows_of(dy_dev, dy_stride, list->n_out, false), rows_of(w_dev, w_stride, list->n_in, true));
     condensa_status s;
     if (split) {
-        s = f16 ? launch_split<ElemF16, false>(d, g, p.bm, blocks, false, vec_wide, st) : launch_split<ElemBF16, false>(d, g, p.bm, blocks, false, vec_wide, st);
+        s = f16 ? launch_split<ElemF16, false>(d, g, p.bm, blocks, false, rows, st) : launch_split<ElemBF16, false>(d, g, p.bm, blocks, false, rows, st);
         if (s != CONDENSA_OK) return s;
     } else {
         s = f16 ? launch_down<ElemF16, false>(d, blocks, st) : launch_down<ElemBF16, false>(d, blocks, st);
         if (s != CONDENSA_OK) return s;
-        if (wide) s = f16 ? launch_wide<ElemF16, false>(g, vec_wide, st) : launch_wide<ElemBF16, false>(g, vec_wide, st);
+        if (wide) s = f16 ? launch_wide<ElemF16, false>(g, rows, st) : launch_wide<ElemBF16, false>(g, rows, st);
         if (s != CONDENSA_OK) return s;
     }
     const u32 joins = split ? (g.n_out + 255) / 256 * T : 0;

@@ -140,12 +140,22 @@ __device__ inline void meet_loads() {
     __builtin_amdgcn_sched_barrier(0);
 }
 
-// Sixteen bytes a lane from `base` (the same in all lanes) + `offset` straight into LDS, at byte `lds` + 16 * lane.  Written out because the
+// Bytes a lane from `base` (the same in all lanes) + `offset` straight into LDS, at byte `lds` + BYTES * lane.  Written out because the
 // compiler, which cannot tell the tiles of one array apart, would wait for every such load before any LDS read; here meet_loads says
 // what has come.  There is no output register that could be reused while the load is under way.
-__device__ inline void load_lds(u32 offset, const void* base, u32 lds) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(lds) : "memory");
+template <u32 BYTES>
+__device__ inline void load_lds(u32 offset, const void* any_base, u32 any_lds) {
+    const u64 a = reinterpret_cast<u64>(any_base);
+    const u32 hi = static_cast<u32>(__builtin_amdgcn_readfirstlane(static_cast<int>(a >> 32))), lo = static_cast<u32>(__builtin_amdgcn_readfirstlane(static_cast<int>(a)));
+    const u64 base = static_cast<u64>(hi) << 32 | lo;
+    const u32 lds = __builtin_amdgcn_readfirstlane(any_lds);
+    if (BYTES == 16) asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(lds) : "memory");
+    else             asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" : : "v"(offset), "s"(base), "s"(lds) : "memory");
 }
+
+// How the rows of an operand lie: 16-byte aligned and a multiple of eight values long; 4-byte aligned (and, where the sum runs across
+// them, an even number of values long); at any address.
+enum : int { kRowsAny = 0, kRows4 = 1, kRows16 = 2 };
 
 // The adapter of a token; -1 for none and for values outside the list.
 __device__ inline int adapter_of(const int* __restrict__ ids, u32 t, u32 n_tokens, u32 n_adapters) {
@@ -176,8 +186,8 @@ struct DownArgs {
     float* z32;                          // [n_tokens, rp] before rounding, or NULL
     u32* row_max;                        // largest finite magnitude of each token's z (bits), or NULL
     u32 vec_x;                           // 16-byte aligned rows of x
-    // blocks past the tiles sort the tokens by adapter (backward)
-    u32 tiles;
+    u32 tiles;                           // of 32 tokens
+    u32 sorters;                         // workgroups that sort the tokens by adapter (backward)
     u32* order;                          // tokens of adapter 0, 1, ... in ascending order
     uint4* slots;                        // [n_slots] of a run of tokens: adapter or ~0, first place in `order`, tokens, tokens of the adapter
     uint2* seg;                          // [n_adapters] first slot, slots
@@ -192,18 +202,20 @@ constexpr u32 down_lds(u32 waves) { return waves * 8192; }
 // each adapter; the slots of different adapters never meet, since ceil(n / run) <= floor((first + n) / run) - floor(first / run) + 1.)
 __device__ inline u32 first_slot(u32 first, u32 run, u32 a) { return first / run + a; }
 
-// One wavefront an adapter: two passes over the ids, the first counts, the second writes.
+// One wavefront an adapter: two passes over the ids, the first counts, the second writes; 1024 ids are under way at once.
 __device__ inline void sort_tokens(const DownArgs& p, u32 a) {
     const u32 lane = threadIdx.x & 63;
+    constexpr u32 kIds = 16;
     u32 less = 0, mine = 0;
-    for (u32 t = 0; t < p.n_tokens; t += 256) {
-        int id[4];
+    for (u32 t = 0; t < p.n_tokens; t += 64 * kIds) {
+        int id[kIds];
 #pragma unroll
-        for (u32 i = 0; i < 4; ++i) id[i] = adapter_of(p.ids, t + i * 64 + lane, p.n_tokens, p.n_adapters);
+        for (u32 i = 0; i < kIds; ++i) { const u32 at = t + i * 64 + lane; id[i] = p.ids[at < p.n_tokens ? at : p.n_tokens - 1]; }
 #pragma unroll
-        for (u32 i = 0; i < 4; ++i) {
-            less += static_cast<u32>(__popcll(__ballot(id[i] >= 0 && id[i] < static_cast<int>(a))));
-            mine += static_cast<u32>(__popcll(__ballot(id[i] == static_cast<int>(a))));
+        for (u32 i = 0; i < kIds; ++i) {
+            const bool there = t + i * 64 + lane < p.n_tokens;
+            less += static_cast<u32>(__popcll(__ballot(there && static_cast<u32>(id[i]) < a)));
+            mine += static_cast<u32>(__popcll(__ballot(there && static_cast<u32>(id[i]) == a)));
         }
     }
     const u32 s0 = first_slot(less, p.run, a), s1 = a + 1 < p.n_adapters ? first_slot(less + mine, p.run, a + 1) : p.n_slots;
@@ -215,14 +227,15 @@ __device__ inline void sort_tokens(const DownArgs& p, u32 a) {
     }
     u32 at = less;
     if (mine == 0) return;                                   // uniform
-    for (u32 t = 0; t < p.n_tokens; t += 256) {
-        int id[4];
+    for (u32 t = 0; t < p.n_tokens; t += 64 * kIds) {
+        int id[kIds];
 #pragma unroll
-        for (u32 i = 0; i < 4; ++i) id[i] = adapter_of(p.ids, t + i * 64 + lane, p.n_tokens, p.n_adapters);
+        for (u32 i = 0; i < kIds; ++i) { const u32 from = t + i * 64 + lane; id[i] = p.ids[from < p.n_tokens ? from : p.n_tokens - 1]; }
 #pragma unroll
-        for (u32 i = 0; i < 4; ++i) {
-            const u64 same = __ballot(id[i] == static_cast<int>(a));
-            if (id[i] == static_cast<int>(a)) p.order[at + static_cast<u32>(__popcll(same & ((1ull << lane) - 1ull)))] = t + i * 64 + lane;
+        for (u32 i = 0; i < kIds; ++i) {
+            const bool is = t + i * 64 + lane < p.n_tokens && static_cast<u32>(id[i]) == a;
+            const u64 same = __ballot(is);
+            if (is) p.order[at + static_cast<u32>(__popcll(same & ((1ull << lane) - 1ull)))] = t + i * 64 + lane;
             at += static_cast<u32>(__popcll(same));
         }
     }
@@ -312,15 +325,16 @@ __device__ inline void down_sums(const DownArgs& p, u32 t0, const u16* m, u32 ra
 // z = s x M_a^T for 32 tokens, where M_a is the adapter's A [rank, n_sum] (ALONG), or its B [n_sum, rank] in the backward pass.  Reading x
 // bounds it: wavefronts take every WAVES-th 64 values of its rows (nothing of x is shared between them) and add their sums up at the
 // end; thirty-two tokens share what is read of M_a.  Four workgroups have the same tile and take its tokens' adapters in turn: most find
-// none, and a tile where one request ends and the next begins takes no longer than the others.  Workgroups past the tiles sort the tokens.
+// none, and a tile where one request ends and the next begins takes no longer than the others.  The first workgroups sort the tokens.
 template <typename E, bool ALONG, bool VECX, u32 WAVES>
 __device__ inline void down_tile(const DownArgs& p, u32 block, char* lds) {
     const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    if (block >= p.tiles * kDownShare) {                     // uniform
-        const u32 a = (block - p.tiles * kDownShare) * WAVES + wave;
+    if (block < p.sorters) {                                 // uniform
+        const u32 a = block * WAVES + wave;
         if (a < p.n_adapters) sort_tokens(p, a);
         return;
     }
+    block -= p.sorters;
     const u32 share = block / p.tiles, t0 = block % p.tiles * kDownTokens;
     const int my_id = lane < kDownTokens ? adapter_of(p.ids, t0 + lane, p.n_tokens, p.n_adapters) : -1;
     const u32 width = p.z && p.ldz > p.rp ? static_cast<u32>(p.ldz) : p.rp;
@@ -475,17 +489,18 @@ __device__ inline u32 die_order(u32 i, u32 n) {
     return die * each + (die < more ? die : more) + k;
 }
 
-// Tiles of BM tokens by BN outputs, summed 64 values a step (whole cache lines of x), NB steps in LDS.  VEC: loads go straight into LDS, up to
+// Tiles of BM tokens by BN outputs, summed 64 values a step (whole cache lines of x), NB steps in LDS.  Loads go straight into LDS, up to
 // NB steps ahead of their use.  A fragment register is read again as soon as its last product has begun, half a step ahead, so that the
 // matrix instructions wait for neither LDS nor memory; wavefronts meet once a step, in its middle, where the next step has come and the
-// last read of this one is done.  Otherwise (rows that are not 16-byte aligned) steps go through registers.
+// last read of this one is done.  Rows that are 4-byte aligned are loaded four bytes a lane; with others steps go through registers.
 // With `part` a workgroup sums a part of the steps and stores it in binary32; the adapters' share is then added with the parts.
 constexpr u32 wide_lds(u32 bm, u32 bn, u32 nb) { return nb * (bm + bn) * 128 + bm * 4; }
-template <typename E, int BM, int BN, int WM, int WN, u32 NB, bool ALONG, bool VEC>
+template <typename E, int BM, int BN, int WM, int WN, u32 NB, bool ALONG, int ROWS>
 __device__ inline void wide_tile(const WideArgs& p, u32 block_id, u32 n_blocks, char* lds) {
     constexpr u32 kThreads = 64 * WM * WN;
     constexpr u32 TM = BM / WM, TN = BN / WN, FM = TM / 16, FN = TN / 16;
-    constexpr u32 kXPieces = BM * 8 / kThreads, kWPieces = BN * 8 / kThreads, kLoads = kXPieces + kWPieces;
+    constexpr u32 kXPieces = BM * 8 / kThreads, kWPieces = BN * 8 / kThreads;          // 16-byte pieces of a step for each thread
+    constexpr u32 kBytes = ROWS == kRows16 ? 16 : 4, kXLoads = kXPieces * 16 / kBytes, kWLoads = kWPieces * 16 / kBytes, kLoads = kXLoads + kWLoads;
     constexpr u32 kTile = (BM + BN) * 64, kEarly = FN < FM ? FN : FN / 2, kEach = FN / kEarly;
     u16* tiles = reinterpret_cast<u16*>(lds);
     int* s_ids = reinterpret_cast<int*>(lds + NB * kTile * 2);
@@ -510,26 +525,27 @@ __device__ inline void wide_tile(const WideArgs& p, u32 block_id, u32 n_blocks, 
 
     for (u32 i = tid; i < BM; i += kThreads) s_ids[i] = adapter_of(p.ids, t0 + i, p.n_tokens, p.n_adapters);
     bool rest = false;                                             // a last step that ends past the sum is left
-    if (VEC) {
-        u32 xo[kXPieces], wo[kWPieces];                            // byte offsets of this lane's pieces
+    if (ROWS != kRowsAny) {
+        u32 xo[kXLoads], wo[kWLoads];                              // byte offsets of what this lane loads
+        constexpr u32 kOf = 16 / kBytes;                           // loads of a piece
 #pragma unroll
-        for (u32 i = 0; i < kXPieces; ++i) {
-            const u32 at = i * kThreads + tid, row = at >> 3, piece = (at & 7u) ^ (row & 7u);
+        for (u32 i = 0; i < kXLoads; ++i) {
+            const u32 at = i * kThreads + tid, row = at / (8 * kOf), piece = (at / kOf & 7u) ^ (row & 7u);
             const u32 r = t0 + row < p.n_tokens ? row : p.n_tokens - 1 - t0;
-            xo[i] = (r * static_cast<u32>(p.ldx) + piece * 8) * 2;
+            xo[i] = (r * static_cast<u32>(p.ldx) + piece * 8) * 2 + at % kOf * kBytes;
         }
 #pragma unroll
-        for (u32 i = 0; i < kWPieces; ++i) {
+        for (u32 i = 0; i < kWLoads; ++i) {
             const u32 at = i * kThreads + tid;
             if (ALONG) {
-                const u32 row = at >> 3, piece = (at & 7u) ^ (row & 7u);
+                const u32 row = at / (8 * kOf), piece = (at / kOf & 7u) ^ (row & 7u);
                 const u32 r = n0 + row < p.n_out ? row : p.n_out - 1 - n0;
-                wo[i] = (r * static_cast<u32>(p.ldw) + piece * 8) * 2;
+                wo[i] = (r * static_cast<u32>(p.ldw) + piece * 8) * 2 + at % kOf * kBytes;
             } else {
                 constexpr u32 kRow = BN / 8;
-                const u32 k = at / kRow;
-                u32 col = across_at<BN>(k, at % kRow) - k * BN;
-                if (n0 + col >= p.n_out) col = p.n_out - 8 - n0;
+                const u32 k = at / (kRow * kOf);
+                u32 col = across_at<BN>(k, at / kOf % kRow) - k * BN + at % kOf * (kBytes / 2);
+                if (n0 + col >= p.n_out) col = p.n_out - kBytes / 2 - n0;
                 wo[i] = (k * static_cast<u32>(p.ldw) + col) * 2;
             }
         }
@@ -538,13 +554,13 @@ __device__ inline void wide_tile(const WideArgs& p, u32 block_id, u32 n_blocks, 
         const char* xs = reinterpret_cast<const char*>(p.x + static_cast<i64>(t0) * p.ldx + begin * 64);
         const char* ws = reinterpret_cast<const char*>(ALONG ? p.w + static_cast<i64>(n0) * p.ldw + begin * 64 : p.w + static_cast<i64>(begin) * 64 * p.ldw + n0);
         const i64 w_step = (ALONG ? 64 : 64 * p.ldw) * 2;
-        const u32 lds0 = static_cast<u32>(reinterpret_cast<uintptr_t>((lds_void*)tiles)) + wave * 1024;
+        const u32 lds0 = static_cast<u32>(reinterpret_cast<uintptr_t>((lds_void*)tiles)) + wave * 64 * kBytes;
         u32 loaded = 0, to = 0;
         auto load = [&]() {                                        // the next step, or the last one again
 #pragma unroll
-            for (u32 i = 0; i < kXPieces; ++i) load_lds(xo[i], xs, lds0 + to + i * kThreads * 16);
+            for (u32 i = 0; i < kXLoads; ++i) load_lds<kBytes>(xo[i], xs, lds0 + to + i * kThreads * kBytes);
 #pragma unroll
-            for (u32 i = 0; i < kWPieces; ++i) load_lds(wo[i], ws, lds0 + to + BM * 128 + i * kThreads * 16);
+            for (u32 i = 0; i < kWLoads; ++i) load_lds<kBytes>(wo[i], ws, lds0 + to + BM * 128 + i * kThreads * kBytes);
             ++loaded;
             const bool more = loaded < full;
             xs += more ? 128 : 0;
@@ -591,7 +607,7 @@ __device__ inline void wide_tile(const WideArgs& p, u32 block_id, u32 n_blocks, 
             meet_loads<0>();
         }
     } else {
-        constexpr u32 kAhead = 3;                                  // steps whose rows are under way
+        constexpr u32 kAhead = 2;                                  // steps whose rows are under way
         u32x4 rx[kAhead][kXPieces], rw[kAhead][kWPieces];
         const i64 sum_end = static_cast<i64>(end) * 64 < p.n_sum ? static_cast<i64>(end) * 64 : p.n_sum;       // zeros from there on
         auto fetch = [&](u32 set, u32 s) {
@@ -688,11 +704,12 @@ __device__ inline void wide_tile(const WideArgs& p, u32 block_id, u32 n_blocks, 
         const i64 ldx = rest ? p.ldx : static_cast<i64>(p.rp), x_end = rest ? p.n_sum : p.rp;
         for (u32 at = me; at < BM * 8; at += kThreads) {
             const u32 row = at >> 3, piece = at & 7u, t = t0 + row < p.n_tokens ? t0 + row : p.n_tokens - 1;
-            if (piece < subs * 4) *reinterpret_cast<u32x4*>(tiles + along_at(row, piece)) = load8<true>(x + static_cast<i64>(t) * ldx, k0 + piece * 8, x_end);
+            const u16* src = x + static_cast<i64>(t) * ldx;
+            if (piece < subs * 4) *reinterpret_cast<u32x4*>(tiles + along_at(row, piece)) = ROWS == kRows16 || !rest ? load8<true>(src, k0 + piece * 8, x_end) : load8<false>(src, k0 + piece * 8, x_end);
         }
         const u16* w = rest ? p.w : m;
         const i64 ldw = rest ? p.ldw : (ALONG ? static_cast<i64>(rank) : static_cast<i64>(p.n_out));
-        const bool vec_w = rest || vec_m;
+        const bool vec_w = rest ? ROWS == kRows16 : vec_m;
         for (u32 at = me; at < BN * 8; at += kThreads) {
             const u32 row = ALONG ? at >> 3 : at / (BN / 8), piece = ALONG ? at & 7u : at % (BN / 8);
             if ((ALONG ? piece >> 2 : row >> 5) >= subs) continue;
@@ -764,19 +781,20 @@ __device__ inline void wide_tile(const WideArgs& p, u32 block_id, u32 n_blocks, 
     }
 }
 
-template <typename E, int BM, int BN, int WM, int WN, u32 NB, bool ALONG, bool VEC>
+template <typename E, int BM, int BN, int WM, int WN, u32 NB, bool ALONG, int ROWS>
 __global__ __launch_bounds__(64 * WM * WN, 2) void k_adapter_wide(WideArgs p) {
     __shared__ __align__(16) char lds[wide_lds(BM, BN, NB)];
-    wide_tile<E, BM, BN, WM, WN, NB, ALONG, VEC>(p, blockIdx.x, gridDim.x, lds);
+    wide_tile<E, BM, BN, WM, WN, NB, ALONG, ROWS>(p, blockIdx.x, gridDim.x, lds);
 }
 
 // Where tiles of 64 outputs are few, the sum is split and z is made in the same launch: nothing in it waits for anything.  z comes first, its
 // chain of loads is the longest.
-template <typename E, bool ALONG, bool VECX, bool VEC, int BM>
+template <typename E, bool ALONG, int ROWS, int BM>
 __global__ __launch_bounds__(256, 2) void k_adapter_split(DownArgs d, WideArgs w, u32 down_blocks, u32 by_token) {
-    constexpr u32 NB = VEC ? 4 : 2;
+    constexpr u32 NB = ROWS != kRowsAny ? 3 : 2;
+    constexpr bool VECX = ROWS == kRows16;
     __shared__ __align__(16) char lds[wide_lds(BM, 64, NB) > down_lds(4) ? wide_lds(BM, 64, NB) : down_lds(4)];
-    if (blockIdx.x >= down_blocks) wide_tile<E, BM, 64, BM / 32, 128 / BM, NB, ALONG, VEC>(w, blockIdx.x - down_blocks, gridDim.x - down_blocks, lds);
+    if (blockIdx.x >= down_blocks) wide_tile<E, BM, 64, BM / 32, 128 / BM, NB, ALONG, ROWS>(w, blockIdx.x - down_blocks, gridDim.x - down_blocks, lds);
     else if (ALONG && by_token) down_token<E, VECX, 4>(d, blockIdx.x);
     else down_tile<E, ALONG, VECX, 4>(d, blockIdx.x, lds);
 }
