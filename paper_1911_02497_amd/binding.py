@@ -713,15 +713,19 @@ def adamw_table(weights, grads, exp_avg, exp_avg_sq, **kw) -> AdamwTable:
 def condensa_lc_adamw_step(table: AdamwTable, lr, step, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0, mu=0.0, seed=None,
                            grad_scale=None, stream=None):
     """Marshals condensa_lc_adamw_step: one update of everything in ``table``.  ``seed``: 8-bit states are rounded by random bits
-    made from it (another one for every step), None: to nearest.  ``grad_scale``: a float32 device scalar."""
+    made from it (another one for every step), None: to nearest; states in 32 bits have nothing that a seed could decide.
+    ``grad_scale``: a float32 device scalar."""
     scale = None
     if grad_scale is not None:
         import torch
         if not (grad_scale.is_cuda and grad_scale.dtype == torch.float32 and grad_scale.numel() == 1):
             raise TypeError("grad_scale is one float32 on the device")
         scale = grad_scale.data_ptr()
-    s = AdamwSettings(lr, betas[0], betas[1], eps, weight_decay, mu, ROUND_NEAREST if seed is None else ROUND_STOCHASTIC, step,
-                      0 if seed is None else seed & 0xFFFFFFFFFFFFFFFF, scale, 0)
+    if seed is None or table.list.state_bits == 32:
+        rounding, seed = ROUND_NEAREST, 0
+    else:
+        rounding, seed = ROUND_STOCHASTIC, seed & 0xFFFFFFFFFFFFFFFF
+    s = AdamwSettings(lr, betas[0], betas[1], eps, weight_decay, mu, rounding, step, seed, scale, 0)
     _check(library().condensa_lc_adamw_step(table.ref, ctypes.byref(s), _stream(stream)))
 
 

@@ -226,3 +226,11 @@ def test_beyond_32_bits():
         code, scale = encode(r[cut:], bits >> np.uint64(16), True)
         assert np.array_equal(v[t][start:].cpu().numpy(), code)
     assert not bool(w[0][: 1 << 20].any()) and not bool(m[0][1 << 31:(1 << 31) + (1 << 20)].any())
+
+
+def test_a_seed_decides_nothing_about_states_in_32_bits():
+    p, q = Problem([700, 33], 32), Problem([700, 33], 32)
+    P.condensa_lc_adamw_step(p.table(), 1e-3, 2, seed=1 << 40, **HYPER)
+    P.condensa_lc_adamw_step(q.table(), 1e-3, 2, **HYPER)
+    for a, b in zip(p.w + p.m + p.v, q.w + q.m + q.v):
+        assert torch.equal(a, b)
