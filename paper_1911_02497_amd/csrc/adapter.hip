@@ -21,19 +21,30 @@ static bool list_ok(const condensa_adapter_list* l) {
            (l->type == CONDENSA_TYPE_F16 || l->type == CONDENSA_TYPE_BF16) && l->n_in >= 1 && l->n_in <= kMaxSide && l->n_out >= 1 && l->n_out <= kMaxSide;
 }
 
-// Tokens of a run of the gradients: short enough that some 1024 workgroups share the columns of x and dy, long enough that the parts of
-// a run, binary32 and as wide as a gradient, are small beside the 16-bit rows that it reads.
+// Tokens of a run of the gradients.  Up to 1536 tokens an adapter's are one run: six passes of a workgroup take no longer than a launch that adds parts.
+// Longer lists: short enough that some 1024 workgroups share the columns of x and dy, long enough that the parts of a run, binary32 and as
+// wide as a gradient, are small beside the 16-bit rows that it reads.
 static u32 run_tokens(i64 n_tokens, i64 n_in, i64 n_out) {
+    if (n_tokens <= 1536) return 1536;
     const i64 tiles = (n_in + kGradCols - 1) / kGradCols + (n_out + kGradCols - 1) / kGradCols;
     i64 run = n_tokens * tiles / 1024;
-    run = run < 256 ? 256 : run;
-    return static_cast<u32>((run + kGradStep - 1) / kGradStep * kGradStep);
+    run = run < 512 ? 512 : run;
+    return static_cast<u32>((run + kGradPass - 1) / kGradPass * kGradPass);
 }
+
+// Ranks that a workgroup of the gradients takes, in sixteens.
+static u32 grad_groups(u32 max_rank) { return max_rank <= 16 ? 1 : (max_rank <= 32 ? 2 : 4); }
+
+// Rows that are no multiple of eight long are copied to aligned rows beside z where more tokens than this use them.
+constexpr i64 kPackTokens = 64;
+static u64 packed_cols(i64 cols) { return static_cast<u64>(cols + 7) / 8 * 8; }
 
 struct Plan {
     bool split = false;
     u32 rp = 0, splits = 1, steps_each = 0, bm = 64;
     u32 run = 0, n_slots = 0, tiles = 0;
+    bool pack_in = false, pack_out = false;                 // rows of n_in (x, W), rows of n_out (dy)
+    size_t xq = 0, wq = 0, dyq = 0;
     size_t zp = 0, z32 = 0, part = 0, part_wide = 0, row_max = 0, order = 0, seg = 0, slots = 0, total = 0;
 };
 
@@ -65,7 +76,7 @@ static Plan make_plan(i64 T, i64 n_in, i64 n_out, u32 n_adapters, u32 max_rank, 
         if (!p.split) p.zp = take(static_cast<u64>(T) * p.rp * 2);
         if (p.split || backward) p.z32 = take(static_cast<u64>(T) * p.rp * 4);
         if (backward) {
-            p.row_max = take(static_cast<u64>(T) * 4);
+            p.row_max = take(static_cast<u64>(T) * (p.rp / kDownRanks) * 4);
             p.run = run_tokens(T, n_in, n_out);
             p.n_slots = static_cast<u32>(T / p.run) + n_adapters;
             p.order = take(static_cast<u64>(T) * 4);
@@ -74,12 +85,20 @@ static Plan make_plan(i64 T, i64 n_in, i64 n_out, u32 n_adapters, u32 max_rank, 
             if (T > p.run) p.part = take(static_cast<u64>(p.n_slots) * max_rank * (n_in + n_out) * 4);
         }
     }
+    p.pack_in = T > kPackTokens && n_in % 8 != 0;
+    p.pack_out = backward && T > kPackTokens && n_out % 8 != 0;
+    if (p.pack_in) {
+        p.xq = take(static_cast<u64>(T) * packed_cols(n_in) * 2);
+        p.wq = take(static_cast<u64>(n_out) * packed_cols(n_in) * 2);
+    }
+    if (p.pack_out) p.dyq = take(static_cast<u64>(T) * packed_cols(n_out) * 2);
     p.total = at;
     return p;
 }
 
 template <typename E, bool ALONG>
 static condensa_status launch_down(const DownArgs& a, u32 blocks, hipStream_t st) {
+    for (const PackArgs& p : a.pack) blocks += p.blocks;
     if (a.vec_x) hipLaunchKernelGGL((k_adapter_down<E, ALONG, true>), dim3(blocks), dim3(64 * kDownWaves), 0, st, a);
     else         hipLaunchKernelGGL((k_adapter_down<E, ALONG, false>), dim3(blocks), dim3(64 * kDownWaves), 0, st, a);
     CONDENSA_LAUNCH_CHECK();
@@ -89,7 +108,7 @@ static condensa_status launch_down(const DownArgs& a, u32 blocks, hipStream_t st
 template <typename E, int BM, int BN, int WM, int WN, u32 NB, bool ALONG, int ROWS>
 static void launch_wide_tile(const WideArgs& a, hipStream_t st) {
     const u64 tiles = (static_cast<u64>(a.n_tokens) + BM - 1) / BM * ((static_cast<u64>(a.n_out) + BN - 1) / BN);
-    hipLaunchKernelGGL((k_adapter_wide<E, BM, BN, WM, WN, NB, ALONG, ROWS>), dim3(static_cast<unsigned>(tiles * a.splits)), dim3(64 * WM * WN), 0, st, a);
+    hipLaunchKernelGGL((k_adapter_wide<E, BM, BN, WM, WN, NB, ALONG, ROWS>), dim3(static_cast<unsigned>(tiles)), dim3(64 * WM * WN), 0, st, a);
 }
 
 template <typename E, bool ALONG>
@@ -117,19 +136,47 @@ static condensa_status launch_wide(WideArgs a, int rows, hipStream_t st) {
 }
 
 template <typename E, bool ALONG, int BM>
-static void launch_split_tile(const DownArgs& d, const WideArgs& w, u32 down_blocks, bool by_token, int rows, hipStream_t st) {
+static void launch_split_tile(const DownArgs& d, const WideArgs& w, u32 down_blocks, int rows, hipStream_t st) {
     const dim3 blocks(down_blocks + (w.n_tokens + BM - 1) / BM * ((w.n_out + 63) / 64) * w.splits);
-    if (rows == kRows16)     hipLaunchKernelGGL((k_adapter_split<E, ALONG, kRows16, BM>), blocks, dim3(256), 0, st, d, w, down_blocks, by_token);
-    else if (rows == kRows4) hipLaunchKernelGGL((k_adapter_split<E, ALONG, kRows4, BM>), blocks, dim3(256), 0, st, d, w, down_blocks, by_token);
-    else                     hipLaunchKernelGGL((k_adapter_split<E, ALONG, kRowsAny, BM>), blocks, dim3(256), 0, st, d, w, down_blocks, by_token);
+    if (rows == kRows16)     hipLaunchKernelGGL((k_adapter_split<E, ALONG, kRows16, BM>), blocks, dim3(256), 0, st, d, w, down_blocks);
+    else if (rows == kRows4) hipLaunchKernelGGL((k_adapter_split<E, ALONG, kRows4, BM>), blocks, dim3(256), 0, st, d, w, down_blocks);
+    else                     hipLaunchKernelGGL((k_adapter_split<E, ALONG, kRowsAny, BM>), blocks, dim3(256), 0, st, d, w, down_blocks);
 }
 
 template <typename E, bool ALONG>
-static condensa_status launch_split(const DownArgs& d, const WideArgs& w, u32 bm, u32 down_blocks, bool by_token, int rows, hipStream_t st) {
-    if (bm == 32) launch_split_tile<E, ALONG, 32>(d, w, down_blocks, by_token, rows, st);
-    else          launch_split_tile<E, ALONG, 64>(d, w, down_blocks, by_token, rows, st);
+static condensa_status launch_split(const DownArgs& d, const WideArgs& w, u32 bm, u32 down_blocks, int rows, hipStream_t st) {
+    if (bm == 32) launch_split_tile<E, ALONG, 32>(d, w, down_blocks, rows, st);
+    else          launch_split_tile<E, ALONG, 64>(d, w, down_blocks, rows, st);
     CONDENSA_LAUNCH_CHECK();
     return CONDENSA_OK;
+}
+
+template <typename E>
+static condensa_status launch_grads(const GradArgs& q, const WideArgs& g, u32 joins, u32 grid, u32 groups, bool vec, hipStream_t st) {
+    const dim3 threads(64 * kGradWaves);
+    if (groups == 1) {
+        if (vec) hipLaunchKernelGGL((k_adapter_grads<E, true, 1>), dim3(grid), threads, 0, st, q, g, joins);
+        else     hipLaunchKernelGGL((k_adapter_grads<E, false, 1>), dim3(grid), threads, 0, st, q, g, joins);
+    } else if (groups == 2) {
+        if (vec) hipLaunchKernelGGL((k_adapter_grads<E, true, 2>), dim3(grid), threads, 0, st, q, g, joins);
+        else     hipLaunchKernelGGL((k_adapter_grads<E, false, 2>), dim3(grid), threads, 0, st, q, g, joins);
+    } else {
+        if (vec) hipLaunchKernelGGL((k_adapter_grads<E, true, 4>), dim3(grid), threads, 0, st, q, g, joins);
+        else     hipLaunchKernelGGL((k_adapter_grads<E, false, 4>), dim3(grid), threads, 0, st, q, g, joins);
+    }
+    CONDENSA_LAUNCH_CHECK();
+    return CONDENSA_OK;
+}
+
+// Names the copy of `rows` rows in the call's workspace and what takes the place of the rows.
+static PackArgs pack_into(const u16** rows, i64* ld, i64 n, i64 cols, u16* copy) {
+    PackArgs p{};
+    p.src = *rows; p.ld = *ld; p.dst = copy;
+    p.rows = static_cast<u32>(n); p.cols = static_cast<u32>(cols);
+    p.blocks = static_cast<u32>((n + kPackRows - 1) / kPackRows);
+    *rows = copy;
+    *ld = static_cast<i64>(packed_cols(cols));
+    return p;
 }
 
 // How rows lie that a sum runs along (x, W forward, dy) or across (W in the backward pass).
@@ -245,9 +292,10 @@ condensa_status condensa_adapter_project(const condensa_adapter_list* list, cons
     hipStream_t st = static_cast<hipStream_t>(stream);
     const bool f16 = list->type == CONDENSA_TYPE_F16;
     const bool vec_x = aligned(x_dev, 16) && x_stride % 8 == 0 && list->n_in % 8 == 0;
-    const int rows = std::min(rows_of(x_dev, x_stride, list->n_in, false), rows_of(w_dev, w_stride, list->n_in, false));
     WideArgs g{};
     g.x = x_dev; g.ldx = x_stride; g.w = w_dev; g.ldw = w_stride; g.y = y_dev; g.ldy = y_stride;
+    const u32 row = static_cast<u32>(p.pack_in ? packed_cols(list->n_in) : list->n_in);
+    g.x_cols = g.w_cols = row;
     g.n_tokens = static_cast<u32>(n_tokens); g.n_out = static_cast<u32>(list->n_out); g.n_sum = static_cast<u32>(list->n_in);
     g.rp = p.rp; g.ids = token_adapter_dev; g.ad = static_cast<const AdapterDesc*>(list->table_dev);
     g.n_adapters = static_cast<u32>(list->n_adapters); g.max_rank = static_cast<u32>(list->max_rank);
@@ -261,10 +309,20 @@ condensa_status condensa_adapter_project(const condensa_adapter_list* list, cons
     d.z32 = p.split ? at<float>(workspace_dev, p.z32) : nullptr;
     d.vec_x = vec_x;
     d.tiles = (g.n_tokens + kDownTokens - 1) / kDownTokens;
+    d.by_token = p.split && n_tokens <= kTokenwise;
+    u32 down = d.by_token ? g.n_tokens : d.tiles * kDownShare;
+    if (p.pack_in) {
+        d.pack[0] = pack_into(&g.w, &g.ldw, list->n_out, list->n_in, at<u16>(workspace_dev, p.wq));
+        d.pack[1] = pack_into(&g.x, &g.ldx, n_tokens, list->n_in, at<u16>(workspace_dev, p.xq));
+    }
+    const int rows = std::min(rows_of(g.x, g.ldx, row, false), rows_of(g.w, g.ldw, row, false));
+    if (p.pack_in || !p.split) {
+        const condensa_status s = f16 ? launch_down<ElemF16, true>(d, down, st) : launch_down<ElemBF16, true>(d, down, st);
+        if (s != CONDENSA_OK) return s;
+        down = 0;
+    }
     if (p.split) {
-        const bool by_token = n_tokens <= kTokenwise;
-        const u32 down = by_token ? g.n_tokens : d.tiles * kDownShare;
-        condensa_status s = f16 ? launch_split<ElemF16, true>(d, g, p.bm, down, by_token, rows, st) : launch_split<ElemBF16, true>(d, g, p.bm, down, by_token, rows, st);
+        const condensa_status s = f16 ? launch_split<ElemF16, true>(d, g, p.bm, down, rows, st) : launch_split<ElemBF16, true>(d, g, p.bm, down, rows, st);
         if (s != CONDENSA_OK) return s;
         const dim3 grid((g.n_out + 255) / 256, g.n_tokens);
         if (f16) hipLaunchKernelGGL((k_adapter_split_join<ElemF16, true>), grid, dim3(256), 0, st, g, static_cast<const float*>(d.z32), p.rp);
@@ -272,8 +330,6 @@ condensa_status condensa_adapter_project(const condensa_adapter_list* list, cons
         CONDENSA_LAUNCH_CHECK();
         return CONDENSA_OK;
     }
-    condensa_status s = f16 ? launch_down<ElemF16, true>(d, d.tiles * kDownShare, st) : launch_down<ElemBF16, true>(d, d.tiles * kDownShare, st);
-    if (s != CONDENSA_OK) return s;
     return f16 ? launch_wide<ElemF16, true>(g, rows, st) : launch_wide<ElemBF16, true>(g, rows, st);
 }
 
@@ -299,12 +355,12 @@ condensa_status condensa_adapter_project_backward(const condensa_adapter_list* l
                      byte_range(z_dev, static_cast<u64>(n_tokens) * z_stride * 2, false), byte_range(dx_dev, rows_bytes(n_tokens, dx_stride, list->n_in, 2), true),
                      byte_range(workspace_dev, p.total, true), byte_range(list->table_dev, condensa_adapter_list_bytes(list->n_adapters), false)};
     if (ranges_conflict(r, sizeof(r) / sizeof(r[0]))) return CONDENSA_ERR_ARG;
-    const u64 grad_blocks = static_cast<u64>((list->max_rank + 63) / 64) * p.n_slots * ((list->n_in + kGradCols - 1) / kGradCols + (list->n_out + kGradCols - 1) / kGradCols);
-    if (grad_blocks >= (static_cast<u64>(1) << 24)) return CONDENSA_ERR_SIZE;
+    const u32 groups = grad_groups(static_cast<u32>(list->max_rank)), rank_groups = (static_cast<u32>(list->max_rank) + 16 * groups - 1) / (16 * groups);
+    const u64 grad_blocks = static_cast<u64>(rank_groups) * p.n_slots * ((list->n_in + kGradCols - 1) / kGradCols + (list->n_out + kGradCols - 1) / kGradCols);
+    if (grad_blocks >= (static_cast<u64>(1) << 22)) return CONDENSA_ERR_SIZE;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const bool f16 = list->type == CONDENSA_TYPE_F16;
     const bool vec_dy = aligned(dy_dev, 16) && dy_stride % 8 == 0 && list->n_out % 8 == 0;
-    const bool vec_x = aligned(x_dev, 16) && x_stride % 8 == 0 && list->n_in % 8 == 0;
     const u32 T = static_cast<u32>(n_tokens), n = static_cast<u32>(list->n_adapters);
     const AdapterDesc* ad = static_cast<const AdapterDesc*>(list->table_dev);
     DownArgs d{};
@@ -316,9 +372,10 @@ condensa_status condensa_adapter_project_backward(const condensa_adapter_list* l
     d.tiles = (T + kDownTokens - 1) / kDownTokens;
     d.order = at<u32>(workspace_dev, p.order); d.seg = at<uint2>(workspace_dev, p.seg); d.slots = at<uint4>(workspace_dev, p.slots);
     d.n_slots = p.n_slots; d.run = p.run;
-    const u32 waves = split ? 4 : kDownWaves;
+    const bool pack = p.pack_in || p.pack_out;                    // a launch of its own for z and the copies
+    const u32 waves = split && !pack ? 4 : kDownWaves;
     d.sorters = (n + waves - 1) / waves;
-    const u32 blocks = d.tiles * kDownShare + d.sorters;
+    u32 blocks = d.tiles * kDownShare + d.sorters;
     if (blocks == 0) return CONDENSA_OK;
     WideArgs g{};
     g.x = dy_dev; g.ldx = dy_stride; g.w = w_dev; g.ldw = w_stride; g.y = dx_dev; g.ldy = dx_stride;
@@ -327,37 +384,45 @@ condensa_status condensa_adapter_project_backward(const condensa_adapter_list* l
     g.vec_y = aligned(dx_dev, 8) && dx_stride % 4 == 0;
     g.splits = p.splits; g.steps_each = p.steps_each;
     g.part = p.split ? at<float>(workspace_dev, p.part_wide) : nullptr;
-    const int rows = std::min(rows_of(dy_dev, dy_stride, list->n_out, false), rows_of(w_dev, w_stride, list->n_in, true));
+    const u32 in_cols = static_cast<u32>(p.pack_in ? packed_cols(list->n_in) : list->n_in), out_cols = static_cast<u32>(p.pack_out ? packed_cols(list->n_out) : list->n_out);
+    g.x_cols = out_cols;
+    g.w_cols = in_cols;
+    const u16* x_rows = x_dev;
+    i64 ldx = x_stride;
+    if (p.pack_out) d.pack[0] = pack_into(&g.x, &g.ldx, n_tokens, list->n_out, at<u16>(workspace_dev, p.dyq));
+    if (p.pack_in) {
+        d.pack[1] = pack_into(&x_rows, &ldx, n_tokens, list->n_in, at<u16>(workspace_dev, p.xq));
+        if (wide) d.pack[2] = pack_into(&g.w, &g.ldw, list->n_out, list->n_in, at<u16>(workspace_dev, p.wq));
+    }
+    const int rows = std::min(rows_of(g.x, g.ldx, out_cols, false), rows_of(g.w, g.ldw, in_cols, true));
     condensa_status s;
-    if (split) {
-        s = f16 ? launch_split<ElemF16, false>(d, g, p.bm, blocks, false, rows, st) : launch_split<ElemBF16, false>(d, g, p.bm, blocks, false, rows, st);
-        if (s != CONDENSA_OK) return s;
-    } else {
+    if (pack || !split) {
         s = f16 ? launch_down<ElemF16, false>(d, blocks, st) : launch_down<ElemBF16, false>(d, blocks, st);
         if (s != CONDENSA_OK) return s;
-        if (wide) s = f16 ? launch_wide<ElemF16, false>(g, rows, st) : launch_wide<ElemBF16, false>(g, rows, st);
+        blocks = 0;
+    }
+    if (split) {
+        s = f16 ? launch_split<ElemF16, false>(d, g, p.bm, blocks, rows, st) : launch_split<ElemBF16, false>(d, g, p.bm, blocks, rows, st);
+        if (s != CONDENSA_OK) return s;
+    } else if (wide) {
+        s = f16 ? launch_wide<ElemF16, false>(g, rows, st) : launch_wide<ElemBF16, false>(g, rows, st);
         if (s != CONDENSA_OK) return s;
     }
     const u32 joins = split ? (g.n_out + 255) / 256 * T : 0;
     if (n == 0 && joins == 0) return CONDENSA_OK;
     GradArgs q{};
-    q.x = x_dev; q.ldx = x_stride; q.n_in = static_cast<u32>(list->n_in); q.dy = dy_dev; q.ldy = dy_stride; q.n_out = static_cast<u32>(list->n_out);
+    q.x = x_rows; q.ldx = ldx; q.n_in = static_cast<u32>(list->n_in); q.dy = g.x; q.ldy = g.ldx; q.n_out = static_cast<u32>(list->n_out);
+    q.x_cols = in_cols; q.dy_cols = out_cols;
     q.dz = d.z32; q.rp = p.rp; q.z = z_dev; q.ldz = z_stride; q.row_max = d.row_max; q.order = d.order; q.seg = d.seg; q.slots = d.slots; q.ad = ad;
     q.max_rank = d.max_rank; q.run = p.run;
     q.tiles_in = (q.n_in + kGradCols - 1) / kGradCols;
     q.tiles = q.tiles_in + (q.n_out + kGradCols - 1) / kGradCols;
     q.part = n_tokens > p.run ? at<float>(workspace_dev, p.part) : nullptr;
-    q.rank_groups = (q.max_rank + 63) / 64;
-    const dim3 grid(joins + static_cast<u32>(n > 0 ? p.n_slots * q.tiles * q.rank_groups : 0));
-    const bool vec = vec_x && vec_dy;
-    if (f16) {
-        if (vec) hipLaunchKernelGGL((k_adapter_grads<ElemF16, true>), grid, dim3(256), 0, st, q, g, joins);
-        else     hipLaunchKernelGGL((k_adapter_grads<ElemF16, false>), grid, dim3(256), 0, st, q, g, joins);
-    } else {
-        if (vec) hipLaunchKernelGGL((k_adapter_grads<ElemBF16, true>), grid, dim3(256), 0, st, q, g, joins);
-        else     hipLaunchKernelGGL((k_adapter_grads<ElemBF16, false>), grid, dim3(256), 0, st, q, g, joins);
-    }
-    CONDENSA_LAUNCH_CHECK();
+    q.rank_groups = rank_groups;
+    const u32 grid = (joins + 1) / 2 + static_cast<u32>(n > 0 ? grad_blocks : 0);
+    const bool vec = aligned(q.x, 16) && q.ldx % 8 == 0 && in_cols % 8 == 0 && aligned(q.dy, 16) && q.ldy % 8 == 0 && out_cols % 8 == 0;
+    s = f16 ? launch_grads<ElemF16>(q, g, joins, grid, groups, vec, st) : launch_grads<ElemBF16>(q, g, joins, grid, groups, vec, st);
+    if (s != CONDENSA_OK) return s;
     if (n > 0 && n_tokens > p.run) {
         const u64 elems = static_cast<u64>(q.max_rank) * (list->n_in + list->n_out);
         u64 each = (elems + 1023) / 1024;

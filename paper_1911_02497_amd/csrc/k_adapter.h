@@ -173,7 +173,23 @@ __device__ inline int next_adapter(int id, int last) {
     return __builtin_amdgcn_readfirstlane(x);          // known to be the same in all lanes: what it selects comes in scalar registers
 }
 
+__device__ inline u32 wave_most(u32 x) {               // largest of 64 lanes' values
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) {
+        const u32 y = static_cast<u32>(__shfl_xor(static_cast<int>(x), d, 64));
+        x = x > y ? x : y;
+    }
+    return x;
+}
+
 // ---- down: the product with the narrow matrix -------------------------------------------------------------------
+
+// Rows at any address and of any length, copied to rows that are 16-byte aligned and end in zeros.
+struct PackArgs {
+    const u16* src; i64 ld;              // [rows, cols]
+    u16* dst;                            // [rows, cols rounded up to eight]
+    u32 rows, cols, blocks;
+};
 
 struct DownArgs {
     const u16* x; i64 ldx;               // [n_tokens, n_sum]
@@ -184,7 +200,7 @@ struct DownArgs {
     u16* zp; u32 rp;                     // [n_tokens, rp] 16-bit, zeros past the rank; rp = max_rank rounded up to 32
     u16* z; i64 ldz;                     // the caller's copy, or NULL; all ldz columns are written
     float* z32;                          // [n_tokens, rp] before rounding, or NULL
-    u32* row_max;                        // largest finite magnitude of each token's z (bits), or NULL
+    u32* row_max;                        // [n_tokens, rp / 32] largest finite magnitude (bits) in 32 values of a token's z, or NULL
     u32 vec_x;                           // 16-byte aligned rows of x
     u32 tiles;                           // of 32 tokens
     u32 sorters;                         // workgroups that sort the tokens by adapter (backward)
@@ -192,6 +208,8 @@ struct DownArgs {
     uint4* slots;                        // [n_slots] of a run of tokens: adapter or ~0, first place in `order`, tokens, tokens of the adapter
     uint2* seg;                          // [n_adapters] first slot, slots
     u32 n_slots, run;                    // tokens of a run
+    u32 by_token;                        // forward: a workgroup has one token instead of a share of a tile
+    PackArgs pack[3];                    // copies made beside z (k_adapter_down)
 };
 
 constexpr int kDownTokens = 32, kDownRanks = 32;
@@ -324,8 +342,9 @@ __device__ inline void down_sums(const DownArgs& p, u32 t0, const u16* m, u32 ra
 
 // z = s x M_a^T for 32 tokens, where M_a is the adapter's A [rank, n_sum] (ALONG), or its B [n_sum, rank] in the backward pass.  Reading x
 // bounds it: wavefronts take every WAVES-th 64 values of its rows (nothing of x is shared between them) and add their sums up at the
-// end; thirty-two tokens share what is read of M_a.  Four workgroups have the same tile and take its tokens' adapters in turn: most find
-// none, and a tile where one request ends and the next begins takes no longer than the others.  The first workgroups sort the tokens.
+// end; thirty-two tokens share what is read of M_a.  Four workgroups have the same tile and take its tokens' adapters, 32 ranks at a time, in
+// turn: a tile where one request ends and the next begins takes no longer than the others, and up to 128 ranks no longer than 32.  The first
+// workgroups sort the tokens.
 template <typename E, bool ALONG, bool VECX, u32 WAVES>
 __device__ inline void down_tile(const DownArgs& p, u32 block, char* lds) {
     const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -354,13 +373,13 @@ __device__ inline void down_tile(const DownArgs& p, u32 block, char* lds) {
     float (*sums)[kDownTokens][kDownRanks] = reinterpret_cast<float (*)[kDownTokens][kDownRanks]>(lds);
     u16* own = reinterpret_cast<u16*>(lds) + wave * 4096;
     u32 turn = 0;
-    for (int a = next_adapter(my_id, -1); a != 0x7FFFFFFF; a = next_adapter(my_id, a), ++turn) {       // uniform over the workgroup
-        if (turn % kDownShare != share) continue;
+    for (int a = next_adapter(my_id, -1); a != 0x7FFFFFFF; a = next_adapter(my_id, a)) {       // uniform over the workgroup
         const AdapterDesc d = p.ad[a];
         const u32 rank = d.rank < p.max_rank ? d.rank : p.max_rank;
         const u16* m = ALONG ? d.a : d.b;
         const bool vec_m = ALONG ? d.vec_a : d.vec_b;
-        for (u32 r0 = 0; r0 < rank; r0 += kDownRanks) {
+        for (u32 r0 = 0; r0 < rank; r0 += kDownRanks, ++turn) {
+            if (turn % kDownShare != share) continue;
             const u32 groups = rank - r0 <= 16 ? 1 : 2;
             f32x4 acc[2][2] = {};
             if (vec_m) {
@@ -396,16 +415,9 @@ __device__ inline void down_tile(const DownArgs& p, u32 block, char* lds) {
                     const u32 u = __float_as_uint(v) & 0x7FFFFFFFu;
                     if (u < 0x7F800000u) most = most > u ? most : u;
                 }
-                if (p.row_max) {                             // the same wavefront has the row in every round
-#pragma unroll
-                    for (int d2 = 32; d2 >= 1; d2 >>= 1) {
-                        const u32 o = static_cast<u32>(__shfl_xor(static_cast<int>(most), d2, 64));
-                        most = most > o ? most : o;
-                    }
-                    if (lane == 0) {
-                        const u32 before = r0 ? p.row_max[t] : 0u;
-                        p.row_max[t] = most > before ? most : before;
-                    }
+                if (p.row_max) {
+                    most = wave_most(most);
+                    if (lane == 0) p.row_max[t * (p.rp / kDownRanks) + r0 / kDownRanks] = most;
                 }
             }
             __syncthreads();                                 // before tiles take the place of the sums
@@ -461,10 +473,37 @@ __device__ inline void down_token(const DownArgs& p, u32 t) {
 }
 
 constexpr u32 kDownWaves = 8;
+constexpr u32 kPackRows = 4 * kDownWaves;                    // of a workgroup, four to a wavefront
+__device__ inline void pack_rows(const PackArgs& p, u32 block) {
+    const u32 lane = threadIdx.x & 63, r0 = block * kPackRows + (threadIdx.x >> 6) * 4, width = (p.cols + 7) / 8 * 8;
+    for (u32 k = lane * 8; k < width; k += 512) {
+        u32x4 v[4];
+#pragma unroll
+        for (u32 i = 0; i < 4; ++i) v[i] = load8<false>(p.src + static_cast<i64>(r0 + i < p.rows ? r0 + i : p.rows - 1) * p.ld, k, p.cols);
+#pragma unroll
+        for (u32 i = 0; i < 4; ++i)
+            if (r0 + i < p.rows) *reinterpret_cast<u32x4*>(p.dst + static_cast<u64>(r0 + i) * width + k) = v[i];
+    }
+}
+
+// z, and beside it aligned copies of what the wide product and the gradients read: loads of the wide product go straight into LDS, 16 bytes a
+// lane, only from aligned rows.
 template <typename E, bool ALONG, bool VECX>
 __global__ __launch_bounds__(64 * kDownWaves) void k_adapter_down(DownArgs p) {
     __shared__ __align__(16) char lds[down_lds(kDownWaves)];
-    down_tile<E, ALONG, VECX, kDownWaves>(p, blockIdx.x, lds);
+    const u32 down = ALONG && p.by_token ? p.n_tokens : p.sorters + p.tiles * kDownShare;
+    u32 block = blockIdx.x;
+    if (block >= down) {                                     // uniform
+        block -= down;
+#pragma unroll
+        for (u32 i = 0; i < 3; ++i) {
+            if (block < p.pack[i].blocks) { pack_rows(p.pack[i], block); return; }
+            block -= p.pack[i].blocks;
+        }
+        return;
+    }
+    if (ALONG && p.by_token) down_token<E, VECX, kDownWaves>(p, block);
+    else down_tile<E, ALONG, VECX, kDownWaves>(p, block, lds);
 }
 
 // ---- the wide product with the adapters' share added ------------------------------------------------------------
@@ -474,6 +513,7 @@ struct WideArgs {
     const u16* w; i64 ldw;               // ALONG: [n_out, n_sum], else [n_sum, n_out]
     u16* y; i64 ldy;                     // [n_tokens, n_out]
     u32 n_tokens, n_out, n_sum;
+    u32 x_cols, w_cols;                  // values of a row of x and of W, with the zeros at the end of a copy
     const u16* zp; u32 rp;
     const int* ids;
     const AdapterDesc* ad;
@@ -545,7 +585,7 @@ __device__ inline void wide_tile(const WideArgs& p, u32 block_id, u32 n_blocks, 
                 constexpr u32 kRow = BN / 8;
                 const u32 k = at / (kRow * kOf);
                 u32 col = across_at<BN>(k, at / kOf % kRow) - k * BN + at % kOf * (kBytes / 2);
-                if (n0 + col >= p.n_out) col = p.n_out - kBytes / 2 - n0;
+                if (n0 + col >= p.w_cols) col = p.w_cols - kBytes / 2 - n0;
                 wo[i] = (k * static_cast<u32>(p.ldw) + col) * 2;
             }
         }
@@ -701,7 +741,7 @@ __device__ inline void wide_tile(const WideArgs& p, u32 block_id, u32 n_blocks, 
         const i64 k_end = rest ? p.n_sum : rank;
         const u32 subs = k_end - k0 > 32 ? 2 : 1;
         const u16* x = rest ? p.x : p.zp;
-        const i64 ldx = rest ? p.ldx : static_cast<i64>(p.rp), x_end = rest ? p.n_sum : p.rp;
+        const i64 ldx = rest ? p.ldx : static_cast<i64>(p.rp), x_end = rest ? p.x_cols : p.rp;
         for (u32 at = me; at < BM * 8; at += kThreads) {
             const u32 row = at >> 3, piece = at & 7u, t = t0 + row < p.n_tokens ? t0 + row : p.n_tokens - 1;
             const u16* src = x + static_cast<i64>(t) * ldx;
@@ -714,7 +754,8 @@ __device__ inline void wide_tile(const WideArgs& p, u32 block_id, u32 n_blocks, 
             const u32 row = ALONG ? at >> 3 : at / (BN / 8), piece = ALONG ? at & 7u : at % (BN / 8);
             if ((ALONG ? piece >> 2 : row >> 5) >= subs) continue;
             const u16* src = ALONG ? w + static_cast<i64>(n0 + row < p.n_out ? n0 + row : p.n_out - 1) * ldw : w + (k0 + row) * ldw;
-            const i64 from = ALONG ? k0 + piece * 8 : n0 + piece * 8, end_at = ALONG ? k_end : (k0 + row < k_end ? p.n_out : 0);
+            const i64 from = ALONG ? k0 + piece * 8 : n0 + piece * 8, cols = rest ? p.w_cols : (ALONG ? rank : p.n_out);
+            const i64 end_at = ALONG || k0 + row < k_end ? cols : 0;
             const u32x4 v = vec_w ? load8<true>(src, from, end_at) : load8<false>(src, from, end_at);
             *reinterpret_cast<u32x4*>(tiles + BM * 64 + (ALONG ? along_at(row, piece) : across_at<BN>(row, piece))) = v;
         }
@@ -790,12 +831,12 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_adapter_wide(WideArgs p) {
 // Where tiles of 64 outputs are few, the sum is split and z is made in the same launch: nothing in it waits for anything.  z comes first, its
 // chain of loads is the longest.
 template <typename E, bool ALONG, int ROWS, int BM>
-__global__ __launch_bounds__(256, 2) void k_adapter_split(DownArgs d, WideArgs w, u32 down_blocks, u32 by_token) {
+__global__ __launch_bounds__(256, 2) void k_adapter_split(DownArgs d, WideArgs w, u32 down_blocks) {
     constexpr u32 NB = ROWS != kRowsAny ? 3 : 2;
     constexpr bool VECX = ROWS == kRows16;
     __shared__ __align__(16) char lds[wide_lds(BM, 64, NB) > down_lds(4) ? wide_lds(BM, 64, NB) : down_lds(4)];
     if (blockIdx.x >= down_blocks) wide_tile<E, BM, 64, BM / 32, 128 / BM, NB, ALONG, ROWS>(w, blockIdx.x - down_blocks, gridDim.x - down_blocks, lds);
-    else if (ALONG && by_token) down_token<E, VECX, 4>(d, blockIdx.x);
+    else if (ALONG && d.by_token) down_token<E, VECX, 4>(d, blockIdx.x);
     else down_tile<E, ALONG, VECX, 4>(d, blockIdx.x, lds);
 }
 
@@ -841,6 +882,7 @@ __global__ __launch_bounds__(256) void k_adapter_split_join(WideArgs w, const fl
 struct GradArgs {
     const u16* x; i64 ldx; u32 n_in;     // grad_a = sum of dz^T x
     const u16* dy; i64 ldy; u32 n_out;   // grad_b = sum of dy^T z
+    u32 x_cols, dy_cols;                 // values of a row, with the zeros at the end of a copy
     const float* dz; u32 rp;
     const u16* z; i64 ldz;
     const u32* row_max;
@@ -852,29 +894,28 @@ struct GradArgs {
     float* part;                         // [n_slots][max_rank (n_in + n_out)]
 };
 
-constexpr u32 kGradCols = 128, kGradStep = 64, kGradTokens = 1024;
+constexpr u32 kGradCols = 128, kGradWaves = 8, kGradPass = 32 * kGradWaves;
 
-// One run of one adapter's tokens times 128 columns of x or of dy: 64 tokens a step, both operands across the rows of their tiles, the next
-// step's rows on their way while this one's are multiplied.  Reading x and dy once more bounds it; the columns are split and not the ranks,
-// so that they are read by one workgroup only (up to 64 ranks).  dz enters as a sum of 16-bit values, three of bfloat16 or two of
-// float16, since a binary32 gradient would keep no more than 8 or 11 bits of one; runs of float16 are scaled by a power of two first, so that the
-// largest dz of the run sits near the top of the type's range.
-// Workgroups before `joins` add the parts of dx.
-template <typename E, bool VEC>
-__global__ __launch_bounds__(256) void k_adapter_grads(GradArgs p, WideArgs dx, u32 joins) {
+// One run of one adapter's tokens times 128 columns of x or of dy and 16 G ranks.  Reading x and dy once more bounds it; the columns are split and
+// not the ranks, so that one workgroup only reads them (up to 64 ranks).  Every wavefront has 32 tokens of each 256 to itself, what one matrix
+// instruction sums, and meets the others only to add the sums up: with barriers for each step, wavefronts waited for memory together, and
+// 212 tokens took 4 steps one after the other.  Rows of x and dy pass through 8 KB of LDS for the transposing load, dz and z come as
+// fragments, a lane's eight tokens one by one; the next pass is on its way meanwhile.  dz enters as a sum of 16-bit values,
+// three of bfloat16 or two of float16, since a binary32 gradient would keep no more than 8 or 11 bits of one; for float16 a wavefront scales its dz by a
+// power of two first, so that the largest sits near the top of the type's range.
+// Workgroups after the gradients' add the parts of dx.
+template <typename E, bool VEC, int G>
+__global__ __launch_bounds__(64 * kGradWaves, G == 1 ? 4 : 2) void k_adapter_grads(GradArgs p, WideArgs dx, u32 joins) {
     constexpr u32 kTerms = E::kNarrow ? 2 : 3;
-    constexpr u32 kVPieces = kGradStep * kGradCols / 8 / 256, kUPieces = kGradStep * 8 / 256;
-    __shared__ __align__(16) u16 sv[kGradStep * kGradCols], su[kTerms][kGradStep * 64];
-    __shared__ u32 s_tok[kGradTokens];
-    __shared__ u32 s_max;
-    const u32 tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const u32 grads = gridDim.x - joins;
+    __shared__ __align__(16) u16 tiles[kGradWaves][32 * kGradCols];
+    const u32 tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const u32 grads = gridDim.x - (joins + 1) / 2;
     if (blockIdx.x >= grads) {                                 // uniform
-        const u32 cols = (dx.n_out + 255) / 256, block = blockIdx.x - grads;
-        join_parts<E, false>(dx, p.dz, p.rp, block / cols, block % cols * 256 + tid);
+        const u32 cols = (dx.n_out + 255) / 256, block = (blockIdx.x - grads) * 2 + wave / 4;
+        if (block < joins) join_parts<E, false>(dx, p.dz, p.rp, block / cols, block % cols * 256 + (tid & 255u));
         return;
     }
-    const u32 col_tile = blockIdx.x % p.tiles, r0 = blockIdx.x / p.tiles % p.rank_groups * 64, slot = blockIdx.x / p.tiles / p.rank_groups;
+    const u32 col_tile = blockIdx.x % p.tiles, r0 = blockIdx.x / p.tiles % p.rank_groups * (16 * G), slot = blockIdx.x / p.tiles / p.rank_groups;
     const uint4 of = p.slots[slot];
     const u32 a = __builtin_amdgcn_readfirstlane(of.x), first = __builtin_amdgcn_readfirstlane(of.y), count = __builtin_amdgcn_readfirstlane(of.z);
     const bool whole = of.w <= p.run;
@@ -884,128 +925,120 @@ __global__ __launch_bounds__(256) void k_adapter_grads(GradArgs p, WideArgs dx, 
     if (r0 >= rank) return;
     const bool of_a = col_tile < p.tiles_in;
     const u32 c0 = (of_a ? col_tile : col_tile - p.tiles_in) * kGradCols;
-    const u32 n_cols = of_a ? p.n_in : p.n_out;
+    const u32 n_cols = of_a ? p.n_in : p.n_out, v_cols = of_a ? p.x_cols : p.dy_cols;
     const u16* v_src = of_a ? p.x : p.dy;
     const i64 ldv = of_a ? p.ldx : p.ldy;
-    const u32 pieces = (rank - r0 < 64 ? rank - r0 + 7 : 64) / 8;             // of eight ranks
+    u16* own = tiles[wave];
     float up = 1.0f, down = 1.0f;
-    f32x4 acc[2][4] = {};
-    for (u32 c = 0; c < count; c += kGradTokens) {
-        const u32 here = count - c < kGradTokens ? count - c : kGradTokens;
-        __syncthreads();
-        if (tid == 0 && c == 0) s_max = 0;
-        for (u32 i = tid; i < here; i += 256) s_tok[i] = p.order[first + c + i];
-        __syncthreads();
-        u32x4 rv[kVPieces], ru[2 * kUPieces];
-        auto fetch = [&](u32 s) {
+    f32x4 acc[8][G] = {};
+    u32x4 rv[8];
+    u32 ru[G][8];
+    // the tokens of the pass that begins at `s` (lane l: l % 32), the last one again past the end
+    auto tokens = [&](u32 s) { const u32 k = s + (lane & 31u); return p.order[first + (k < count ? k : count - 1)]; };
+    auto fetch = [&](u32 s, u32 tok) {
 #pragma unroll
-            for (u32 i = 0; i < kVPieces; ++i) {
-                const u32 at = i * 256 + tid, k = s + at / (kGradCols / 8), piece = at % (kGradCols / 8);
-                rv[i] = u32x4{0u, 0u, 0u, 0u};
-                if (k < here) rv[i] = load8<VEC>(v_src + static_cast<i64>(s_tok[k]) * ldv, c0 + piece * 8, n_cols);
+        for (u32 i = 0; i < 8; ++i) {
+            const u32 k = i * 4 + (lane >> 4);
+            const i64 t = static_cast<u32>(__shfl(static_cast<int>(tok), static_cast<int>(k), 64));
+            rv[i] = load8<VEC>(v_src + t * ldv, c0 + (lane & 15u) * 8, s + k < count ? v_cols : 0);
+        }
+#pragma unroll
+        for (u32 q = 0; q < 8; ++q) {
+            const u32 k = (lane >> 4) * 8 + q;
+            const u64 t = static_cast<u32>(__shfl(static_cast<int>(tok), static_cast<int>(k), 64));
+#pragma unroll
+            for (u32 g = 0; g < G; ++g) {
+                const u32 j = r0 + g * 16 + (lane & 15u);
+                ru[g][q] = 0;
+                if (s + k >= count || j >= rank) continue;
+                ru[g][q] = of_a ? __float_as_uint(p.dz[t * p.rp + j]) : load2(p.z + t * p.ldz + j);
             }
-#pragma unroll
-            for (u32 i = 0; i < kUPieces; ++i) {
-                const u32 at = i * 256 + tid, k = s + (at >> 3), piece = at & 7u;
-                ru[2 * i] = ru[2 * i + 1] = u32x4{0u, 0u, 0u, 0u};
-                if (k < here && piece < pieces) {
-                    if (of_a) {                                // rows of rp values, zeros past the rank
-                        const u32x4* src = reinterpret_cast<const u32x4*>(p.dz + static_cast<u64>(s_tok[k]) * p.rp + r0 + piece * 8);
-                        ru[2 * i] = src[0];
-                        ru[2 * i + 1] = src[1];
-                    } else {
-                        ru[2 * i] = load8<false>(p.z + static_cast<i64>(s_tok[k]) * p.ldz, r0 + piece * 8, rank);
-                    }
+        }
+    };
+    u32 s = wave * 32;
+    if (s < count) {                                           // uniform in a wavefront
+        const u32 tok = tokens(s);
+        u32 next = tokens(s + kGradPass);
+        fetch(s, tok);
+        if (E::kNarrow && of_a) {
+            u32 most = 0;
+            const u32 groups = (rank + kDownRanks - 1) / kDownRanks;
+            for (u32 k0 = s; k0 < count; k0 += 2 * kGradPass) {
+                const u32 k = k0 + (lane >> 5) * kGradPass + (lane & 31u);
+                if (k >= count) continue;
+                const u64 t = p.order[first + k];
+                for (u32 g = 0; g < groups; ++g) {
+                    const u32 m = p.row_max[t * (p.rp / kDownRanks) + g];
+                    most = most > m ? most : m;
                 }
             }
-        };
-        fetch(0);
-        if (E::kNarrow && of_a && c == 0) {
-            u32 most = 0;
-            for (u32 i = tid; i < count; i += 256) {
-                const u32 m = p.row_max[i < here ? s_tok[i] : p.order[first + i]];
-                most = most > m ? most : m;
-            }
-            atomicMax(&s_max, most);
-            __syncthreads();
-            int e = 14 - (static_cast<int>(s_max >> 23) - 127);                // the largest becomes 2^14 .. 2^15
+            most = wave_most(most);
+            int e = 14 - (static_cast<int>(most >> 23) - 127);                 // the largest becomes 2^14 .. 2^15
             e = e > 120 ? 120 : (e < -100 ? -100 : e);
             up = __uint_as_float(static_cast<u32>(127 + e) << 23);
             down = __uint_as_float(static_cast<u32>(127 - e) << 23);
         }
-        for (u32 s = 0; s < here; s += kGradStep) {
+        for (; s < count; s += kGradPass) {
+            u32x4 fu[G][kTerms] = {};
 #pragma unroll
-            for (u32 i = 0; i < kVPieces; ++i) {
-                const u32 at = i * 256 + tid;
-                *reinterpret_cast<u32x4*>(sv + across_at<kGradCols>(at / (kGradCols / 8), at % (kGradCols / 8))) = rv[i];
-            }
+            for (u32 i = 0; i < 8; ++i) *reinterpret_cast<u32x4*>(own + across_at<kGradCols>(i * 4 + (lane >> 4), lane & 15u)) = rv[i];
 #pragma unroll
-            for (u32 i = 0; i < kUPieces; ++i) {
-                const u32 at = i * 256 + tid, to = across_at<64>(at >> 3, at & 7u);
-                if ((at & 7u) >= ((pieces + 1) & ~1u)) continue;       // no fragment reads it
-                if (of_a) {
-                    u32x4 term[kTerms] = {};
+            for (u32 g = 0; g < G; ++g)
 #pragma unroll
-                    for (u32 q = 0; q < 8; ++q) {
-                        float f = __uint_as_float(ru[2 * i + (q >> 2)][q & 3u]) * up;
+                for (u32 q = 0; q < 8; ++q) {
+                    if (of_a) {
+                        float f = __uint_as_float(ru[g][q]) * up;
 #pragma unroll
                         for (u32 t = 0; t < kTerms; ++t) {
                             const u16 h = E::enc(f);
-                            term[t][q >> 1] |= static_cast<u32>(h) << (16 * (q & 1u));
+                            fu[g][t][q >> 1] |= static_cast<u32>(h) << (16 * (q & 1u));
                             f -= E::dec(h);
                             f = __builtin_fabsf(f) < INFINITY ? f : 0.0f;
                         }
+                    } else {
+                        fu[g][0][q >> 1] |= ru[g][q] << (16 * (q & 1u));
                     }
-#pragma unroll
-                    for (u32 t = 0; t < kTerms; ++t) *reinterpret_cast<u32x4*>(su[t] + to) = term[t];
-                } else {
-                    *reinterpret_cast<u32x4*>(su[0] + to) = ru[2 * i];
                 }
+            if (s + kGradPass < count) {
+                fetch(s + kGradPass, next);
+                next = tokens(s + 2 * kGradPass);
             }
-            __syncthreads();
-            if (s + kGradStep < here) fetch(s + kGradStep);
 #pragma unroll
-            for (u32 sub = 0; sub < 2; ++sub) {
-                u32x4 fv[2];
+            for (u32 c = 0; c < 8; ++c) {
+                const u32x4 fv = across_frag<kGradCols>(own, c * 16, 0);
 #pragma unroll
-                for (u32 i = 0; i < 2; ++i) fv[i] = across_frag<kGradCols>(sv, wave * 32 + i * 16, sub);
-#pragma unroll
-                for (u32 g = 0; g < 4; ++g) {
+                for (u32 g = 0; g < G; ++g) {
                     if (r0 + g * 16 >= rank) continue;
                     if (of_a) {
 #pragma unroll
-                        for (u32 t = kTerms; t-- > 0;) {
-                            const u32x4 fu = across_frag<64>(su[t], g * 16, sub);
-#pragma unroll
-                            for (u32 i = 0; i < 2; ++i) acc[i][g] = E::mfma(fv[i], fu, acc[i][g]);
-                        }
-                    } else {
-                        const u32x4 fu = across_frag<64>(su[0], g * 16, sub);
-#pragma unroll
-                        for (u32 i = 0; i < 2; ++i) acc[i][g] = E::mfma(fu, fv[i], acc[i][g]);
+                        for (u32 t = kTerms; t-- > 1;) acc[c][g] = E::mfma(fv, fu[g][t], acc[c][g]);
                     }
+                    acc[c][g] = E::mfma(fv, fu[g][0], acc[c][g]);
                 }
             }
-            __syncthreads();
         }
     }
     float* out = whole ? (of_a ? d.grad_a : d.grad_b)
                        : p.part + static_cast<u64>(slot) * p.max_rank * (static_cast<u64>(p.n_in) + p.n_out) + (of_a ? 0 : static_cast<u64>(rank) * p.n_in);
+    const u32 used = count < kGradPass ? (count + 31) / 32 : kGradWaves;       // wavefronts that had tokens
+    f32x4* sums = reinterpret_cast<f32x4*>(&tiles[0][0]);
 #pragma unroll
-    for (u32 i = 0; i < 2; ++i)
+    for (u32 g = 0; g < G; ++g) {
+        if (r0 + g * 16 >= rank) continue;                     // uniform over the workgroup
+        __syncthreads();                                       // sums take the place of tiles and of the sums before
+        if (wave < used) {
 #pragma unroll
-        for (u32 g = 0; g < 4; ++g)
+            for (u32 c = 0; c < 8; ++c) sums[wave * 512 + c * 64 + lane] = acc[c][g] * down;
+        }
+        __syncthreads();
+        f32x4 v = {};
+        for (u32 w = 0; w < used; ++w) v += sums[w * 512 + tid];
+        const u32 r = r0 + g * 16 + (lane & 15u), c = c0 + wave * 16 + (lane >> 4) * 4;
+        if (r >= rank) continue;
 #pragma unroll
-            for (u32 q = 0; q < 4; ++q) {
-                const float v = acc[i][g][q] * down;
-                if (of_a) {                                    // rows of the result are columns of x
-                    const u32 r = r0 + g * 16 + (lane & 15), c = c0 + wave * 32 + i * 16 + (lane >> 4) * 4 + q;
-                    if (r < rank && c < n_cols) out[static_cast<u64>(r) * p.n_in + c] = v;
-                } else {
-                    const u32 r = r0 + g * 16 + (lane >> 4) * 4 + q, c = c0 + wave * 32 + i * 16 + (lane & 15);
-                    if (r < rank && c < n_cols) out[static_cast<u64>(c) * rank + r] = v;
-                }
-            }
+        for (u32 q = 0; q < 4; ++q)
+            if (c + q < n_cols) out[of_a ? static_cast<u64>(r) * p.n_in + c + q : static_cast<u64>(c + q) * rank + r] = v[q];
+    }
 }
 
 // Adapters with several runs: their parts, added in order.
