@@ -33,7 +33,10 @@ static u32 run_tokens(i64 n_tokens, i64 n_in, i64 n_out) {
 }
 
 // Ranks that a workgroup of the gradients takes, in sixteens.
-static u32 grad_groups(u32 max_rank) { return max_rank <= 16 ? 1 : (max_rank <= 32 ? 2 : 4); }
+static u32 grad_groups(u32 max_rank) { return max_rank <= 16 ? 1 : 2; }
+
+// Workgroups that share the adapters of a tile of z: more where tiles are few.
+static u32 down_shares(u32 tiles) { return tiles >= 64 ? 4 : (tiles >= 16 ? 8 : 16); }
 
 // Rows that are no multiple of eight long are copied to aligned rows beside z where more tokens than this use them.
 constexpr i64 kPackTokens = 64;
@@ -157,12 +160,9 @@ static condensa_status launch_grads(const GradArgs& q, const WideArgs& g, u32 jo
     if (groups == 1) {
         if (vec) hipLaunchKernelGGL((k_adapter_grads<E, true, 1>), dim3(grid), threads, 0, st, q, g, joins);
         else     hipLaunchKernelGGL((k_adapter_grads<E, false, 1>), dim3(grid), threads, 0, st, q, g, joins);
-    } else if (groups == 2) {
+    } else {
         if (vec) hipLaunchKernelGGL((k_adapter_grads<E, true, 2>), dim3(grid), threads, 0, st, q, g, joins);
         else     hipLaunchKernelGGL((k_adapter_grads<E, false, 2>), dim3(grid), threads, 0, st, q, g, joins);
-    } else {
-        if (vec) hipLaunchKernelGGL((k_adapter_grads<E, true, 4>), dim3(grid), threads, 0, st, q, g, joins);
-        else     hipLaunchKernelGGL((k_adapter_grads<E, false, 4>), dim3(grid), threads, 0, st, q, g, joins);
     }
     CONDENSA_LAUNCH_CHECK();
     return CONDENSA_OK;
@@ -309,8 +309,9 @@ condensa_status condensa_adapter_project(const condensa_adapter_list* list, cons
     d.z32 = p.split ? at<float>(workspace_dev, p.z32) : nullptr;
     d.vec_x = vec_x;
     d.tiles = (g.n_tokens + kDownTokens - 1) / kDownTokens;
+    d.shares = down_shares(d.tiles);
     d.by_token = p.split && n_tokens <= kTokenwise;
-    u32 down = d.by_token ? g.n_tokens : d.tiles * kDownShare;
+    u32 down = d.by_token ? g.n_tokens : d.tiles * d.shares;
     if (p.pack_in) {
         d.pack[0] = pack_into(&g.w, &g.ldw, list->n_out, list->n_in, at<u16>(workspace_dev, p.wq));
         d.pack[1] = pack_into(&g.x, &g.ldx, n_tokens, list->n_in, at<u16>(workspace_dev, p.xq));
@@ -370,12 +371,13 @@ condensa_status condensa_adapter_project_backward(const condensa_adapter_list* l
     d.zp = p.split || !wide ? nullptr : at<u16>(workspace_dev, p.zp); d.rp = p.rp; d.z32 = at<float>(workspace_dev, p.z32); d.row_max = at<u32>(workspace_dev, p.row_max);
     d.vec_x = vec_dy;
     d.tiles = (T + kDownTokens - 1) / kDownTokens;
+    d.shares = down_shares(d.tiles);
     d.order = at<u32>(workspace_dev, p.order); d.seg = at<uint2>(workspace_dev, p.seg); d.slots = at<uint4>(workspace_dev, p.slots);
     d.n_slots = p.n_slots; d.run = p.run;
     const bool pack = p.pack_in || p.pack_out;                    // a launch of its own for z and the copies
     const u32 waves = split && !pack ? 4 : kDownWaves;
     d.sorters = (n + waves - 1) / waves;
-    u32 blocks = d.tiles * kDownShare + d.sorters;
+    u32 blocks = d.tiles * d.shares + d.sorters;
     if (blocks == 0) return CONDENSA_OK;
     WideArgs g{};
     g.x = dy_dev; g.ldx = dy_stride; g.w = w_dev; g.ldw = w_stride; g.y = dx_dev; g.ldy = dx_stride;

@@ -202,7 +202,7 @@ struct DownArgs {
     float* z32;                          // [n_tokens, rp] before rounding, or NULL
     u32* row_max;                        // [n_tokens, rp / 32] largest finite magnitude (bits) in 32 values of a token's z, or NULL
     u32 vec_x;                           // 16-byte aligned rows of x
-    u32 tiles;                           // of 32 tokens
+    u32 tiles, shares;                   // of 32 tokens; workgroups that share the adapters of a tile
     u32 sorters;                         // workgroups that sort the tokens by adapter (backward)
     u32* order;                          // tokens of adapter 0, 1, ... in ascending order
     uint4* slots;                        // [n_slots] of a run of tokens: adapter or ~0, first place in `order`, tokens, tokens of the adapter
@@ -213,7 +213,6 @@ struct DownArgs {
 };
 
 constexpr int kDownTokens = 32, kDownRanks = 32;
-constexpr u32 kDownShare = 4;                                // workgroups that share the adapters of a tile
 constexpr u32 down_lds(u32 waves) { return waves * 8192; }
 
 // Places of the runs of an adapter whose tokens begin at `first`: run j of it is slot first / run + a + j.  (One slot at least for
@@ -268,7 +267,6 @@ __device__ inline void down_sums(const DownArgs& p, u32 t0, const u16* m, u32 ra
     u32 lane = threadIdx.x & 63;
     asm volatile("" : "+v"(lane));                         // keeps the places of each form out of the registers of the others
     const u32 wave = threadIdx.x >> 6, piece = lane & 7u;
-    const u32 full = p.n_sum / 64;
     constexpr u32 kPieces = 2 * G;                         // 16-byte pieces of the narrow matrix for each lane and step
     u16* own_m = own + kDownTokens * 64;
     const u16* xr[4];
@@ -283,7 +281,7 @@ __device__ inline void down_sums(const DownArgs& p, u32 t0, const u16* m, u32 ra
         const u32 j = r0 + i * 8 + (lane >> 3);
         mr[i] = ALONG ? m + static_cast<i64>(j < rank ? j : rank - 1) * p.n_sum : m;
     }
-    // GUARD: the step that ends past the sum
+    // GUARD: the step may end past the sum
     auto fetch = [&](auto guard, u32 s, u32x4 (&x)[4], u32x4 (&v)[kPieces]) {
         constexpr bool GUARD = decltype(guard)::value;
         const i64 k = static_cast<i64>(s) * 64 + piece * 8;
@@ -319,32 +317,33 @@ __device__ inline void down_sums(const DownArgs& p, u32 t0, const u16* m, u32 ra
             }
         }
     };
-    constexpr u32 kAhead = G == 1 ? 3 : 2;                 // steps whose loads are under way at once
+    // Steps whose loads are under way at once.  A step is fetched where the one before it in the same registers has been multiplied.
+    constexpr u32 kAhead = (G == 1 ? 3 : 2) + (WAVES > 4 ? 1 : 0);         // of four wavefronts three workgroups share a unit's registers
+    constexpr bool kGuard = VECX;                          // costs nothing where rows are whole pieces; others take the last step by itself
+    const u32 steps = kGuard ? (p.n_sum + 63) / 64 : p.n_sum / 64;
     u32x4 x[kAhead][4], v[kAhead][kPieces];
-    u32 s = wave;
-    for (; s + (kAhead - 1) * WAVES < full; s += kAhead * WAVES) {
 #pragma unroll
-        for (u32 i = 0; i < kAhead; ++i) fetch(std::false_type{}, s + i * WAVES, x[i], v[i]);
-        __builtin_amdgcn_sched_barrier(0);                 // all of them before the first product
+    for (u32 i = 0; i < kAhead; ++i)
+        if (wave + i * WAVES < steps) fetch(std::bool_constant<kGuard>{}, wave + i * WAVES, x[i], v[i]);
+    for (u32 s = wave; s < steps; s += kAhead * WAVES) {
 #pragma unroll
-        for (u32 i = 0; i < kAhead; ++i) add(x[i], v[i]);
+        for (u32 i = 0; i < kAhead; ++i) {
+            const u32 now = s + i * WAVES, later = now + kAhead * WAVES;
+            if (now < steps) add(x[i], v[i]);
+            if (later < steps) fetch(std::bool_constant<kGuard>{}, later, x[i], v[i]);
+        }
     }
-#pragma unroll 1
-    for (; s < full; s += WAVES) {
-        fetch(std::false_type{}, s, x[0], v[0]);
-        add(x[0], v[0]);
-    }
-    if (s == full && (p.n_sum & 63u)) {
-        fetch(std::true_type{}, s, x[0], v[0]);
+    if (!kGuard && (p.n_sum & 63u) && steps % WAVES == wave) {
+        fetch(std::true_type{}, steps, x[0], v[0]);
         add(x[0], v[0]);
     }
 }
 
 // z = s x M_a^T for 32 tokens, where M_a is the adapter's A [rank, n_sum] (ALONG), or its B [n_sum, rank] in the backward pass.  Reading x
 // bounds it: wavefronts take every WAVES-th 64 values of its rows (nothing of x is shared between them) and add their sums up at the
-// end; thirty-two tokens share what is read of M_a.  Four workgroups have the same tile and take its tokens' adapters, 32 ranks at a time, in
-// turn: a tile where one request ends and the next begins takes no longer than the others, and up to 128 ranks no longer than 32.  The first
-// workgroups sort the tokens.
+// end; thirty-two tokens share what is read of M_a.  Four to sixteen workgroups have the same tile and take its tokens' adapters, 32 ranks at a
+// time, in turn: a tile where one request ends and the next begins takes no longer than the others, and up to 128 ranks no longer than 32.
+// The first workgroups sort the tokens.
 template <typename E, bool ALONG, bool VECX, u32 WAVES>
 __device__ inline void down_tile(const DownArgs& p, u32 block, char* lds) {
     const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -379,7 +378,7 @@ __device__ inline void down_tile(const DownArgs& p, u32 block, char* lds) {
         const u16* m = ALONG ? d.a : d.b;
         const bool vec_m = ALONG ? d.vec_a : d.vec_b;
         for (u32 r0 = 0; r0 < rank; r0 += kDownRanks, ++turn) {
-            if (turn % kDownShare != share) continue;
+            if (turn % p.shares != share) continue;
             const u32 groups = rank - r0 <= 16 ? 1 : 2;
             f32x4 acc[2][2] = {};
             if (vec_m) {
@@ -491,7 +490,7 @@ __device__ inline void pack_rows(const PackArgs& p, u32 block) {
 template <typename E, bool ALONG, bool VECX>
 __global__ __launch_bounds__(64 * kDownWaves) void k_adapter_down(DownArgs p) {
     __shared__ __align__(16) char lds[down_lds(kDownWaves)];
-    const u32 down = ALONG && p.by_token ? p.n_tokens : p.sorters + p.tiles * kDownShare;
+    const u32 down = ALONG && p.by_token ? p.n_tokens : p.sorters + p.tiles * p.shares;
     u32 block = blockIdx.x;
     if (block >= down) {                                     // uniform
         block -= down;
@@ -831,7 +830,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_adapter_wide(WideArgs p) {
 // Where tiles of 64 outputs are few, the sum is split and z is made in the same launch: nothing in it waits for anything.  z comes first, its
 // chain of loads is the longest.
 template <typename E, bool ALONG, int ROWS, int BM>
-__global__ __launch_bounds__(256, 2) void k_adapter_split(DownArgs d, WideArgs w, u32 down_blocks) {
+__global__ __launch_bounds__(256, 3) void k_adapter_split(DownArgs d, WideArgs w, u32 down_blocks) {
     constexpr u32 NB = ROWS != kRowsAny ? 3 : 2;
     constexpr bool VECX = ROWS == kRows16;
     __shared__ __align__(16) char lds[wide_lds(BM, 64, NB) > down_lds(4) ? wide_lds(BM, 64, NB) : down_lds(4)];
@@ -897,7 +896,7 @@ struct GradArgs {
 constexpr u32 kGradCols = 128, kGradWaves = 8, kGradPass = 32 * kGradWaves;
 
 // One run of one adapter's tokens times 128 columns of x or of dy and 16 G ranks.  Reading x and dy once more bounds it; the columns are split and
-// not the ranks, so that one workgroup only reads them (up to 64 ranks).  Every wavefront has 32 tokens of each 256 to itself, what one matrix
+// not the ranks, so that one workgroup only reads them (up to 32 ranks; with 64 in a workgroup registers were spilled).  Every wavefront has 32 tokens of each 256 to itself, what one matrix
 // instruction sums, and meets the others only to add the sums up: with barriers for each step, wavefronts waited for memory together, and
 // 212 tokens took 4 steps one after the other.  Rows of x and dy pass through 8 KB of LDS for the transposing load, dz and z come as
 // fragments, a lane's eight tokens one by one; the next pass is on its way meanwhile.  dz enters as a sum of 16-bit values,
@@ -935,12 +934,14 @@ __global__ __launch_bounds__(64 * kGradWaves, G == 1 ? 4 : 2) void k_adapter_gra
     u32 ru[G][8];
     // the tokens of the pass that begins at `s` (lane l: l % 32), the last one again past the end
     auto tokens = [&](u32 s) { const u32 k = s + (lane & 31u); return p.order[first + (k < count ? k : count - 1)]; };
-    auto fetch = [&](u32 s, u32 tok) {
+    // Columns past the last and ranks past the last are others again: their sums are not stored.
+    const u32 col0 = c0 + (lane & 15u) * 8, col = VEC && col0 >= v_cols ? v_cols - 8 : col0;
+    auto fetch = [&](u32 tok) {
 #pragma unroll
         for (u32 i = 0; i < 8; ++i) {
             const u32 k = i * 4 + (lane >> 4);
             const i64 t = static_cast<u32>(__shfl(static_cast<int>(tok), static_cast<int>(k), 64));
-            rv[i] = load8<VEC>(v_src + t * ldv, c0 + (lane & 15u) * 8, s + k < count ? v_cols : 0);
+            rv[i] = VEC ? load16(v_src + t * ldv + col) : load8<false>(v_src + t * ldv, col, v_cols);
         }
 #pragma unroll
         for (u32 q = 0; q < 8; ++q) {
@@ -948,10 +949,8 @@ __global__ __launch_bounds__(64 * kGradWaves, G == 1 ? 4 : 2) void k_adapter_gra
             const u64 t = static_cast<u32>(__shfl(static_cast<int>(tok), static_cast<int>(k), 64));
 #pragma unroll
             for (u32 g = 0; g < G; ++g) {
-                const u32 j = r0 + g * 16 + (lane & 15u);
-                ru[g][q] = 0;
-                if (s + k >= count || j >= rank) continue;
-                ru[g][q] = of_a ? __float_as_uint(p.dz[t * p.rp + j]) : load2(p.z + t * p.ldz + j);
+                const u32 j = r0 + g * 16 + (lane & 15u), there = j < rank ? j : rank - 1;
+                ru[g][q] = of_a ? __float_as_uint(p.dz[t * p.rp + there]) : load2(p.z + t * p.ldz + there);
             }
         }
     };
@@ -959,7 +958,7 @@ __global__ __launch_bounds__(64 * kGradWaves, G == 1 ? 4 : 2) void k_adapter_gra
     if (s < count) {                                           // uniform in a wavefront
         const u32 tok = tokens(s);
         u32 next = tokens(s + kGradPass);
-        fetch(s, tok);
+        fetch(tok);
         if (E::kNarrow && of_a) {
             u32 most = 0;
             const u32 groups = (rank + kDownRanks - 1) / kDownRanks;
@@ -980,6 +979,16 @@ __global__ __launch_bounds__(64 * kGradWaves, G == 1 ? 4 : 2) void k_adapter_gra
         }
         for (; s < count; s += kGradPass) {
             u32x4 fu[G][kTerms] = {};
+            if (s + 32 > count) {                              // tokens past the last: zeros on both sides
+#pragma unroll
+                for (u32 i = 0; i < 8; ++i)
+                    if (s + i * 4 + (lane >> 4) >= count) rv[i] = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+                for (u32 g = 0; g < G; ++g)
+#pragma unroll
+                    for (u32 q = 0; q < 8; ++q)
+                        if (s + (lane >> 4) * 8 + q >= count) ru[g][q] = 0;
+            }
 #pragma unroll
             for (u32 i = 0; i < 8; ++i) *reinterpret_cast<u32x4*>(own + across_at<kGradCols>(i * 4 + (lane >> 4), lane & 15u)) = rv[i];
 #pragma unroll
@@ -1000,7 +1009,7 @@ __global__ __launch_bounds__(64 * kGradWaves, G == 1 ? 4 : 2) void k_adapter_gra
                     }
                 }
             if (s + kGradPass < count) {
-                fetch(s + kGradPass, next);
+                fetch(next);
                 next = tokens(s + 2 * kGradPass);
             }
 #pragma unroll
