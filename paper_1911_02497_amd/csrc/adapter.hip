@@ -40,13 +40,15 @@ static u32 down_shares(u32 tiles) { return tiles >= 64 ? 4 : (tiles >= 16 ? 8 : 
 
 // Rows that are no multiple of eight long are copied to aligned rows beside z where more tokens than this use them.
 constexpr i64 kPackTokens = 64;
-static u64 packed_cols(i64 cols) { return static_cast<u64>(cols + 7) / 8 * 8; }
+// Sums run over whole steps of 64 of what is copied, into zeros: a last step of its own, with nothing under way before it, took 2 us.
+static i64 up_to(i64 n, i64 unit) { return (n + unit - 1) / unit * unit; }
 
 struct Plan {
     bool split = false;
     u32 rp = 0, splits = 1, steps_each = 0, bm = 64;
     u32 run = 0, n_slots = 0, tiles = 0;
     bool pack_in = false, pack_out = false;                 // rows of n_in (x, W), rows of n_out (dy)
+    i64 in_cols = 0, out_cols = 0, w_rows = 0;              // sizes of the copies, or of what is not copied
     size_t xq = 0, wq = 0, dyq = 0;
     size_t zp = 0, z32 = 0, part = 0, part_wide = 0, row_max = 0, order = 0, seg = 0, slots = 0, total = 0;
 };
@@ -71,6 +73,7 @@ static Plan make_plan(i64 T, i64 n_in, i64 n_out, u32 n_adapters, u32 max_rank, 
             u32 s = static_cast<u32>(room / tiles), most = steps / 2;
             s = s > most ? most : s;
             s = s > 16 ? 16 : (s < 1 ? 1 : s);
+            if (T > kTokenwise && tiles > 128) s = 1;       // a tile a unit, with many steps under way
             p.split = s > 1 || T <= kTokenwise;
             p.steps_each = (steps + s - 1) / s;
             p.splits = (steps + p.steps_each - 1) / p.steps_each;
@@ -90,11 +93,14 @@ static Plan make_plan(i64 T, i64 n_in, i64 n_out, u32 n_adapters, u32 max_rank, 
     }
     p.pack_in = T > kPackTokens && n_in % 8 != 0;
     p.pack_out = backward && T > kPackTokens && n_out % 8 != 0;
+    p.in_cols = p.pack_in ? up_to(n_in, backward ? 8 : 64) : n_in;
+    p.out_cols = p.pack_out ? up_to(n_out, 64) : n_out;
+    p.w_rows = p.pack_in && p.pack_out ? p.out_cols : n_out;
     if (p.pack_in) {
-        p.xq = take(static_cast<u64>(T) * packed_cols(n_in) * 2);
-        p.wq = take(static_cast<u64>(n_out) * packed_cols(n_in) * 2);
+        p.xq = take(static_cast<u64>(T) * p.in_cols * 2);
+        p.wq = take(static_cast<u64>(p.w_rows) * p.in_cols * 2);
     }
-    if (p.pack_out) p.dyq = take(static_cast<u64>(T) * packed_cols(n_out) * 2);
+    if (p.pack_out) p.dyq = take(static_cast<u64>(T) * p.out_cols * 2);
     p.total = at;
     return p;
 }
@@ -127,10 +133,14 @@ static condensa_status launch_wide(WideArgs a, int rows, hipStream_t st) {
         if (cost(192) < cost(256)) launch_wide_tile<E, 256, 192, 2, 4, 2, ALONG, kRows16>(a, st);
         else                       launch_wide_tile<E, 256, 256, 2, 4, 2, ALONG, kRows16>(a, st);
     } else if (rows != kRowsAny && tiles(128, 128) >= (rows == kRows16 ? 192 : 512)) {
-        if (rows == kRows16) launch_wide_tile<E, 128, 128, 2, 2, 2, ALONG, kRows16>(a, st);
-        else                 launch_wide_tile<E, 128, 128, 2, 2, 2, ALONG, kRows4>(a, st);
+        // One workgroup a unit, or two: what waits for memory is hidden by steps under way or by the other workgroup.
+        if (rows != kRows16)                launch_wide_tile<E, 128, 128, 2, 2, 2, ALONG, kRows4>(a, st);
+        else if (tiles(128, 128) <= 256)    launch_wide_tile<E, 128, 128, 2, 2, 4, ALONG, kRows16>(a, st);
+        else                                launch_wide_tile<E, 128, 128, 2, 2, 2, ALONG, kRows16>(a, st);
     } else {
-        if (rows == kRows16)     launch_wide_tile<E, 64, 64, 2, 2, 3, ALONG, kRows16>(a, st);
+        if (rows == kRows16 && tiles(64, 64) <= 256)      launch_wide_tile<E, 64, 64, 2, 2, 8, ALONG, kRows16>(a, st);
+        else if (rows == kRows16 && tiles(64, 64) <= 512) launch_wide_tile<E, 64, 64, 2, 2, 4, ALONG, kRows16>(a, st);
+        else if (rows == kRows16)     launch_wide_tile<E, 64, 64, 2, 2, 3, ALONG, kRows16>(a, st);
         else if (rows == kRows4) launch_wide_tile<E, 64, 64, 2, 2, 3, ALONG, kRows4>(a, st);
         else                     launch_wide_tile<E, 64, 64, 2, 2, 2, ALONG, kRowsAny>(a, st);
     }
@@ -168,14 +178,15 @@ static condensa_status launch_grads(const GradArgs& q, const WideArgs& g, u32 jo
     return CONDENSA_OK;
 }
 
-// Names the copy of `rows` rows in the call's workspace and what takes the place of the rows.
-static PackArgs pack_into(const u16** rows, i64* ld, i64 n, i64 cols, u16* copy) {
+// Names the copy of rows in the call's workspace and puts it in their place.
+static PackArgs pack_into(const u16** rows, i64* ld, i64 n, i64 cols, i64 all_rows, i64 width, u16* copy) {
     PackArgs p{};
     p.src = *rows; p.ld = *ld; p.dst = copy;
     p.rows = static_cast<u32>(n); p.cols = static_cast<u32>(cols);
-    p.blocks = static_cast<u32>((n + kPackRows - 1) / kPackRows);
+    p.all_rows = static_cast<u32>(all_rows); p.width = static_cast<u32>(width);
+    p.blocks = static_cast<u32>((all_rows + kPackRows - 1) / kPackRows);
     *rows = copy;
-    *ld = static_cast<i64>(packed_cols(cols));
+    *ld = width;
     return p;
 }
 
@@ -294,9 +305,8 @@ condensa_status condensa_adapter_project(const condensa_adapter_list* list, cons
     const bool vec_x = aligned(x_dev, 16) && x_stride % 8 == 0 && list->n_in % 8 == 0;
     WideArgs g{};
     g.x = x_dev; g.ldx = x_stride; g.w = w_dev; g.ldw = w_stride; g.y = y_dev; g.ldy = y_stride;
-    const u32 row = static_cast<u32>(p.pack_in ? packed_cols(list->n_in) : list->n_in);
-    g.x_cols = g.w_cols = row;
-    g.n_tokens = static_cast<u32>(n_tokens); g.n_out = static_cast<u32>(list->n_out); g.n_sum = static_cast<u32>(list->n_in);
+    g.x_cols = g.w_cols = static_cast<u32>(p.in_cols);
+    g.n_tokens = static_cast<u32>(n_tokens); g.n_out = static_cast<u32>(list->n_out); g.n_sum = static_cast<u32>(p.in_cols);
     g.rp = p.rp; g.ids = token_adapter_dev; g.ad = static_cast<const AdapterDesc*>(list->table_dev);
     g.n_adapters = static_cast<u32>(list->n_adapters); g.max_rank = static_cast<u32>(list->max_rank);
     g.vec_y = aligned(y_dev, 8) && y_stride % 4 == 0;
@@ -304,7 +314,7 @@ condensa_status condensa_adapter_project(const condensa_adapter_list* list, cons
     g.part = p.split ? at<float>(workspace_dev, p.part_wide) : nullptr;
     g.zp = p.split ? nullptr : at<u16>(workspace_dev, p.zp);
     DownArgs d{};
-    d.x = x_dev; d.ldx = x_stride; d.n_tokens = g.n_tokens; d.n_sum = g.n_sum; d.ids = g.ids; d.ad = g.ad; d.n_adapters = g.n_adapters; d.max_rank = g.max_rank;
+    d.x = x_dev; d.ldx = x_stride; d.n_tokens = g.n_tokens; d.n_sum = static_cast<u32>(list->n_in); d.ids = g.ids; d.ad = g.ad; d.n_adapters = g.n_adapters; d.max_rank = g.max_rank;
     d.zp = p.split ? nullptr : at<u16>(workspace_dev, p.zp); d.rp = p.rp; d.z = z_dev; d.ldz = z_stride;
     d.z32 = p.split ? at<float>(workspace_dev, p.z32) : nullptr;
     d.vec_x = vec_x;
@@ -313,10 +323,10 @@ condensa_status condensa_adapter_project(const condensa_adapter_list* list, cons
     d.by_token = p.split && n_tokens <= kTokenwise;
     u32 down = d.by_token ? g.n_tokens : d.tiles * d.shares;
     if (p.pack_in) {
-        d.pack[0] = pack_into(&g.w, &g.ldw, list->n_out, list->n_in, at<u16>(workspace_dev, p.wq));
-        d.pack[1] = pack_into(&g.x, &g.ldx, n_tokens, list->n_in, at<u16>(workspace_dev, p.xq));
+        d.pack[0] = pack_into(&g.w, &g.ldw, list->n_out, list->n_in, list->n_out, p.in_cols, at<u16>(workspace_dev, p.wq));
+        d.pack[1] = pack_into(&g.x, &g.ldx, n_tokens, list->n_in, n_tokens, p.in_cols, at<u16>(workspace_dev, p.xq));
     }
-    const int rows = std::min(rows_of(g.x, g.ldx, row, false), rows_of(g.w, g.ldw, row, false));
+    const int rows = std::min(rows_of(g.x, g.ldx, p.in_cols, false), rows_of(g.w, g.ldw, p.in_cols, false));
     if (p.pack_in || !p.split) {
         const condensa_status s = f16 ? launch_down<ElemF16, true>(d, down, st) : launch_down<ElemBF16, true>(d, down, st);
         if (s != CONDENSA_OK) return s;
@@ -381,22 +391,21 @@ condensa_status condensa_adapter_project_backward(const condensa_adapter_list* l
     if (blocks == 0) return CONDENSA_OK;
     WideArgs g{};
     g.x = dy_dev; g.ldx = dy_stride; g.w = w_dev; g.ldw = w_stride; g.y = dx_dev; g.ldy = dx_stride;
-    g.n_tokens = T; g.n_out = static_cast<u32>(list->n_in); g.n_sum = static_cast<u32>(list->n_out);
+    g.n_tokens = T; g.n_out = static_cast<u32>(list->n_in); g.n_sum = static_cast<u32>(p.w_rows);
     g.zp = d.zp; g.rp = p.rp; g.ids = token_adapter_dev; g.ad = ad; g.n_adapters = n; g.max_rank = d.max_rank;
     g.vec_y = aligned(dx_dev, 8) && dx_stride % 4 == 0;
     g.splits = p.splits; g.steps_each = p.steps_each;
     g.part = p.split ? at<float>(workspace_dev, p.part_wide) : nullptr;
-    const u32 in_cols = static_cast<u32>(p.pack_in ? packed_cols(list->n_in) : list->n_in), out_cols = static_cast<u32>(p.pack_out ? packed_cols(list->n_out) : list->n_out);
-    g.x_cols = out_cols;
-    g.w_cols = in_cols;
+    g.x_cols = static_cast<u32>(p.out_cols);
+    g.w_cols = static_cast<u32>(p.in_cols);
     const u16* x_rows = x_dev;
     i64 ldx = x_stride;
-    if (p.pack_out) d.pack[0] = pack_into(&g.x, &g.ldx, n_tokens, list->n_out, at<u16>(workspace_dev, p.dyq));
+    if (p.pack_out) d.pack[0] = pack_into(&g.x, &g.ldx, n_tokens, list->n_out, n_tokens, p.out_cols, at<u16>(workspace_dev, p.dyq));
     if (p.pack_in) {
-        d.pack[1] = pack_into(&x_rows, &ldx, n_tokens, list->n_in, at<u16>(workspace_dev, p.xq));
-        if (wide) d.pack[2] = pack_into(&g.w, &g.ldw, list->n_out, list->n_in, at<u16>(workspace_dev, p.wq));
+        d.pack[1] = pack_into(&x_rows, &ldx, n_tokens, list->n_in, n_tokens, p.in_cols, at<u16>(workspace_dev, p.xq));
+        if (wide) d.pack[2] = pack_into(&g.w, &g.ldw, list->n_out, list->n_in, p.w_rows, p.in_cols, at<u16>(workspace_dev, p.wq));
     }
-    const int rows = std::min(rows_of(g.x, g.ldx, out_cols, false), rows_of(g.w, g.ldw, in_cols, true));
+    const int rows = std::min(rows_of(g.x, g.ldx, p.out_cols, false), rows_of(g.w, g.ldw, p.in_cols, true));
     condensa_status s;
     if (pack || !split) {
         s = f16 ? launch_down<ElemF16, false>(d, blocks, st) : launch_down<ElemBF16, false>(d, blocks, st);
@@ -414,7 +423,7 @@ condensa_status condensa_adapter_project_backward(const condensa_adapter_list* l
     if (n == 0 && joins == 0) return CONDENSA_OK;
     GradArgs q{};
     q.x = x_rows; q.ldx = ldx; q.n_in = static_cast<u32>(list->n_in); q.dy = g.x; q.ldy = g.ldx; q.n_out = static_cast<u32>(list->n_out);
-    q.x_cols = in_cols; q.dy_cols = out_cols;
+    q.x_cols = g.w_cols; q.dy_cols = g.x_cols;
     q.dz = d.z32; q.rp = p.rp; q.z = z_dev; q.ldz = z_stride; q.row_max = d.row_max; q.order = d.order; q.seg = d.seg; q.slots = d.slots; q.ad = ad;
     q.max_rank = d.max_rank; q.run = p.run;
     q.tiles_in = (q.n_in + kGradCols - 1) / kGradCols;
@@ -422,7 +431,7 @@ condensa_status condensa_adapter_project_backward(const condensa_adapter_list* l
     q.part = n_tokens > p.run ? at<float>(workspace_dev, p.part) : nullptr;
     q.rank_groups = rank_groups;
     const u32 grid = (joins + 1) / 2 + static_cast<u32>(n > 0 ? grad_blocks : 0);
-    const bool vec = aligned(q.x, 16) && q.ldx % 8 == 0 && in_cols % 8 == 0 && aligned(q.dy, 16) && q.ldy % 8 == 0 && out_cols % 8 == 0;
+    const bool vec = aligned(q.x, 16) && q.ldx % 8 == 0 && p.in_cols % 8 == 0 && aligned(q.dy, 16) && q.ldy % 8 == 0 && p.out_cols % 8 == 0;
     s = f16 ? launch_grads<ElemF16>(q, g, joins, grid, groups, vec, st) : launch_grads<ElemBF16>(q, g, joins, grid, groups, vec, st);
     if (s != CONDENSA_OK) return s;
     if (n > 0 && n_tokens > p.run) {

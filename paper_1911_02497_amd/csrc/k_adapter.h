@@ -187,8 +187,8 @@ __device__ inline u32 wave_most(u32 x) {               // largest of 64 lanes' v
 // Rows at any address and of any length, copied to rows that are 16-byte aligned and end in zeros.
 struct PackArgs {
     const u16* src; i64 ld;              // [rows, cols]
-    u16* dst;                            // [rows, cols rounded up to eight]
-    u32 rows, cols, blocks;
+    u16* dst;                            // [all_rows, width]: zeros beside and below
+    u32 rows, cols, all_rows, width, blocks;
 };
 
 struct DownArgs {
@@ -281,6 +281,8 @@ __device__ inline void down_sums(const DownArgs& p, u32 t0, const u16* m, u32 ra
         const u32 j = r0 + i * 8 + (lane >> 3);
         mr[i] = ALONG ? m + static_cast<i64>(j < rank ? j : rank - 1) * p.n_sum : m;
     }
+    // negative by what is left of the matrix behind the last piece of a step, at step 0
+    const i64 last_row = 63 * static_cast<i64>(rank) + r0 + 16 * G - static_cast<i64>(p.n_sum) * rank - 1;
     // GUARD: the step may end past the sum
     auto fetch = [&](auto guard, u32 s, u32x4 (&x)[4], u32x4 (&v)[kPieces]) {
         constexpr bool GUARD = decltype(guard)::value;
@@ -292,9 +294,12 @@ __device__ inline void down_sums(const DownArgs& p, u32 t0, const u16* m, u32 ra
             if (ALONG) {
                 v[i] = GUARD ? load8<VECM>(mr[i], k, p.n_sum) : load8_inside<VECM>(mr[i] + k);
             } else {
-                const u32 at = i * 64 + lane;
+                const u32 at = i * 64 + lane, r = r0 + at % (2 * G) * 8;
                 const i64 n = static_cast<i64>(s) * 64 + at / (2 * G);
-                v[i] = load8<VECM>(m + n * rank, r0 + at % (2 * G) * 8, !GUARD || n < p.n_sum ? rank : 0);
+                // Rows follow each other without a gap, and what a lane has past the rank goes into sums that are not stored: only the
+                // end of the matrix needs care.
+                if (!VECM && last_row + s * 64 * static_cast<i64>(rank) < 0) v[i] = load16_any(m + n * rank + r);
+                else v[i] = load8<VECM>(m + n * rank, r, !GUARD || n < p.n_sum ? rank : 0);
             }
         }
     };
@@ -474,14 +479,14 @@ __device__ inline void down_token(const DownArgs& p, u32 t) {
 constexpr u32 kDownWaves = 8;
 constexpr u32 kPackRows = 4 * kDownWaves;                    // of a workgroup, four to a wavefront
 __device__ inline void pack_rows(const PackArgs& p, u32 block) {
-    const u32 lane = threadIdx.x & 63, r0 = block * kPackRows + (threadIdx.x >> 6) * 4, width = (p.cols + 7) / 8 * 8;
-    for (u32 k = lane * 8; k < width; k += 512) {
+    const u32 lane = threadIdx.x & 63, r0 = block * kPackRows + (threadIdx.x >> 6) * 4;
+    for (u32 k = lane * 8; k < p.width; k += 512) {
         u32x4 v[4];
 #pragma unroll
-        for (u32 i = 0; i < 4; ++i) v[i] = load8<false>(p.src + static_cast<i64>(r0 + i < p.rows ? r0 + i : p.rows - 1) * p.ld, k, p.cols);
+        for (u32 i = 0; i < 4; ++i) v[i] = load8<false>(p.src + static_cast<i64>(r0 + i < p.rows ? r0 + i : p.rows - 1) * p.ld, k, r0 + i < p.rows ? p.cols : 0);
 #pragma unroll
         for (u32 i = 0; i < 4; ++i)
-            if (r0 + i < p.rows) *reinterpret_cast<u32x4*>(p.dst + static_cast<u64>(r0 + i) * width + k) = v[i];
+            if (r0 + i < p.all_rows) *reinterpret_cast<u32x4*>(p.dst + static_cast<u64>(r0 + i) * p.width + k) = v[i];
     }
 }
 
