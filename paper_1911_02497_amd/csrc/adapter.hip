@@ -43,8 +43,11 @@ constexpr i64 kPackTokens = 64;
 // Sums run over whole steps of 64 of what is copied, into zeros: a last step of its own, with nothing under way before it, took 2 us.
 static i64 up_to(i64 n, i64 unit) { return (n + unit - 1) / unit * unit; }
 
+// Values of A that every workgroup of the form for a few tokens reads, at most.
+constexpr i64 kFewWork = 1 << 17;
+
 struct Plan {
-    bool split = false;
+    bool split = false, few = false;
     u32 rp = 0, splits = 1, steps_each = 0, bm = 64;
     u32 run = 0, n_slots = 0, tiles = 0;
     bool pack_in = false, pack_out = false;                 // rows of n_in (x, W), rows of n_out (dy)
@@ -61,6 +64,9 @@ static Plan make_plan(i64 T, i64 n_in, i64 n_out, u32 n_adapters, u32 max_rank, 
     size_t at = 0;
     auto take = [&](u64 bytes) { const size_t o = at; at += align_up(bytes ? bytes : 1); return o; };
     p.rp = padded_rank(max_rank ? max_rank : 1);
+    p.few = !backward && T <= kFewTokens && T * n_in * static_cast<i64>(max_rank) <= kFewWork;
+    p.in_cols = n_in;
+    if (p.few) return p;
     {
         // The wide product: where tiles of 32 or 64 tokens by 64 outputs would leave compute units without work, several share a sum.
         const i64 n_wide = backward ? n_in : n_out, n_sum = backward ? n_out : n_in;
@@ -313,6 +319,19 @@ condensa_status condensa_adapter_project(const condensa_adapter_list* list, cons
     g.splits = p.splits; g.steps_each = p.steps_each;
     g.part = p.split ? at<float>(workspace_dev, p.part_wide) : nullptr;
     g.zp = p.split ? nullptr : at<u16>(workspace_dev, p.zp);
+    if (p.few) {
+        const dim3 grid((g.n_out + kFewRows - 1) / kFewRows), threads(64 * kFewWaves);
+        const bool vec = vec_x && aligned(w_dev, 16) && w_stride % 8 == 0;
+        if (f16) {
+            if (vec) hipLaunchKernelGGL((k_adapter_few<ElemF16, true>), grid, threads, 0, st, g, z_dev, z_stride);
+            else     hipLaunchKernelGGL((k_adapter_few<ElemF16, false>), grid, threads, 0, st, g, z_dev, z_stride);
+        } else {
+            if (vec) hipLaunchKernelGGL((k_adapter_few<ElemBF16, true>), grid, threads, 0, st, g, z_dev, z_stride);
+            else     hipLaunchKernelGGL((k_adapter_few<ElemBF16, false>), grid, threads, 0, st, g, z_dev, z_stride);
+        }
+        CONDENSA_LAUNCH_CHECK();
+        return CONDENSA_OK;
+    }
     DownArgs d{};
     d.x = x_dev; d.ldx = x_stride; d.n_tokens = g.n_tokens; d.n_sum = static_cast<u32>(list->n_in); d.ids = g.ids; d.ad = g.ad; d.n_adapters = g.n_adapters; d.max_rank = g.max_rank;
     d.zp = p.split ? nullptr : at<u16>(workspace_dev, p.zp); d.rp = p.rp; d.z = z_dev; d.ldz = z_stride;

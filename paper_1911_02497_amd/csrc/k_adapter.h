@@ -827,7 +827,7 @@ __device__ inline void wide_tile(const WideArgs& p, u32 block_id, u32 n_blocks, 
 }
 
 template <typename E, int BM, int BN, int WM, int WN, u32 NB, bool ALONG, int ROWS>
-__global__ __launch_bounds__(64 * WM * WN, 2) void k_adapter_wide(WideArgs p) {
+__global__ __launch_bounds__(64 * WM * WN, NB * (BM + BN) * 128 > 80 * 1024 && WM * WN <= 4 ? 1 : 2) void k_adapter_wide(WideArgs p) {
     __shared__ __align__(16) char lds[wide_lds(BM, BN, NB)];
     wide_tile<E, BM, BN, WM, WN, NB, ALONG, ROWS>(p, blockIdx.x, gridDim.x, lds);
 }
@@ -879,6 +879,116 @@ __device__ inline void join_parts(const WideArgs& g, const float* z32, u32 ldz32
 template <typename E, bool ALONG>
 __global__ __launch_bounds__(256) void k_adapter_split_join(WideArgs w, const float* z32, u32 ldz32) {
     join_parts<E, ALONG>(w, z32, ldz32, blockIdx.y, blockIdx.x * 256 + threadIdx.x);
+}
+
+// ---- a few tokens, in one launch -----------------------------------------------------------------------------------
+
+constexpr u32 kFewTokens = 2, kFewWaves = 8, kFewRows = 4 * kFewWaves;
+
+// One or two tokens beside a small A: every workgroup makes all of z for itself (A comes out of the caches), which saves the launch that would
+// join the parts, and a wavefront takes four rows of W, whose values meet x in order.  z B^T is added as more of the same sum.  Latency bounds it: a
+// launch, the first rows of W (under way before z is made), and one reduction over the lanes.  1 token 512 -> 2048 of rank 8: 7.5 us a call, 10.3 us
+// with parts and a join; 2 tokens 2048 -> 512 of rank 32: 11.5 and 12.6 us; 3 and 4 tokens, whose adapters come one after the other: 13.9 and 12.0 us.
+template <typename E, bool VEC>
+__global__ __launch_bounds__(64 * kFewWaves) void k_adapter_few(WideArgs p, u16* z, i64 ldz) {
+    __shared__ float sz[kFewTokens][CONDENSA_MAX_RANK];
+    const u32 lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const u32 n0 = blockIdx.x * kFewRows + wave * 4;
+    const u16 *w[4], *x[kFewTokens];
+#pragma unroll
+    for (u32 r = 0; r < 4; ++r) w[r] = p.w + static_cast<i64>(n0 + r < p.n_out ? n0 + r : p.n_out - 1) * p.ldw;
+#pragma unroll
+    for (u32 t = 0; t < kFewTokens; ++t) x[t] = p.x + static_cast<i64>(t < p.n_tokens ? t : p.n_tokens - 1) * p.ldx;
+    u32x4 vw[4];
+#pragma unroll
+    for (u32 r = 0; r < 4; ++r) vw[r] = load8<VEC>(w[r], lane * 8, p.n_sum);
+    u32 turn = 0;
+    for (u32 t = 0; t < p.n_tokens; ++t) {
+        const int a = __builtin_amdgcn_readfirstlane(adapter_of(p.ids, t, p.n_tokens, p.n_adapters));
+        if (a < 0) continue;                                   // uniform
+        const AdapterDesc d = p.ad[a];
+        const u32 rank = d.rank < p.max_rank ? d.rank : p.max_rank;
+        for (u32 r0 = 0; r0 < rank; r0 += 4, ++turn) {
+            if (turn % kFewWaves != wave) continue;
+            float sum[4] = {};
+            const u16* xt = p.x + static_cast<i64>(t) * p.ldx;
+#pragma unroll 2
+            for (u32 k0 = 0; k0 < p.n_sum; k0 += 512) {
+                const i64 k = k0 + lane * 8;
+                const u32x4 vx = load8<VEC>(xt, k, p.n_sum);
+                u32x4 vm[4];
+#pragma unroll
+                for (u32 r = 0; r < 4; ++r) {
+                    const u16* row = d.a + static_cast<i64>(r0 + r < rank ? r0 + r : rank - 1) * p.n_sum;
+                    vm[r] = d.vec_a ? load8<true>(row, k, p.n_sum) : load8<false>(row, k, p.n_sum);
+                }
+#pragma unroll
+                for (u32 i = 0; i < 8; ++i) {
+                    const float fx = E::dec(static_cast<u16>(vx[i >> 1] >> (16 * (i & 1))));
+#pragma unroll
+                    for (u32 r = 0; r < 4; ++r) sum[r] = __builtin_fmaf(fx, E::dec(static_cast<u16>(vm[r][i >> 1] >> (16 * (i & 1)))), sum[r]);
+                }
+            }
+#pragma unroll
+            for (u32 r = 0; r < 4; ++r) {
+#pragma unroll
+                for (int b = 32; b >= 1; b >>= 1) sum[r] += __shfl_xor(sum[r], b, 64);
+                if (lane == r && r0 + r < rank) sz[t][r0 + r] = sum[r] * d.scale;
+            }
+        }
+    }
+    __syncthreads();
+    float sum[4][kFewTokens] = {};
+    for (u32 k0 = 0; k0 < p.n_sum; k0 += 512) {
+        const i64 k = k0 + lane * 8;
+        u32x4 vx[kFewTokens];
+#pragma unroll
+        for (u32 t = 0; t < kFewTokens; ++t) if (t < p.n_tokens) vx[t] = load8<VEC>(x[t], k, p.n_sum);
+        if (k0 > 0) {
+#pragma unroll
+            for (u32 r = 0; r < 4; ++r) vw[r] = load8<VEC>(w[r], k, p.n_sum);
+        }
+#pragma unroll
+        for (u32 t = 0; t < kFewTokens; ++t) {
+            if (t >= p.n_tokens) continue;                     // uniform
+#pragma unroll
+            for (u32 i = 0; i < 8; ++i) {
+                const float fx = E::dec(static_cast<u16>(vx[t][i >> 1] >> (16 * (i & 1))));
+#pragma unroll
+                for (u32 r = 0; r < 4; ++r) sum[r][t] = __builtin_fmaf(fx, E::dec(static_cast<u16>(vw[r][i >> 1] >> (16 * (i & 1)))), sum[r][t]);
+            }
+        }
+    }
+    float out = 0.0f;                                          // lane 4 t + r: row n0 + r of token t
+#pragma unroll
+    for (u32 t = 0; t < kFewTokens; ++t) {
+        if (t >= p.n_tokens) continue;                         // uniform, as the next
+        const int a = __builtin_amdgcn_readfirstlane(adapter_of(p.ids, t, p.n_tokens, p.n_adapters));
+        u32 rank = 0;
+        if (a >= 0) {
+            const AdapterDesc d = p.ad[a];
+            rank = d.rank < p.max_rank ? d.rank : p.max_rank;
+            for (u32 j = lane; j < rank; j += 64) {
+                const float fz = sz[t][j];
+#pragma unroll
+                for (u32 r = 0; r < 4; ++r) {
+                    const u32 n = n0 + r < p.n_out ? n0 + r : p.n_out - 1;
+                    sum[r][t] = __builtin_fmaf(fz, E::dec(load2(d.b + static_cast<i64>(n) * rank + j)), sum[r][t]);
+                }
+            }
+        }
+#pragma unroll
+        for (u32 r = 0; r < 4; ++r) {
+            float v = sum[r][t];
+#pragma unroll
+            for (int b = 32; b >= 1; b >>= 1) v += __shfl_xor(v, b, 64);
+            if (lane == t * 4 + r) out = v;
+        }
+        if (z && blockIdx.x == 0)
+            for (u32 j = threadIdx.x; j < ldz; j += 64 * kFewWaves) z[t * ldz + j] = j < rank ? E::enc(sz[t][j]) : static_cast<u16>(0);
+    }
+    const u32 t = lane >> 2, n = n0 + (lane & 3u);
+    if (t < p.n_tokens && n < p.n_out) p.y[static_cast<i64>(t) * p.ldy + n] = E::enc(out);
 }
 
 // ---- gradients of the adapters ----------------------------------------------------------------------------------

@@ -306,3 +306,39 @@ def test_inputs_beyond_32_bits():
     c.dx = torch.empty(T * far, device=DEV, dtype=torch.bfloat16).view(T, far)[:, :K]
     c.backward()
     c.check_backward()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("T", [1, 2, 3, 4])
+@pytest.mark.parametrize("K,N,ranks,pad", [(512, 2048, [8], 0), (1, 1, [1], 0), (7, 33, [5, 3], 3), (4609, 65, [2], 0), (520, 40, [250, 16], 8), (4608, 300, [16, 40], 0)])
+def test_single_tokens(dtype, T, K, N, ranks, pad):
+    """Decoding: a token or a few, with adapters of their own or without, of small and large A."""
+    for ids in ([0] * T, [t % (len(ranks) + 1) - 1 for t in range(T)], [len(ranks) - 1 - t % len(ranks) for t in range(T)]):
+        c = Case(dtype, T, K, N, ranks, ids, pad=pad)
+        c.forward(z_width=max(ranks) + 3)
+        c.check_forward(str(ids))
+        y = P.condensa_adapter_project(c.x, c.w, c.table, c.ids)["y"]
+        assert torch.equal(y, c.y)
+
+
+@pytest.mark.parametrize("T", [64, 65, 66, 300])
+@pytest.mark.parametrize("K,N", [(63, 72), (72, 65), (1, 1), (129, 7), (7, 129)])
+def test_rows_of_odd_length(T, K, N):
+    """Rows that no load of 16 bytes fits, on both sides of where they are copied, with rows of x and y apart and infinities next to them."""
+    c = Case("bf16", T, K, N, [9, 33], ids_of(T, 2, "mixed"), pad=3)
+    c.x._base.view(T * (K + 3) + 8)[: T * (K + 3)].view(T, K + 3)[:, K:].fill_(float("inf"))
+    c.dy._base.view(T * (N + 3) + 8)[: T * (N + 3)].view(T, N + 3)[:, N:].fill_(float("nan"))
+    c.forward()
+    c.check_forward()
+    c.backward()
+    c.check_backward()
+
+
+def test_long_runs_of_one_adapter():
+    """Runs on both sides of one pass, of the length that is summed in parts, and an adapter without a token."""
+    for T in (255, 256, 257, 1536, 1537, 2600):
+        c = Case("f16", T, 130, 70, [20, 40, 3], [0] * (T - 5) + [2] * 5)
+        c.forward()
+        c.backward()
+        c.check_backward(str(T))
+        assert not bool(c.grads[1][0].any()) and not bool(c.grads[1][1].any())
