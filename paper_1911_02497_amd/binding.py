@@ -790,6 +790,13 @@ def adapter_workspace(table: AdapterTable, n_tokens: int, backward: bool = False
     return torch.empty(need, dtype=torch.uint8, device=table.device)
 
 
+def _used_on(stream, *made):
+    """Memory made for a call on another stream than the current one is not handed out again before that call is done."""
+    if stream is not None:
+        for t in made:
+            t.record_stream(stream)
+
+
 def _rows(name, t, table, n_tokens, width):
     """(address, row stride) of a two-dimensional operand whose rows are contiguous."""
     shape, stride = t.shape, t.stride()
@@ -827,13 +834,16 @@ def condensa_adapter_project(x, w, table: AdapterTable, token_adapter, y=None, z
     ids = _token_ids(token_adapter, table, T)
     if y is None:
         y = table.empty(T, table.n_out)
+        _used_on(stream, y)
     py, ldy = _rows("y", y, table, T, table.n_out)
     if z is True:
         z = table.empty(T, max(table.max_rank, 1))
+        _used_on(stream, z)
     z = None if z is False else z
     pz, ldz = (None, 0) if z is None else _kept_z(z, table, T)
     if workspace is None:
         workspace = adapter_workspace(table, T)
+        _used_on(stream, workspace)
     _check(library().condensa_adapter_project(table.ref, px, ldx, T, pw, ldw, ids, py, ldy, pz, ldz, workspace.data_ptr(),
                                               workspace.numel(), _stream(stream)))
     return {"y": y, "z": z, "workspace": workspace}
@@ -850,9 +860,11 @@ def condensa_adapter_project_backward(dy, x, w, table: AdapterTable, token_adapt
     pz, ldz = _kept_z(z, table, T)
     if dx is True:
         dx = table.empty(T, table.n_in)
+        _used_on(stream, dx)
     pdx, lddx = (None, 0) if dx is False else _rows("dx", dx, table, T, table.n_in)
     if workspace is None:
         workspace = adapter_workspace(table, T, backward=True)
+        _used_on(stream, workspace)
     _check(library().condensa_adapter_project_backward(table.ref, pdy, lddy, px, ldx, T, pw, ldw, ids, pz, ldz, pdx, lddx,
                                                        workspace.data_ptr(), workspace.numel(), _stream(stream)))
     return {"dx": None if dx is False else dx, "grads": table.grads, "workspace": workspace}

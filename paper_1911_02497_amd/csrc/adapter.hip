@@ -135,7 +135,8 @@ static condensa_status launch_wide(WideArgs a, int rows, hipStream_t st) {
     // A tile of 256 rows fills a compute unit.  The one whose rounds over the 256 of them cost less is taken: 8192 x 4608 outputs are 2.25 rounds
     // of 256 x 256, which take as long as three, and three of 256 x 192.
     const auto cost = [&](u64 n) { return (tiles(256, n) + 255) / 256 * n; };
-    if (rows == kRows16 && tiles(256, 256) >= 192) {
+    // Short sums are left to smaller tiles, whose adapters' share costs less.
+    if (rows == kRows16 && tiles(256, 256) >= 192 && a.n_sum >= 1024) {
         if (cost(192) < cost(256)) launch_wide_tile<E, 256, 192, 2, 4, 2, ALONG, kRows16>(a, st);
         else                       launch_wide_tile<E, 256, 256, 2, 4, 2, ALONG, kRows16>(a, st);
     } else if (rows != kRowsAny && tiles(128, 128) >= (rows == kRows16 ? 192 : 512)) {
@@ -153,6 +154,9 @@ static condensa_status launch_wide(WideArgs a, int rows, hipStream_t st) {
     CONDENSA_LAUNCH_CHECK();
     return CONDENSA_OK;
 }
+
+// The grid of the smallest tiles has to stay below 2^32 threads.
+static bool grid_fits(i64 n_tokens, i64 n_wide) { return static_cast<u64>((n_tokens + 63) / 64) * ((n_wide + 63) / 64) < (static_cast<u64>(1) << 24); }
 
 template <typename E, bool ALONG, int BM>
 static void launch_split_tile(const DownArgs& d, const WideArgs& w, u32 down_blocks, int rows, hipStream_t st) {
@@ -301,6 +305,7 @@ condensa_status condensa_adapter_project(const condensa_adapter_list* list, cons
     const condensa_status rc = check_call(n_tokens > 0, n_tokens, token_adapter_dev, workspace_dev, workspace_bytes, p);
     if (rc != CONDENSA_OK) return rc;
     if (n_tokens == 0) return CONDENSA_OK;
+    if (!grid_fits(n_tokens, list->n_out)) return CONDENSA_ERR_SIZE;
     ByteRange r[] = {byte_range(x_dev, rows_bytes(n_tokens, x_stride, list->n_in, 2), false), byte_range(w_dev, rows_bytes(list->n_out, w_stride, list->n_in, 2), false),
                      byte_range(token_adapter_dev, static_cast<u64>(n_tokens) * 4, false), byte_range(y_dev, rows_bytes(n_tokens, y_stride, list->n_out, 2), true),
                      byte_range(z_dev, static_cast<u64>(n_tokens) * z_stride * 2, true), byte_range(workspace_dev, p.total, true),
@@ -315,7 +320,6 @@ condensa_status condensa_adapter_project(const condensa_adapter_list* list, cons
     g.n_tokens = static_cast<u32>(n_tokens); g.n_out = static_cast<u32>(list->n_out); g.n_sum = static_cast<u32>(p.in_cols);
     g.rp = p.rp; g.ids = token_adapter_dev; g.ad = static_cast<const AdapterDesc*>(list->table_dev);
     g.n_adapters = static_cast<u32>(list->n_adapters); g.max_rank = static_cast<u32>(list->max_rank);
-    g.vec_y = aligned(y_dev, 8) && y_stride % 4 == 0;
     g.splits = p.splits; g.steps_each = p.steps_each;
     g.part = p.split ? at<float>(workspace_dev, p.part_wide) : nullptr;
     g.zp = p.split ? nullptr : at<u16>(workspace_dev, p.zp);
@@ -387,7 +391,7 @@ condensa_status condensa_adapter_project_backward(const condensa_adapter_list* l
     if (ranges_conflict(r, sizeof(r) / sizeof(r[0]))) return CONDENSA_ERR_ARG;
     const u32 groups = grad_groups(static_cast<u32>(list->max_rank)), rank_groups = (static_cast<u32>(list->max_rank) + 16 * groups - 1) / (16 * groups);
     const u64 grad_blocks = static_cast<u64>(rank_groups) * p.n_slots * ((list->n_in + kGradCols - 1) / kGradCols + (list->n_out + kGradCols - 1) / kGradCols);
-    if (grad_blocks >= (static_cast<u64>(1) << 22)) return CONDENSA_ERR_SIZE;
+    if (grad_blocks >= (static_cast<u64>(1) << 22) || (dx_dev && !grid_fits(n_tokens, list->n_in))) return CONDENSA_ERR_SIZE;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const bool f16 = list->type == CONDENSA_TYPE_F16;
     const bool vec_dy = aligned(dy_dev, 16) && dy_stride % 8 == 0 && list->n_out % 8 == 0;
@@ -412,7 +416,6 @@ condensa_status condensa_adapter_project_backward(const condensa_adapter_list* l
     g.x = dy_dev; g.ldx = dy_stride; g.w = w_dev; g.ldw = w_stride; g.y = dx_dev; g.ldy = dx_stride;
     g.n_tokens = T; g.n_out = static_cast<u32>(list->n_in); g.n_sum = static_cast<u32>(p.w_rows);
     g.zp = d.zp; g.rp = p.rp; g.ids = token_adapter_dev; g.ad = ad; g.n_adapters = n; g.max_rank = d.max_rank;
-    g.vec_y = aligned(dx_dev, 8) && dx_stride % 4 == 0;
     g.splits = p.splits; g.steps_each = p.steps_each;
     g.part = p.split ? at<float>(workspace_dev, p.part_wide) : nullptr;
     g.x_cols = static_cast<u32>(p.out_cols);

@@ -57,6 +57,8 @@ __global__ __launch_bounds__(256) void k_adapter_list(AdapterDesc* __restrict__ 
 // Sixteen bytes from global memory; of the second form at any address that a 16-bit value may have.  The address space is given because
 // pointers that come out of the device list would otherwise be taken for pointers to any memory.
 typedef u32 u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef u32 u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 __device__ inline u32x4 load16(const u16* p) { return *reinterpret_cast<const __attribute__((address_space(1))) u32x4*>((u64)p); }
 __device__ inline u32x4 load16_any(const u16* p) { return *reinterpret_cast<const __attribute__((address_space(1))) u32x4_any*>((u64)p); }
 __device__ inline u16 load2(const u16* p) { return *reinterpret_cast<const __attribute__((address_space(1))) u16*>((u64)p); }
@@ -84,6 +86,20 @@ __device__ inline u32x4 load8(const u16* p, i64 k, i64 n) {
                 if (k + i < n) v[i >> 1] |= static_cast<u32>(load2(p + k + i)) << (16 * (i & 1));
         }
     }
+    return v;
+}
+// The same at any address without a branch that waits: what follows a row, up to the end of the matrix, is loaded and masked.  `left`: values
+// from p[k] to that end.
+__device__ inline u32x4 load8_masked(const u16* p, i64 k, i64 n, i64 left) {
+    const i64 rest = n - k;
+    const int there = rest >= 8 ? 8 : (rest <= 0 ? 0 : static_cast<int>(rest));
+    u32x4 v = {0u, 0u, 0u, 0u};
+    if (there > 0) {
+        if (left >= 8) v = load16_any(p + k);
+        else v = load8<false>(p, k, n);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] &= there >= 2 * i + 2 ? ~0u : (there == 2 * i + 1 ? 0xFFFFu : 0u);
     return v;
 }
 template <bool VEC>
@@ -483,7 +499,10 @@ __device__ inline void pack_rows(const PackArgs& p, u32 block) {
     for (u32 k = lane * 8; k < p.width; k += 512) {
         u32x4 v[4];
 #pragma unroll
-        for (u32 i = 0; i < 4; ++i) v[i] = load8<false>(p.src + static_cast<i64>(r0 + i < p.rows ? r0 + i : p.rows - 1) * p.ld, k, r0 + i < p.rows ? p.cols : 0);
+        for (u32 i = 0; i < 4; ++i) {
+            const u32 r = r0 + i < p.rows ? r0 + i : p.rows - 1;
+            v[i] = load8_masked(p.src + static_cast<i64>(r) * p.ld, k, r0 + i < p.rows ? p.cols : 0, static_cast<i64>(p.rows - 1 - r) * p.ld + p.cols - k);
+        }
 #pragma unroll
         for (u32 i = 0; i < 4; ++i)
             if (r0 + i < p.all_rows) *reinterpret_cast<u32x4*>(p.dst + static_cast<u64>(r0 + i) * p.width + k) = v[i];
@@ -522,7 +541,6 @@ struct WideArgs {
     const int* ids;
     const AdapterDesc* ad;
     u32 n_adapters, max_rank;
-    u32 vec_y;                           // 8-byte aligned groups of four outputs
     u32 splits, steps_each;              // steps of 64 values that a split sums
     float* part;                         // [splits][n_tokens][n_out], or NULL: y is written
 };
@@ -659,18 +677,18 @@ __device__ inline void wide_tile(const WideArgs& p, u32 block_id, u32 n_blocks, 
 #pragma unroll
             for (u32 i = 0; i < kXPieces; ++i) {
                 const u32 at = i * kThreads + tid, t = t0 + (at >> 3) < p.n_tokens ? t0 + (at >> 3) : p.n_tokens - 1;
-                rx[set][i] = load8<false>(p.x + static_cast<i64>(t) * p.ldx, k0 + (at & 7u) * 8, sum_end);
+                rx[set][i] = load8_masked(p.x + static_cast<i64>(t) * p.ldx, k0 + (at & 7u) * 8, sum_end, static_cast<i64>(p.n_tokens - 1 - t) * p.ldx + p.n_sum - (k0 + (at & 7u) * 8));
             }
 #pragma unroll
             for (u32 i = 0; i < kWPieces; ++i) {
                 const u32 at = i * kThreads + tid;
                 if (ALONG) {
                     const u32 n = n0 + (at >> 3) < p.n_out ? n0 + (at >> 3) : p.n_out - 1;
-                    rw[set][i] = load8<false>(p.w + static_cast<i64>(n) * p.ldw, k0 + (at & 7u) * 8, sum_end);
+                    rw[set][i] = load8_masked(p.w + static_cast<i64>(n) * p.ldw, k0 + (at & 7u) * 8, sum_end, static_cast<i64>(p.n_out - 1 - n) * p.ldw + p.n_sum - (k0 + (at & 7u) * 8));
                 } else {
                     constexpr u32 kRow = BN / 8;
                     const i64 k = k0 + at / kRow;
-                    rw[set][i] = load8<false>(p.w + k * p.ldw, n0 + (at % kRow) * 8, k < sum_end ? p.n_out : 0);
+                    rw[set][i] = load8_masked(p.w + k * p.ldw, n0 + (at % kRow) * 8, k < sum_end ? p.n_out : 0, (p.n_sum - 1 - k) * p.ldw + p.n_out - (n0 + (at % kRow) * 8));
                 }
             }
         };
@@ -746,22 +764,42 @@ __device__ inline void wide_tile(const WideArgs& p, u32 block_id, u32 n_blocks, 
         const u32 subs = k_end - k0 > 32 ? 2 : 1;
         const u16* x = rest ? p.x : p.zp;
         const i64 ldx = rest ? p.ldx : static_cast<i64>(p.rp), x_end = rest ? p.x_cols : p.rp;
-        for (u32 at = me; at < BM * 8; at += kThreads) {
-            const u32 row = at >> 3, piece = at & 7u, t = t0 + row < p.n_tokens ? t0 + row : p.n_tokens - 1;
-            const u16* src = x + static_cast<i64>(t) * ldx;
-            if (piece < subs * 4) *reinterpret_cast<u32x4*>(tiles + along_at(row, piece)) = ROWS == kRows16 || !rest ? load8<true>(src, k0 + piece * 8, x_end) : load8<false>(src, k0 + piece * 8, x_end);
+        // Loads before stores, four at once; tiles of 256 rows, which have no registers for that, one by one.
+        constexpr u32 kOnce = BM * BN <= 128 * 128 ? (kXPieces < kWPieces ? kXPieces : kWPieces) : 1;
+#pragma unroll 1
+        for (u32 at0 = me; at0 < BM * 8; at0 += kOnce * kThreads) {
+            if (kOnce == 1 && (at0 & 7u) >= subs * 4) continue;    // the second half is not read
+            u32x4 v[kOnce];
+#pragma unroll
+            for (u32 i = 0; i < kOnce; ++i) {
+                const u32 at = at0 + i * kThreads, row = at >> 3, t = t0 + row < p.n_tokens ? t0 + row : p.n_tokens - 1;
+                const u16* src = x + static_cast<i64>(t) * ldx;
+                const i64 k = k0 + (at & 7u) * 8;
+                v[i] = ROWS == kRows16 || !rest ? load8<true>(src, k, x_end) : load8<false>(src, k, x_end);
+            }
+#pragma unroll
+            for (u32 i = 0; i < kOnce; ++i) *reinterpret_cast<u32x4*>(tiles + along_at((at0 + i * kThreads) >> 3, at0 & 7u)) = v[i];
         }
         const u16* w = rest ? p.w : m;
         const i64 ldw = rest ? p.ldw : (ALONG ? static_cast<i64>(rank) : static_cast<i64>(p.n_out));
+        const i64 cols = rest ? p.w_cols : (ALONG ? rank : p.n_out), rows = ALONG ? p.n_out : k_end;
         const bool vec_w = rest ? ROWS == kRows16 : vec_m;
-        for (u32 at = me; at < BN * 8; at += kThreads) {
-            const u32 row = ALONG ? at >> 3 : at / (BN / 8), piece = ALONG ? at & 7u : at % (BN / 8);
-            if ((ALONG ? piece >> 2 : row >> 5) >= subs) continue;
-            const u16* src = ALONG ? w + static_cast<i64>(n0 + row < p.n_out ? n0 + row : p.n_out - 1) * ldw : w + (k0 + row) * ldw;
-            const i64 from = ALONG ? k0 + piece * 8 : n0 + piece * 8, cols = rest ? p.w_cols : (ALONG ? rank : p.n_out);
-            const i64 end_at = ALONG || k0 + row < k_end ? cols : 0;
-            const u32x4 v = vec_w ? load8<true>(src, from, end_at) : load8<false>(src, from, end_at);
-            *reinterpret_cast<u32x4*>(tiles + BM * 64 + (ALONG ? along_at(row, piece) : across_at<BN>(row, piece))) = v;
+#pragma unroll 1
+        for (u32 at0 = me; at0 < BN * 8; at0 += kOnce * kThreads) {
+            if (kOnce == 1 && (ALONG ? (at0 & 7u) >> 2 : at0 / (BN / 8) >> 5) >= subs) continue;
+            u32x4 v[kOnce];
+#pragma unroll
+            for (u32 i = 0; i < kOnce; ++i) {
+                const u32 at = at0 + i * kThreads, row = ALONG ? at >> 3 : at / (BN / 8), piece = ALONG ? at & 7u : at % (BN / 8);
+                const i64 want = ALONG ? n0 + row : k0 + row, r = want < rows ? want : rows - 1, from = ALONG ? k0 + piece * 8 : n0 + piece * 8;
+                const i64 end_at = ALONG || want < rows ? cols : 0;
+                v[i] = vec_w ? load8<true>(w + r * ldw, from, end_at) : load8_masked(w + r * ldw, from, end_at, (rows - 1 - r) * ldw + cols - from);
+            }
+#pragma unroll
+            for (u32 i = 0; i < kOnce; ++i) {
+                const u32 at = at0 + i * kThreads;
+                *reinterpret_cast<u32x4*>(tiles + BM * 64 + (ALONG ? along_at(at >> 3, at & 7u) : across_at<BN>(at / (BN / 8), at % (BN / 8)))) = v[i];
+            }
         }
         __syncthreads();
         for (u32 sub = 0; sub < subs; ++sub) {
@@ -793,7 +831,7 @@ __device__ inline void wide_tile(const WideArgs& p, u32 block_id, u32 n_blocks, 
 #pragma unroll
             for (u32 i = 0; i < FN; ++i) {
                 const u32 n = n0 + wn * TN + i * 16 + (lane >> 4) * 4;
-                if ((p.n_out & 3u) == 0 && n + 4 <= p.n_out) *reinterpret_cast<f32x4*>(out + n) = acc[i][j];
+                if (n + 4 <= p.n_out) *reinterpret_cast<f32x4_any*>(out + n) = acc[i][j];
                 else
 #pragma unroll
                     for (u32 k = 0; k < 4; ++k) if (n + k < p.n_out) out[n + k] = acc[i][j][k];
@@ -813,11 +851,11 @@ __device__ inline void wide_tile(const WideArgs& p, u32 block_id, u32 n_blocks, 
             u16 h[4];
 #pragma unroll
             for (u32 k = 0; k < 4; ++k) h[k] = E::enc(acc[i][j][k]);
-            if (p.vec_y && n + 4 <= p.n_out) {
+            if (n + 4 <= p.n_out) {                                // at any address: one by one they took ten times as long
                 u32x2 v;
                 v.x = static_cast<u32>(h[0]) | static_cast<u32>(h[1]) << 16;
                 v.y = static_cast<u32>(h[2]) | static_cast<u32>(h[3]) << 16;
-                *reinterpret_cast<u32x2*>(out + n) = v;
+                *reinterpret_cast<u32x2_any*>(out + n) = v;
             } else {
 #pragma unroll
                 for (u32 k = 0; k < 4; ++k) if (n + k < p.n_out) out[n + k] = h[k];
