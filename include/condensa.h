@@ -521,8 +521,9 @@ condensa_status condensa_adapter_list_init(const condensa_adapter* adapters, int
 size_t condensa_adapter_workspace_bytes(const condensa_adapter_list* list, int64_t n_tokens, int backward);
 
 /*
- * Forward pass.  n_tokens may be 0 (up to 2^24).  Strides count elements; the rows of x, W and y may be any distance apart and at any address
- * (16-byte aligned rows of a multiple of eight values are fastest).  token_adapter_dev: device int32 [n_tokens], an index into
+ * Forward pass.  n_tokens may be 0 (up to 2^24, and fewer than 2^24 tiles of 64 tokens by 64 outputs: CONDENSA_ERR_SIZE).  Strides
+ * count elements; the rows of x, W and y may be any distance apart and at any address (16-byte aligned rows are fastest; rows that
+ * are no multiple of eight values long are copied within the call, into the workspace, from 65 tokens on).  token_adapter_dev: device int32 [n_tokens], an index into
  * the list; any other value means no adapter.  z_dev: NULL, or [n_tokens, z_stride] with z_stride >= the largest rank: receives z, zeros after
  * the adapter's rank, which the backward pass wants.  No buffer may overlap y or z.
  */

@@ -384,14 +384,14 @@ condensa_status condensa_adapter_project_backward(const condensa_adapter_list* l
     const Plan p = make_plan(n_tokens, list->n_in, list->n_out, static_cast<u32>(list->n_adapters), static_cast<u32>(list->max_rank), true);
     const condensa_status rc = check_call(n_tokens > 0 || list->n_adapters > 0, n_tokens, token_adapter_dev, workspace_dev, workspace_bytes, p);
     if (rc != CONDENSA_OK) return rc;
+    const u32 groups = grad_groups(static_cast<u32>(list->max_rank)), rank_groups = (static_cast<u32>(list->max_rank) + 16 * groups - 1) / (16 * groups);
+    const u64 grad_blocks = static_cast<u64>(rank_groups) * p.n_slots * ((list->n_in + kGradCols - 1) / kGradCols + (list->n_out + kGradCols - 1) / kGradCols);
+    if (grad_blocks >= (static_cast<u64>(1) << 22) || (dx_dev && !grid_fits(n_tokens, list->n_in))) return CONDENSA_ERR_SIZE;
     ByteRange r[] = {byte_range(dy_dev, rows_bytes(n_tokens, dy_stride, list->n_out, 2), false), byte_range(x_dev, rows_bytes(n_tokens, x_stride, list->n_in, 2), false),
                      byte_range(w_dev, rows_bytes(list->n_out, w_stride, list->n_in, 2), false), byte_range(token_adapter_dev, static_cast<u64>(n_tokens) * 4, false),
                      byte_range(z_dev, static_cast<u64>(n_tokens) * z_stride * 2, false), byte_range(dx_dev, rows_bytes(n_tokens, dx_stride, list->n_in, 2), true),
                      byte_range(workspace_dev, p.total, true), byte_range(list->table_dev, condensa_adapter_list_bytes(list->n_adapters), false)};
     if (ranges_conflict(r, sizeof(r) / sizeof(r[0]))) return CONDENSA_ERR_ARG;
-    const u32 groups = grad_groups(static_cast<u32>(list->max_rank)), rank_groups = (static_cast<u32>(list->max_rank) + 16 * groups - 1) / (16 * groups);
-    const u64 grad_blocks = static_cast<u64>(rank_groups) * p.n_slots * ((list->n_in + kGradCols - 1) / kGradCols + (list->n_out + kGradCols - 1) / kGradCols);
-    if (grad_blocks >= (static_cast<u64>(1) << 22) || (dx_dev && !grid_fits(n_tokens, list->n_in))) return CONDENSA_ERR_SIZE;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const bool f16 = list->type == CONDENSA_TYPE_F16;
     const bool vec_dy = aligned(dy_dev, 16) && dy_stride % 8 == 0 && list->n_out % 8 == 0;

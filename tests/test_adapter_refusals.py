@@ -142,3 +142,9 @@ def test_binding_checks():
         P.adapter_table([(a.float(), b.float(), 1.0)])
     with pytest.raises(TypeError):
         P.adapter_table([], n_in=64, n_out=64)
+
+
+def test_grids_beyond_the_largest_launch():
+    big = the_list(n_in=1 << 20, n_out=1 << 20)
+    assert project(big, T=1 << 24, ldx=1 << 20, ldw=1 << 20, ldy=1 << 20, size=1 << 62) == SIZE
+    assert backward(big, T=1 << 24, lddy=1 << 20, ldx=1 << 20, ldw=1 << 20, lddx=1 << 20, size=1 << 62) == SIZE
