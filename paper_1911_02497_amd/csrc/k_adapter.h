@@ -107,7 +107,6 @@ __device__ inline u32x4 load8_inside(const u16* p) { return VEC ? load16(p) : lo
 
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef __attribute__((address_space(3))) void lds_void;
-typedef const __attribute__((address_space(1))) void global_void;
 
 // Tiles with the summed axis along their rows: [rows][64], 16-byte pieces of a row at piece ^ (row & 7), so that eight rows of a
 // fragment lie in different banks although rows are 128 bytes apart.
@@ -140,8 +139,6 @@ __device__ inline u32x4 across_frag(const u16* tile, u32 col0, u32 sub) {
     return v;
 }
 
-__device__ __align__(256) const u16 g_zeros[64] = {};        // where pieces outside a matrix are read from
-
 // Every wavefront's loads into LDS but the last N and all its LDS reads are done, then the workgroup meets.  (A barrier alone orders LDS
 // accesses, but loads into LDS count as loads from memory, and waiting for all of them would wait for tiles that are wanted later.)
 // Nothing is moved across it.
@@ -158,7 +155,8 @@ __device__ inline void meet_loads() {
 
 // Bytes a lane from `base` (the same in all lanes) + `offset` straight into LDS, at byte `lds` + BYTES * lane.  Written out because the
 // compiler, which cannot tell the tiles of one array apart, would wait for every such load before any LDS read; here meet_loads says
-// what has come.  There is no output register that could be reused while the load is under way.
+// what has come.  There is no output register that could be reused while the load is under way, and
+// nothing else in these kernels keeps a value in m0.
 template <u32 BYTES>
 __device__ inline void load_lds(u32 offset, const void* any_base, u32 any_lds) {
     const u64 a = reinterpret_cast<u64>(any_base);
