@@ -491,9 +491,10 @@ condensa_status condensa_lc_adamw_step(const condensa_adamw_list* list, const co
  *   forward:   z[t] = s_a (x[t] A_a^T);   y[t] = x[t] W^T + z[t] B_a^T
  *   backward:  dz[t] = s_a (dy[t] B_a);   dx[t] = dy[t] W + dz[t] A_a;
  *              grad_A_a = sum of dz[t]^T x[t],  grad_B_a = sum of dy[t]^T z[t]  over the tokens of a
- * All sums are binary32 in an order that depends on sizes and on the tokens' adapters alone, so equal calls give equal bits.  z and dz are
- * rounded to the 16-bit type where they enter a product that is rounded to it anyway (y, dx); the gradients' product with dz keeps 16
- * bits of it and more.  y, z and dx are rounded to nearest, ties to even; values outside the range of binary16 become infinite.
+ * All sums are binary32 in an order that depends on sizes and on the tokens' adapters alone, so equal calls give equal bits.  z and dz
+ * enter y, dx and the gradients with 16 bits or more of their own and over the whole range of binary32, whatever the number of tokens: only
+ * the z that is returned is rounded to the 16-bit type.  y, z and dx are rounded to nearest, ties to even; values outside the range of
+ * binary16 become infinite.
  *
  * A list names the adapters that the calls may use, laid out on the device once; it has to stay as it is while it is in use, as
  * have the adapters' buffers (their values may change between calls).  list_dev: condensa_adapter_list_bytes(n) bytes, 256-byte

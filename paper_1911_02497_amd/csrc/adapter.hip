@@ -85,10 +85,10 @@ static Plan make_plan(i64 T, i64 n_in, i64 n_out, u32 n_adapters, u32 max_rank, 
             p.splits = (steps + p.steps_each - 1) / p.steps_each;
             if (p.split) p.part_wide = take(static_cast<u64>(p.splits) * T * n_wide * 4);
         }
-        if (!p.split) p.zp = take(static_cast<u64>(T) * p.rp * 2);
+        if (!p.split) p.zp = take(static_cast<u64>(T) * p.rp * 4);
         if (p.split || backward) p.z32 = take(static_cast<u64>(T) * p.rp * 4);
+        if (!p.split || backward) p.row_max = take(static_cast<u64>(T) * (p.rp / kDownRanks) * 4);
         if (backward) {
-            p.row_max = take(static_cast<u64>(T) * (p.rp / kDownRanks) * 4);
             p.run = run_tokens(T, n_in, n_out);
             p.n_slots = static_cast<u32>(T / p.run) + n_adapters;
             p.order = take(static_cast<u64>(T) * 4);
@@ -323,6 +323,7 @@ condensa_status condensa_adapter_project(const condensa_adapter_list* list, cons
     g.splits = p.splits; g.steps_each = p.steps_each;
     g.part = p.split ? at<float>(workspace_dev, p.part_wide) : nullptr;
     g.zp = p.split ? nullptr : at<u16>(workspace_dev, p.zp);
+    g.row_max = f16 && !p.split ? at<u32>(workspace_dev, p.row_max) : nullptr;
     if (p.few) {
         const dim3 grid((g.n_out + kFewRows - 1) / kFewRows), threads(64 * kFewWaves);
         const bool vec = vec_x && aligned(w_dev, 16) && w_stride % 8 == 0;
@@ -340,6 +341,7 @@ condensa_status condensa_adapter_project(const condensa_adapter_list* list, cons
     d.x = x_dev; d.ldx = x_stride; d.n_tokens = g.n_tokens; d.n_sum = static_cast<u32>(list->n_in); d.ids = g.ids; d.ad = g.ad; d.n_adapters = g.n_adapters; d.max_rank = g.max_rank;
     d.zp = p.split ? nullptr : at<u16>(workspace_dev, p.zp); d.rp = p.rp; d.z = z_dev; d.ldz = z_stride;
     d.z32 = p.split ? at<float>(workspace_dev, p.z32) : nullptr;
+    d.row_max = f16 && !p.split ? at<u32>(workspace_dev, p.row_max) : nullptr;
     d.vec_x = vec_x;
     d.tiles = (g.n_tokens + kDownTokens - 1) / kDownTokens;
     d.shares = down_shares(d.tiles);
@@ -401,7 +403,7 @@ condensa_status condensa_adapter_project_backward(const condensa_adapter_list* l
     d.x = dy_dev; d.ldx = dy_stride; d.n_tokens = T; d.n_sum = static_cast<u32>(list->n_out); d.ids = token_adapter_dev; d.ad = ad; d.n_adapters = n;
     d.max_rank = static_cast<u32>(list->max_rank);
     const bool wide = dx_dev && T > 0, split = wide && p.split;
-    d.zp = p.split || !wide ? nullptr : at<u16>(workspace_dev, p.zp); d.rp = p.rp; d.z32 = at<float>(workspace_dev, p.z32); d.row_max = at<u32>(workspace_dev, p.row_max);
+    d.zp = p.split || !wide ? nullptr : at<u16>(workspace_dev, p.zp); d.rp = p.rp; d.z32 = at<float>(workspace_dev, p.z32); d.row_max = f16 ? at<u32>(workspace_dev, p.row_max) : nullptr;
     d.vec_x = vec_dy;
     d.tiles = (T + kDownTokens - 1) / kDownTokens;
     d.shares = down_shares(d.tiles);
@@ -415,7 +417,7 @@ condensa_status condensa_adapter_project_backward(const condensa_adapter_list* l
     WideArgs g{};
     g.x = dy_dev; g.ldx = dy_stride; g.w = w_dev; g.ldw = w_stride; g.y = dx_dev; g.ldy = dx_stride;
     g.n_tokens = T; g.n_out = static_cast<u32>(list->n_in); g.n_sum = static_cast<u32>(p.w_rows);
-    g.zp = d.zp; g.rp = p.rp; g.ids = token_adapter_dev; g.ad = ad; g.n_adapters = n; g.max_rank = d.max_rank;
+    g.zp = d.zp; g.row_max = d.row_max; g.rp = p.rp; g.ids = token_adapter_dev; g.ad = ad; g.n_adapters = n; g.max_rank = d.max_rank;
     g.splits = p.splits; g.steps_each = p.steps_each;
     g.part = p.split ? at<float>(workspace_dev, p.part_wide) : nullptr;
     g.x_cols = static_cast<u32>(p.out_cols);

@@ -24,6 +24,10 @@ struct ElemF16 {
     static __device__ inline u16 enc(float x) { return f32_to_f16_rne(x); }
     static __device__ inline float dec(u16 h) { return f16_bits_to_f32(h); }
     static constexpr bool kNarrow = true;      // exponents of 5 bits: what is split into two values is scaled first
+    static __device__ inline u16 cut(float x) {
+        const auto h = __builtin_amdgcn_cvt_pkrtz(x, 0.0f);
+        return __builtin_bit_cast(u16, h[0]);
+    }
 };
 struct ElemBF16 {
     static __device__ inline f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
@@ -32,6 +36,7 @@ struct ElemBF16 {
     static __device__ inline u16 enc(float x) { return f32_to_bf16_rne(x); }
     static __device__ inline float dec(u16 h) { return bf16_bits_to_f32(h); }
     static constexpr bool kNarrow = false;
+    static __device__ inline u16 cut(float x) { return static_cast<u16>(__float_as_uint(x) >> 16); }
 };
 
 struct AdapterDesc {
@@ -196,6 +201,28 @@ __device__ inline u32 wave_most(u32 x) {               // largest of 64 lanes' v
     return x;
 }
 
+// Power of two, as its exponent, that brings the largest of some finite magnitudes (its bits) to 2^14 .. 2^15, the top of float16's range.
+__device__ inline int scale_exponent(u32 most) {
+    const int e = 14 - (static_cast<int>(most >> 23) - 127);
+    return e > 120 ? 120 : e;
+}
+__device__ inline float power_of_two(int e) { return __uint_as_float(static_cast<u32>(127 + e) << 23); }
+
+// Two 16-bit values of one sign whose sum is x but for u^2 of it (u: half a step of the type at 1): x cut off and what was cut, rounded.  An infinity that
+// both meet in a product stays one of that sign, so the second is the type's smallest value where nothing was cut.
+template <typename E>
+__device__ inline void two_values(float x, u16* hi, u16* lo) {
+    const u32 u = __float_as_uint(x), sign = u >> 16 & 0x8000u;
+    if ((u & 0x7FFFFFFFu) >= 0x7F800000u) {                  // infinities and NaN
+        *hi = E::enc(x);
+        *lo = 0;
+        return;
+    }
+    *hi = E::cut(x);
+    const u16 rest = E::enc(x - E::dec(*hi));
+    *lo = (rest & 0x7FFFu) != 0 || (u & 0x7FFFFFFFu) == 0 ? rest : static_cast<u16>(sign | 1u);
+}
+
 // ---- down: the product with the narrow matrix -------------------------------------------------------------------
 
 // Rows at any address and of any length, copied to rows that are 16-byte aligned and end in zeros.
@@ -211,10 +238,11 @@ struct DownArgs {
     const int* ids;
     const AdapterDesc* ad;
     u32 n_adapters, max_rank;
-    u16* zp; u32 rp;                     // [n_tokens, rp] 16-bit, zeros past the rank; rp = max_rank rounded up to 32
+    u16* zp; u32 rp;                     // [n_tokens, rp / 32][2][32]: z as sums of two 16-bit values, zeros past the rank; rp = max_rank rounded up to 32
     u16* z; i64 ldz;                     // the caller's copy, or NULL; all ldz columns are written
     float* z32;                          // [n_tokens, rp] before rounding, or NULL
-    u32* row_max;                        // [n_tokens, rp / 32] largest finite magnitude (bits) in 32 values of a token's z, or NULL
+    u32* row_max;                        // [n_tokens, rp / 32] largest finite magnitude (bits) in 32 values of a token's z, or NULL;
+                                         // those of zp are scaled by scale_exponent of it (float16)
     u32 vec_x;                           // 16-byte aligned rows of x
     u32 tiles, shares;                   // of 32 tokens; workgroups that share the adapters of a tile
     u32 sorters;                         // workgroups that sort the tokens by adapter (backward)
@@ -375,18 +403,23 @@ __device__ inline void down_tile(const DownArgs& p, u32 block, char* lds) {
     const u32 share = block / p.tiles, t0 = block % p.tiles * kDownTokens;
     const int my_id = lane < kDownTokens ? adapter_of(p.ids, t0 + lane, p.n_tokens, p.n_adapters) : -1;
     const u32 width = p.z && p.ldz > p.rp ? static_cast<u32>(p.ldz) : p.rp;
-    auto put = [&](u64 t, u32 j, float v) {
-        const u16 h = E::enc(v);
+    auto put = [&](u64 t, u32 j, float v, float up) {
         if (j < p.rp) {
-            if (p.zp) p.zp[t * p.rp + j] = h;
+            if (p.zp) {
+                u16 hi, lo;
+                two_values<E>(E::kNarrow ? v * up : v, &hi, &lo);
+                u16* to = p.zp + (t * p.rp + j / kDownRanks * kDownRanks) * 2 + j % kDownRanks;
+                to[0] = hi;
+                to[kDownRanks] = lo;
+            }
             if (p.z32) p.z32[t * p.rp + j] = v;
         }
-        if (p.z && j < p.ldz) p.z[t * p.ldz + j] = h;
+        if (p.z && j < p.ldz) p.z[t * p.ldz + j] = E::enc(v);
     };
     if (share == 0)                                          // tokens without an adapter
         for (u32 i = wave; i < kDownTokens; i += WAVES) {
             if (t0 + i >= p.n_tokens || __shfl(my_id, static_cast<int>(i), 64) >= 0) continue;
-            for (u32 j = lane; j < width; j += 64) put(t0 + i, j, 0.0f);
+            for (u32 j = lane; j < width; j += 64) put(t0 + i, j, 0.0f, 1.0f);
         }
     float (*sums)[kDownTokens][kDownRanks] = reinterpret_cast<float (*)[kDownTokens][kDownRanks]>(lds);
     u16* own = reinterpret_cast<u16*>(lds) + wave * 4096;
@@ -418,25 +451,30 @@ __device__ inline void down_tile(const DownArgs& p, u32 block, char* lds) {
                 }
             __syncthreads();
             const u32 end = r0 + kDownRanks >= rank ? width : r0 + kDownRanks;
-            for (u32 i = wave; i < kDownTokens; i += WAVES) {
-                if (__shfl(my_id, static_cast<int>(i), 64) != a) continue;       // uniform
+            const u32 lane32 = lane & 31u;
+            for (u32 i = wave * 2 + (lane >> 5); i < kDownTokens; i += WAVES * 2) {          // a token for each half of a wavefront
+                if (__shfl(my_id, static_cast<int>(i), 64) != a) continue;
                 const u64 t = t0 + i;
-                u32 most = 0;
-                for (u32 j = r0 + lane; j < end; j += 64) {
-                    float v = 0.0f;
-                    if (j < rank && j < r0 + kDownRanks) {
+                const u32 j = r0 + lane32;
+                float v = 0.0f, up = 1.0f;
+                if (j < rank) {
 #pragma unroll
-                        for (u32 w = 0; w < WAVES; ++w) v += sums[w][i][j - r0];
-                        v *= d.scale;
-                    }
-                    put(t, j, v);
-                    const u32 u = __float_as_uint(v) & 0x7FFFFFFFu;
-                    if (u < 0x7F800000u) most = most > u ? most : u;
+                    for (u32 w = 0; w < WAVES; ++w) v += sums[w][i][lane32];
+                    v *= d.scale;
                 }
                 if (p.row_max) {
-                    most = wave_most(most);
-                    if (lane == 0) p.row_max[t * (p.rp / kDownRanks) + r0 / kDownRanks] = most;
+                    const u32 u = __float_as_uint(v) & 0x7FFFFFFFu;
+                    u32 most = u < 0x7F800000u ? u : 0u;
+#pragma unroll
+                    for (int k = 16; k >= 1; k >>= 1) {
+                        const u32 y = static_cast<u32>(__shfl_xor(static_cast<int>(most), k, 64));
+                        most = most > y ? most : y;
+                    }
+                    if (lane32 == 0) p.row_max[t * (p.rp / kDownRanks) + r0 / kDownRanks] = most;
+                    up = power_of_two(scale_exponent(most));
                 }
+                put(t, j, v, up);
+                for (u32 k = r0 + kDownRanks + lane32; k < end; k += 32) put(t, k, 0.0f, 1.0f);
             }
             __syncthreads();                                 // before tiles take the place of the sums
         }
@@ -535,7 +573,8 @@ struct WideArgs {
     u16* y; i64 ldy;                     // [n_tokens, n_out]
     u32 n_tokens, n_out, n_sum;
     u32 x_cols, w_cols;                  // values of a row of x and of W, with the zeros at the end of a copy
-    const u16* zp; u32 rp;
+    const u16* zp; u32 rp;               // of DownArgs
+    const u32* row_max;                  // of DownArgs (float16)
     const int* ids;
     const AdapterDesc* ad;
     u32 n_adapters, max_rank;
@@ -556,7 +595,7 @@ __device__ inline u32 die_order(u32 i, u32 n) {
 // With `part` a workgroup sums a part of the steps and stores it in binary32; the adapters' share is then added with the parts.
 // Matrix instructions bound large products (8192 tokens, 4608 -> 4096: 288 us, 1.08 PFLOP/s), reading W those of few tokens, latency those between
 // (1333 tokens, 650 -> 2600: 25.7 us).
-constexpr u32 wide_lds(u32 bm, u32 bn, u32 nb) { return nb * (bm + bn) * 128 + bm * 4; }
+constexpr u32 wide_lds(u32 bm, u32 bn, u32 nb) { return nb * (bm + bn) * 128 + bm * 12; }
 template <typename E, int BM, int BN, int WM, int WN, u32 NB, bool ALONG, int ROWS>
 __device__ inline void wide_tile(const WideArgs& p, u32 block_id, u32 n_blocks, char* lds) {
     constexpr u32 kThreads = 64 * WM * WN;
@@ -566,6 +605,7 @@ __device__ inline void wide_tile(const WideArgs& p, u32 block_id, u32 n_blocks, 
     constexpr u32 kTile = (BM + BN) * 64, kEarly = FN < FM ? FN : FN / 2, kEach = FN / kEarly;
     u16* tiles = reinterpret_cast<u16*>(lds);
     int* s_ids = reinterpret_cast<int*>(lds + NB * kTile * 2);
+    float* s_down = reinterpret_cast<float*>(s_ids + BM);          // what undoes the scale of a token's z, for two groups of 32 ranks (float16)
     const u32 tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const u32 wm = wave / WN, wn = wave % WN;
     const u32 tiles_m = (p.n_tokens + BM - 1) / BM, tiles_n = (p.n_out + BN - 1) / BN;
@@ -731,16 +771,17 @@ __device__ inline void wide_tile(const WideArgs& p, u32 block_id, u32 n_blocks, 
     }
     __syncthreads();
 
-    // What is left of the sum, then the adapters' share: 64 values of rank for each adapter that the tile's tokens have.  A product is added
-    // where the token is the adapter's and nowhere else: zeros in its place would spread infinities and NaN of one request's adapter to its
-    // neighbours.
-    u32 me = tid;
-    asm volatile("" : "+v"(me));                                  // keeps the places below out of registers while the sum runs
+    // What is left of the sum, then the adapters' share: 64 ranks at a time for each adapter that the tile's tokens have, in two groups of 32
+    // with a tile in LDS each.  z comes as sums of two 16-bit values, 32 of the first beside 32 of the second, so its product keeps 16 bits of it or
+    // more and y is rounded once; both meet the same fragments of the adapter's matrix.  A product is added where the token is the adapter's and
+    // nowhere else: zeros in its place would spread infinities and NaN of one request's adapter to its neighbours.
     int a = -1;
     u32 r0 = 0, rank = 0;
     const u16* m = nullptr;
     bool vec_m = false;
     for (;;) {                                                     // uniform
+        u32 me = tid;
+        asm volatile("" : "+v"(me));                              // keeps the places below out of registers while the sum runs, and between passes
         if (!rest) {
             if (p.part) break;                                     // added with the parts
             r0 += 64;
@@ -759,62 +800,101 @@ __device__ inline void wide_tile(const WideArgs& p, u32 block_id, u32 n_blocks, 
                 r0 = 0;
             }
         }
+        const u32 groups = !rest && rank - r0 > kDownRanks ? 2 : 1;
+        static_assert(BM * 2 <= kThreads, "a thread for each scale");
+        float down = 1.0f;
+        if (E::kNarrow && !rest && me < BM * groups) {
+            const u64 t = t0 + me % BM < p.n_tokens ? t0 + me % BM : p.n_tokens - 1;
+            down = power_of_two(-scale_exponent(p.row_max[t * (p.rp / kDownRanks) + r0 / kDownRanks + me / BM]));
+        }
         const i64 k0 = rest ? static_cast<i64>(all_steps - 1) * 64 : r0;
         const i64 k_end = rest ? p.n_sum : rank;
-        const u32 subs = k_end - k0 > 32 ? 2 : 1;
         const u16* x = rest ? p.x : p.zp;
-        const i64 ldx = rest ? p.ldx : static_cast<i64>(p.rp), x_end = rest ? p.x_cols : p.rp;
-        // Loads before stores, four at once; tiles of 256 rows, which have no registers for that, one by one.
-        constexpr u32 kOnce = BM * BN <= 128 * 128 ? (kXPieces < kWPieces ? kXPieces : kWPieces) : 1;
-#pragma unroll 1
-        for (u32 at0 = me; at0 < BM * 8; at0 += kOnce * kThreads) {
-            if (kOnce == 1 && (at0 & 7u) >= subs * 4) continue;    // the second half is not read
-            u32x4 v[kOnce];
-#pragma unroll
-            for (u32 i = 0; i < kOnce; ++i) {
-                const u32 at = at0 + i * kThreads, row = at >> 3, t = t0 + row < p.n_tokens ? t0 + row : p.n_tokens - 1;
-                const u16* src = x + static_cast<i64>(t) * ldx;
-                const i64 k = k0 + (at & 7u) * 8;
-                v[i] = ROWS == kRows16 || !rest ? load8<true>(src, k, x_end) : load8<false>(src, k, x_end);
-            }
-#pragma unroll
-            for (u32 i = 0; i < kOnce; ++i) *reinterpret_cast<u32x4*>(tiles + along_at((at0 + i * kThreads) >> 3, at0 & 7u)) = v[i];
-        }
+        const i64 ldx = rest ? p.ldx : static_cast<i64>(p.rp) * 2, x_end = rest ? p.x_cols : ldx, x0 = rest ? k0 : k0 * 2;
         const u16* w = rest ? p.w : m;
         const i64 ldw = rest ? p.ldw : (ALONG ? static_cast<i64>(rank) : static_cast<i64>(p.n_out));
         const i64 cols = rest ? p.w_cols : (ALONG ? rank : p.n_out), rows = ALONG ? p.n_out : k_end;
         const bool vec_w = rest ? ROWS == kRows16 : vec_m;
-#pragma unroll 1
-        for (u32 at0 = me; at0 < BN * 8; at0 += kOnce * kThreads) {
-            if (kOnce == 1 && (ALONG ? (at0 & 7u) >> 2 : at0 / (BN / 8) >> 5) >= subs) continue;
-            u32x4 v[kOnce];
+        auto load_x = [&](u32 at, u32 group) {
+            const u32 row = at >> 3, t = t0 + row < p.n_tokens ? t0 + row : p.n_tokens - 1;
+            const u16* src = x + static_cast<i64>(t) * ldx;
+            const i64 k = x0 + group * 64 + (at & 7u) * 8;
+            return ROWS == kRows16 || !rest ? load8<true>(src, k, x_end) : load8<false>(src, k, x_end);
+        };
+        auto store_x = [&](u32 at, u32 group, u32x4 v) { *reinterpret_cast<u32x4*>(tiles + group * kTile + along_at(at >> 3, at & 7u)) = v; };
+        auto load_w = [&](u32 at) {
+            const u32 row = ALONG ? at >> 3 : at / (BN / 8), piece = ALONG ? at & 7u : at % (BN / 8);
+            const i64 want = ALONG ? n0 + row : k0 + row, r = want < rows ? want : rows - 1, from = ALONG ? k0 + piece * 8 : n0 + piece * 8;
+            const i64 end_at = ALONG || want < rows ? cols : 0;
+            return vec_w ? load8<true>(w + r * ldw, from, end_at) : load8_masked(w + r * ldw, from, end_at, (rows - 1 - r) * ldw + cols - from);
+        };
+        auto store_w = [&](u32 at, u32x4 v) {
+            const u32 row = ALONG ? at >> 3 : at / (BN / 8), piece = ALONG ? at & 7u : at % (BN / 8);
+            const u32 group = rest ? 0 : (ALONG ? piece / 4 : row / kDownRanks);
+            const u32 to = ALONG ? along_at(row, piece - group * 4) : across_at<BN>(row - group * kDownRanks, piece);
+            *reinterpret_cast<u32x4*>(tiles + group * kTile + BM * 64 + to) = v;
+        };
+        // All loads before the stores; tiles of 256 rows, which have no registers for that, one by one.
+        constexpr bool kAtOnce = BM * BN <= 128 * 128;
+        if (kAtOnce) {
+            u32x4 vx[2][kXPieces], vw[kWPieces];
 #pragma unroll
-            for (u32 i = 0; i < kOnce; ++i) {
-                const u32 at = at0 + i * kThreads, row = ALONG ? at >> 3 : at / (BN / 8), piece = ALONG ? at & 7u : at % (BN / 8);
-                const i64 want = ALONG ? n0 + row : k0 + row, r = want < rows ? want : rows - 1, from = ALONG ? k0 + piece * 8 : n0 + piece * 8;
-                const i64 end_at = ALONG || want < rows ? cols : 0;
-                v[i] = vec_w ? load8<true>(w + r * ldw, from, end_at) : load8_masked(w + r * ldw, from, end_at, (rows - 1 - r) * ldw + cols - from);
+            for (u32 i = 0; i < kWPieces; ++i) vw[i] = load_w(me + i * kThreads);
+#pragma unroll
+            for (u32 i = 0; i < kXPieces; ++i) vx[0][i] = load_x(me + i * kThreads, 0);
+            if (groups == 2) {
+#pragma unroll
+                for (u32 i = 0; i < kXPieces; ++i) vx[1][i] = load_x(me + i * kThreads, 1);
             }
 #pragma unroll
-            for (u32 i = 0; i < kOnce; ++i) {
-                const u32 at = at0 + i * kThreads;
-                *reinterpret_cast<u32x4*>(tiles + BM * 64 + (ALONG ? along_at(at >> 3, at & 7u) : across_at<BN>(at / (BN / 8), at % (BN / 8)))) = v[i];
+            for (u32 i = 0; i < kWPieces; ++i) store_w(me + i * kThreads, vw[i]);
+#pragma unroll
+            for (u32 i = 0; i < kXPieces; ++i) store_x(me + i * kThreads, 0, vx[0][i]);
+            if (groups == 2) {
+#pragma unroll
+                for (u32 i = 0; i < kXPieces; ++i) store_x(me + i * kThreads, 1, vx[1][i]);
+            }
+        } else {
+            for (u32 group = 0; group < groups; ++group)
+#pragma unroll 1
+                for (u32 at = me; at < BM * 8; at += kThreads) store_x(at, group, load_x(at, group));
+#pragma unroll 1
+            for (u32 at = me; at < BN * 8; at += kThreads) {
+                if (!rest && groups == 1 && (ALONG ? (at & 7u) >= 4 : at / (BN / 8) >= kDownRanks)) continue;      // not read
+                store_w(at, load_w(at));
             }
         }
+        if (E::kNarrow && me < BM * groups) s_down[me] = down;
         __syncthreads();
-        for (u32 sub = 0; sub < subs; ++sub) {
+#pragma unroll 1
+        for (u32 group = 0; group < groups; ++group) {
+            const u16* sx = tiles + group * kTile;
+            u32x4 second[FN];
 #pragma unroll
-            for (u32 i = 0; i < FN; ++i) fw[i] = frag_w(tiles, i, sub);
+            for (u32 i = 0; i < FN; ++i) {
+                fw[i] = frag_w(sx, i, 0);
+                second[i] = rest ? frag_w(sx, i, 1) : fw[i];
+            }
 #pragma unroll
             for (u32 j = 0; j < FM; ++j) {
-                fx[0] = frag_x(tiles, j, sub);
-                const bool mine = rest || s_ids[wm * TM + j * 16 + (me & 15u)] == a;
+                const u32 row = wm * TM + j * 16 + (me & 15u);
+                const int id = s_ids[row];
+                u32 mine = static_cast<u32>(rest) | static_cast<u32>(id == a) ? ~0u : 0u;
+                if (kAtOnce && __ballot(mine != 0) == 0) continue;             // sixteen rows without a token of the adapter
+                asm volatile("" : "+v"(mine));                    // a mask and no branch: with branches the tiles of 256 rows spilled 90 registers
+                const u32x4 x_first = frag_x(sx, j, 0), x_second = frag_x(sx, j, 1);
+                const float undo = E::kNarrow ? __uint_as_float(__float_as_uint(s_down[group * BM + row]) & mine) : 1.0f;
 #pragma unroll
                 for (u32 i = 0; i < FN; ++i) {
-                    const f32x4 v = E::mfma(fw[i], fx[0], f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+                    f32x4 v = E::mfma(second[i], x_second, f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+                    v = E::mfma(fw[i], x_first, v);
 #pragma unroll
-                    for (u32 k = 0; k < 4; ++k) acc[i][j][k] = mine ? acc[i][j][k] + v[k] : acc[i][j][k];
+                    for (u32 k = 0; k < 4; ++k) {
+                        const float f = __uint_as_float(__float_as_uint(v[k]) & mine);
+                        acc[i][j][k] = E::kNarrow ? __builtin_fmaf(f, undo, acc[i][j][k]) : acc[i][j][k] + f;
+                    }
                 }
+                if (!kAtOnce) __builtin_amdgcn_sched_barrier(0);               // sixteen rows at a time: there are no registers for more
             }
         }
         __syncthreads();
