@@ -50,6 +50,7 @@ struct Plan {
     bool split = false, few = false;
     u32 rp = 0, splits = 1, steps_each = 0, bm = 64;
     u32 run = 0, n_slots = 0, tiles = 0;
+    bool many = false;                                      // adapters than runs: how the parts of gradients are numbered
     bool pack_in = false, pack_out = false;                 // rows of n_in (x, W), rows of n_out (dy)
     i64 in_cols = 0, out_cols = 0, w_rows = 0;              // sizes of the copies, or of what is not copied
     size_t xq = 0, wq = 0, dyq = 0;
@@ -94,7 +95,8 @@ static Plan make_plan(i64 T, i64 n_in, i64 n_out, u32 n_adapters, u32 max_rank, 
             p.order = take(static_cast<u64>(T) * 4);
             p.seg = take(static_cast<u64>(n_adapters) * sizeof(uint2));
             p.slots = take(static_cast<u64>(p.n_slots) * sizeof(uint4));
-            if (T > p.run) p.part = take(static_cast<u64>(p.n_slots) * max_rank * (n_in + n_out) * 4);
+            p.many = n_adapters > T / p.run;
+            if (T > p.run) p.part = take(static_cast<u64>(p.many ? 2 * (T / p.run) : p.n_slots) * max_rank * (n_in + n_out) * 4);
         }
     }
     p.pack_in = T > kPackTokens && n_in % 8 != 0;
@@ -452,6 +454,7 @@ condensa_status condensa_adapter_project_backward(const condensa_adapter_list* l
     q.max_rank = d.max_rank; q.run = p.run;
     q.tiles_in = (q.n_in + kGradCols - 1) / kGradCols;
     q.tiles = q.tiles_in + (q.n_out + kGradCols - 1) / kGradCols;
+    q.many = p.many;
     q.part = n_tokens > p.run ? at<float>(workspace_dev, p.part) : nullptr;
     q.rank_groups = rank_groups;
     const u32 grid = (joins + 1) / 2 + static_cast<u32>(n > 0 ? grad_blocks : 0);

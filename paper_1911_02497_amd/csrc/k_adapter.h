@@ -260,6 +260,10 @@ constexpr u32 down_lds(u32 waves) { return waves * 8192; }
 // Places of the runs of an adapter whose tokens begin at `first`: run j of it is slot first / run + a + j.  (One slot at least for
 // each adapter; the slots of different adapters never meet, since ceil(n / run) <= floor((first + n) / run) - floor(first / run) + 1.)
 __device__ inline u32 first_slot(u32 first, u32 run, u32 a) { return first / run + a; }
+// Place of the parts of run j of adapter a, whose first slot is s0.  Only adapters with several runs have parts.  Where there are more adapters
+// than runs of tokens, places are 2 (first / run) + j: several runs are at most twice as many as whole ones, so places do not meet either
+// and 2 (tokens / run) of them are enough.
+__device__ inline u32 part_place(u32 a, u32 s0, u32 j, bool many) { return many ? 2 * (s0 - a) + j : s0 + j; }
 
 // One wavefront an adapter: two passes over the ids, the first counts, the second writes; 1024 ids are under way at once.
 __device__ inline void sort_tokens(const DownArgs& p, u32 a) {
@@ -1123,7 +1127,8 @@ struct GradArgs {
     const uint2* seg;
     const AdapterDesc* ad;
     u32 max_rank, run, tiles_in, tiles, rank_groups;
-    float* part;                         // [n_slots][max_rank (n_in + n_out)]
+    u32 many;                            // how part_place numbers them
+    float* part;                         // [places][max_rank (n_in + n_out)]
 };
 
 constexpr u32 kGradCols = 128, kGradWaves = 8, kGradPass = 32 * kGradWaves;
@@ -1260,8 +1265,11 @@ __global__ __launch_bounds__(64 * kGradWaves, G == 1 ? 4 : 2) void k_adapter_gra
             }
         }
     }
-    float* out = whole ? (of_a ? d.grad_a : d.grad_b)
-                       : p.part + static_cast<u64>(slot) * p.max_rank * (static_cast<u64>(p.n_in) + p.n_out) + (of_a ? 0 : static_cast<u64>(rank) * p.n_in);
+    float* out = of_a ? d.grad_a : d.grad_b;
+    if (!whole) {
+        const u32 s0 = p.seg[a].x;
+        out = p.part + static_cast<u64>(part_place(a, s0, slot - s0, p.many)) * p.max_rank * (static_cast<u64>(p.n_in) + p.n_out) + (of_a ? 0 : static_cast<u64>(rank) * p.n_in);
+    }
     const u32 used = count < kGradPass ? (count + 31) / 32 : kGradWaves;       // wavefronts that had tokens
     f32x4* sums = reinterpret_cast<f32x4*>(&tiles[0][0]);
 #pragma unroll
@@ -1292,11 +1300,11 @@ __global__ __launch_bounds__(256) void k_adapter_join(GradArgs p, u32 blocks_eac
     const u32 rank = d.rank < p.max_rank ? d.rank : p.max_rank;
     const u64 na = static_cast<u64>(rank) * p.n_in, n = na + static_cast<u64>(rank) * p.n_out;
     const u64 each = static_cast<u64>(p.max_rank) * (static_cast<u64>(p.n_in) + p.n_out);
-    const u32 s0 = seg.x, runs = seg.y;
+    const u32 first = part_place(a, seg.x, 0, p.many), runs = seg.y;
     for (u64 i = static_cast<u64>(blockIdx.x % blocks_each) * 256 + threadIdx.x; i < n; i += static_cast<u64>(blocks_each) * 256) {
-        float v = p.part[s0 * each + i];
+        float v = p.part[first * each + i];
 #pragma unroll 4
-        for (u32 r = 1; r < runs; ++r) v += p.part[(s0 + r) * each + i];
+        for (u32 r = 1; r < runs; ++r) v += p.part[(first + r) * each + i];
         if (i < na) d.grad_a[i] = v;
         else d.grad_b[i - na] = v;
     }
