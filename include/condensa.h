@@ -518,7 +518,7 @@ typedef struct {
 size_t condensa_adapter_list_bytes(int n_adapters);
 condensa_status condensa_adapter_list_init(const condensa_adapter* adapters, int n_adapters, int type, int64_t n_in, int64_t n_out,
                                            void* list_dev, size_t list_bytes, void* stream, condensa_adapter_list* list);
-/* Bytes of workspace (256-byte aligned device memory) of a call with n_tokens tokens; 0 for invalid arguments. */
+/* Bytes of workspace (256-byte aligned device memory) of calls with n_tokens tokens or fewer; 0 for invalid arguments.  The two directions differ. */
 size_t condensa_adapter_workspace_bytes(const condensa_adapter_list* list, int64_t n_tokens, int backward);
 
 /*

@@ -782,7 +782,7 @@ def adapter_table(adapters, grads=None, **kw) -> AdapterTable:
 
 
 def adapter_workspace(table: AdapterTable, n_tokens: int, backward: bool = False):
-    """Workspace of calls with ``n_tokens`` tokens, to be kept between them."""
+    """Workspace of calls of one direction with ``n_tokens`` tokens or fewer, to be kept between them."""
     import torch
     need = int(library().condensa_adapter_workspace_bytes(ctypes.byref(table.list), int(n_tokens), int(backward)))
     if need == 0:

@@ -113,6 +113,37 @@ static Plan make_plan(i64 T, i64 n_in, i64 n_out, u32 n_adapters, u32 max_rank, 
     return p;
 }
 
+// Workspace that a call with n_tokens tokens and every call with fewer can do with: each piece of the plan, at least as large as it is at any
+// number of tokens up to this one.  (A plan by itself is not: split sums have parts, larger batches none.)
+static size_t workspace_for(i64 T, i64 n_in, i64 n_out, u32 n_adapters, u32 max_rank, bool backward) {
+    const Plan p = make_plan(T, n_in, n_out, n_adapters, max_rank, backward);
+    if (p.few || T == 0) return p.total;
+    size_t total = 0;
+    auto take = [&](u64 bytes) { total += align_up(bytes ? bytes : 1); };
+    const u64 t = static_cast<u64>(T), n_wide = backward ? n_in : n_out, n_sum = backward ? n_out : n_in, columns = (n_wide + 63) / 64;
+    // Split sums: below 512 tiles of 64 rows or fewer; at most 16 parts, at most half as many as steps, and 768 tiles of parts where there are several.
+    const u64 split_tokens = std::min(t, 511 / columns * 64), steps = (n_sum + 63) / 64;
+    const u64 splits = std::max<u64>(1, std::min<u64>(16, steps / 2));
+    take(std::min(splits * split_tokens * n_wide * 4, static_cast<u64>(768) * 64 * 64 * 4));
+    take(t * p.rp * 4);
+    take((backward ? t : split_tokens) * p.rp * 4);
+    take(t * (p.rp / kDownRanks) * 4);
+    if (backward) {
+        const u64 tiles = (n_in + kGradCols - 1) / kGradCols + (n_out + kGradCols - 1) / kGradCols;
+        const u64 runs = T <= 1536 ? t / 1536 : std::min<u64>(t / 512, 1024 / tiles + 1);        // of run_tokens, whole ones
+        take(t * 4);
+        take(static_cast<u64>(n_adapters) * sizeof(uint2));
+        take((runs + n_adapters) * sizeof(uint4));
+        take(T <= 1536 ? 0 : std::min(2 * runs, runs + n_adapters) * max_rank * (n_in + n_out) * 4);
+    }
+    if (p.pack_in) {
+        take(t * p.in_cols * 2);
+        take(static_cast<u64>(p.w_rows) * p.in_cols * 2);
+    }
+    if (p.pack_out) take(t * p.out_cols * 2);
+    return total;
+}
+
 template <typename E, bool ALONG>
 static condensa_status launch_down(const DownArgs& a, u32 blocks, hipStream_t st) {
     for (const PackArgs& p : a.pack) blocks += p.blocks;
@@ -287,7 +318,7 @@ condensa_status condensa_adapter_list_init(const condensa_adapter* adapters, int
 
 size_t condensa_adapter_workspace_bytes(const condensa_adapter_list* list, int64_t n_tokens, int backward) {
     if (!list_ok(list) || n_tokens < 0 || n_tokens > kMaxTokens) return 0;
-    const size_t b = make_plan(n_tokens, list->n_in, list->n_out, static_cast<u32>(list->n_adapters), static_cast<u32>(list->max_rank), backward != 0).total;
+    const size_t b = workspace_for(n_tokens, list->n_in, list->n_out, static_cast<u32>(list->n_adapters), static_cast<u32>(list->max_rank), backward != 0);
     return b ? b : 256;
 }
 
