@@ -419,9 +419,7 @@ condensa_status condensa_adapter_project_backward(const condensa_adapter_list* l
     const Plan p = make_plan(n_tokens, list->n_in, list->n_out, static_cast<u32>(list->n_adapters), static_cast<u32>(list->max_rank), true);
     const condensa_status rc = check_call(n_tokens > 0 || list->n_adapters > 0, n_tokens, token_adapter_dev, workspace_dev, workspace_bytes, p);
     if (rc != CONDENSA_OK) return rc;
-    const u32 groups = grad_groups(static_cast<u32>(list->max_rank)), rank_groups = (static_cast<u32>(list->max_rank) + 16 * groups - 1) / (16 * groups);
-    const u64 grad_blocks = static_cast<u64>(rank_groups) * p.n_slots * ((list->n_in + kGradCols - 1) / kGradCols + (list->n_out + kGradCols - 1) / kGradCols);
-    if (grad_blocks >= (static_cast<u64>(1) << 22) || (dx_dev && !grid_fits(n_tokens, list->n_in))) return CONDENSA_ERR_SIZE;
+    if (dx_dev && !grid_fits(n_tokens, list->n_in)) return CONDENSA_ERR_SIZE;
     ByteRange r[] = {byte_range(dy_dev, rows_bytes(n_tokens, dy_stride, list->n_out, 2), false), byte_range(x_dev, rows_bytes(n_tokens, x_stride, list->n_in, 2), false),
                      byte_range(w_dev, rows_bytes(list->n_out, w_stride, list->n_in, 2), false), byte_range(token_adapter_dev, static_cast<u64>(n_tokens) * 4, false),
                      byte_range(z_dev, static_cast<u64>(n_tokens) * z_stride * 2, false), byte_range(dx_dev, rows_bytes(n_tokens, dx_stride, list->n_in, 2), true),
@@ -487,11 +485,20 @@ condensa_status condensa_adapter_project_backward(const condensa_adapter_list* l
     q.tiles = q.tiles_in + (q.n_out + kGradCols - 1) / kGradCols;
     q.many = p.many;
     q.part = n_tokens > p.run ? at<float>(workspace_dev, p.part) : nullptr;
-    q.rank_groups = rank_groups;
-    const u32 grid = (joins + 1) / 2 + static_cast<u32>(n > 0 ? grad_blocks : 0);
+    const u32 groups = grad_groups(q.max_rank);
+    q.rank_groups = (q.max_rank + 16 * groups - 1) / (16 * groups);
     const bool vec = aligned(q.x, 16) && q.ldx % 8 == 0 && p.in_cols % 8 == 0 && aligned(q.dy, 16) && q.ldy % 8 == 0 && p.out_cols % 8 == 0;
-    s = f16 ? launch_grads<ElemF16>(q, g, joins, grid, groups, vec, st) : launch_grads<ElemBF16>(q, g, joins, grid, groups, vec, st);
-    if (s != CONDENSA_OK) return s;
+    // As many slots a launch as keep it below 2^22 workgroups of 512; dx's parts are added beside the first.
+    const u32 each_slot = q.rank_groups * q.tiles, all_slots = n > 0 && each_slot > 0 ? p.n_slots : 0;
+    u32 join_blocks = joins;
+    do {
+        const u32 slots = all_slots ? std::min(all_slots - q.slot0, (1u << 22) / each_slot) : 0;
+        const u32 grid = (join_blocks + 1) / 2 + slots * each_slot;
+        s = f16 ? launch_grads<ElemF16>(q, g, join_blocks, grid, groups, vec, st) : launch_grads<ElemBF16>(q, g, join_blocks, grid, groups, vec, st);
+        if (s != CONDENSA_OK) return s;
+        q.slot0 += slots;
+        join_blocks = 0;
+    } while (q.slot0 < all_slots);
     if (n > 0 && n_tokens > p.run) {
         const u64 elems = static_cast<u64>(q.max_rank) * (list->n_in + list->n_out);
         u64 each = (elems + 1023) / 1024;

@@ -1127,6 +1127,7 @@ struct GradArgs {
     const uint2* seg;
     const AdapterDesc* ad;
     u32 max_rank, run, tiles_in, tiles, rank_groups;
+    u32 slot0;                           // of this launch
     u32 many;                            // how part_place numbers them
     float* part;                         // [places][max_rank (n_in + n_out)]
 };
@@ -1152,7 +1153,7 @@ __global__ __launch_bounds__(64 * kGradWaves, G == 1 ? 4 : 2) void k_adapter_gra
         if (block < joins) join_parts<E, false>(dx, p.dz, p.rp, block / cols, block % cols * 256 + (tid & 255u));
         return;
     }
-    const u32 col_tile = blockIdx.x % p.tiles, r0 = blockIdx.x / p.tiles % p.rank_groups * (16 * G), slot = blockIdx.x / p.tiles / p.rank_groups;
+    const u32 col_tile = blockIdx.x % p.tiles, r0 = blockIdx.x / p.tiles % p.rank_groups * (16 * G), slot = p.slot0 + blockIdx.x / p.tiles / p.rank_groups;
     const uint4 of = p.slots[slot];
     const u32 a = __builtin_amdgcn_readfirstlane(of.x), first = __builtin_amdgcn_readfirstlane(of.y), count = __builtin_amdgcn_readfirstlane(of.z);
     const bool whole = of.w <= p.run;
