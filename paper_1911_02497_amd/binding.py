@@ -190,10 +190,18 @@ def _check(code: int) -> None:
         raise CondensaError(code, msg)
 
 
+@functools.lru_cache(None)
+def _raw_stream():
+    """Device index -> handle of its current stream.  torch's own function for that makes no Stream object, which is a microsecond less
+    a call; it is not public, so the public way stands in where a version of torch lacks it."""
+    import torch
+    return getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: int(torch.cuda.current_stream(index).cuda_stream))
+
+
 def _stream(stream) -> int:
     import torch
-    if stream is None:                       # the current stream of the current device, without a Stream object made for it
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    if stream is None:
+        return _raw_stream()(torch.cuda.current_device())
     return int(stream.cuda_stream)
 
 
