@@ -646,16 +646,43 @@ def _type_of(dtype):
     return {torch.float32: TYPE_F32, torch.float16: TYPE_F16, torch.bfloat16: TYPE_BF16}.get(dtype)
 
 
-def _stream_of(stream):
+def _device_of(tensors, what):
+    """The one device that the tensors of a table lie on; the current one without any."""
     import torch
-    return torch.cuda.current_stream() if stream is None else stream
+    devices = {t.device for t in tensors}
+    if len(devices) > 1:
+        raise TypeError(f"{what} lie on one device")
+    return devices.pop() if devices else torch.device("cuda", torch.cuda.current_device())
+
+
+def _stream_on(device, stream):
+    """The stream of a call for tensors of ``device``: the given one or that device's current one."""
+    import torch
+    if stream is None:
+        return torch.cuda.current_stream(device)
+    if stream.device != device:
+        raise ValueError(f"a stream of {stream.device} for tensors of {device}")
+    return stream
 
 
 def _wait_unless_captured(stream):
     """A list on the device is read by calls on any stream later on: it is whole before the program goes on."""
     import torch
-    if not torch.cuda.is_current_stream_capturing():
+    with torch.cuda.stream(stream):
+        captured = torch.cuda.is_current_stream_capturing()
+    if not captured:
         stream.synchronize()
+
+
+def _run(table, stream, entry, *args):
+    """One call of a table's entry point, on the table's device and the given stream or that device's current one."""
+    import torch
+    handle = _raw_stream()(table.index) if stream is None else int(_stream_on(table.device, stream).cuda_stream)
+    if torch.cuda.current_device() == table.index:
+        _check(entry(*args, handle))
+    else:
+        with torch.cuda.device(table.index):
+            _check(entry(*args, handle))
 
 
 class AdamwTable:
@@ -682,7 +709,6 @@ class AdamwTable:
         if grad_type is None or code_type in (None, TYPE_F32):
             raise TypeError("gradients are float32, float16 or bfloat16 and codes are float16 or bfloat16")
         want = {"exp_avg": state, "exp_avg_sq": state, "grad": None if g0 is None else g0.dtype, "codes": None if c0 is None else c0.dtype}
-        dev = weights[0].device if n else torch.device("cuda")
         arr = (AdamwTensor * max(n, 1))()
         for i, w in enumerate(weights):
             if not (w.is_cuda and w.dtype == torch.float32 and w.is_contiguous()):
@@ -697,17 +723,18 @@ class AdamwTable:
                 if not (t.device == w.device and t.dtype == want.get(k, torch.float32) and t.is_contiguous() and t.numel() == elems):
                     raise TypeError(f"{k.rstrip('_')} of tensor {i}: a contiguous tensor of {elems} elements beside the weights, one type for all")
                 setattr(arr[i], k, t.data_ptr() or None)
+        dev = _device_of(weights, "weights")
         lib = library()
         need = int(lib.condensa_adamw_list_bytes(arr, n))
-        self._memory = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
         self._keep = (list(weights), lists)
         self.list = AdamwList()
-        st = _stream_of(stream)
-        with torch.cuda.device(dev):
+        st = _stream_on(dev, stream)
+        with torch.cuda.stream(st):                                   # its memory too: other streams may not be done with what they freed
+            self._memory = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
             _check(lib.condensa_adamw_list_init(arr, n, bits, grad_type, code_type, self._memory.data_ptr(), self._memory.numel(),
                                                 int(st.cuda_stream), ctypes.byref(self.list)))
             _wait_unless_captured(st)
-        self.ref = ctypes.byref(self.list)
+        self.ref, self.device, self.index = ctypes.byref(self.list), dev, dev.index
 
 
 def adamw_table(weights, grads, exp_avg, exp_avg_sq, **kw) -> AdamwTable:
@@ -726,15 +753,15 @@ def condensa_lc_adamw_step(table: AdamwTable, lr, step, betas=(0.9, 0.999), eps=
     scale = None
     if grad_scale is not None:
         import torch
-        if not (grad_scale.is_cuda and grad_scale.dtype == torch.float32 and grad_scale.numel() == 1):
-            raise TypeError("grad_scale is one float32 on the device")
+        if not (grad_scale.get_device() == table.index and grad_scale.dtype == torch.float32 and grad_scale.numel() == 1):
+            raise TypeError("grad_scale is one float32 on the device of the weights")
         scale = grad_scale.data_ptr()
     if seed is None or table.list.state_bits == 32:
         rounding, seed = ROUND_NEAREST, 0
     else:
         rounding, seed = ROUND_STOCHASTIC, seed & 0xFFFFFFFFFFFFFFFF
     s = AdamwSettings(lr, betas[0], betas[1], eps, weight_decay, mu, rounding, step, seed, scale, 0)
-    _check(library().condensa_lc_adamw_step(table.ref, ctypes.byref(s), _stream(stream)))
+    _run(table, stream, library().condensa_lc_adamw_step, table.ref, ctypes.byref(s))
 
 
 class AdapterTable:
@@ -768,10 +795,10 @@ class AdapterTable:
         lib = library()
         self.dtype, self.device, self.grads = dtype, dev, grads
         self._keep = adapters
-        self._memory = torch.empty(max(int(lib.condensa_adapter_list_bytes(len(adapters))), 256), dtype=torch.uint8, device=dev)
         self.list = AdapterList()
-        st = _stream_of(stream)
-        with torch.cuda.device(dev):
+        st = _stream_on(dev, stream)
+        with torch.cuda.stream(st):                                   # its memory too: other streams may not be done with what they freed
+            self._memory = torch.empty(max(int(lib.condensa_adapter_list_bytes(len(adapters))), 256), dtype=torch.uint8, device=dev)
             _check(lib.condensa_adapter_list_init(arr, len(adapters), _type_of(dtype), int(n_in or 0), int(n_out or 0), self._memory.data_ptr(),
                                                   self._memory.numel(), int(st.cuda_stream), ctypes.byref(self.list)))
             _wait_unless_captured(st)
@@ -852,8 +879,8 @@ def condensa_adapter_project(x, w, table: AdapterTable, token_adapter, y=None, z
     if workspace is None:
         workspace = adapter_workspace(table, T)
         _used_on(stream, workspace)
-    _check(library().condensa_adapter_project(table.ref, px, ldx, T, pw, ldw, ids, py, ldy, pz, ldz, workspace.data_ptr(),
-                                              workspace.numel(), _stream(stream)))
+    _run(table, stream, library().condensa_adapter_project, table.ref, px, ldx, T, pw, ldw, ids, py, ldy, pz, ldz, workspace.data_ptr(),
+         workspace.numel())
     return {"y": y, "z": z, "workspace": workspace}
 
 
@@ -873,8 +900,8 @@ def condensa_adapter_project_backward(dy, x, w, table: AdapterTable, token_adapt
     if workspace is None:
         workspace = adapter_workspace(table, T, backward=True)
         _used_on(stream, workspace)
-    _check(library().condensa_adapter_project_backward(table.ref, pdy, lddy, px, ldx, T, pw, ldw, ids, pz, ldz, pdx, lddx,
-                                                       workspace.data_ptr(), workspace.numel(), _stream(stream)))
+    _run(table, stream, library().condensa_adapter_project_backward, table.ref, pdy, lddy, px, ldx, T, pw, ldw, ids, pz, ldz, pdx, lddx,
+         workspace.data_ptr(), workspace.numel())
     return {"dx": None if dx is False else dx, "grads": table.grads, "workspace": workspace}
 
 
