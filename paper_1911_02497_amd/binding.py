@@ -685,7 +685,25 @@ def _run(table, stream, entry, *args):
             _check(entry(*args, handle))
 
 
-class AdamwTable:
+class _Table:
+    """What calls on any stream read of a table: the list of descriptors and the tensors that it names."""
+
+    def _holds(self, tensors):
+        self._held, self._streams = [t for t in tensors if t is not None], set()
+
+    def keep_for(self, stream):
+        """Before a call on a stream: what the table holds is not handed out again before the work of that stream is done, although table and
+        tensors are dropped.  (A graph that captured a call needs the table for as long as it is replayed.)"""
+        import torch
+        handle = _raw_stream()(self.index) if stream is None else int(stream.cuda_stream)
+        if handle not in self._streams:
+            stream = torch.cuda.current_stream(self.device) if stream is None else stream
+            for t in self._held:
+                t.record_stream(stream)
+            self._streams.add(handle)
+
+
+class AdamwTable(_Table):
     """Weights, gradients and states of condensa_lc_adamw_step, laid out on the device once for many steps.  The tensors must
     keep their storage.  See ``adamw_table``."""
 
@@ -735,6 +753,7 @@ class AdamwTable:
                                                 int(st.cuda_stream), ctypes.byref(self.list)))
             _wait_unless_captured(st)
         self.ref, self.device, self.index = ctypes.byref(self.list), dev, dev.index
+        self._holds([self._memory, *weights, *(t for v in lists.values() for t in v)])
 
 
 def adamw_table(weights, grads, exp_avg, exp_avg_sq, **kw) -> AdamwTable:
@@ -761,10 +780,11 @@ def condensa_lc_adamw_step(table: AdamwTable, lr, step, betas=(0.9, 0.999), eps=
     else:
         rounding, seed = ROUND_STOCHASTIC, seed & 0xFFFFFFFFFFFFFFFF
     s = AdamwSettings(lr, betas[0], betas[1], eps, weight_decay, mu, rounding, step, seed, scale, 0)
+    table.keep_for(stream)
     _run(table, stream, library().condensa_lc_adamw_step, table.ref, ctypes.byref(s))
 
 
-class AdapterTable:
+class AdapterTable(_Table):
     """Adapters beside one shared projection, laid out on the device once for many calls.  The tensors must keep their storage.
     See ``adapter_table``."""
 
@@ -804,6 +824,7 @@ class AdapterTable:
             _wait_unless_captured(st)
         self.n_in, self.n_out, self.max_rank = self.list.n_in, self.list.n_out, self.list.max_rank
         self.ref, self.index = ctypes.byref(self.list), dev.index
+        self._holds([self._memory, *(t for a, b, _ in adapters for t in (a, b)), *(t for pair in grads or () for t in pair)])
 
     def empty(self, rows, cols):
         import torch
@@ -879,6 +900,7 @@ def condensa_adapter_project(x, w, table: AdapterTable, token_adapter, y=None, z
     if workspace is None:
         workspace = adapter_workspace(table, T)
         _used_on(stream, workspace)
+    table.keep_for(stream)
     _run(table, stream, library().condensa_adapter_project, table.ref, px, ldx, T, pw, ldw, ids, py, ldy, pz, ldz, workspace.data_ptr(),
          workspace.numel())
     return {"y": y, "z": z, "workspace": workspace}
@@ -900,6 +922,7 @@ def condensa_adapter_project_backward(dy, x, w, table: AdapterTable, token_adapt
     if workspace is None:
         workspace = adapter_workspace(table, T, backward=True)
         _used_on(stream, workspace)
+    table.keep_for(stream)
     _run(table, stream, library().condensa_adapter_project_backward, table.ref, pdy, lddy, px, ldx, T, pw, ldw, ids, pz, ldz, pdx, lddx,
          workspace.data_ptr(), workspace.numel())
     return {"dx": None if dx is False else dx, "grads": table.grads, "workspace": workspace}
