@@ -846,11 +846,16 @@ def adapter_workspace(table: AdapterTable, n_tokens: int, backward: bool = False
     return torch.empty(need, dtype=torch.uint8, device=table.device)
 
 
-def _used_on(stream, *made):
-    """Memory made for a call on another stream than the current one is not handed out again before that call is done."""
-    if stream is not None:
-        for t in made:
-            t.record_stream(stream)
+def _made_for(stream, make, *args, **kw):
+    """A tensor made for a call: on another stream than the current one from that stream's memory, which work that is still under way on the
+    current one cannot reach, and not handed out again before the current one, where the program goes on, is done with it."""
+    if stream is None:
+        return make(*args, **kw)
+    import torch
+    with torch.cuda.stream(stream):
+        t = make(*args, **kw)
+    t.record_stream(torch.cuda.current_stream(t.device))
+    return t
 
 
 def _rows(name, t, table, n_tokens, width):
@@ -889,17 +894,14 @@ def condensa_adapter_project(x, w, table: AdapterTable, token_adapter, y=None, z
     pw, ldw = _rows("w", w, table, table.n_out, table.n_in)
     ids = _token_ids(token_adapter, table, T)
     if y is None:
-        y = table.empty(T, table.n_out)
-        _used_on(stream, y)
+        y = _made_for(stream, table.empty, T, table.n_out)
     py, ldy = _rows("y", y, table, T, table.n_out)
     if z is True:
-        z = table.empty(T, max(table.max_rank, 1))
-        _used_on(stream, z)
+        z = _made_for(stream, table.empty, T, max(table.max_rank, 1))
     z = None if z is False else z
     pz, ldz = (None, 0) if z is None else _kept_z(z, table, T)
     if workspace is None:
-        workspace = adapter_workspace(table, T)
-        _used_on(stream, workspace)
+        workspace = _made_for(stream, adapter_workspace, table, T)
     table.keep_for(stream)
     _run(table, stream, library().condensa_adapter_project, table.ref, px, ldx, T, pw, ldw, ids, py, ldy, pz, ldz, workspace.data_ptr(),
          workspace.numel())
@@ -916,12 +918,10 @@ def condensa_adapter_project_backward(dy, x, w, table: AdapterTable, token_adapt
     ids = _token_ids(token_adapter, table, T)
     pz, ldz = _kept_z(z, table, T)
     if dx is True:
-        dx = table.empty(T, table.n_in)
-        _used_on(stream, dx)
+        dx = _made_for(stream, table.empty, T, table.n_in)
     pdx, lddx = (None, 0) if dx is False else _rows("dx", dx, table, T, table.n_in)
     if workspace is None:
-        workspace = adapter_workspace(table, T, backward=True)
-        _used_on(stream, workspace)
+        workspace = _made_for(stream, adapter_workspace, table, T, backward=True)
     table.keep_for(stream)
     _run(table, stream, library().condensa_adapter_project_backward, table.ref, pdy, lddy, px, ldx, T, pw, ldw, ids, pz, ldz, pdx, lddx,
          workspace.data_ptr(), workspace.numel())

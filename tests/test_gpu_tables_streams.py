@@ -77,3 +77,46 @@ def test_a_table_dropped_while_another_stream_reads_it(what, given):
     side.synchronize()
     assert not any(found)
     assert bool(torch.isfinite(keep).all())
+
+
+def test_outputs_made_for_another_stream():
+    """What a call on another stream returns does not lie in memory that the current stream, still at work, was given back.  (The workspaces,
+    which hold places of tokens, are the test's own: nothing but values is at stake.)"""
+    T = 300
+    c = Case("bf16", T, 512, 4096, [8, 16], [t % 2 for t in range(T)])
+    ws, wb = P.adapter_workspace(c.table, T), P.adapter_workspace(c.table, T, backward=True)
+    c.forward(workspace=ws)
+    c.backward(workspace=wb)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    old = [torch.empty(t.numel(), dtype=t.dtype, device=DEV) for t in (c.y, c.z, c.dx) for _ in range(8)]
+    keep = busy(torch.cuda.current_stream())
+    for t in old:
+        t.fill_(float("nan"))
+    del old, t
+    out = P.condensa_adapter_project(c.x, c.w, c.table, c.ids, z=True, workspace=ws, stream=side)
+    back = P.condensa_adapter_project_backward(c.dy, c.x, c.w, c.table, c.ids, out["z"], workspace=wb, stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(out["y"], c.y) and torch.equal(out["z"], c.z) and torch.equal(back["dx"], c.dx)
+    assert bool(torch.isfinite(keep).all())
+
+
+def test_workspaces_made_for_another_stream():
+    """Nor does the workspace that such a call makes: looked at by address, with no work under way."""
+    T = 300
+    c = Case("bf16", T, 512, 4096, [8, 16], [t % 2 for t in range(T)])
+    c.forward()
+    side = torch.cuda.Stream()
+    for backward in (False, True):
+        n = P.adapter_workspace(c.table, T, backward=backward).numel()
+        old = [torch.empty(n, dtype=torch.uint8, device=DEV) for _ in range(4)]
+        places = [t.data_ptr() for t in old]
+        del old
+        torch.cuda.synchronize()
+        if backward:
+            out = P.condensa_adapter_project_backward(c.dy, c.x, c.w, c.table, c.ids, c.z, dx=c.dx, stream=side)
+        else:
+            out = P.condensa_adapter_project(c.x, c.w, c.table, c.ids, y=c.y, stream=side)
+        torch.cuda.synchronize()
+        at = out["workspace"].data_ptr()
+        assert not any(abs(at - p) < n for p in places)
