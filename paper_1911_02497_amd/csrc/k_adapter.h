@@ -1211,10 +1211,9 @@ __global__ __launch_bounds__(64 * kGradWaves, G == 1 ? 4 : 2) void k_adapter_gra
                 }
             }
             most = wave_most(most);
-            int e = 14 - (static_cast<int>(most >> 23) - 127);                 // the largest becomes 2^14 .. 2^15
-            e = e > 120 ? 120 : (e < -100 ? -100 : e);
-            up = __uint_as_float(static_cast<u32>(127 + e) << 23);
-            down = __uint_as_float(static_cast<u32>(127 - e) << 23);
+            const int e = scale_exponent(most);
+            up = power_of_two(e);
+            down = power_of_two(-e);
         }
         for (; s < count; s += kGradPass) {
             u32x4 fu[G][kTerms] = {};

@@ -128,3 +128,21 @@ def test_what_the_workspace_held_does_not_matter(dtype, T, K, N):
         back.check_forward(how)
         back.backward(workspace=w)
         back.check_backward(how)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("scale", [2.0 ** 126, 2.0 ** -112])
+def test_gradients_beside_scales_of_any_size(dtype, scale):
+    """dz near both ends of binary32: the gradients' 16-bit values are scaled as far as it takes."""
+    T, K, N, r = 150, 96, 64, 9
+    c = Case(dtype, T, K, N, [r], [0] * T, scale_x=0.1)
+    A, B, _ = c.adapters[0]
+    c.x.mul_(2.0 ** -6)
+    table = P.adapter_table([(A, B, scale)], grads=c.grads)
+    z = torch.zeros(T, r, device=DEV, dtype=c.t)
+    P.condensa_adapter_project_backward(c.dy, c.x, c.w, table, c.ids, z, dx=False)
+    dy, x = c.dy.double(), c.x.double()
+    dz, dzs = scale * (dy @ B.double()), scale * (dy.abs() @ B.double().abs())
+    tol = 1.01 * (((N + 16) * H * dzs + 2 * c.u ** 2 * dz.abs()).t().contiguous() @ x.abs() + (2 * T + 16) * H * (dz.abs().t().contiguous() @ x.abs()))
+    tol = tol + 2.0 ** -38 * dz.abs().max() * x.abs().sum(0)[None] + 2.0 ** -140 * T
+    c.within(c.grads[0][0], dz.t().contiguous() @ x, tol, "grad_A")
