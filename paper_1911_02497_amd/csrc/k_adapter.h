@@ -208,19 +208,25 @@ __device__ inline int scale_exponent(u32 most) {
 }
 __device__ inline float power_of_two(int e) { return __uint_as_float(static_cast<u32>(127 + e) << 23); }
 
-// Two 16-bit values of one sign whose sum is x but for u^2 of it (u: half a step of the type at 1): x cut off and what was cut, rounded.  An infinity that
-// both meet in a product stays one of that sign, so the second is the type's smallest value where nothing was cut.
-template <typename E>
-__device__ inline void two_values(float x, u16* hi, u16* lo) {
-    const u32 u = __float_as_uint(x), sign = u >> 16 & 0x8000u;
-    if ((u & 0x7FFFFFFFu) >= 0x7F800000u) {                  // infinities and NaN
-        *hi = E::enc(x);
-        *lo = 0;
-        return;
+// N 16-bit values of one sign whose sum is x, but for (2 u)^(N - 1) u of it (u: half a step of the type at 1): x cut off, what was cut, cut off again,
+// and so on, and the last one rounded.  An infinity that all of them meet in a product stays one of that sign, so the type's smallest value stands where
+// nothing is left.
+template <typename E, u32 N>
+__device__ inline void in_terms(float x, u16 (&h)[N]) {
+    const u32 u = __float_as_uint(x), size = u & 0x7FFFFFFFu;
+    const bool finite = size < 0x7F800000u;
+    float rest = x;
+#pragma unroll
+    for (u32 t = 0; t < N; ++t) {
+        if (t + 1 < N && (t > 0 || finite)) {
+            h[t] = E::cut(rest);
+            rest -= E::dec(h[t]);
+        } else {
+            h[t] = E::enc(rest);
+            if (!finite) rest = 0.0f;
+        }
+        if (t > 0 && finite && size != 0 && (h[t] & 0x7FFFu) == 0) h[t] = static_cast<u16>((u >> 16 & 0x8000u) | 1u);
     }
-    *hi = E::cut(x);
-    const u16 rest = E::enc(x - E::dec(*hi));
-    *lo = (rest & 0x7FFFu) != 0 || (u & 0x7FFFFFFFu) == 0 ? rest : static_cast<u16>(sign | 1u);
 }
 
 // ---- down: the product with the narrow matrix -------------------------------------------------------------------
@@ -410,11 +416,11 @@ __device__ inline void down_tile(const DownArgs& p, u32 block, char* lds) {
     auto put = [&](u64 t, u32 j, float v, float up) {
         if (j < p.rp) {
             if (p.zp) {
-                u16 hi, lo;
-                two_values<E>(E::kNarrow ? v * up : v, &hi, &lo);
+                u16 h[2];
+                in_terms<E, 2>(E::kNarrow ? v * up : v, h);
                 u16* to = p.zp + (t * p.rp + j / kDownRanks * kDownRanks) * 2 + j % kDownRanks;
-                to[0] = hi;
-                to[kDownRanks] = lo;
+                to[0] = h[0];
+                to[kDownRanks] = h[1];
             }
             if (p.z32) p.z32[t * p.rp + j] = v;
         }
@@ -1234,14 +1240,10 @@ __global__ __launch_bounds__(64 * kGradWaves, G == 1 ? 4 : 2) void k_adapter_gra
 #pragma unroll
                 for (u32 q = 0; q < 8; ++q) {
                     if (of_a) {
-                        float f = __uint_as_float(ru[g][q]) * up;
+                        u16 h[kTerms];
+                        in_terms<E, kTerms>(__uint_as_float(ru[g][q]) * up, h);
 #pragma unroll
-                        for (u32 t = 0; t < kTerms; ++t) {
-                            const u16 h = E::enc(f);
-                            fu[g][t][q >> 1] |= static_cast<u32>(h) << (16 * (q & 1u));
-                            f -= E::dec(h);
-                            f = __builtin_fabsf(f) < INFINITY ? f : 0.0f;
-                        }
+                        for (u32 t = 0; t < kTerms; ++t) fu[g][t][q >> 1] |= static_cast<u32>(h[t]) << (16 * (q & 1u));
                     } else {
                         fu[g][0][q >> 1] |= ru[g][q] << (16 * (q & 1u));
                     }

@@ -146,3 +146,22 @@ def test_gradients_beside_scales_of_any_size(dtype, scale):
     tol = 1.01 * (((N + 16) * H * dzs + 2 * c.u ** 2 * dz.abs()).t().contiguous() @ x.abs() + (2 * T + 16) * H * (dz.abs().t().contiguous() @ x.abs()))
     tol = tol + 2.0 ** -38 * dz.abs().max() * x.abs().sum(0)[None] + 2.0 ** -140 * T
     c.within(c.grads[0][0], dz.t().contiguous() @ x, tol, "grad_A")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_infinities_of_x_keep_their_sign_in_gradients(dtype):
+    """dz times an infinity of x is an infinity of its sign, also where dz needs no more than one 16-bit value."""
+    T, K, N, r = 70, 64, 48, 6
+    c = Case(dtype, T, K, N, [r], [0] * T)
+    A, B, s = c.adapters[0]
+    B[:, 0] = 0
+    B[3, 0] = 1                                                      # dz of rank 0 is a value of dy times the scale
+    c.z = torch.zeros(T, r, device=DEV, dtype=c.t)
+    c.x[5, 7], c.x[5, 9] = float("inf"), float("-inf")
+    assert bool((c.dy[5, 3] != 0).all())
+    c.backward()
+    dz = s * (c.dy.double() @ B.double())
+    got = c.grads[0][0].double()
+    assert torch.equal(got[:, 7], torch.sign(dz[5]) * float("inf")) and torch.equal(got[:, 9], torch.sign(dz[5]) * float("-inf"))
+    got[:, 7] = got[:, 9] = 0
+    assert bool(torch.isfinite(got).all()) and bool(torch.isfinite(c.grads[0][1]).all())
