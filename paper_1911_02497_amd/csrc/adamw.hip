@@ -131,7 +131,8 @@ condensa_status condensa_adamw_list_init(const condensa_adamw_tensor* tensors, i
 condensa_status condensa_lc_adamw_step(const condensa_adamw_list* list, const condensa_adamw_settings* s, void* stream) {
     if (list == nullptr || s == nullptr) return CONDENSA_ERR_NULL;
     if (list->table_dev == nullptr || list->map_dev == nullptr) return CONDENSA_ERR_NULL;
-    if ((list->state_bits != 32 && list->state_bits != 8) || !known_type(list->grad_type) || list->n_chunks * kAdamwChunk > kMaxElems + static_cast<u64>(CONDENSA_MAX_TENSORS) * kAdamwChunk)
+    if ((list->state_bits != 32 && list->state_bits != 8) || !known_type(list->grad_type) || (list->code_type != CONDENSA_TYPE_F16 && list->code_type != CONDENSA_TYPE_BF16) ||
+        list->n_chunks > kMaxElems / kAdamwChunk + static_cast<u64>(CONDENSA_MAX_TENSORS))
         return CONDENSA_ERR_ARG;
     if (s->rounding != CONDENSA_ROUND_NEAREST && s->rounding != CONDENSA_ROUND_STOCHASTIC) return CONDENSA_ERR_ARG;
     if (s->rounding == CONDENSA_ROUND_STOCHASTIC && list->state_bits != 8) return CONDENSA_ERR_ARG;
