@@ -51,7 +51,7 @@ def run(steps, dev="cuda"):
         losses.append(error.square().mean())
         dy = (error * (2 / error.numel()) * 2.0 ** 10).bfloat16()                # scaled up for the 16-bit type, and back in the step
         P.condensa_adapter_project_backward(dy, x, w, adapters, ids, z, dx=False, workspace=backward)
-        P.condensa_lc_adamw_step(adamw, 5e-3, step, seed=step, grad_scale=torch.full((1,), 2.0 ** -10, device=dev))
+        P.condensa_lc_adamw_step(adamw, 5e-3, step, seed=step * 0x9E3779B97F4A7C15, grad_scale=torch.full((1,), 2.0 ** -10, device=dev))
     one = torch.arange(0, TOKENS, TOKENS // REQUESTS, device=dev)
     answer = P.condensa_adapter_project(x[one], w, adapters, ids[one])["y"]
     return float(losses[0]), float(losses[-1]), float((answer.float() - target[one]).square().mean())

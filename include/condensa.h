@@ -434,7 +434,9 @@ enum { CONDENSA_TYPE_F32 = 0, CONDENSA_TYPE_F16 = 1, CONDENSA_TYPE_BF16 = 2 };
  * computes with the values before they are rounded.  Codes are rounded to the nearest (ties to even) or, with
  * CONDENSA_ROUND_STOCHASTIC, up with the probability that keeps the mean: rounding to nearest leaves a state where it is when one
  * step moves it by less than half the distance of two codes, which for beta2 near 1 is always.  The random bits are a hash of
- * `seed` (another one for every step) and of the element's place in the list, so equal seeds give equal results.  A positive
+ * `seed` (another one for every step) and of the element's place in the list, so equal seeds give equal results.  The seed's low half
+ * meets the place before it is mixed: seeds that differ in their low eight bits alone give the elements of a block the same words in another order.  A
+ * counter is better multiplied by an odd 64-bit constant first, which changes both halves from step to step.  A positive
  * sqrt(v) never becomes 0, infinities saturate, a NaN stays the element's own.
  */
 #define CONDENSA_STATE_BLOCK 256

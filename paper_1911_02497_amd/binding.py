@@ -767,7 +767,10 @@ def adamw_table(weights, grads, exp_avg, exp_avg_sq, **kw) -> AdamwTable:
 def condensa_lc_adamw_step(table: AdamwTable, lr, step, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0, mu=0.0, seed=None,
                            grad_scale=None, stream=None):
     """Marshals condensa_lc_adamw_step: one update of everything in ``table``.  ``seed``: 8-bit states are rounded by random bits
-    made from it (another one for every step), None: to nearest; states in 32 bits have nothing that a seed could decide.
+    made from it, another one for every step, best one whose high and low half both change (a counter times an odd 64-bit constant).
+    Without one they are rounded to nearest, where a second moment that moves by less than half the distance of two codes in a step,
+    which with betas[1] near 1 is all of them, keeps its ratio to the block's largest: give a seed to train with 8-bit states.  States in
+    32 bits have nothing that a seed could decide.
     ``grad_scale``: a float32 device scalar."""
     scale = None
     if grad_scale is not None:
