@@ -679,10 +679,12 @@ def _run(table, stream, entry, *args):
     import torch
     handle = _raw_stream()(table.index) if stream is None else int(_stream_on(table.device, stream).cuda_stream)
     if torch.cuda.current_device() == table.index:
-        _check(entry(*args, handle))
+        code = entry(*args, handle)
     else:
         with torch.cuda.device(table.index):
-            _check(entry(*args, handle))
+            code = entry(*args, handle)
+    if code:
+        _check(code)
 
 
 class _Table:
@@ -694,9 +696,9 @@ class _Table:
     def keep_for(self, stream):
         """Before a call on a stream: what the table holds is not handed out again before the work of that stream is done, although table and
         tensors are dropped.  (A graph that captured a call needs the table for as long as it is replayed.)"""
-        import torch
         handle = _raw_stream()(self.index) if stream is None else int(stream.cuda_stream)
         if handle not in self._streams:
+            import torch
             stream = torch.cuda.current_stream(self.device) if stream is None else stream
             for t in self._held:
                 t.record_stream(stream)
