@@ -674,15 +674,29 @@ def _wait_unless_captured(stream):
         stream.synchronize()
 
 
-def _run(table, stream, entry, *args):
-    """One call of a table's entry point, on the table's device and the given stream or that device's current one."""
+@functools.lru_cache(None)
+def _one_device():
     import torch
-    handle = _raw_stream()(table.index) if stream is None else int(_stream_on(table.device, stream).cuda_stream)
-    if torch.cuda.current_device() == table.index:
+    return torch.cuda.device_count() == 1
+
+
+def _handle_on(table, stream):
+    """Handle of the given stream or of the current one of the table's device."""
+    return _raw_stream()(table.index) if stream is None else int(_stream_on(table.device, stream).cuda_stream)
+
+
+def _run(table, stream, entry, *args):
+    """One call of a table's entry point, on the table's device and the given stream (or its handle) or that device's current one."""
+    handle = stream if type(stream) is int else _handle_on(table, stream)
+    if _one_device():
         code = entry(*args, handle)
     else:
-        with torch.cuda.device(table.index):
+        import torch
+        if torch.cuda.current_device() == table.index:
             code = entry(*args, handle)
+        else:
+            with torch.cuda.device(table.index):
+                code = entry(*args, handle)
     if code:
         _check(code)
 
@@ -694,15 +708,15 @@ class _Table:
         self._held, self._streams = [t for t in tensors if t is not None], set()
 
     def keep_for(self, stream):
-        """Before a call on a stream: what the table holds is not handed out again before the work of that stream is done, although table and
-        tensors are dropped.  (A graph that captured a call needs the table for as long as it is replayed.)"""
-        handle = _raw_stream()(self.index) if stream is None else int(stream.cuda_stream)
+        """Before a call on a stream, whose handle it returns: what the table holds is not handed out again before the work of that stream is
+        done, although table and tensors are dropped.  (A graph that captured a call needs the table for as long as it is replayed.)"""
+        handle = _handle_on(self, stream)
         if handle not in self._streams:
-            import torch
-            stream = torch.cuda.current_stream(self.device) if stream is None else stream
+            stream = _stream_on(self.device, stream)
             for t in self._held:
                 t.record_stream(stream)
             self._streams.add(handle)
+        return handle
 
 
 class AdamwTable(_Table):
@@ -785,8 +799,7 @@ def condensa_lc_adamw_step(table: AdamwTable, lr, step, betas=(0.9, 0.999), eps=
     else:
         rounding, seed = ROUND_STOCHASTIC, seed & 0xFFFFFFFFFFFFFFFF
     s = AdamwSettings(lr, betas[0], betas[1], eps, weight_decay, mu, rounding, step, seed, scale, 0)
-    table.keep_for(stream)
-    _run(table, stream, library().condensa_lc_adamw_step, table.ref, ctypes.byref(s))
+    _run(table, table.keep_for(stream), library().condensa_lc_adamw_step, table.ref, ctypes.byref(s))
 
 
 class AdapterTable(_Table):
@@ -907,8 +920,7 @@ def condensa_adapter_project(x, w, table: AdapterTable, token_adapter, y=None, z
     pz, ldz = (None, 0) if z is None else _kept_z(z, table, T)
     if workspace is None:
         workspace = _made_for(stream, adapter_workspace, table, T)
-    table.keep_for(stream)
-    _run(table, stream, library().condensa_adapter_project, table.ref, px, ldx, T, pw, ldw, ids, py, ldy, pz, ldz, workspace.data_ptr(),
+    _run(table, table.keep_for(stream), library().condensa_adapter_project, table.ref, px, ldx, T, pw, ldw, ids, py, ldy, pz, ldz, workspace.data_ptr(),
          workspace.numel())
     return {"y": y, "z": z, "workspace": workspace}
 
@@ -927,8 +939,7 @@ def condensa_adapter_project_backward(dy, x, w, table: AdapterTable, token_adapt
     pdx, lddx = (None, 0) if dx is False else _rows("dx", dx, table, T, table.n_in)
     if workspace is None:
         workspace = _made_for(stream, adapter_workspace, table, T, backward=True)
-    table.keep_for(stream)
-    _run(table, stream, library().condensa_adapter_project_backward, table.ref, pdy, lddy, px, ldx, T, pw, ldw, ids, pz, ldz, pdx, lddx,
+    _run(table, table.keep_for(stream), library().condensa_adapter_project_backward, table.ref, pdy, lddy, px, ldx, T, pw, ldw, ids, pz, ldz, pdx, lddx,
          workspace.data_ptr(), workspace.numel())
     return {"dx": None if dx is False else dx, "grads": table.grads, "workspace": workspace}
 
