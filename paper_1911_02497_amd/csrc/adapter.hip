@@ -35,10 +35,13 @@ static u32 run_tokens(i64 n_tokens, i64 n_in, i64 n_out) {
 // Ranks that a workgroup of the gradients takes, in sixteens.
 static u32 grad_groups(u32 max_rank) { return max_rank <= 16 ? 1 : 2; }
 
-// Workgroups that share the adapters of a tile of z: more where tiles are few.
+// Workgroups that share the adapters of a tile of z: more where tiles are few.  us of a forward call, 4608 -> 4096, with 4, 8 and 16: 700 tokens of 64
+// requests (22 tiles) 97, 90 and 90; 8192 tokens (256 tiles) 289, 292 and 304.
 static u32 down_shares(u32 tiles) { return tiles >= 64 ? 4 : (tiles >= 16 ? 8 : 16); }
 
-// Rows that are no multiple of eight long are copied to aligned rows beside z where more tokens than this use them.
+// Rows that are no multiple of eight long are copied to aligned rows beside z where more tokens than this use them.  650 -> 2600, us with copies and
+// without: 40 tokens 17.7 and 12.1, 400 tokens 20.6 and 23.8.  Up to 256 tokens, whose sums are split, rows as they are would be the faster ones
+// (96 tokens: 19.4 and 14.2).
 constexpr i64 kPackTokens = 64;
 // Sums run over whole steps of 64 of what is copied, into zeros: a last step of its own, with nothing under way before it, took 2 us.
 static i64 up_to(i64 n, i64 unit) { return (n + unit - 1) / unit * unit; }
@@ -57,7 +60,8 @@ struct Plan {
     size_t zp = 0, z32 = 0, part = 0, part_wide = 0, row_max = 0, order = 0, seg = 0, slots = 0, total = 0;
 };
 
-// Forward passes of up to this many tokens make z token by token.
+// Forward passes of up to this many tokens make z token by token and split their sums wherever tiles are few.  4608 -> 4096, us split and not: 192 tokens 27 and
+// 64; 384 tokens of 16 adapters 41 and 73, so more tokens than these would gain too.
 constexpr i64 kTokenwise = 256;
 
 static Plan make_plan(i64 T, i64 n_in, i64 n_out, u32 n_adapters, u32 max_rank, bool backward) {
@@ -79,8 +83,11 @@ static Plan make_plan(i64 T, i64 n_in, i64 n_out, u32 n_adapters, u32 max_rank, 
             const u64 others = backward || T > kTokenwise ? 128 : static_cast<u64>(T), room = 768 - others;
             u32 s = static_cast<u32>(room / tiles), most = steps / 2;
             s = s > most ? most : s;
+            // At most 16: 32 tokens 4608 -> 2048 take 17.3 us with up to 32, 16.3 with 16, and 13.4 with 4, which write fewer parts.
             s = s > 16 ? 16 : (s < 1 ? 1 : s);
-            if (T > kTokenwise && tiles > 128) s = 1;       // a tile a unit, with many steps under way
+            // A tile a unit, with many steps under way.  us whole and split: 512 tokens 4608 -> 1024 (128 tiles) 39 and 25, 1000 tokens 512 -> 512 (128) 17.0
+            // and 13.4, 1000 tokens 512 -> 1024 (256) 17.3 and 15.0: the border could lie higher.
+            if (T > kTokenwise && tiles > 128) s = 1;
             p.split = s > 1 || T <= kTokenwise;
             p.steps_each = (steps + s - 1) / s;
             p.splits = (steps + p.steps_each - 1) / p.steps_each;
@@ -168,7 +175,9 @@ static condensa_status launch_wide(WideArgs a, int rows, hipStream_t st) {
     // A tile of 256 rows fills a compute unit.  The one whose rounds over the 256 of them cost less is taken: 8192 x 4608 outputs are 2.25 rounds
     // of 256 x 256, which take as long as three, and three of 256 x 192.
     const auto cost = [&](u64 n) { return (tiles(256, n) + 255) / 256 * n; };
-    // Short sums are left to smaller tiles, whose adapters' share costs less.
+    // Short sums are left to smaller tiles.  8192 tokens -> 4096, us with 256 and with 128 rows: sums of 1024 113 and 120, of 512 88 and 91, of 256 76 and 75.
+    // Three quarters of a round are wanted: 3584 tokens 4608 -> 4096 (224 tiles) take 134 and 152 us, 2048 tokens (128 tiles) 100 and 88; 2816 tokens (176
+    // tiles), which this leaves to 128 rows, 109 and 132.
     if (rows == kRows16 && tiles(256, 256) >= 192 && a.n_sum >= 1024) {
         if (cost(192) < cost(256)) launch_wide_tile<E, 256, 192, 2, 4, 2, ALONG, kRows16>(a, st);
         else                       launch_wide_tile<E, 256, 256, 2, 4, 2, ALONG, kRows16>(a, st);

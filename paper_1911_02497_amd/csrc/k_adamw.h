@@ -161,7 +161,7 @@ __device__ inline float load_grad1(const void* p, u64 e) {
 // Every value is read once and written once and nothing is shared, so the bytes bound it.  A wavefront takes one block of 256
 // elements, four to a lane: 128-bit accesses of what is held in 32 bits are contiguous across it, and the largest magnitude of a
 // block of 8-bit states is found across its lanes alone.  604 M weights, states in 32 bits with penalty and 16-bit copy: 3.75 ms, 6.1 TB/s;
-// 44 M weights with 8-bit states rounded by random bits: 152 us, 4.6 TB/s, held up by the hash and the rounding beside the memory.
+// 44 M weights with 8-bit states rounded by random bits: 158 us, 4.5 TB/s, held up by the hash and the rounding beside the memory.
 template <int GRAD, bool STATE8, bool SR>
 __global__ __launch_bounds__(64) void k_adamw(AdamwArgs a) {
     constexpr u32 kSub = kAdamwChunk / kStateBlock;

@@ -400,7 +400,7 @@ __device__ inline void down_sums(const DownArgs& p, u32 t0, const u16* m, u32 ra
 // bounds it: wavefronts take every WAVES-th 64 values of its rows (nothing of x is shared between them) and add their sums up at the
 // end; thirty-two tokens share what is read of M_a.  Four to sixteen workgroups have the same tile and take its tokens' adapters, 32 ranks at a
 // time, in turn: a tile where one request ends and the next begins takes no longer than the others, and up to 128 ranks no longer than 32.
-// The first workgroups sort the tokens.  8192 tokens of 4608 values, rank 16: 27.6 us, 2.7 TB/s.
+// The first workgroups sort the tokens.  8192 tokens of 4608 values, rank 16: 30 us, 2.5 TB/s.
 template <typename E, bool ALONG, bool VECX, u32 WAVES>
 __device__ inline void down_tile(const DownArgs& p, u32 block, char* lds) {
     const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -603,8 +603,9 @@ __device__ inline u32 die_order(u32 i, u32 n) {
 // matrix instructions wait for neither LDS nor memory; wavefronts meet once a step, in its middle, where the next step has come and the
 // last read of this one is done.  Rows that are 4-byte aligned are loaded four bytes a lane; with others steps go through registers.
 // With `part` a workgroup sums a part of the steps and stores it in binary32; the adapters' share is then added with the parts.
-// Matrix instructions bound large products (8192 tokens, 4608 -> 4096: 288 us, 1.08 PFLOP/s), reading W those of few tokens, latency those between
-// (1333 tokens, 650 -> 2600: 25.7 us).
+// Matrix instructions bound large products (8192 tokens, 4608 -> 4096: 263 us, 1.18 PFLOP/s; the units' matrix pipes are busy 63 % of the time, and
+// 57 % backward, where the transposing LDS reads meet in banks in 21 % of LDS's cycles), reading W those of few tokens, latency those between
+// (1333 tokens, 650 -> 2600: 27.4 us).
 constexpr u32 wide_lds(u32 bm, u32 bn, u32 nb) { return nb * (bm + bn) * 128 + bm * 12; }
 template <typename E, int BM, int BN, int WM, int WN, u32 NB, bool ALONG, int ROWS>
 __device__ inline void wide_tile(const WideArgs& p, u32 block_id, u32 n_blocks, char* lds) {
@@ -961,7 +962,7 @@ __global__ __launch_bounds__(64 * WM * WN, NB * (BM + BN) * 128 > 80 * 1024 && W
 }
 
 // Where tiles of 64 outputs are few, the sum is split and z is made in the same launch: nothing in it waits for anything.  z comes first, its
-// chain of loads is the longest.  64 tokens of 64 adapters, 4608 -> 4096: 14.0 us, 4.1 TB/s, and 6.1 us for the join.
+// chain of loads is the longest.  64 tokens of 64 adapters, 4608 -> 4096: 17.4 us, 3.4 TB/s, and 5.8 us for the join.
 template <typename E, bool ALONG, int ROWS, int BM>
 __global__ __launch_bounds__(256, 3) void k_adapter_split(DownArgs d, WideArgs w, u32 down_blocks) {
     constexpr u32 NB = ROWS != kRowsAny ? 3 : 2;
@@ -1147,7 +1148,7 @@ constexpr u32 kGradCols = 128, kGradWaves = 8, kGradPass = 32 * kGradWaves;
 // fragments, a lane's eight tokens one by one; the next pass is on its way meanwhile.  dz enters as a sum of 16-bit values,
 // three of bfloat16 or two of float16, since a binary32 gradient would keep no more than 8 or 11 bits of one; for float16 a wavefront scales its dz by a
 // power of two first, so that the largest sits near the top of the type's range.
-// 8192 tokens, 4608 -> 4096, 8 adapters of rank 16: 33 us, 4.3 TB/s.  Workgroups after the gradients' add the parts of dx.
+// 8192 tokens, 4608 -> 4096, 8 adapters of rank 16: 35 us, 4.0 TB/s.  Workgroups after the gradients' add the parts of dx.
 template <typename E, bool VEC, int G>
 __global__ __launch_bounds__(64 * kGradWaves, G == 1 ? 4 : 2) void k_adapter_grads(GradArgs p, WideArgs dx, u32 joins) {
     constexpr u32 kTerms = E::kNarrow ? 2 : 3;
