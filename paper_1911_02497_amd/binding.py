@@ -655,14 +655,23 @@ def _device_of(tensors, what):
     return devices.pop() if devices else torch.device("cuda", torch.cuda.current_device())
 
 
+def _handle_on(device, stream):
+    """Handle of the stream of a call for tensors of ``device``: of the given one, which may be any object with a ``cuda_stream``, or of that
+    device's current one."""
+    if stream is None:
+        return _raw_stream()(device.index)
+    if getattr(stream, "device", device) != device:
+        raise ValueError(f"a stream of {stream.device} for tensors of {device}")
+    return int(stream.cuda_stream)
+
+
 def _stream_on(device, stream):
-    """The stream of a call for tensors of ``device``: the given one or that device's current one."""
+    """The same as torch's object."""
     import torch
+    handle = _handle_on(device, stream)
     if stream is None:
         return torch.cuda.current_stream(device)
-    if stream.device != device:
-        raise ValueError(f"a stream of {stream.device} for tensors of {device}")
-    return stream
+    return stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(handle, device=device)
 
 
 def _wait_unless_captured(stream):
@@ -680,14 +689,9 @@ def _one_device():
     return torch.cuda.device_count() == 1
 
 
-def _handle_on(table, stream):
-    """Handle of the given stream or of the current one of the table's device."""
-    return _raw_stream()(table.index) if stream is None else int(_stream_on(table.device, stream).cuda_stream)
-
-
 def _run(table, stream, entry, *args):
     """One call of a table's entry point, on the table's device and the given stream (or its handle) or that device's current one."""
-    handle = stream if type(stream) is int else _handle_on(table, stream)
+    handle = stream if type(stream) is int else _handle_on(table.device, stream)
     if _one_device():
         code = entry(*args, handle)
     else:
@@ -710,7 +714,7 @@ class _Table:
     def keep_for(self, stream):
         """Before a call on a stream, whose handle it returns: what the table holds is not handed out again before the work of that stream is
         done, although table and tensors are dropped.  (A graph that captured a call needs the table for as long as it is replayed.)"""
-        handle = _handle_on(self, stream)
+        handle = _handle_on(self.device, stream)
         if handle not in self._streams:
             stream = _stream_on(self.device, stream)
             for t in self._held:
@@ -864,15 +868,15 @@ def adapter_workspace(table: AdapterTable, n_tokens: int, backward: bool = False
     return torch.empty(need, dtype=torch.uint8, device=table.device)
 
 
-def _made_for(stream, make, *args, **kw):
+def _made_for(table, stream, make, *args, **kw):
     """A tensor made for a call: on another stream than the current one from that stream's memory, which work that is still under way on the
     current one cannot reach, and not handed out again before the current one, where the program goes on, is done with it."""
     if stream is None:
         return make(*args, **kw)
     import torch
-    with torch.cuda.stream(stream):
+    with torch.cuda.stream(_stream_on(table.device, stream)):
         t = make(*args, **kw)
-    t.record_stream(torch.cuda.current_stream(t.device))
+    t.record_stream(torch.cuda.current_stream(table.device))
     return t
 
 
@@ -912,14 +916,14 @@ def condensa_adapter_project(x, w, table: AdapterTable, token_adapter, y=None, z
     pw, ldw = _rows("w", w, table, table.n_out, table.n_in)
     ids = _token_ids(token_adapter, table, T)
     if y is None:
-        y = _made_for(stream, table.empty, T, table.n_out)
+        y = _made_for(table, stream, table.empty, T, table.n_out)
     py, ldy = _rows("y", y, table, T, table.n_out)
     if z is True:
-        z = _made_for(stream, table.empty, T, max(table.max_rank, 1))
+        z = _made_for(table, stream, table.empty, T, max(table.max_rank, 1))
     z = None if z is False else z
     pz, ldz = (None, 0) if z is None else _kept_z(z, table, T)
     if workspace is None:
-        workspace = _made_for(stream, adapter_workspace, table, T)
+        workspace = _made_for(table, stream, adapter_workspace, table, T)
     _run(table, table.keep_for(stream), library().condensa_adapter_project, table.ref, px, ldx, T, pw, ldw, ids, py, ldy, pz, ldz, workspace.data_ptr(),
          workspace.numel())
     return {"y": y, "z": z, "workspace": workspace}
@@ -935,10 +939,10 @@ def condensa_adapter_project_backward(dy, x, w, table: AdapterTable, token_adapt
     ids = _token_ids(token_adapter, table, T)
     pz, ldz = _kept_z(z, table, T)
     if dx is True:
-        dx = _made_for(stream, table.empty, T, table.n_in)
+        dx = _made_for(table, stream, table.empty, T, table.n_in)
     pdx, lddx = (None, 0) if dx is False else _rows("dx", dx, table, T, table.n_in)
     if workspace is None:
-        workspace = _made_for(stream, adapter_workspace, table, T, backward=True)
+        workspace = _made_for(table, stream, adapter_workspace, table, T, backward=True)
     _run(table, table.keep_for(stream), library().condensa_adapter_project_backward, table.ref, pdy, lddy, px, ldx, T, pw, ldw, ids, pz, ldz, pdx, lddx,
          workspace.data_ptr(), workspace.numel())
     return {"dx": None if dx is False else dx, "grads": table.grads, "workspace": workspace}

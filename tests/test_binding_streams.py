@@ -88,3 +88,10 @@ def test_whether_a_stream_is_captured_is_asked_of_that_stream(streams):
         streams.setattr(torch.cuda, "is_current_stream_capturing", lambda captured=captured: current[-1] == captured)
         B._wait_unless_captured(types.SimpleNamespace(name=asked, synchronize=lambda: waited.append(asked)))
         assert waited == want
+
+
+def test_any_object_with_a_stream_handle(streams):
+    assert B._handle_on(torch.device("cuda", 1), types.SimpleNamespace(cuda_stream=5)) == 5
+    calls = []
+    B._run(types.SimpleNamespace(index=1, device=torch.device("cuda", 1)), types.SimpleNamespace(cuda_stream=5), lambda *args: calls.append(args))
+    assert calls == [(5,)]

@@ -120,3 +120,24 @@ def test_workspaces_made_for_another_stream():
         torch.cuda.synchronize()
         at = out["workspace"].data_ptr()
         assert not any(abs(at - p) < n for p in places)
+
+
+def test_a_stream_that_is_only_a_handle():
+    """As the other entry points, tables' calls take any object that has a stream's handle."""
+    class Handle:
+        def __init__(self, stream):
+            self.cuda_stream = stream.cuda_stream
+
+    c = Case("bf16", 300, 128, 96, [8], [0] * 300)
+    c.forward()
+    c.backward()
+    want = [t.clone() for t in (c.y, c.z, c.dx, *c.grads[0])]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    handle = Handle(side)
+    table = P.adapter_table(c.adapters, grads=c.grads, stream=handle)
+    out = P.condensa_adapter_project(c.x, c.w, table, c.ids, z=True, stream=handle)
+    back = P.condensa_adapter_project_backward(c.dy, c.x, c.w, table, c.ids, out["z"], stream=handle)
+    torch.cuda.synchronize()
+    for got, right in zip((out["y"], out["z"], back["dx"], *c.grads[0]), want):
+        assert torch.equal(got, right)
