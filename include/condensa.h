@@ -544,6 +544,103 @@ condensa_status condensa_adapter_project_backward(const condensa_adapter_list* l
                                                   const uint16_t* z_dev, int64_t z_stride, uint16_t* dx_dev, int64_t dx_stride,
                                                   void* workspace_dev, size_t workspace_bytes, void* stream);
 
+/*
+ * ---- Matrices held in 8 bits with a scale for each block of 128, products with them, and the norm that feeds them ------
+ *
+ * A matrix [rows, cols] of E4M3 codes (condensa_quantize_fp8) with one binary32 scale for every block of block_rows x CONDENSA_FP8_BLOCK
+ * elements; its elements are code * scale.  block_rows = 1 is what activations and gradients have (a token's scales stand in its own
+ * row), block_rows = CONDENSA_FP8_BLOCK what weights have.  Blocks at the ends of rows and columns may be smaller.  Codes of a row are contiguous, rows q_stride
+ * bytes apart; scale is [ceil(rows / block_rows), ceil(cols / CONDENSA_FP8_BLOCK)] with rows scale_stride floats apart.  Any address and any
+ * stride will do; products are fastest where q and q_stride are multiples of 16.  Bytes between rows are neither read as
+ * elements nor written.  rows may be 0, with NULL pointers.
+ */
+#define CONDENSA_FP8_BLOCK 128
+typedef struct {
+    uint8_t* q;                     /* device [rows, cols]                                                    */
+    float*   scale;                 /* device, 4-byte aligned                                                 */
+    int64_t  rows, cols;            /* 0..2^24, 1..2^20                                                       */
+    int64_t  q_stride;              /* cols..2^22                                                             */
+    int64_t  scale_stride;          /* ceil(cols / CONDENSA_FP8_BLOCK)..2^20                                  */
+    int32_t  block_rows;            /* 1 or CONDENSA_FP8_BLOCK                                                */
+    int32_t  reserved;              /* must be 0                                                              */
+} condensa_fp8_matrix;
+
+/*
+ * Quantize for such matrices, and back.  scale = (largest finite magnitude of the block) / 448, or 0 where that magnitude is below 2^-100;
+ * code = the nearest code to x * 448 / (that magnitude), ties to the even fraction, of the exact quotient.  Infinities saturate, a NaN stays the
+ * element's own, a block of scale 0 has codes of zeros (NaN but for).  Zeros stay zeros.  x and dq have the type CONDENSA_TYPE_F32, _F16 or _BF16,
+ * contiguous rows x_stride / dq_stride elements apart (up to 2^22); dq = code * scale in binary32, rounded to the type.  No workspace; q and scale of `m` are what the first call
+ * writes and the second reads.
+ */
+condensa_status condensa_quantize_fp8_blocks(const void* x_dev, int type, int64_t x_stride, const condensa_fp8_matrix* m, void* stream);
+condensa_status condensa_dequantize_fp8_blocks(const condensa_fp8_matrix* m, void* dq_dev, int type, int64_t dq_stride, void* stream);
+
+/*
+ * Root-mean-square norm with the residual's addition, answered in 16 bits, in codes, or both.  For every token (row)
+ *   h = x + residual, rounded to the 16-bit type (h = x without a residual);   y = h * weight / sqrt(mean of h^2 + eps)
+ * and the codes are those of y in binary32, one scale for 128 columns.  Sums are binary32 in an order that depends on width and n_tokens alone.
+ * Squares outside the range of binary32 do not matter.  `sum` receives h; it may be `residual` or `x` itself (the same address and stride).
+ * n_tokens 0..2^24, width 1..CONDENSA_MAX_NORM_WIDTH, strides in elements, up to 2^22; x, residual, sum and y of `type` (CONDENSA_TYPE_F16 or
+ * _BF16), weight of weight_type (that one, or CONDENSA_TYPE_F32).  One launch, no workspace.
+ */
+#define CONDENSA_MAX_NORM_WIDTH 65536
+typedef struct {
+    const uint16_t* x;              /* device [n_tokens, width]                                               */
+    const uint16_t* residual;       /* NULL: none                                                             */
+    const void*     weight;         /* device [width], aligned for its type                                   */
+    uint16_t*       sum;            /* NULL: h is not wanted                                                  */
+    uint16_t*       y;              /* NULL: y is not wanted in 16 bits                                       */
+    const condensa_fp8_matrix* codes; /* host, NULL: no codes; [n_tokens, width], block_rows 1                */
+    int64_t         n_tokens, width;
+    int64_t         x_stride, residual_stride, sum_stride, y_stride;
+    int32_t         type, weight_type;
+    float           eps;            /* finite and positive                                                    */
+    int32_t         reserved;       /* must be 0                                                              */
+} condensa_rms_norm_call;
+condensa_status condensa_rms_norm(const condensa_rms_norm_call* call, void* stream);
+
+/*
+ * Its gradients.  With u = h / sqrt(mean of h^2 + eps) and g = dy * weight, for every token
+ *   dx = (g - u * mean of (g u)) / sqrt(mean of h^2 + eps) + dsum;   dweight = sum of dy * u over the tokens
+ * where dsum is the gradient that reaches h from elsewhere (NULL: none).  dx is the gradient of x and of the residual alike; it is answered in 16
+ * bits, in codes (a product's backward pass wants them), or both; dx may be dsum itself.  h is what the forward pass took the norm of.  dweight
+ * (NULL: not wanted) is binary32, written and not added to, zeros without a token.  Workspace: condensa_rms_norm_workspace_bytes, for calls with n_tokens
+ * tokens or fewer, 256-byte aligned; without dweight it may be NULL.
+ */
+typedef struct {
+    const uint16_t* dy;             /* device [n_tokens, width]                                               */
+    const uint16_t* h;
+    const uint16_t* dsum;           /* NULL: none                                                             */
+    const void*     weight;
+    uint16_t*       dx;             /* NULL: not wanted in 16 bits                                            */
+    float*          dweight;        /* NULL: not wanted                                                       */
+    const condensa_fp8_matrix* codes;
+    int64_t         n_tokens, width;
+    int64_t         dy_stride, h_stride, dsum_stride, dx_stride;
+    int32_t         type, weight_type;
+    float           eps;
+    int32_t         reserved;
+} condensa_rms_norm_grad_call;
+size_t condensa_rms_norm_workspace_bytes(int64_t n_tokens, int64_t width);        /* 0: invalid arguments */
+condensa_status condensa_rms_norm_backward(const condensa_rms_norm_grad_call* call, void* workspace_dev, size_t workspace_bytes, void* stream);
+
+/*
+ * Products with a weight matrix W [n_out, n_in] in 8 bits (block_rows CONDENSA_FP8_BLOCK), shared and not trained, as W of condensa_adapter_project is.
+ *   forward:   y[t]  = x[t] W^T,    x [n_tokens, n_in] in codes, block_rows 1;    y  [n_tokens, n_out]
+ *   backward:  dx[t] = dy[t] W,    dy [n_tokens, n_out] in codes, block_rows 1;   dx [n_tokens, n_in]
+ * y and dx have the 16-bit `type`, rounded to nearest, ties to even; values outside the range of binary16 become infinite.  The matrix instructions for 8-bit
+ * codes align eight neighbouring products to the largest of their exponents e and cut what lies below 2^(e - 13); sums of such eights, their scales and everything
+ * after are binary32, in an order that depends on the sizes and on how rows lie alone: equal calls give equal bits.  (For normal values the cut is a tenth of a rounding to
+ * bfloat16.)  NaN codes reach their own token's outputs and those of their own row or column of W alone.
+ * n_tokens as the adapters' (CONDENSA_ERR_SIZE); row strides of y and dx up to 2^22.  Workspace for calls with n_tokens tokens or
+ * fewer, 256-byte aligned; the two directions differ.
+ */
+size_t condensa_project_fp8_workspace_bytes(const condensa_fp8_matrix* w, int64_t n_tokens, int backward);        /* 0: invalid arguments */
+condensa_status condensa_project_fp8(const condensa_fp8_matrix* x, const condensa_fp8_matrix* w, uint16_t* y_dev, int64_t y_stride, int type,
+                                     void* workspace_dev, size_t workspace_bytes, void* stream);
+condensa_status condensa_project_fp8_backward(const condensa_fp8_matrix* dy, const condensa_fp8_matrix* w, uint16_t* dx_dev, int64_t dx_stride, int type,
+                                              void* workspace_dev, size_t workspace_bytes, void* stream);
+
 /* ---- process-wide DEFAULTS of the knobs above: what a NULL config stands for ---------------------- */
 enum {
     CONDENSA_OPT_SELECT_PATH   = 0, /* condensa_config.select_path   */

@@ -11,4 +11,6 @@ from .binding import (  # noqa: F401
     condensa_workspace_bytes, select_records, condensa_profile_read, condensa_profile_reset, condensa_launch_count,
     STATE_BLOCK, TYPE_F32, TYPE_F16, TYPE_BF16, ROUND_NEAREST, ROUND_STOCHASTIC, AdamwTable, adamw_table, condensa_lc_adamw_step,
     AdapterTable, adapter_table, adapter_workspace, condensa_adapter_project, condensa_adapter_project_backward,
+    FP8_BLOCK, Fp8Matrix, fp8_matrix, condensa_quantize_fp8_blocks, condensa_dequantize_fp8_blocks, condensa_rms_norm, rms_norm_workspace,
+    condensa_rms_norm_backward, project_fp8_workspace, condensa_project_fp8, condensa_project_fp8_backward,
 )

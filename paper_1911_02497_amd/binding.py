@@ -70,7 +70,36 @@ class AdapterList(ctypes.Structure):
                 ("max_rank", ctypes.c_int32), ("type", ctypes.c_int32), ("flags", ctypes.c_int32)]
 
 
+class Fp8MatrixDesc(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("q_stride", ctypes.c_int64),
+                ("scale_stride", ctypes.c_int64), ("block_rows", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class RmsNormCall(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("residual", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("sum", ctypes.c_void_p), ("y", ctypes.c_void_p),
+                ("codes", ctypes.POINTER(Fp8MatrixDesc)), ("n_tokens", ctypes.c_int64), ("width", ctypes.c_int64), ("x_stride", ctypes.c_int64),
+                ("residual_stride", ctypes.c_int64), ("sum_stride", ctypes.c_int64), ("y_stride", ctypes.c_int64), ("type", ctypes.c_int32),
+                ("weight_type", ctypes.c_int32), ("eps", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class RmsNormGradCall(ctypes.Structure):
+    _fields_ = [("dy", ctypes.c_void_p), ("h", ctypes.c_void_p), ("dsum", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("dx", ctypes.c_void_p),
+                ("dweight", ctypes.c_void_p), ("codes", ctypes.POINTER(Fp8MatrixDesc)), ("n_tokens", ctypes.c_int64), ("width", ctypes.c_int64),
+                ("dy_stride", ctypes.c_int64), ("h_stride", ctypes.c_int64), ("dsum_stride", ctypes.c_int64), ("dx_stride", ctypes.c_int64),
+                ("type", ctypes.c_int32), ("weight_type", ctypes.c_int32), ("eps", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
 _PROTOTYPES = {
+    "condensa_quantize_fp8_blocks": (ctypes.c_int32, [ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.POINTER(Fp8MatrixDesc), ctypes.c_void_p]),
+    "condensa_dequantize_fp8_blocks": (ctypes.c_int32, [ctypes.POINTER(Fp8MatrixDesc), ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_void_p]),
+    "condensa_rms_norm": (ctypes.c_int32, [ctypes.POINTER(RmsNormCall), ctypes.c_void_p]),
+    "condensa_rms_norm_workspace_bytes": (ctypes.c_size_t, [ctypes.c_int64, ctypes.c_int64]),
+    "condensa_rms_norm_backward": (ctypes.c_int32, [ctypes.POINTER(RmsNormGradCall), ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    "condensa_project_fp8_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(Fp8MatrixDesc), ctypes.c_int64, ctypes.c_int]),
+    "condensa_project_fp8": (ctypes.c_int32, [ctypes.POINTER(Fp8MatrixDesc), ctypes.POINTER(Fp8MatrixDesc), ctypes.c_void_p, ctypes.c_int64, ctypes.c_int,
+                                              ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    "condensa_project_fp8_backward": (ctypes.c_int32, [ctypes.POINTER(Fp8MatrixDesc), ctypes.POINTER(Fp8MatrixDesc), ctypes.c_void_p, ctypes.c_int64,
+                                                       ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
     "condensa_adapter_list_bytes": (ctypes.c_size_t, [ctypes.c_int]),
     "condensa_adapter_list_init": (ctypes.c_int32, [ctypes.POINTER(Adapter), ctypes.c_int, ctypes.c_int, ctypes.c_int64, ctypes.c_int64,
                                                     ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p, ctypes.POINTER(AdapterList)]),
@@ -946,6 +975,246 @@ def condensa_adapter_project_backward(dy, x, w, table: AdapterTable, token_adapt
     _run(table, table.keep_for(stream), library().condensa_adapter_project_backward, table.ref, pdy, lddy, px, ldx, T, pw, ldw, ids, pz, ldz, pdx, lddx,
          workspace.data_ptr(), workspace.numel())
     return {"dx": None if dx is False else dx, "grads": table.grads, "workspace": workspace}
+
+
+FP8_BLOCK = 128                     # columns (and rows, of a weight matrix) that share the scale of an 8-bit matrix
+
+
+@functools.lru_cache(None)
+def _types():
+    """dtype -> CONDENSA_TYPE_*, without a lookup of torch's module for every call."""
+    import torch
+    return {torch.float32: TYPE_F32, torch.float16: TYPE_F16, torch.bfloat16: TYPE_BF16}
+
+
+class _Place:
+    """A device as ``_run`` and ``_made_for`` want it."""
+
+    def __init__(self, device):
+        self.device, self.index = device, device.index
+
+
+@functools.lru_cache(None)
+def _place(index):
+    import torch
+    return _Place(torch.device("cuda", index))
+
+
+def _place_of(t, what):
+    if not t.is_cuda:
+        raise TypeError(f"{what} lies on a device")
+    return _place(t.get_device())
+
+
+class Fp8Matrix:
+    """condensa_fp8_matrix: E4M3 codes ``q`` (uint8 [rows, cols]) and ``scale`` (float32, one for every ``block_rows`` x 128 elements), rows of both contiguous.
+    The tensors must keep their storage.  ``block_rows`` is 1 for activations and gradients, 128 for weights.  See ``fp8_matrix``."""
+
+    def __init__(self, q, scale, block_rows=1):
+        import torch
+        rows, cols = q.shape if q.dim() == 2 else (-1, -1)
+        want = (-(-rows // block_rows) if block_rows in (1, FP8_BLOCK) else -1, -(-cols // FP8_BLOCK))
+        if not (q.is_cuda and q.dtype == torch.uint8 and q.dim() == 2 and cols > 0 and (q.stride(1) == 1 or cols == 1 or rows == 0)
+                and (rows <= 1 or q.stride(0) >= cols)):
+            raise TypeError("q: a uint8 device tensor [rows, cols] with contiguous rows")
+        if not (scale.device == q.device and scale.dtype == torch.float32 and tuple(scale.shape) == want and (scale.stride(1) == 1 or want[1] == 1 or rows == 0)
+                and (want[0] <= 1 or scale.stride(0) >= want[1])):
+            raise TypeError(f"scale: a float32 tensor {list(want)} with contiguous rows beside q, block_rows 1 or {FP8_BLOCK}")
+        self.q, self.scale, self.rows, self.cols, self.block_rows = q, scale, rows, cols, block_rows
+        self.device, self.index = q.device, q.get_device()
+        self.desc = Fp8MatrixDesc(q.data_ptr() or None, scale.data_ptr() or None, rows, cols, q.stride(0) if rows > 1 else cols,
+                                  scale.stride(0) if want[0] > 1 else want[1], block_rows, 0)
+        self.ref = ctypes.byref(self.desc)
+
+
+def fp8_matrix(rows, cols, block_rows=1, device="cuda") -> Fp8Matrix:
+    """Room for a matrix in 8 bits, in rows that begin at multiples of 128 bytes: products are fastest with those."""
+    import torch
+    q = torch.empty((rows, -(-cols // FP8_BLOCK) * FP8_BLOCK), dtype=torch.uint8, device=device)[:, :cols]
+    return Fp8Matrix(q, torch.empty((-(-rows // block_rows), -(-cols // FP8_BLOCK)), dtype=torch.float32, device=device), block_rows)
+
+
+def _operand(name, t, place, dtype, rows, cols):
+    """(address, row stride) of a two-dimensional operand whose rows are contiguous."""
+    shape, stride = t.shape, t.stride()
+    if not (len(shape) == 2 and shape[0] == rows and shape[1] == cols and t.dtype is dtype and t.get_device() == place.index
+            and (stride[1] == 1 or cols == 1 or rows == 0) and (rows <= 1 or stride[0] >= cols)):
+        raise TypeError(f"{name}: a {dtype} tensor [{rows}, {cols}] with contiguous rows on {place.device}")
+    return t.data_ptr() or None, (stride[0] if rows > 1 else cols)
+
+
+def _codes_for(codes, place, stream, rows, cols):
+    """The matrix that a call writes codes into: the given one, or room for it; None for none."""
+    if codes is None or codes is False:
+        return None
+    if codes is True:
+        return _made_matrix(place, stream, rows, cols, 1)
+    if not (codes.index == place.index and codes.rows == rows and codes.cols == cols and codes.block_rows == 1):
+        raise TypeError(f"codes: an Fp8Matrix [{rows}, {cols}] with block_rows 1 on {place.device}")
+    return codes
+
+
+def _made_matrix(place, stream, rows, cols, block_rows):
+    if stream is None:
+        return fp8_matrix(rows, cols, block_rows, place.device)
+    import torch
+    with torch.cuda.stream(_stream_on(place.device, stream)):
+        m = fp8_matrix(rows, cols, block_rows, place.device)
+    for t in (m.q, m.scale):
+        t.record_stream(torch.cuda.current_stream(place.device))
+    return m
+
+
+def _empty_like_rows(rows, cols, dtype, device):
+    import torch
+    return torch.empty((rows, cols), dtype=dtype, device=device)
+
+
+def condensa_quantize_fp8_blocks(x, out: Optional[Fp8Matrix] = None, block_rows=1, stream=None) -> Fp8Matrix:
+    """Marshals condensa_quantize_fp8_blocks: codes and scales of ``x`` (float32, float16 or bfloat16 [rows, cols]), into ``out`` or into a new matrix with
+    ``block_rows`` (1 for activations and gradients, 128 for weights)."""
+    place = _place_of(x, "x")
+    if x.dim() != 2 or x.dtype not in _types():
+        raise TypeError("x: a float32, float16 or bfloat16 tensor [rows, cols]")
+    rows, cols = x.shape
+    if out is None:
+        out = _made_matrix(place, stream, rows, cols, block_rows)
+    elif not (out.index == place.index and out.rows == rows and out.cols == cols):
+        raise TypeError(f"out: an Fp8Matrix [{rows}, {cols}] on {place.device}")
+    px, ldx = _operand("x", x, place, x.dtype, rows, cols)
+    _run(place, stream, library().condensa_quantize_fp8_blocks, px, _types()[x.dtype], ldx, out.ref)
+    return out
+
+
+def condensa_dequantize_fp8_blocks(m: Fp8Matrix, out=None, dtype=None, stream=None):
+    """Marshals condensa_dequantize_fp8_blocks: the values that ``m`` stands for, into ``out`` or into a new tensor of ``dtype`` (float32 by default)."""
+    import torch
+    place = _place(m.index)
+    if out is None:
+        out = _made_for(place, stream, _empty_like_rows, m.rows, m.cols, dtype or torch.float32, m.device)
+    if out.dtype not in _types():
+        raise TypeError("out is float32, float16 or bfloat16")
+    p, ld = _operand("out", out, place, out.dtype, m.rows, m.cols)
+    _run(place, stream, library().condensa_dequantize_fp8_blocks, m.ref, p, _types()[out.dtype], ld)
+    return out
+
+
+def _norm_weight(weight, place, dtype, width):
+    if not (weight.dim() == 1 and weight.shape[0] == width and weight.get_device() == place.index and weight.is_contiguous()
+            and (weight.dtype is dtype or _types().get(weight.dtype) == TYPE_F32)):
+        raise TypeError(f"weight: {width} contiguous values of {dtype} or float32 on {place.device}")
+    return weight.data_ptr(), _types()[weight.dtype]
+
+
+def _norm_rows(name, t, place):
+    if t.dim() != 2 or _types().get(t.dtype) not in (TYPE_F16, TYPE_BF16):
+        raise TypeError(f"{name}: a float16 or bfloat16 tensor [tokens, width]")
+    return t.shape[0], t.shape[1], t.dtype
+
+
+def _optional(name, t, place, dtype, rows, cols):
+    return (None, cols) if t is None else _operand(name, t, place, dtype, rows, cols)
+
+
+def condensa_rms_norm(x, weight, residual=None, eps=1e-6, sum=None, y=None, codes=None, stream=None):
+    """Marshals condensa_rms_norm.  ``sum`` (h = x + residual) is made where there is a residual and no tensor is given for it; False for none; it may be
+    ``residual`` or ``x`` itself.  ``y`` and ``codes``: a tensor and an Fp8Matrix to write, True to make one.  With neither, y is made."""
+    place = _place_of(x, "x")
+    T, n, dtype = _norm_rows("x", x, place)
+    made = lambda: _made_for(place, stream, _empty_like_rows, T, n, dtype, place.device)  # noqa: E731
+    if sum is True or (sum is None and residual is not None):
+        sum = made()
+    sum = None if sum is False else sum
+    if y is True or ((y is None or y is False) and (codes is None or codes is False)):
+        y = made()
+    y = None if y is False else y
+    codes = _codes_for(codes, place, stream, T, n)
+    px, ldx = _operand("x", x, place, dtype, T, n)
+    pr, ldr = _optional("residual", residual, place, dtype, T, n)
+    ps, lds = _optional("sum", sum, place, dtype, T, n)
+    py, ldy = _optional("y", y, place, dtype, T, n)
+    pw, wt = _norm_weight(weight, place, dtype, n)
+    call = RmsNormCall(px, pr, pw, ps, py, None if codes is None else ctypes.pointer(codes.desc), T, n, ldx, ldr, lds, ldy, _types()[dtype], wt, eps, 0)
+    _run(place, stream, library().condensa_rms_norm, ctypes.byref(call))
+    return {"sum": sum, "y": y, "codes": codes}
+
+
+def rms_norm_workspace(n_tokens, width, device="cuda"):
+    """Workspace of condensa_rms_norm_backward with ``n_tokens`` tokens or fewer, to be kept between calls."""
+    import torch
+    need = int(library().condensa_rms_norm_workspace_bytes(int(n_tokens), int(width)))
+    if need == 0:
+        raise ValueError("n_tokens or width is out of range")
+    return torch.empty(need, dtype=torch.uint8, device=device)
+
+
+def condensa_rms_norm_backward(dy, h, weight, dsum=None, eps=1e-6, dx=True, dweight=True, codes=None, workspace=None, stream=None):
+    """Marshals condensa_rms_norm_backward.  ``h``: what the norm was taken of (``sum`` of the forward call, or its x); ``dsum``: the gradient that reaches h from
+    elsewhere.  ``dx``, ``dweight`` and ``codes`` (dx in 8 bits): what to write, True to make one, False or None for none; ``dx`` may be ``dsum`` itself."""
+    place = _place_of(dy, "dy")
+    T, n, dtype = _norm_rows("dy", dy, place)
+    if dx is True:
+        dx = _made_for(place, stream, _empty_like_rows, T, n, dtype, place.device)
+    dx = None if dx is False else dx
+    if dweight is True:
+        import torch
+        dweight = _made_for(place, stream, torch.empty, n, dtype=torch.float32, device=place.device)
+    dweight = None if dweight is False else dweight
+    if dweight is not None and not (dweight.dim() == 1 and dweight.shape[0] == n and _types().get(dweight.dtype) == TYPE_F32 and dweight.get_device() == place.index
+                                    and dweight.is_contiguous()):
+        raise TypeError(f"dweight: {n} contiguous float32 on {place.device}")
+    codes = _codes_for(codes, place, stream, T, n)
+    if dweight is not None and workspace is None:
+        workspace = _made_for(place, stream, rms_norm_workspace, T, n, place.device)
+    pdy, lddy = _operand("dy", dy, place, dtype, T, n)
+    ph, ldh = _operand("h", h, place, dtype, T, n)
+    ps, lds = _optional("dsum", dsum, place, dtype, T, n)
+    pdx, lddx = _optional("dx", dx, place, dtype, T, n)
+    pw, wt = _norm_weight(weight, place, dtype, n)
+    call = RmsNormGradCall(pdy, ph, ps, pw, pdx, None if dweight is None else dweight.data_ptr(), None if codes is None else ctypes.pointer(codes.desc), T, n,
+                           lddy, ldh, lds, lddx, _types()[dtype], wt, eps, 0)
+    pws, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
+    _run(place, stream, library().condensa_rms_norm_backward, ctypes.byref(call), pws, size)
+    return {"dx": dx, "dweight": dweight, "codes": codes, "workspace": workspace}
+
+
+def project_fp8_workspace(w: Fp8Matrix, n_tokens, backward=False):
+    """Workspace of products of one direction with ``n_tokens`` tokens or fewer, to be kept between calls."""
+    import torch
+    need = int(library().condensa_project_fp8_workspace_bytes(w.ref, int(n_tokens), int(backward)))
+    if need == 0:
+        raise ValueError("n_tokens is out of range, or w has not blocks of 128 x 128")
+    return torch.empty(need, dtype=torch.uint8, device=w.device)
+
+
+def _product(entry, x, w, out, width, dtype, workspace, stream, backward):
+    if x.index != w.index:
+        raise TypeError("both matrices lie on one device")
+    place = _place(w.index)
+    if out is None:
+        if _types().get(dtype) not in (TYPE_F16, TYPE_BF16):
+            raise TypeError("without a tensor to write, dtype is float16 or bfloat16")
+        out = _made_for(place, stream, _empty_like_rows, x.rows, width, dtype, w.device)
+    kind = _types().get(out.dtype)
+    if kind not in (TYPE_F16, TYPE_BF16):
+        raise TypeError("products are float16 or bfloat16")
+    p, ld = _operand("the product", out, place, out.dtype, x.rows, width)
+    if workspace is None:
+        workspace = _made_for(place, stream, project_fp8_workspace, w, x.rows, backward)
+    _run(place, stream, entry, x.ref, w.ref, p, ld, kind, workspace.data_ptr(), workspace.numel())
+    return out, workspace
+
+
+def condensa_project_fp8(x: Fp8Matrix, w: Fp8Matrix, y=None, dtype=None, workspace=None, stream=None):
+    """Marshals condensa_project_fp8: y = x W^T, into ``y`` or into a new tensor of ``dtype`` (float16 or bfloat16)."""
+    y, workspace = _product(library().condensa_project_fp8, x, w, y, w.rows, dtype, workspace, stream, False)
+    return {"y": y, "workspace": workspace}
+
+
+def condensa_project_fp8_backward(dy: Fp8Matrix, w: Fp8Matrix, dx=None, dtype=None, workspace=None, stream=None):
+    """Marshals condensa_project_fp8_backward: dx = dy W, into ``dx`` or into a new tensor of ``dtype`` (float16 or bfloat16)."""
+    dx, workspace = _product(library().condensa_project_fp8_backward, dy, w, dx, w.cols, dtype, workspace, stream, True)
+    return {"dx": dx, "workspace": workspace}
 
 
 def condensa_mu_schedule(mu0: float, a: float, j: int) -> float:

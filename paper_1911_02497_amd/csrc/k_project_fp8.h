@@ -1,0 +1,212 @@
+// Products of matrices in E4M3 codes with a scale for each block of 128: y[t, n] = sum over blocks b of sx[t, b] sw[n / 128, b] sum over b's k of x[t, k] W[n, k], and
+// the same with W's other axis summed.
+//
+// All products run on the matrix instruction of 16 x 16 outputs and 128 products each, which is one block: its result, started from zero, is scaled and added
+// to binary32 sums.  An operand fragment of a wavefront is 16 rows of 128 codes: lane l holds row l % 16, codes 16 g .. + 15 and 64 + 16 g .. + 15 with
+// g = l / 16.  (Which codes a lane holds is free as long as both operands agree.)  Where the summed axis is the rows of a matrix in memory, tiles of it lie in
+// LDS as they are and the transposing LDS load collects the fragment.  A result puts its column in lane l % 16 and its rows 4 (l / 16) .. + 3 in four registers.
+#pragma once
+#include "k_rows.h"
+
+namespace condensa {
+
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef u32 u32x8 __attribute__((ext_vector_type(8)));
+typedef u32 u32x4_bytes __attribute__((ext_vector_type(4), aligned(1)));
+typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
+
+constexpr u32 kStep = CONDENSA_FP8_BLOCK;       // codes of a row that a step sums
+
+// Within eight neighbouring products what lies below 2^-13 of the largest (of its exponent) is cut, by this instruction and by the one for 32 products alike; the alternative is to widen
+// codes to 16 bits, at half the rate and twice the LDS.  Random codes: 2.7e-5 of the largest of 128 products on the mean, 3e-5 of their sum; bfloat16 rounds by 1.7e-3.
+__device__ inline f32x4 mfma_codes(u32x8 a, u32x8 b) {
+    // (no scales of the instruction's own: zeros for them choose the form without)
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(__builtin_bit_cast(i32x8, a), __builtin_bit_cast(i32x8, b), f32x4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0, 0, 0, 0);
+}
+
+// ---- tiles in LDS ---------------------------------------------------------------------------------------------------
+
+// Tiles with the summed axis along their rows: [rows][128], 16-byte pieces of a row at piece ^ (row & 7), so that eight rows of a fragment lie in
+// different banks although rows are 128 bytes apart.
+__device__ inline u32 codes_along_at(u32 row, u32 piece) { return row * kStep + ((piece ^ (row & 7u)) << 4); }
+__device__ inline u32x8 codes_along_frag(const u8* tile, u32 row0) {
+    const u32 l = threadIdx.x & 63, row = row0 + (l & 15), g = l >> 4;
+    const u32x4 a = *reinterpret_cast<const u32x4*>(tile + codes_along_at(row, g)), b = *reinterpret_cast<const u32x4*>(tile + codes_along_at(row, g + 4));
+    return u32x8{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+}
+
+// Tiles with the summed axis across their rows: [128][COLS].  The transposing load hands 16 lanes eight rows of 16 columns: lane s reads row s / 2, columns
+// 8 (s % 2) .. + 7, and receives column s of the eight rows.  Pieces of 16 bytes are moved so that the rows that 32 lanes read together (eight, and the
+// eight that are 16 further on) lie in different banks.
+template <u32 COLS>
+__device__ inline u32 codes_across_at(u32 k, u32 piece) {
+    constexpr u32 kPieces = COLS / 16;
+    static_assert(kPieces == 4 || kPieces == 8 || kPieces % 16 == 0, "widths of tiles");
+    const u32 slot = kPieces % 16 == 0 ? (k & 7u) | (k >> 1 & 8u) : (kPieces == 8 ? (k >> 1 & 3u) | (k >> 2 & 4u) : (k >> 2 & 1u) | (k >> 3 & 2u));
+    return k * COLS + ((piece ^ slot) << 4);
+}
+template <u32 COLS>
+__device__ inline u32x8 codes_across_frag(const u8* tile, u32 col0) {
+    const u32 l = threadIdx.x & 63, s = l & 15, k0 = (l >> 4) * 16 + (s >> 1);
+    u32x8 v;
+#pragma unroll
+    for (u32 i = 0; i < 4; ++i) {
+        const u8* at = tile + codes_across_at<COLS>(k0 + (i & 1) * 8 + (i >> 1) * 64, col0 >> 4) + (s & 1) * 8;
+        const i32x2 t = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)at);
+        v[2 * i] = static_cast<u32>(t.x);
+        v[2 * i + 1] = static_cast<u32>(t.y);
+    }
+    return v;
+}
+
+// Sixteen codes p[k .. k+15] of a row of n at any address, zeros past its end; what follows a row, up to the end of the matrix, is loaded and masked.  `left`: codes from
+// p[k] to that end.
+__device__ inline u32x4 load16_codes(const u8* p, i64 k, i64 n, i64 left) {
+    const i64 rest = n - k;
+    const int there = rest >= 16 ? 16 : (rest <= 0 ? 0 : static_cast<int>(rest));
+    u32x4 v = {0u, 0u, 0u, 0u};
+    if (there > 0) {
+        if (left >= 16) {
+            v = *reinterpret_cast<const u32x4_bytes*>(p + k);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 15; ++i) if (i < there) v[i >> 2] |= static_cast<u32>(p[k + i]) << (8 * (i & 3));
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int in = there - 4 * i;                        // codes of this word
+        v[i] &= in >= 4 ? ~0u : (in <= 0 ? 0u : (1u << (8 * in)) - 1u);
+    }
+    return v;
+}
+
+// ---- the product ----------------------------------------------------------------------------------------------------
+
+struct ProductArgs {
+    const u8* x; i64 ldx;                // [n_tokens, n_sum]
+    const float* xs; i64 ldxs;           // [n_tokens, steps]
+    const u8* w; i64 ldw;                // ALONG: [n_out, n_sum], else [n_sum, n_out]
+    const float* ws; i64 ldws;           // a scale for 128 x 128 of w
+    u16* y; i64 ldy;                     // [n_tokens, n_out]
+    u32 n_tokens, n_out, n_sum;
+    u32 splits, steps_each;              // steps of 128 codes that a split sums
+    float* part;                         // [splits][n_tokens][n_out], or NULL: y is written
+    u32 bf16;
+};
+
+__device__ inline u16 product_code(float x, u32 bf16) { return bf16 ? f32_to_bf16_rne(x) : f32_to_f16_rne(x); }
+
+// Four neighbouring outputs of a token, or parts of them.
+__device__ inline void store_product(const ProductArgs& p, u32 split, u32 t, u32 n, f32x4 v) {
+    if (t >= p.n_tokens) return;
+    if (p.part) {
+        float* out = p.part + (static_cast<u64>(split) * p.n_tokens + t) * p.n_out;
+        if (n + 4 <= p.n_out) *reinterpret_cast<f32x4_any*>(out + n) = v;
+        else
+#pragma unroll
+            for (u32 k = 0; k < 4; ++k) if (n + k < p.n_out) out[n + k] = v[k];
+        return;
+    }
+    u16* out = p.y + static_cast<i64>(t) * p.ldy;
+    u16 h[4];
+#pragma unroll
+    for (u32 k = 0; k < 4; ++k) h[k] = product_code(v[k], p.bf16);
+    if (n + 4 <= p.n_out) {
+        *reinterpret_cast<u32x2_any*>(out + n) = u32x2{static_cast<u32>(h[0]) | static_cast<u32>(h[1]) << 16, static_cast<u32>(h[2]) | static_cast<u32>(h[3]) << 16};
+    } else {
+#pragma unroll
+        for (u32 k = 0; k < 4; ++k) if (n + k < p.n_out) out[n + k] = h[k];
+    }
+}
+
+// Tiles of 64 tokens by 64 outputs, rows at any address: steps go through registers, where what lies past the end of a row is masked.
+template <bool ALONG>
+__global__ __launch_bounds__(256) void k_product_any(ProductArgs p) {
+    __shared__ __align__(16) u8 lds[2][128 * kStep];
+    const u32 tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave >> 1, wn = wave & 1;
+    const u32 tiles_n = (p.n_out + 63) / 64;
+    const u32 block = die_order(blockIdx.x, gridDim.x), tile = block / p.splits, split = block % p.splits;
+    const u32 t0 = tile / tiles_n * 64, n0 = tile % tiles_n * 64;
+    const u32 all = (p.n_sum + kStep - 1) / kStep, begin = split * p.steps_each, end = begin + p.steps_each < all ? begin + p.steps_each : all;
+    f32x4 acc[2][2] = {};
+    u32x4 rx[2], rw[2];
+    auto fetch = [&](u32 s) {
+        const i64 k0 = static_cast<i64>(s) * kStep;
+#pragma unroll
+        for (u32 i = 0; i < 2; ++i) {
+            const u32 at = i * 256 + tid, row = at >> 3;
+            const i64 k = k0 + (at & 7u) * 16;
+            const u32 t = t0 + row < p.n_tokens ? t0 + row : p.n_tokens - 1;
+            rx[i] = load16_codes(p.x + static_cast<i64>(t) * p.ldx, k, p.n_sum, static_cast<i64>(p.n_tokens - 1 - t) * p.ldx + p.n_sum - k);
+            if (ALONG) {
+                const u32 n = n0 + row < p.n_out ? n0 + row : p.n_out - 1;
+                rw[i] = load16_codes(p.w + static_cast<i64>(n) * p.ldw, k, p.n_sum, static_cast<i64>(p.n_out - 1 - n) * p.ldw + p.n_sum - k);
+            } else {
+                const i64 r = k0 + (at >> 2), n = n0 + (at & 3u) * 16;
+                rw[i] = load16_codes(p.w + r * p.ldw, n, r < p.n_sum ? p.n_out : 0, (p.n_sum - 1 - r) * p.ldw + p.n_out - n);
+            }
+        }
+    };
+    if (begin < end) fetch(begin);
+    u32 to = 0;
+    for (u32 s = begin; s < end; ++s) {
+        u8* sx = lds[to];
+        u8* sw = sx + 64 * kStep;
+#pragma unroll
+        for (u32 i = 0; i < 2; ++i) {
+            const u32 at = i * 256 + tid;
+            *reinterpret_cast<u32x4*>(sx + codes_along_at(at >> 3, at & 7u)) = rx[i];
+            *reinterpret_cast<u32x4*>(sw + (ALONG ? codes_along_at(at >> 3, at & 7u) : codes_across_at<64>(at >> 2, at & 3u))) = rw[i];
+        }
+        const float by = p.ws[ALONG ? static_cast<i64>(n0 / kStep) * p.ldws + s : static_cast<i64>(s) * p.ldws + n0 / kStep];
+        float scale[2];
+#pragma unroll
+        for (u32 j = 0; j < 2; ++j) {
+            const u32 t = t0 + wm * 32 + j * 16 + (lane & 15);
+            scale[j] = p.xs[static_cast<i64>(t < p.n_tokens ? t : p.n_tokens - 1) * p.ldxs + s] * by;
+        }
+        __syncthreads();
+        if (s + 1 < end) fetch(s + 1);
+        u32x8 fw[2];
+#pragma unroll
+        for (u32 i = 0; i < 2; ++i) fw[i] = ALONG ? codes_along_frag(sw, wn * 32 + i * 16) : codes_across_frag<64>(sw, wn * 32 + i * 16);
+#pragma unroll
+        for (u32 j = 0; j < 2; ++j) {
+            const u32x8 fx = codes_along_frag(sx, wm * 32 + j * 16);
+#pragma unroll
+            for (u32 i = 0; i < 2; ++i) {
+                const f32x4 v = mfma_codes(fw[i], fx);
+#pragma unroll
+                for (u32 k = 0; k < 4; ++k) acc[i][j][k] = __builtin_fmaf(v[k], scale[j], acc[i][j][k]);
+            }
+        }
+        to ^= 1;                                              // the one that all have read since the barrier before this one
+    }
+#pragma unroll
+    for (u32 j = 0; j < 2; ++j)
+#pragma unroll
+        for (u32 i = 0; i < 2; ++i) store_product(p, split, t0 + wm * 32 + j * 16 + (lane & 15), n0 + wn * 32 + i * 16 + (lane >> 4) * 4, acc[i][j]);
+}
+
+// The parts of split sums, added in order, four outputs a thread.
+__global__ __launch_bounds__(256) void k_product_join(ProductArgs p) {
+    const u32 n = (blockIdx.x * 256 + threadIdx.x) * 4, t = blockIdx.y;
+    if (n >= p.n_out) return;
+    const u64 each = static_cast<u64>(p.n_tokens) * p.n_out;
+    const float* from = p.part + static_cast<u64>(t) * p.n_out + n;
+    f32x4 v = {};
+    if (n + 4 <= p.n_out) {
+        for (u32 s = 0; s < p.splits; ++s) v += *reinterpret_cast<const f32x4_any*>(from + s * each);
+    } else {
+        for (u32 s = 0; s < p.splits; ++s)
+#pragma unroll
+            for (u32 k = 0; k < 4; ++k) if (n + k < p.n_out) v[k] += from[s * each + k];
+    }
+    ProductArgs q = p;
+    q.part = nullptr;
+    store_product(q, 0, t, n, v);
+}
+
+}  // namespace condensa

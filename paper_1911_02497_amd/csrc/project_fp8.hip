@@ -1,0 +1,94 @@
+// C-ABI entry points of products with matrices in 8 bits (include/condensa.h): checks, choice of form, launches.
+#include "fp8_matrix.h"
+#include "k_project_fp8.h"
+
+namespace condensa {
+
+struct ProductPlan {
+    u32 splits = 1, steps_each = 0;
+    size_t part = 0;                                          // bytes of the parts
+};
+
+constexpr u32 kMostSplits = 16;
+constexpr u64 kSplitTiles = 512;                              // tiles of parts that sums are split into, at most
+
+static ProductPlan make_plan(i64 T, i64 n_out, i64 n_sum) {
+    ProductPlan p;
+    const u32 steps = static_cast<u32>(blocks_of(n_sum));
+    const u64 tiles = static_cast<u64>((T + 63) / 64) * ((n_out + 63) / 64);
+    u64 s = tiles ? kSplitTiles / tiles : 1;
+    s = std::min<u64>(s, std::min<u64>(kMostSplits, steps / 2));
+    s = s < 1 ? 1 : s;
+    p.steps_each = static_cast<u32>((steps + s - 1) / s);
+    p.splits = (steps + p.steps_each - 1) / p.steps_each;
+    if (p.splits > 1) p.part = align_up(static_cast<u64>(p.splits) * T * n_out * 4);
+    return p;
+}
+// What a call with T tokens and every call with fewer can do with: parts of most splits, or of as many tiles as sums are split into at all.
+static size_t workspace_for(i64 T, i64 n_out) {
+    const u64 b = std::min(static_cast<u64>(T) * n_out * 4 * kMostSplits, kSplitTiles * 64 * 64 * 4);
+    return b ? align_up(b) : 256;
+}
+
+static bool grid_fits(i64 n_tokens, i64 n_wide) { return static_cast<u64>((n_tokens + 63) / 64) * ((n_wide + 63) / 64) < (static_cast<u64>(1) << 24); }
+
+static condensa_status product(const condensa_fp8_matrix* x, const condensa_fp8_matrix* w, uint16_t* y, i64 y_stride, int type, void* workspace, size_t workspace_bytes,
+                               bool along, void* stream) {
+    condensa_status rc = check_matrix(w, CONDENSA_FP8_BLOCK);
+    if (rc == CONDENSA_OK) rc = check_matrix(x, 1);
+    if (rc != CONDENSA_OK) return rc;
+    if (w->rows < 1 || w->rows > kMaxFp8Cols) return CONDENSA_ERR_SHAPE;
+    const i64 T = x->rows, n_sum = along ? w->cols : w->rows, n_out = along ? w->rows : w->cols;
+    if (x->cols != n_sum || y_stride < n_out || y_stride > kMaxRowStride) return CONDENSA_ERR_SHAPE;
+    if (type != CONDENSA_TYPE_F16 && type != CONDENSA_TYPE_BF16) return CONDENSA_ERR_ARG;
+    if (T > 0 && !y) return CONDENSA_ERR_NULL;
+    if (!aligned_to(y, 2)) return CONDENSA_ERR_ARG;
+    if (T == 0) return CONDENSA_OK;
+    if (!grid_fits(T, n_out)) return CONDENSA_ERR_SIZE;
+    const ProductPlan p = make_plan(T, n_out, n_sum);
+    if (!workspace || !aligned_to(workspace, 256) || workspace_bytes < p.part) return CONDENSA_ERR_WORKSPACE;
+    ByteRange r[] = {codes_range(x, false), scales_range(x, false), codes_range(w, false), scales_range(w, false),
+                     byte_range(y, rows_bytes(T, y_stride, n_out, 2), true), byte_range(p.part ? workspace : nullptr, p.part, true)};
+    if (ranges_conflict(r, sizeof(r) / sizeof(r[0]))) return CONDENSA_ERR_ARG;
+    ProductArgs a{};
+    a.x = x->q; a.ldx = x->q_stride; a.xs = x->scale; a.ldxs = x->scale_stride;
+    a.w = w->q; a.ldw = w->q_stride; a.ws = w->scale; a.ldws = w->scale_stride;
+    a.y = y; a.ldy = y_stride;
+    a.n_tokens = static_cast<u32>(T); a.n_out = static_cast<u32>(n_out); a.n_sum = static_cast<u32>(n_sum);
+    a.splits = p.splits; a.steps_each = p.steps_each;
+    a.part = p.part ? static_cast<float*>(workspace) : nullptr;
+    a.bf16 = type == CONDENSA_TYPE_BF16;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const dim3 grid((a.n_tokens + 63) / 64 * ((a.n_out + 63) / 64) * a.splits);
+    if (along) hipLaunchKernelGGL((k_product_any<true>), grid, dim3(256), 0, st, a);
+    else       hipLaunchKernelGGL((k_product_any<false>), grid, dim3(256), 0, st, a);
+    CONDENSA_LAUNCH_CHECK();
+    if (a.part) {
+        hipLaunchKernelGGL(k_product_join, dim3((a.n_out + 1023) / 1024, a.n_tokens), dim3(256), 0, st, a);
+        CONDENSA_LAUNCH_CHECK();
+    }
+    return CONDENSA_OK;
+}
+
+}  // namespace condensa
+
+using namespace condensa;
+
+extern "C" {
+
+size_t condensa_project_fp8_workspace_bytes(const condensa_fp8_matrix* w, int64_t n_tokens, int backward) {
+    if (check_matrix(w, CONDENSA_FP8_BLOCK) != CONDENSA_OK || w->rows < 1 || w->rows > kMaxFp8Cols || n_tokens < 0 || n_tokens > kMaxFp8Rows) return 0;
+    return workspace_for(n_tokens, backward ? w->cols : w->rows);
+}
+
+condensa_status condensa_project_fp8(const condensa_fp8_matrix* x, const condensa_fp8_matrix* w, uint16_t* y_dev, int64_t y_stride, int type,
+                                     void* workspace_dev, size_t workspace_bytes, void* stream) {
+    return product(x, w, y_dev, y_stride, type, workspace_dev, workspace_bytes, true, stream);
+}
+
+condensa_status condensa_project_fp8_backward(const condensa_fp8_matrix* dy, const condensa_fp8_matrix* w, uint16_t* dx_dev, int64_t dx_stride, int type,
+                                              void* workspace_dev, size_t workspace_bytes, void* stream) {
+    return product(dy, w, dx_dev, dx_stride, type, workspace_dev, workspace_bytes, false, stream);
+}
+
+}  // extern "C"
