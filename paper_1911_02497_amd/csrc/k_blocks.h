@@ -131,38 +131,29 @@ __device__ inline BlockBy block_by(u32 top_bits) {
     return b;
 }
 
-// Four codes of x 448 / top.  EXACT: of the exact quotient.  The product with a rounded reciprocal is up to 1.5 units off, which decides wrongly where the quotient is
-// the middle of two codes, as it often is for short significands, or within those units of one.  Its remainder, which two fused operations give, brings it to the
-// nearest value; the sign of what then remains is put below its last bit, where it decides what would be a tie.
-template <bool EXACT>
+// Four codes of x 448 / top, of the exact quotient.  The product with a rounded reciprocal is up to 1.5 units off, which decides wrongly where the quotient is the middle of
+// two codes, as it often is for short significands, or within those units of one.  Its remainder, which two fused operations give, brings it to the nearest value; the
+// sign of what then remains is put below its last bit, where it decides what would be a tie.
 __device__ inline u32 codes4(const float* x, const BlockBy& b) {
     float y[4];
-    const float pre = EXACT && b.top >= 0x1p64f ? 0x1p-64f : 1.0f, top = b.top * pre, down = EXACT ? b.by * (1.0f / 448.0f) / pre : 0.0f;
+    const float pre = b.top >= 0x1p64f ? 0x1p-64f : 1.0f, top = b.top * pre, down = b.by * (1.0f / 448.0f) / pre;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        float q;
-        if (EXACT) {
-            const float a = __builtin_fabsf(x[k]), p = a * pre * 448.0f, rest = __builtin_fmaf(a * pre, 448.0f, -p);
-            q = a * b.by;
-            q = __builtin_fmaf(__builtin_fmaf(-q, top, p) + rest, down, q);
-            const float left = __builtin_fmaf(-q, top, p) + rest;
-            u32 bits = __float_as_uint(q);
-            if (left != 0.0f && bits != 0) bits = (bits - (left < 0.0f ? 1u : 0u)) | 1u;
-            q = __builtin_copysignf(__uint_as_float(bits), x[k]);
-        } else {
-            q = x[k] * b.by;
-        }
+        const float a = __builtin_fabsf(x[k]), p = a * pre * 448.0f, rest = __builtin_fmaf(a * pre, 448.0f, -p);
+        float q = a * b.by;
+        q = __builtin_fmaf(__builtin_fmaf(-q, top, p) + rest, down, q);
+        const float left = __builtin_fmaf(-q, top, p) + rest;
+        u32 bits = __float_as_uint(q);
+        if (left != 0.0f && bits != 0) bits = (bits - (left < 0.0f ? 1u : 0u)) | 1u;
+        q = __builtin_copysignf(__uint_as_float(bits), x[k]);
         // what is larger than the largest finite value is infinite
-        y[k] = __builtin_fabsf(x[k]) > b.top ? __builtin_copysignf(b.kept ? 448.0f : 0.0f, x[k]) : (__builtin_fabsf(q) > 448.0f ? __builtin_copysignf(448.0f, q) : q);
-        if (!b.kept && !(x[k] != x[k])) y[k] = __builtin_copysignf(0.0f, x[k]);
+        y[k] = a > b.top ? __builtin_copysignf(b.kept ? 448.0f : 0.0f, x[k]) : (__builtin_fabsf(q) > 448.0f ? __builtin_copysignf(448.0f, q) : q);
+        if (!b.kept && a == a) y[k] = __builtin_copysignf(0.0f, x[k]);
     }
     const int p = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
     return static_cast<u32>(__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], p, true));
 }
-template <bool EXACT>
-__device__ inline u32x2 codes8(const float (&x)[8], const BlockBy& b) {
-    return u32x2{codes4<EXACT>(x, b), codes4<EXACT>(x + 4, b)};
-}
+__device__ inline u32x2 codes8(const float (&x)[8], const BlockBy& b) { return u32x2{codes4(x, b), codes4(x + 4, b)}; }
 
 // ---- the codec ------------------------------------------------------------------------------------------------------
 
@@ -185,7 +176,7 @@ __global__ __launch_bounds__(256) void k_block_encode_rows(BlockArgs p) {
     float v[8];
     R::template load<VEC>(static_cast<const typename R::elem*>(p.x) + static_cast<i64>(row) * p.ldx, k, p.cols, v);
     const BlockBy b = block_by(largest_of16(largest8(v)));
-    store8_codes(p.q + static_cast<i64>(row) * p.ldq, k, p.cols, codes8<true>(v, b));
+    store8_codes(p.q + static_cast<i64>(row) * p.ldq, k, p.cols, codes8(v, b));
     if ((lane & 15u) == 0 && k < p.cols) p.scale[static_cast<i64>(row) * p.lds + k / kFp8Block] = b.scale;
 }
 
@@ -217,7 +208,7 @@ __global__ __launch_bounds__(256) void k_block_encode_squares(BlockArgs p) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const u32 row = row0 + i * 16;
-        if (row < p.rows) store8_codes(p.q + static_cast<i64>(row) * p.ldq, k, p.cols, codes8<true>(v[i], b));
+        if (row < p.rows) store8_codes(p.q + static_cast<i64>(row) * p.ldq, k, p.cols, codes8(v[i], b));
     }
     if (threadIdx.x == 0) p.scale[static_cast<i64>(row0 / kFp8Block) * p.lds + block] = b.scale;
 }
@@ -374,7 +365,7 @@ __global__ __launch_bounds__(64 * kNormWaves) void k_rms_norm(NormArgs p) {
         if (p.y) store8<VEC>(p.y + static_cast<i64>(row) * p.ldy, k, p.n, pack8<R>(a));
         if (p.q) {
             const BlockBy b = block_by(largest_of16(largest8(a)));
-            store8_codes(p.q + static_cast<i64>(row) * p.ldq, k, p.n, codes8<false>(a, b));
+            store8_codes(p.q + static_cast<i64>(row) * p.ldq, k, p.n, codes8(a, b));
             if ((lane & 15u) == 0 && k < p.n) p.scale[static_cast<i64>(row) * p.lds + k / kFp8Block] = b.scale;
         }
     }
@@ -454,7 +445,7 @@ __global__ __launch_bounds__(64 * kNormWaves) void k_rms_norm_grad(NormGradArgs 
             if (p.dx) store8<VEC>(p.dx + static_cast<i64>(row) * p.lddx, k, p.n, pack8<R>(a));
             if (p.q) {
                 const BlockBy b = block_by(largest_of16(largest8(a)));
-                store8_codes(p.q + static_cast<i64>(row) * p.ldq, k, p.n, codes8<false>(a, b));
+                store8_codes(p.q + static_cast<i64>(row) * p.ldq, k, p.n, codes8(a, b));
                 if ((lane & 15u) == 0 && k < p.n) p.scale[static_cast<i64>(row) * p.lds + k / kFp8Block] = b.scale;
             }
         }

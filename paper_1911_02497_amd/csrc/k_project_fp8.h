@@ -190,6 +190,195 @@ __global__ __launch_bounds__(256) void k_product_any(ProductArgs p) {
         for (u32 i = 0; i < 2; ++i) store_product(p, split, t0 + wm * 32 + j * 16 + (lane & 15), n0 + wn * 32 + i * 16 + (lane >> 4) * 4, acc[i][j]);
 }
 
+// Tiles of BM tokens by BN outputs of rows that are 16-byte aligned, NB steps in LDS.  Loads go straight into LDS, NB steps ahead of their use; a token's and W's scales of a step
+// come with it.  Sixteen tokens at a time meet the wavefront's fragments of W, their results are scaled and added while the next sixteen are multiplied, and the fragments of the
+// next step are read beside the last sixteen: wavefronts meet once a step, there, when the next step has come and the last read of this one is done.
+constexpr u32 product_lds(u32 bm, u32 bn, u32 nb) { return nb * ((bm + bn) * kStep + bm * 4 + 256); }
+template <int BM, int BN, int WM, int WN, int NB, bool ALONG>
+__device__ inline void product_tile(const ProductArgs& p, u32 block_id, u32 n_blocks, u8* lds) {
+    constexpr u32 kThreads = 64 * WM * WN, TM = BM / WM, TN = BN / WN, FM = TM / 16, FN = TN / 16;
+    constexpr u32 kXLoads = BM * 8 / kThreads, kWLoads = BN * 8 / kThreads, kLoads = kXLoads + kWLoads + 1;
+    constexpr u32 kTile = (BM + BN) * kStep, kBuffer = kTile + BM * 4 + 256;
+    constexpr bool kOneBlock = (BN % 128 == 0 || BN == 64) && 128 % TN == 0;             // a wavefront's outputs lie in one block of W
+    static_assert(WM * WN > BM / 64, "a wavefront for W's scales");
+    const u32 tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const u32 wm = wave / WN, wn = wave % WN;
+    const u32 tiles_m = (p.n_tokens + BM - 1) / BM, tiles_n = (p.n_out + BN - 1) / BN;
+    const u32 block = die_order(block_id, n_blocks);
+    const u32 tile = block / p.splits, split = block % p.splits;
+    // four rows of tiles at a time: tiles that run together share rows of x and of W
+    const u32 band = tile / (4 * tiles_n), in_band = tile % (4 * tiles_n), high = tiles_m - band * 4 < 4 ? tiles_m - band * 4 : 4;
+    const u32 t0 = (band * 4 + in_band % high) * BM, n0 = in_band / high * BN;
+    const u32 all = (p.n_sum + kStep - 1) / kStep, begin = split * p.steps_each, end = begin + p.steps_each < all ? begin + p.steps_each : all;
+    const u32 steps = end - begin;                                  // one at least
+    const u32 valid = end == all ? p.n_sum - (all - 1) * kStep : kStep;                  // codes of the last step
+
+    u32 xo[kXLoads], wo[kWLoads], so;                               // byte offsets of what this lane loads
+#pragma unroll
+    for (u32 i = 0; i < kXLoads; ++i) {
+        const u32 at = i * kThreads + tid, row = at >> 3, r = t0 + row < p.n_tokens ? row : p.n_tokens - 1 - t0;
+        xo[i] = r * static_cast<u32>(p.ldx) + ((at ^ row) & 7u) * 16;
+    }
+#pragma unroll
+    for (u32 i = 0; i < kWLoads; ++i) {
+        const u32 at = i * kThreads + tid;
+        if (ALONG) {
+            const u32 row = at >> 3, r = n0 + row < p.n_out ? row : p.n_out - 1 - n0;
+            wo[i] = r * static_cast<u32>(p.ldw) + ((at ^ row) & 7u) * 16;
+        } else {
+            constexpr u32 kRow = BN / 16;
+            const u32 k = at / kRow;
+            u32 col = codes_across_at<BN>(k, at % kRow) - k * BN;
+            if (n0 + col >= p.n_out) col = (p.n_out - 1 - n0) & ~15u;
+            wo[i] = k * static_cast<u32>(p.ldw) + col;
+        }
+    }
+    const char* xs = reinterpret_cast<const char*>(p.x + static_cast<i64>(t0) * p.ldx + begin * kStep);
+    const char* ws = reinterpret_cast<const char*>(ALONG ? p.w + static_cast<i64>(n0) * p.ldw + begin * kStep : p.w + static_cast<i64>(begin) * kStep * p.ldw + n0);
+    const char* ss;
+    const bool of_x = wave < BM / 64;                               // the wavefront loads scales of 64 tokens; else those of W
+    const u32 b0 = n0 / kStep, last_block = (p.n_out - 1) / kStep;
+    if (of_x) {
+        const u32 r = wave * 64 + lane;
+        so = (t0 + r < p.n_tokens ? r : p.n_tokens - 1 - t0) * static_cast<u32>(p.ldxs) * 4;
+        ss = reinterpret_cast<const char*>(p.xs + static_cast<i64>(t0) * p.ldxs + begin);
+    } else {
+        const u32 b = lane & 3u, at = b0 + b < last_block ? b : last_block - b0;
+        so = (ALONG ? at * static_cast<u32>(p.ldws) : at) * 4;
+        ss = reinterpret_cast<const char*>(p.ws + (ALONG ? static_cast<i64>(b0) * p.ldws + begin : static_cast<i64>(begin) * p.ldws + b0));
+    }
+    const i64 w_step = ALONG ? kStep : kStep * p.ldw, s_step = of_x || ALONG ? 4 : 4 * p.ldws;
+    const u32 lds0 = static_cast<u32>(reinterpret_cast<uintptr_t>((lds_void*)lds)), s_at = kTile + (of_x ? wave * 256 : BM * 4);
+
+    u32 loaded = 0, to = 0;
+    auto load = [&]() {                                             // the next step, or the last one again
+        if (loaded + 1 == steps && valid < kStep) {                 // what lies past the sum is loaded from its last codes
+#pragma unroll
+            for (u32 i = 0; i < kXLoads; ++i) {
+                const u32 at = i * kThreads + tid, piece = (at ^ (at >> 3)) & 7u;
+                xo[i] -= piece * 16 < valid ? 0 : (piece - (valid - 1) / 16) * 16;
+            }
+#pragma unroll
+            for (u32 i = 0; i < kWLoads; ++i) {
+                const u32 at = i * kThreads + tid;
+                if (ALONG) {
+                    const u32 piece = (at ^ (at >> 3)) & 7u;
+                    wo[i] -= piece * 16 < valid ? 0 : (piece - (valid - 1) / 16) * 16;
+                } else {
+                    const u32 k = at / (BN / 16);
+                    wo[i] -= k < valid ? 0 : (k - (valid - 1)) * static_cast<u32>(p.ldw);
+                }
+            }
+        }
+#pragma unroll
+        for (u32 i = 0; i < kXLoads; ++i) load_lds<16>(xo[i], xs, lds0 + to + (i * kThreads + wave * 64) * 16);
+#pragma unroll
+        for (u32 i = 0; i < kWLoads; ++i) load_lds<16>(wo[i], ws, lds0 + to + BM * kStep + (i * kThreads + wave * 64) * 16);
+        load_lds<4>(so, ss, lds0 + to + s_at);
+        ++loaded;
+        const bool more = loaded < steps;
+        xs += more ? kStep : 0;
+        ws += more ? w_step : 0;
+        ss += more ? s_step : 0;
+        to = to + kBuffer == NB * kBuffer ? 0 : to + kBuffer;
+    };
+    // zeros for what the last step has past the sum
+    auto clear = [&](u8* buffer) {
+        for (u32 at = tid; at < (ALONG ? BM + BN : BM) * 8; at += kThreads) {
+            const u32 piece = at & 7u;
+            if (piece * 16 + 16 <= valid) continue;
+            u32x4* v = reinterpret_cast<u32x4*>(buffer + codes_along_at(at >> 3, piece));
+            u32x4 t = *v;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int in = static_cast<int>(valid) - static_cast<int>(piece * 16 + 4 * i);
+                t[i] &= in >= 4 ? ~0u : (in <= 0 ? 0u : (1u << (8 * in)) - 1u);
+            }
+            *v = t;
+        }
+        if (!ALONG)
+            for (u32 at = valid * (BN / 16) + tid; at < kStep * (BN / 16); at += kThreads) *reinterpret_cast<u32x4*>(buffer + BM * kStep + at * 16) = u32x4{0u, 0u, 0u, 0u};
+        __syncthreads();
+    };
+
+    f32x4 acc[FN][FM] = {};
+    u32x8 fw[FN], fx;
+    float scale[FM], by[FN];
+    auto read_w = [&](const u8* buffer) {
+#pragma unroll
+        for (u32 i = 0; i < FN; ++i) fw[i] = ALONG ? codes_along_frag(buffer + BM * kStep, wn * TN + i * 16) : codes_across_frag<BN>(buffer + BM * kStep, wn * TN + i * 16);
+    };
+    auto read_x = [&](const u8* buffer, u32 j) { return codes_along_frag(buffer, wm * TM + j * 16); };
+    auto read_scales = [&](const u8* buffer) {
+        const float* s = reinterpret_cast<const float*>(buffer + kTile);
+#pragma unroll
+        for (u32 i = 0; i < (kOneBlock ? 1 : FN); ++i) by[i] = s[BM + (n0 % kStep + wn * TN + i * 16) / kStep];
+#pragma unroll
+        for (u32 j = 0; j < FM; ++j) scale[j] = s[wm * TM + j * 16 + (lane & 15)];
+        if (kOneBlock)
+#pragma unroll
+            for (u32 j = 0; j < FM; ++j) scale[j] *= by[0];
+    };
+    f32x4 v[2][FN];
+    auto add = [&](u32 j) {
+#pragma unroll
+        for (u32 i = 0; i < FN; ++i) {
+            const float s = kOneBlock ? scale[j] : scale[j] * by[i];
+#pragma unroll
+            for (u32 k = 0; k < 4; ++k) acc[i][j][k] = __builtin_fmaf(v[j & 1][i][k], s, acc[i][j][k]);
+            asm volatile("" : "+v"(acc[i][j]));                     // here, and not all of them at the end of the step, where results would wait in registers that there are not
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < NB; ++i) load();
+    meet_loads<(NB - 1) * kLoads>();
+    if (steps == 1 && valid < kStep) clear(lds);
+    read_w(lds);
+    fx = read_x(lds, 0);
+    read_scales(lds);
+    u32 from = 0;
+    for (u32 s = 0; s < steps; ++s) {
+        const u8* cur = lds + from;
+#pragma unroll
+        for (u32 j = 0; j < FM; ++j) {
+            u32x8 next;
+            if (j + 1 < FM) next = read_x(cur, j + 1);
+#pragma unroll
+            for (u32 i = 0; i < FN; ++i) v[j & 1][i] = mfma_codes(fw[i], fx);
+            if (j > 0 && j + 1 < FM) add(j - 1);
+            if (j + 1 < FM) fx = next;
+            // the order that is meant: the next sixteen tokens' reads, then products with the additions of the last ones' between them
+            if (j + 1 < FM) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+#pragma unroll
+            for (u32 i = 0; i < FN; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                if (j > 0 && j + 1 < FM) __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        meet_loads<(NB - 2) * kLoads>();
+        load();                                                     // where this step was
+        from = from + kBuffer == NB * kBuffer ? 0 : from + kBuffer;
+        u8* nxt = lds + from;
+        if (s + 2 == steps && valid < kStep) clear(nxt);
+        if (FM > 1) add(FM - 2);
+        read_w(nxt);
+        fx = read_x(nxt, 0);
+        add(FM - 1);
+        read_scales(nxt);
+    }
+    meet_loads<0>();
+#pragma unroll
+    for (u32 j = 0; j < FM; ++j)
+#pragma unroll
+        for (u32 i = 0; i < FN; ++i) store_product(p, split, t0 + wm * TM + j * 16 + (lane & 15), n0 + wn * TN + i * 16 + (lane >> 4) * 4, acc[i][j]);
+}
+template <int BM, int BN, int WM, int WN, int NB, bool ALONG>
+__global__ __launch_bounds__(64 * WM * WN, WM * WN <= 4 && product_lds(BM, BN, NB) > 80 * 1024 ? 1 : 2) void k_product(ProductArgs p) {
+    __shared__ __align__(16) u8 lds[product_lds(BM, BN, NB)];
+    product_tile<BM, BN, WM, WN, NB, ALONG>(p, blockIdx.x, gridDim.x, lds);
+}
+
 // The parts of split sums, added in order, four outputs a thread.
 __global__ __launch_bounds__(256) void k_product_join(ProductArgs p) {
     const u32 n = (blockIdx.x * 256 + threadIdx.x) * 4, t = blockIdx.y;

@@ -32,6 +32,29 @@ static size_t workspace_for(i64 T, i64 n_out) {
 
 static bool grid_fits(i64 n_tokens, i64 n_wide) { return static_cast<u64>((n_tokens + 63) / 64) * ((n_wide + 63) / 64) < (static_cast<u64>(1) << 24); }
 
+template <int BM, int BN, int WM, int WN, int NB, bool ALONG>
+static void launch_tile(const ProductArgs& a, hipStream_t st) {
+    const u64 tiles = (static_cast<u64>(a.n_tokens) + BM - 1) / BM * ((static_cast<u64>(a.n_out) + BN - 1) / BN) * a.splits;
+    hipLaunchKernelGGL((k_product<BM, BN, WM, WN, NB, ALONG>), dim3(static_cast<unsigned>(tiles)), dim3(64 * WM * WN), 0, st, a);
+}
+
+template <bool ALONG>
+static void launch_product(const ProductArgs& a, bool rows16, hipStream_t st) {
+    const auto tiles = [&](u64 m, u64 n) { return (a.n_tokens + m - 1) / m * ((a.n_out + n - 1) / n); };
+    if (!rows16) {
+        hipLaunchKernelGGL((k_product_any<ALONG>), dim3(static_cast<unsigned>(tiles(64, 64) * a.splits)), dim3(256), 0, st, a);
+    } else if (a.splits == 1 && tiles(256, 256) >= 192) {
+        launch_tile<256, 256, 2, 4, 2, ALONG>(a, st);
+    } else if (a.splits == 1 && tiles(128, 128) >= 192) {
+        launch_tile<128, 128, 2, 2, 2, ALONG>(a, st);
+    } else {
+        launch_tile<64, 64, 2, 2, 4, ALONG>(a, st);
+    }
+}
+
+// Rows that are 16-byte aligned.
+static bool rows16(const void* p, i64 stride) { return aligned_to(p, 16) && stride % 16 == 0; }
+
 static condensa_status product(const condensa_fp8_matrix* x, const condensa_fp8_matrix* w, uint16_t* y, i64 y_stride, int type, void* workspace, size_t workspace_bytes,
                                bool along, void* stream) {
     condensa_status rc = check_matrix(w, CONDENSA_FP8_BLOCK);
@@ -59,9 +82,9 @@ static condensa_status product(const condensa_fp8_matrix* x, const condensa_fp8_
     a.part = p.part ? static_cast<float*>(workspace) : nullptr;
     a.bf16 = type == CONDENSA_TYPE_BF16;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const dim3 grid((a.n_tokens + 63) / 64 * ((a.n_out + 63) / 64) * a.splits);
-    if (along) hipLaunchKernelGGL((k_product_any<true>), grid, dim3(256), 0, st, a);
-    else       hipLaunchKernelGGL((k_product_any<false>), grid, dim3(256), 0, st, a);
+    const bool fast = rows16(a.x, a.ldx) && rows16(a.w, a.ldw);
+    if (along) launch_product<true>(a, fast, st);
+    else       launch_product<false>(a, fast, st);
     CONDENSA_LAUNCH_CHECK();
     if (a.part) {
         hipLaunchKernelGGL(k_product_join, dim3((a.n_out + 1023) / 1024, a.n_tokens), dim3(256), 0, st, a);
