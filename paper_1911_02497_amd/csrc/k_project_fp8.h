@@ -42,7 +42,7 @@ __device__ inline u32x8 codes_along_frag(const u8* tile, u32 row0) {
 template <u32 COLS>
 __device__ inline u32 codes_across_at(u32 k, u32 piece) {
     constexpr u32 kPieces = COLS / 16;
-    static_assert(kPieces == 4 || kPieces == 8 || kPieces % 16 == 0, "widths of tiles");
+    static_assert(kPieces % 16 == 0 || kPieces == 8 || kPieces % 4 == 0, "widths of tiles");
     const u32 slot = kPieces % 16 == 0 ? (k & 7u) | (k >> 1 & 8u) : (kPieces == 8 ? (k >> 1 & 3u) | (k >> 2 & 4u) : (k >> 2 & 1u) | (k >> 3 & 2u));
     return k * COLS + ((piece ^ slot) << 4);
 }
@@ -98,17 +98,9 @@ struct ProductArgs {
 
 __device__ inline u16 product_code(float x, u32 bf16) { return bf16 ? f32_to_bf16_rne(x) : f32_to_f16_rne(x); }
 
-// Four neighbouring outputs of a token, or parts of them.
-__device__ inline void store_product(const ProductArgs& p, u32 split, u32 t, u32 n, f32x4 v) {
+// Four neighbouring outputs of a token.
+__device__ inline void store_outputs(const ProductArgs& p, u32 t, u32 n, f32x4 v) {
     if (t >= p.n_tokens) return;
-    if (p.part) {
-        float* out = p.part + (static_cast<u64>(split) * p.n_tokens + t) * p.n_out;
-        if (n + 4 <= p.n_out) *reinterpret_cast<f32x4_any*>(out + n) = v;
-        else
-#pragma unroll
-            for (u32 k = 0; k < 4; ++k) if (n + k < p.n_out) out[n + k] = v[k];
-        return;
-    }
     u16* out = p.y + static_cast<i64>(t) * p.ldy;
     u16 h[4];
 #pragma unroll
@@ -118,6 +110,17 @@ __device__ inline void store_product(const ProductArgs& p, u32 split, u32 t, u32
     } else {
 #pragma unroll
         for (u32 k = 0; k < 4; ++k) if (n + k < p.n_out) out[n + k] = h[k];
+    }
+}
+// Parts of them.
+__device__ inline void store_part(const ProductArgs& p, u32 split, u32 t, u32 n, f32x4 v) {
+    if (t >= p.n_tokens) return;
+    float* out = p.part + (static_cast<u64>(split) * p.n_tokens + t) * p.n_out;
+    if (n + 4 <= p.n_out) {
+        *reinterpret_cast<f32x4_any*>(out + n) = v;
+    } else {
+#pragma unroll
+        for (u32 k = 0; k < 4; ++k) if (n + k < p.n_out) out[n + k] = v[k];
     }
 }
 
@@ -187,7 +190,11 @@ __global__ __launch_bounds__(256) void k_product_any(ProductArgs p) {
 #pragma unroll
     for (u32 j = 0; j < 2; ++j)
 #pragma unroll
-        for (u32 i = 0; i < 2; ++i) store_product(p, split, t0 + wm * 32 + j * 16 + (lane & 15), n0 + wn * 32 + i * 16 + (lane >> 4) * 4, acc[i][j]);
+        for (u32 i = 0; i < 2; ++i) {
+            const u32 t = t0 + wm * 32 + j * 16 + (lane & 15), n = n0 + wn * 32 + i * 16 + (lane >> 4) * 4;
+            if (p.part) store_part(p, split, t, n, acc[i][j]);      // uniform
+            else        store_outputs(p, t, n, acc[i][j]);
+        }
 }
 
 // Tiles of BM tokens by BN outputs of rows that are 16-byte aligned, NB steps in LDS.  Loads go straight into LDS, NB steps ahead of their use; a token's and W's scales of a step
@@ -200,6 +207,7 @@ __device__ inline void product_tile(const ProductArgs& p, u32 block_id, u32 n_bl
     constexpr u32 kXLoads = BM * 8 / kThreads, kWLoads = BN * 8 / kThreads, kLoads = kXLoads + kWLoads + 1;
     constexpr u32 kTile = (BM + BN) * kStep, kBuffer = kTile + BM * 4 + 256;
     constexpr bool kOneBlock = (BN % 128 == 0 || BN == 64) && 128 % TN == 0;             // a wavefront's outputs lie in one block of W
+    constexpr u32 kEach = (kLoads + FM / 2 - 1) / (FM / 2);         // loads beside sixteen tokens, in the first half of a step
     static_assert(WM * WN > BM / 64, "a wavefront for W's scales");
     const u32 tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const u32 wm = wave / WN, wn = wave % WN;
@@ -251,7 +259,8 @@ __device__ inline void product_tile(const ProductArgs& p, u32 block_id, u32 n_bl
     const u32 lds0 = static_cast<u32>(reinterpret_cast<uintptr_t>((lds_void*)lds)), s_at = kTile + (of_x ? wave * 256 : BM * 4);
 
     u32 loaded = 0, to = 0;
-    auto load = [&]() {                                             // the next step, or the last one again
+    // Loads of the next step, or of the last one again, part by part.
+    auto load_begin = [&]() {
         if (loaded + 1 == steps && valid < kStep) {                 // what lies past the sum is loaded from its last codes
 #pragma unroll
             for (u32 i = 0; i < kXLoads; ++i) {
@@ -270,11 +279,13 @@ __device__ inline void product_tile(const ProductArgs& p, u32 block_id, u32 n_bl
                 }
             }
         }
-#pragma unroll
-        for (u32 i = 0; i < kXLoads; ++i) load_lds<16>(xo[i], xs, lds0 + to + (i * kThreads + wave * 64) * 16);
-#pragma unroll
-        for (u32 i = 0; i < kWLoads; ++i) load_lds<16>(wo[i], ws, lds0 + to + BM * kStep + (i * kThreads + wave * 64) * 16);
-        load_lds<4>(so, ss, lds0 + to + s_at);
+    };
+    auto load_part = [&](u32 q) {
+        if (q < kXLoads)             load_lds<16>(xo[q], xs, lds0 + to + (q * kThreads + wave * 64) * 16);
+        else if (q + 1 < kLoads)     load_lds<16>(wo[q - kXLoads], ws, lds0 + to + BM * kStep + ((q - kXLoads) * kThreads + wave * 64) * 16);
+        else if (q + 1 == kLoads)    load_lds<4>(so, ss, lds0 + to + s_at);
+    };
+    auto load_end = [&]() {
         ++loaded;
         const bool more = loaded < steps;
         xs += more ? kStep : 0;
@@ -301,12 +312,11 @@ __device__ inline void product_tile(const ProductArgs& p, u32 block_id, u32 n_bl
         __syncthreads();
     };
 
-    f32x4 acc[FN][FM] = {};
+    f32x4 acc[FN][FM] = {}, v[2][FN] = {};
     u32x8 fw[FN], fx;
-    float scale[FM], by[FN];
-    auto read_w = [&](const u8* buffer) {
-#pragma unroll
-        for (u32 i = 0; i < FN; ++i) fw[i] = ALONG ? codes_along_frag(buffer + BM * kStep, wn * TN + i * 16) : codes_across_frag<BN>(buffer + BM * kStep, wn * TN + i * 16);
+    float scale[FM], by[FN], last = 0.0f, last_by[FN] = {};
+    auto read_w = [&](const u8* buffer, u32 i) {
+        fw[i] = ALONG ? codes_along_frag(buffer + BM * kStep, wn * TN + i * 16) : codes_across_frag<BN>(buffer + BM * kStep, wn * TN + i * 16);
     };
     auto read_x = [&](const u8* buffer, u32 j) { return codes_along_frag(buffer, wm * TM + j * 16); };
     auto read_scales = [&](const u8* buffer) {
@@ -315,63 +325,114 @@ __device__ inline void product_tile(const ProductArgs& p, u32 block_id, u32 n_bl
         for (u32 i = 0; i < (kOneBlock ? 1 : FN); ++i) by[i] = s[BM + (n0 % kStep + wn * TN + i * 16) / kStep];
 #pragma unroll
         for (u32 j = 0; j < FM; ++j) scale[j] = s[wm * TM + j * 16 + (lane & 15)];
-        if (kOneBlock)
-#pragma unroll
-            for (u32 j = 0; j < FM; ++j) scale[j] *= by[0];
     };
-    f32x4 v[2][FN];
-    auto add = [&](u32 j) {
+    // results of sixteen tokens, scaled and added
+    auto add = [&](u32 j, float s, const float* s_by) {
 #pragma unroll
         for (u32 i = 0; i < FN; ++i) {
-            const float s = kOneBlock ? scale[j] : scale[j] * by[i];
+            const float f = s * s_by[kOneBlock ? 0 : i];
 #pragma unroll
-            for (u32 k = 0; k < 4; ++k) acc[i][j][k] = __builtin_fmaf(v[j & 1][i][k], s, acc[i][j][k]);
+            for (u32 k = 0; k < 4; ++k) acc[i][j][k] = __builtin_fmaf(v[j & 1][i][k], f, acc[i][j][k]);
             asm volatile("" : "+v"(acc[i][j]));                     // here, and not all of them at the end of the step, where results would wait in registers that there are not
         }
     };
+    static_assert(FM % 2 == 0, "two sets of results in turn");
 #pragma unroll
-    for (int i = 0; i < NB; ++i) load();
-    meet_loads<(NB - 1) * kLoads>();
+    for (int i = 0; i + 1 < NB; ++i) {
+        load_begin();
+#pragma unroll
+        for (u32 q = 0; q < kLoads; ++q) load_part(q);
+        load_end();
+    }
+    meet_loads<(NB - 2) * kLoads>();
     if (steps == 1 && valid < kStep) clear(lds);
-    read_w(lds);
+#pragma unroll
+    for (u32 i = 0; i < FN; ++i) read_w(lds, i);
     fx = read_x(lds, 0);
     read_scales(lds);
     u32 from = 0;
     for (u32 s = 0; s < steps; ++s) {
         const u8* cur = lds + from;
+        load_begin();                                               // where the step before this one was
 #pragma unroll
-        for (u32 j = 0; j < FM; ++j) {
-            u32x8 next;
-            if (j + 1 < FM) next = read_x(cur, j + 1);
+        for (u32 j = 0; j + 1 < FM; ++j) {
+            const u32x8 next = read_x(cur, j + 1);
+#pragma unroll
+            for (u32 q = j * kEach; q < (j + 1) * kEach; ++q) load_part(q);
 #pragma unroll
             for (u32 i = 0; i < FN; ++i) v[j & 1][i] = mfma_codes(fw[i], fx);
-            if (j > 0 && j + 1 < FM) add(j - 1);
-            if (j + 1 < FM) fx = next;
+            if (j == 0) add(FM - 1, last, last_by);
+            else        add(j - 1, scale[j - 1], by);
+            fx = next;
             // the order that is meant: the next sixteen tokens' reads, then products with the additions of the last ones' between them
-            if (j + 1 < FM) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
 #pragma unroll
             for (u32 i = 0; i < FN; ++i) {
                 __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                if (j > 0 && j + 1 < FM) __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
+                __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
+        load_end();
         meet_loads<(NB - 2) * kLoads>();
-        load();                                                     // where this step was
         from = from + kBuffer == NB * kBuffer ? 0 : from + kBuffer;
         u8* nxt = lds + from;
         if (s + 2 == steps && valid < kStep) clear(nxt);
-        if (FM > 1) add(FM - 2);
-        read_w(nxt);
+#pragma unroll
+        for (u32 i = 0; i < FN; ++i) {
+            v[(FM - 1) & 1][i] = mfma_codes(fw[i], fx);
+            read_w(nxt, i);
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, ALONG ? 2 : 4, 0);
+        }
         fx = read_x(nxt, 0);
-        add(FM - 1);
+        add(FM - 2, scale[FM - 2], by);
+        last = scale[FM - 1];
+#pragma unroll
+        for (u32 i = 0; i < (kOneBlock ? 1 : FN); ++i) last_by[i] = by[i];
         read_scales(nxt);
     }
+    add(FM - 1, last, last_by);
     meet_loads<0>();
+    if (p.part) {                                                   // uniform
 #pragma unroll
-    for (u32 j = 0; j < FM; ++j)
+        for (u32 j = 0; j < FM; ++j)
 #pragma unroll
-        for (u32 i = 0; i < FN; ++i) store_product(p, split, t0 + wm * TM + j * 16 + (lane & 15), n0 + wn * TN + i * 16 + (lane >> 4) * 4, acc[i][j]);
+            for (u32 i = 0; i < FN; ++i) store_part(p, split, t0 + wm * TM + j * 16 + (lane & 15), n0 + wn * TN + i * 16 + (lane >> 4) * 4, acc[i][j]);
+        return;
+    }
+    // Outputs pass through LDS, so that rows are stored in whole cache lines; 16-byte pieces at piece ^ (row & 7).  (Eight bytes a lane in sixteen rows: 15 us for a tile.)
+    constexpr u32 kPieces = BN / 8;
+    auto out_at = [&](u32 row, u32 piece) { return lds + row * (BN * 2) + ((piece ^ (row & 7u)) << 4); };
+    auto to_lds = [&](auto enc) {
+#pragma unroll
+        for (u32 j = 0; j < FM; ++j) {
+            const u32 row = wm * TM + j * 16 + (lane & 15);
+#pragma unroll
+            for (u32 i = 0; i < FN; ++i) {
+                const u32 col = wn * TN + i * 16 + (lane >> 4) * 4;
+                u16 h[4];
+#pragma unroll
+                for (u32 k = 0; k < 4; ++k) h[k] = enc(acc[i][j][k]);
+                *reinterpret_cast<u32x2*>(out_at(row, col / 8) + (col & 4u) * 2) =
+                    u32x2{static_cast<u32>(h[0]) | static_cast<u32>(h[1]) << 16, static_cast<u32>(h[2]) | static_cast<u32>(h[3]) << 16};
+            }
+        }
+    };
+    if (p.bf16) to_lds([](float x) { return f32_to_bf16_rne(x); });
+    else        to_lds([](float x) { return f32_to_f16_rne(x); });
+    __syncthreads();
+#pragma unroll 4
+    for (u32 at = tid; at < BM * kPieces; at += kThreads) {
+        const u32 row = at / kPieces, piece = at % kPieces, t = t0 + row, n = n0 + piece * 8;
+        if (t >= p.n_tokens || n >= p.n_out) continue;
+        const u32x4 v = *reinterpret_cast<const u32x4*>(out_at(row, piece));
+        u16* out = p.y + static_cast<i64>(t) * p.ldy + n;
+        if (n + 8 <= p.n_out) *reinterpret_cast<u32x4_any*>(out) = v;
+        else
+#pragma unroll
+            for (u32 k = 0; k < 7; ++k) if (n + k < p.n_out) out[k] = static_cast<u16>(v[k >> 1] >> (16 * (k & 1)));
+    }
 }
 template <int BM, int BN, int WM, int WN, int NB, bool ALONG>
 __global__ __launch_bounds__(64 * WM * WN, WM * WN <= 4 && product_lds(BM, BN, NB) > 80 * 1024 ? 1 : 2) void k_product(ProductArgs p) {
@@ -393,9 +454,7 @@ __global__ __launch_bounds__(256) void k_product_join(ProductArgs p) {
 #pragma unroll
             for (u32 k = 0; k < 4; ++k) if (n + k < p.n_out) v[k] += from[s * each + k];
     }
-    ProductArgs q = p;
-    q.part = nullptr;
-    store_product(q, 0, t, n, v);
+    store_outputs(p, t, n, v);
 }
 
 }  // namespace condensa

@@ -44,7 +44,11 @@ static void launch_product(const ProductArgs& a, bool rows16, hipStream_t st) {
     if (!rows16) {
         hipLaunchKernelGGL((k_product_any<ALONG>), dim3(static_cast<unsigned>(tiles(64, 64) * a.splits)), dim3(256), 0, st, a);
     } else if (a.splits == 1 && tiles(256, 256) >= 192) {
-        launch_tile<256, 256, 2, 4, 2, ALONG>(a, st);
+        // A tile of 256 rows fills a compute unit.  The one whose rounds over the 256 of them cost less is taken: 8192 x 4608 outputs are 2.25 rounds
+        // of 256 x 256, which take as long as three (193 us), and three of 256 x 192 (178 us).
+        const auto cost = [&](u64 n) { return (tiles(256, n) + 255) / 256 * n; };
+        if (cost(192) < cost(256)) launch_tile<256, 192, 2, 4, 2, ALONG>(a, st);
+        else                       launch_tile<256, 256, 2, 4, 2, ALONG>(a, st);
     } else if (a.splits == 1 && tiles(128, 128) >= 192) {
         launch_tile<128, 128, 2, 2, 2, ALONG>(a, st);
     } else {
