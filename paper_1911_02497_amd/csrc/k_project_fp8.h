@@ -200,14 +200,17 @@ __global__ __launch_bounds__(256) void k_product_any(ProductArgs p) {
 // Tiles of BM tokens by BN outputs of rows that are 16-byte aligned, NB steps in LDS.  Loads go straight into LDS, NB steps ahead of their use; a token's and W's scales of a step
 // come with it.  Sixteen tokens at a time meet the wavefront's fragments of W, their results are scaled and added while the next sixteen are multiplied, and the fragments of the
 // next step are read beside the last sixteen: wavefronts meet once a step, there, when the next step has come and the last read of this one is done.
-constexpr u32 product_lds(u32 bm, u32 bn, u32 nb) { return nb * ((bm + bn) * kStep + bm * 4 + 256); }
+constexpr u32 product_lds(u32 bm, u32 bn, u32 nb) { return nb * ((bm + bn) * kStep + bm * 4 + 256) + (bm == 256 ? 256 : 0); }
 template <int BM, int BN, int WM, int WN, int NB, bool ALONG>
 __device__ inline void product_tile(const ProductArgs& p, u32 block_id, u32 n_blocks, u8* lds) {
     constexpr u32 kThreads = 64 * WM * WN, TM = BM / WM, TN = BN / WN, FM = TM / 16, FN = TN / 16;
-    constexpr u32 kXLoads = BM * 8 / kThreads, kWLoads = BN * 8 / kThreads, kLoads = kXLoads + kWLoads + 1;
+    constexpr u32 kXLoads = BM * 8 / kThreads, kWLoads = BN * 8 / kThreads;
+    constexpr bool kFar = BM == 256;                                // one workgroup a unit, two steps in LDS: lines of later steps are asked for
+    constexpr u32 kLoads = kXLoads + kWLoads + 1 + kFar;
     constexpr u32 kTile = (BM + BN) * kStep, kBuffer = kTile + BM * 4 + 256;
     constexpr bool kOneBlock = (BN % 128 == 0 || BN == 64) && 128 % TN == 0;             // a wavefront's outputs lie in one block of W
     constexpr u32 kEach = (kLoads + FM / 2 - 1) / (FM / 2);         // loads beside sixteen tokens, in the first half of a step
+    constexpr u32 kAhead = 2;
     static_assert(WM * WN > BM / 64, "a wavefront for W's scales");
     const u32 tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const u32 wm = wave / WN, wn = wave % WN;
@@ -255,6 +258,23 @@ __device__ inline void product_tile(const ProductArgs& p, u32 block_id, u32 n_bl
         so = (ALONG ? at * static_cast<u32>(p.ldws) : at) * 4;
         ss = reinterpret_cast<const char*>(p.ws + (ALONG ? static_cast<i64>(b0) * p.ldws + begin : static_cast<i64>(begin) * p.ldws + b0));
     }
+    // Where only two steps fit LDS, a step's time does not hide a line that has to come from memory.  So one value of each line is loaded two steps before the
+    // line is, which brings it into the die's cache: a part of the lines by each of the tiles that run together and share them, x's by even wavefronts, W's by odd ones.
+    u32 fo = 0;
+    if (kFar) {
+        if ((wave & 1u) == 0) {
+            const u32 row = n0 / BN % 8 * 32 + wave / 2 * 8 + (lane & 7u);
+            fo = (t0 + row < p.n_tokens ? row : p.n_tokens - 1 - t0) * static_cast<u32>(p.ldx);
+        } else {
+            const u32 line = t0 / BM % 4 * 64 + wave / 2 * 16 + (lane & 15u);
+            if (ALONG) {
+                fo = (n0 + line < p.n_out ? line : p.n_out - 1 - n0) * static_cast<u32>(p.ldw);
+            } else {
+                const u32 col = (line & 1u) * kStep;
+                fo = (line >> 1) * static_cast<u32>(p.ldw) + (n0 + col < p.n_out ? col : 0);
+            }
+        }
+    }
     const i64 w_step = ALONG ? kStep : kStep * p.ldw, s_step = of_x || ALONG ? 4 : 4 * p.ldws;
     const u32 lds0 = static_cast<u32>(reinterpret_cast<uintptr_t>((lds_void*)lds)), s_at = kTile + (of_x ? wave * 256 : BM * 4);
 
@@ -282,8 +302,13 @@ __device__ inline void product_tile(const ProductArgs& p, u32 block_id, u32 n_bl
     };
     auto load_part = [&](u32 q) {
         if (q < kXLoads)             load_lds<16>(xo[q], xs, lds0 + to + (q * kThreads + wave * 64) * 16);
-        else if (q + 1 < kLoads)     load_lds<16>(wo[q - kXLoads], ws, lds0 + to + BM * kStep + ((q - kXLoads) * kThreads + wave * 64) * 16);
-        else if (q + 1 == kLoads)    load_lds<4>(so, ss, lds0 + to + s_at);
+        else if (q < kXLoads + kWLoads) load_lds<16>(wo[q - kXLoads], ws, lds0 + to + BM * kStep + ((q - kXLoads) * kThreads + wave * 64) * 16);
+        else if (q == kXLoads + kWLoads) load_lds<4>(so, ss, lds0 + to + s_at);
+        else if (q < kLoads) {
+            const bool there = loaded + kAhead < steps - (valid < kStep);          // a whole step; else the first value of what is loaded now
+            const char* at = (wave & 1u) == 0 ? xs + (there ? kAhead * kStep : 0) : ws + (there ? kAhead * w_step : 0);
+            load_lds<4>(there ? fo : 0u, at, lds0 + NB * kBuffer);
+        }
     };
     auto load_end = [&]() {
         ++loaded;
@@ -344,7 +369,7 @@ __device__ inline void product_tile(const ProductArgs& p, u32 block_id, u32 n_bl
         for (u32 q = 0; q < kLoads; ++q) load_part(q);
         load_end();
     }
-    meet_loads<(NB - 2) * kLoads>();
+    meet_loads<(NB - 2) * kLoads + kFar>();
     if (steps == 1 && valid < kStep) clear(lds);
 #pragma unroll
     for (u32 i = 0; i < FN; ++i) read_w(lds, i);
@@ -374,7 +399,7 @@ __device__ inline void product_tile(const ProductArgs& p, u32 block_id, u32 n_bl
             __builtin_amdgcn_sched_barrier(0);
         }
         load_end();
-        meet_loads<(NB - 2) * kLoads>();
+        meet_loads<(NB - 2) * kLoads + kFar>();
         from = from + kBuffer == NB * kBuffer ? 0 : from + kBuffer;
         u8* nxt = lds + from;
         if (s + 2 == steps && valid < kStep) clear(nxt);
@@ -438,6 +463,81 @@ template <int BM, int BN, int WM, int WN, int NB, bool ALONG>
 __global__ __launch_bounds__(64 * WM * WN, WM * WN <= 4 && product_lds(BM, BN, NB) > 80 * 1024 ? 1 : 2) void k_product(ProductArgs p) {
     __shared__ __align__(16) u8 lds[product_lds(BM, BN, NB)];
     product_tile<BM, BN, WM, WN, NB, ALONG>(p, blockIdx.x, gridDim.x, lds);
+}
+
+// ---- a few tokens, in one launch ------------------------------------------------------------------------------------
+
+constexpr u32 kFewTokens = 64, kFewWaves = 8;
+
+// Up to 16 TF tokens times sixteen rows of W a workgroup, whose wavefronts take steps of the sum in turn and add their sums up in LDS, in order.  Fragments come straight from memory: a
+// lane's 16-byte pieces of W are read once, x comes out of the caches.  Rows at any address.
+template <int TF>
+__global__ __launch_bounds__(64 * kFewWaves) void k_product_few(ProductArgs p) {
+    __shared__ __align__(16) f32x4 sums[kFewWaves][TF][64];
+    const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, g = lane >> 4;
+    const u32 n0 = blockIdx.x * 16, all = (p.n_sum + kStep - 1) / kStep, whole = p.n_sum / kStep;
+    constexpr u32 kAhead = TF > 2 ? 2 : 4;                          // steps whose codes are under way
+    const u32 n = n0 + (lane & 15) < p.n_out ? n0 + (lane & 15) : p.n_out - 1;
+    const u8* w = p.w + static_cast<i64>(n) * p.ldw;
+    const i64 w_left = static_cast<i64>(p.n_out - 1 - n) * p.ldw + p.n_sum;
+    const u8* x[TF];
+    const float* xs[TF];
+    i64 x_left[TF];
+#pragma unroll
+    for (int f = 0; f < TF; ++f) {
+        const u32 t = f * 16 + (lane & 15) < p.n_tokens ? f * 16 + (lane & 15) : p.n_tokens - 1;
+        x[f] = p.x + static_cast<i64>(t) * p.ldx;
+        xs[f] = p.xs + static_cast<i64>(t) * p.ldxs;
+        x_left[f] = static_cast<i64>(p.n_tokens - 1 - t) * p.ldx + p.n_sum;
+    }
+    const float* ws = p.ws + static_cast<i64>(n0 / kStep) * p.ldws;
+    f32x4 acc[TF] = {};
+    auto load = [&](const u8* row, i64 left, u32 s) {
+        const i64 a = static_cast<i64>(s) * kStep + g * 16, b = a + 64;
+        u32x4 lo, hi;
+        if (s < whole) {                                            // the same in the wavefront
+            lo = *reinterpret_cast<const u32x4_bytes*>(row + a);
+            hi = *reinterpret_cast<const u32x4_bytes*>(row + b);
+        } else {
+            lo = load16_codes(row, a, p.n_sum, left - a);
+            hi = load16_codes(row, b, p.n_sum, left - b);
+        }
+        return u32x8{lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+    };
+    for (u32 s0 = wave; s0 < all; s0 += kAhead * waves) {
+        u32x8 fw[kAhead], fx[kAhead][TF];
+        float scale[kAhead][TF];
+#pragma unroll
+        for (u32 q = 0; q < kAhead; ++q) {
+            const u32 s = s0 + q * waves;
+            if (s >= all) break;                                    // the same in the wavefront
+            fw[q] = load(w, w_left, s);
+            const float by = ws[s];
+#pragma unroll
+            for (int f = 0; f < TF; ++f) {
+                fx[q][f] = load(x[f], x_left[f], s);
+                scale[q][f] = xs[f][s] * by;
+            }
+        }
+#pragma unroll
+        for (u32 q = 0; q < kAhead; ++q) {
+            if (s0 + q * waves >= all) break;
+#pragma unroll
+            for (int f = 0; f < TF; ++f) {
+                const f32x4 v = mfma_codes(fw[q], fx[q][f]);
+#pragma unroll
+                for (u32 k = 0; k < 4; ++k) acc[f][k] = __builtin_fmaf(v[k], scale[q][f], acc[f][k]);
+            }
+        }
+    }
+#pragma unroll
+    for (int f = 0; f < TF; ++f) sums[wave][f][lane] = acc[f];
+    __syncthreads();
+    for (u32 f = wave; f < TF; f += waves) {
+        f32x4 v = sums[0][f][lane];
+        for (u32 k = 1; k < waves; ++k) v += sums[k][f][lane];
+        store_outputs(p, f * 16 + (lane & 15), n0 + g * 4, v);
+    }
 }
 
 // The parts of split sums, added in order, four outputs a thread.

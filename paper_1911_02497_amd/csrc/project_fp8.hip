@@ -5,6 +5,7 @@
 namespace condensa {
 
 struct ProductPlan {
+    bool few = false;
     u32 splits = 1, steps_each = 0;
     size_t part = 0;                                          // bytes of the parts
 };
@@ -12,8 +13,10 @@ struct ProductPlan {
 constexpr u32 kMostSplits = 16;
 constexpr u64 kSplitTiles = 512;                              // tiles of parts that sums are split into, at most
 
-static ProductPlan make_plan(i64 T, i64 n_out, i64 n_sum) {
+static ProductPlan make_plan(i64 T, i64 n_out, i64 n_sum, bool along) {
     ProductPlan p;
+    p.few = along && T <= kFewTokens;
+    if (p.few) return p;
     const u32 steps = static_cast<u32>(blocks_of(n_sum));
     const u64 tiles = static_cast<u64>((T + 63) / 64) * ((n_out + 63) / 64);
     u64 s = tiles ? kSplitTiles / tiles : 1;
@@ -72,7 +75,7 @@ static condensa_status product(const condensa_fp8_matrix* x, const condensa_fp8_
     if (!aligned_to(y, 2)) return CONDENSA_ERR_ARG;
     if (T == 0) return CONDENSA_OK;
     if (!grid_fits(T, n_out)) return CONDENSA_ERR_SIZE;
-    const ProductPlan p = make_plan(T, n_out, n_sum);
+    const ProductPlan p = make_plan(T, n_out, n_sum, along);
     if (!workspace || !aligned_to(workspace, 256) || workspace_bytes < p.part) return CONDENSA_ERR_WORKSPACE;
     ByteRange r[] = {codes_range(x, false), scales_range(x, false), codes_range(w, false), scales_range(w, false),
                      byte_range(y, rows_bytes(T, y_stride, n_out, 2), true), byte_range(p.part ? workspace : nullptr, p.part, true)};
@@ -86,6 +89,15 @@ static condensa_status product(const condensa_fp8_matrix* x, const condensa_fp8_
     a.part = p.part ? static_cast<float*>(workspace) : nullptr;
     a.bf16 = type == CONDENSA_TYPE_BF16;
     hipStream_t st = static_cast<hipStream_t>(stream);
+    if (p.few) {
+        const u32 waves = std::min(kFewWaves, static_cast<u32>(blocks_of(n_sum)));
+        const dim3 grid((a.n_out + 15) / 16), threads(64 * waves);
+        if (T <= 16)      hipLaunchKernelGGL(k_product_few<1>, grid, threads, 0, st, a);
+        else if (T <= 32) hipLaunchKernelGGL(k_product_few<2>, grid, threads, 0, st, a);
+        else              hipLaunchKernelGGL(k_product_few<4>, grid, threads, 0, st, a);
+        CONDENSA_LAUNCH_CHECK();
+        return CONDENSA_OK;
+    }
     const bool fast = rows16(a.x, a.ldx) && rows16(a.w, a.ldw);
     if (along) launch_product<true>(a, fast, st);
     else       launch_product<false>(a, fast, st);
