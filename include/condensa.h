@@ -583,7 +583,7 @@ condensa_status condensa_dequantize_fp8_blocks(const condensa_fp8_matrix* m, voi
  * n_tokens 0..2^24, width 1..CONDENSA_MAX_NORM_WIDTH, strides in elements, up to 2^22; x, residual, sum and y of `type` (CONDENSA_TYPE_F16 or
  * _BF16), weight of weight_type (that one, or CONDENSA_TYPE_F32).  One launch, no workspace.
  */
-#define CONDENSA_MAX_NORM_WIDTH 65536
+#define CONDENSA_MAX_NORM_WIDTH 32768
 typedef struct {
     const uint16_t* x;              /* device [n_tokens, width]                                               */
     const uint16_t* residual;       /* NULL: none                                                             */

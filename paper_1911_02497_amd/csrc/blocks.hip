@@ -67,10 +67,16 @@ static RowShare share_row(i64 width, u32 least_each) {
     while ((pieces + each - 1) / each > kNormWaves) each *= 2;
     return RowShare{each, (pieces + each - 1) / each};
 }
-static_assert(CONDENSA_MAX_NORM_WIDTH == kNormWaves * kWaveCols * 8, "the widest row: eight pieces a wavefront");
+static_assert(CONDENSA_MAX_NORM_WIDTH == kNormWaves * kWaveCols * 4, "the widest row: four pieces a wavefront");
 
-// Workgroups that share the rows of a backward pass.
-static u32 grad_groups(i64 n_tokens) { return static_cast<u32>(n_tokens < 512 ? n_tokens : 512); }
+// Workgroups that share the rows of a backward pass: one a unit for wide rows, more for narrow ones, and rows enough for each that its part of the weight's gradient
+// is small beside them.  8192 tokens of 4608, us with 256, 512 and 1024: 72, 77 and 78, and 2.7, 3.5 and 5.0 to add the parts up.
+static u32 grad_groups(i64 n_tokens, i64 width) {
+    const u32 waves = share_row(width, 1).waves;
+    const u32 slots = waves == 1 ? kNormSlots : 1, most = 256 * (waves >= 8 || waves == 1 ? 1 : 8 / waves);
+    const u64 rows = (static_cast<u64>(n_tokens) + 2 * slots - 1) / (2 * slots);
+    return static_cast<u32>(rows < most ? rows : most);
+}
 
 // Calls launch(pieces of a wavefront, vec) with both as constants.
 template <typename F>
@@ -79,8 +85,7 @@ static void with_share(u32 each, bool vec, F&& launch) {
         switch (each) {
             case 1: launch(std::integral_constant<u32, 1>{}, v); break;
             case 2: launch(std::integral_constant<u32, 2>{}, v); break;
-            case 4: launch(std::integral_constant<u32, 4>{}, v); break;
-            default: launch(std::integral_constant<u32, 8>{}, v);
+            default: launch(std::integral_constant<u32, 4>{}, v);
         }
     };
     if (vec) pick(std::true_type{});
@@ -159,14 +164,14 @@ condensa_status condensa_rms_norm(const condensa_rms_norm_call* c, void* stream)
     a.sum = c->sum; a.ldsum = c->sum_stride; a.y = c->y; a.ldy = c->y_stride;
     if (c->codes) { a.q = c->codes->q; a.ldq = c->codes->q_stride; a.scale = c->codes->scale; a.lds = c->codes->scale_stride; }
     a.n_tokens = static_cast<u32>(c->n_tokens); a.n = static_cast<u32>(c->width); a.eps = c->eps;
-    const RowShare share = share_row(c->width, 1);
+    const RowShare share = share_row(c->width, 2);
     a.waves = share.waves;
     const u32 rows_each = share.waves == 1 ? 4 : 1;
     const dim3 grid((a.n_tokens + rows_each - 1) / rows_each), threads(64 * share.waves * rows_each);
     hipStream_t st = static_cast<hipStream_t>(stream);
     with_types(c->type, c->weight_type, [&](auto rows_type, auto weight_type) {
         with_share(share.each, vec, [&](auto each, auto v) {
-            hipLaunchKernelGGL((k_rms_norm<decltype(rows_type), decltype(weight_type), decltype(each)::value, decltype(v)::value>), grid, threads, 0, st, a);
+            if constexpr (decltype(each)::value > 1) hipLaunchKernelGGL((k_rms_norm<decltype(rows_type), decltype(weight_type), decltype(each)::value, decltype(v)::value>), grid, threads, 0, st, a);
         });
     });
     CONDENSA_LAUNCH_CHECK();
@@ -175,7 +180,7 @@ condensa_status condensa_rms_norm(const condensa_rms_norm_call* c, void* stream)
 
 size_t condensa_rms_norm_workspace_bytes(int64_t n_tokens, int64_t width) {
     if (n_tokens < 0 || n_tokens > kMaxFp8Rows || width < 1 || width > CONDENSA_MAX_NORM_WIDTH) return 0;
-    const size_t b = align_up(static_cast<u64>(grad_groups(n_tokens)) * width * 4);
+    const size_t b = align_up(static_cast<u64>(grad_groups(n_tokens, width)) * width * 4);
     return b ? b : 256;
 }
 
@@ -209,12 +214,12 @@ condensa_status condensa_rms_norm_backward(const condensa_rms_norm_grad_call* c,
     a.n_tokens = static_cast<u32>(c->n_tokens); a.n = static_cast<u32>(c->width); a.eps = c->eps;
     const RowShare share = share_row(c->width, 1);
     a.waves = share.waves;
-    const u32 groups = grad_groups(c->n_tokens);
+    const u32 groups = grad_groups(c->n_tokens, c->width);
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (groups) {
         with_types(c->type, c->weight_type, [&](auto rows_type, auto weight_type) {
             with_share(share.each, vec, [&](auto each, auto v) {
-                hipLaunchKernelGGL((k_rms_norm_grad<decltype(rows_type), decltype(weight_type), decltype(each)::value, decltype(v)::value>), dim3(groups), dim3(64 * share.waves), 0, st, a);
+                hipLaunchKernelGGL((k_rms_norm_grad<decltype(rows_type), decltype(weight_type), decltype(each)::value, decltype(v)::value>), dim3(groups), dim3(64 * (share.waves == 1 ? kNormSlots : share.waves)), 0, st, a);
             });
         });
         CONDENSA_LAUNCH_CHECK();

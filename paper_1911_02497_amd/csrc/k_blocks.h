@@ -11,6 +11,8 @@ constexpr u32 kLaneCols = 8, kWaveCols = 64 * kLaneCols;
 
 // ---- rows of eight values a lane ----------------------------------------------------------------------------------
 
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 b16x2 __attribute__((ext_vector_type(2)));
 typedef u32 u32x2_bytes __attribute__((ext_vector_type(2), aligned(1)));
 
 struct RowsF16 {
@@ -19,9 +21,13 @@ struct RowsF16 {
     static __device__ inline void load(const elem* p, i64 k, i64 n, float (&v)[8]) { unpack(load8<VEC>(p, k, n), v); }
     static __device__ inline void unpack(u32x4 t, float (&v)[8]) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = CodecF16::dec(static_cast<u16>(t[i >> 1] >> (16 * (i & 1))));
+        for (int i = 0; i < 4; ++i) {
+            const f16x2 h = __builtin_bit_cast(f16x2, static_cast<u32>(t[i]));
+            v[2 * i] = static_cast<float>(h.x);
+            v[2 * i + 1] = static_cast<float>(h.y);
+        }
     }
-    static __device__ inline u16 enc(float x) { return CodecF16::enc(x); }
+    static __device__ inline u32 enc2(float a, float b) { return __builtin_bit_cast(u32, f16x2{static_cast<_Float16>(a), static_cast<_Float16>(b)}); }
 };
 struct RowsBF16 {
     typedef u16 elem;
@@ -34,7 +40,7 @@ struct RowsBF16 {
             v[2 * i + 1] = __uint_as_float(t[i] & 0xFFFF0000u);
         }
     }
-    static __device__ inline u16 enc(float x) { return CodecBF16::enc(x); }
+    static __device__ inline u32 enc2(float a, float b) { return __builtin_bit_cast(u32, b16x2{static_cast<__bf16>(a), static_cast<__bf16>(b)}); }
 };
 struct RowsF32 {
     typedef float elem;
@@ -73,7 +79,7 @@ template <typename R>
 __device__ inline u32x4 pack8(const float (&v)[8]) {
     u32x4 t;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) t[i] = static_cast<u32>(R::enc(v[2 * i])) | static_cast<u32>(R::enc(v[2 * i + 1])) << 16;
+    for (int i = 0; i < 4; ++i) t[i] = R::enc2(v[2 * i], v[2 * i + 1]);
     return t;
 }
 // Eight codes, at any address.
@@ -98,33 +104,52 @@ __device__ inline u32x2 load8_codes(const u8* p, i64 k, i64 n) {
 
 // ---- codes of a block -----------------------------------------------------------------------------------------------
 
-// Largest finite magnitude of eight values, as its bits.
-__device__ inline u32 largest8(const float (&v)[8]) {
-    u32 top = 0;
+// Value of another lane of the same sixteen: the neighbour, the other pair of four, the other four of eight, the other eight (each the mirror image, which is as good
+// where the lanes of a half already agree).
+template <int CTRL>
+__device__ inline float lane_of16(float x) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xF, 0xF, true)); }
+enum : int { kNeighbour = 0xB1, kOtherPair = 0x4E, kOtherFour = 0x141, kOtherEight = 0x140 };
+
+// Largest magnitude of eight values; NaN count as nothing.
+__device__ inline float largest8(const float (&v)[8]) {
+    float top = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const u32 a = __float_as_uint(v[i]) & 0x7FFFFFFFu, b = a < 0x7F800000u ? a : 0u;
-        top = top > b ? top : b;
-    }
+    for (int i = 0; i < 8; i += 2) top = __builtin_fmaxf(top, __builtin_fmaxf(__builtin_fabsf(v[i]), __builtin_fabsf(v[i + 1])));
     return top;
 }
-__device__ inline u32 largest_of16(u32 x) {                // of sixteen lanes' values
+__device__ inline float finite_largest8(const float (&v)[8]) {
+    float top = 0.0f;
 #pragma unroll
-    for (int d = 8; d >= 1; d >>= 1) {
-        const u32 y = static_cast<u32>(__shfl_xor(static_cast<int>(x), d, 64));
-        x = x > y ? x : y;
-    }
-    return x;
+    for (int i = 0; i < 8; ++i) top = __builtin_fabsf(v[i]) < __builtin_inff() ? __builtin_fmaxf(top, __builtin_fabsf(v[i])) : top;
+    return top;
+}
+__device__ inline float largest_of16(float x) {            // of sixteen lanes' values
+    x = __builtin_fmaxf(x, lane_of16<kNeighbour>(x));
+    x = __builtin_fmaxf(x, lane_of16<kOtherPair>(x));
+    x = __builtin_fmaxf(x, lane_of16<kOtherFour>(x));
+    return __builtin_fmaxf(x, lane_of16<kOtherEight>(x));
+}
+__device__ inline float across16(float x, int sixteen) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), sixteen * 16)); }
+__device__ inline float wave_largest(float x) {
+    x = largest_of16(x);
+    return __builtin_fmaxf(__builtin_fmaxf(across16(x, 0), across16(x, 1)), __builtin_fmaxf(across16(x, 2), across16(x, 3)));
+}
+__device__ inline float wave_sum(float x) {
+    x += lane_of16<kNeighbour>(x);
+    x += lane_of16<kOtherPair>(x);
+    x += lane_of16<kOtherFour>(x);
+    x += lane_of16<kOtherEight>(x);
+    return (across16(x, 0) + across16(x, 1)) + (across16(x, 2) + across16(x, 3));
 }
 
-// What makes codes of a block from the bits of its largest finite magnitude.
+// What makes codes of a block from its largest finite magnitude.
 struct BlockBy {
     float top, by, scale;
     bool kept;
 };
-__device__ inline BlockBy block_by(u32 top_bits) {
+__device__ inline BlockBy block_by(float top) {
     BlockBy b;
-    b.top = __uint_as_float(top_bits);
+    b.top = top;
     b.kept = b.top >= 0x1p-100f;                            // below, the reciprocal would leave the range
     b.by = b.kept ? __fdiv_rn(448.0f, b.top) : 0.0f;
     b.scale = b.kept ? __fdiv_rn(b.top, 448.0f) : 0.0f;
@@ -155,6 +180,65 @@ __device__ inline u32 codes4(const float* x, const BlockBy& b) {
 }
 __device__ inline u32x2 codes8(const float (&x)[8], const BlockBy& b) { return u32x2{codes4(x, b), codes4(x + 4, b)}; }
 
+// The same for finite values (or NaN) whose largest is between 2^-100 and 2^100, without what then remains: exact where x 448 is, for significands of up to 21 bits, since a
+// quotient of two such values is the middle of two codes or not within a unit of it.  A third of the instructions.
+__device__ inline u32x2 codes8_plain(const float (&x)[8], const BlockBy& b) {
+    const float down = b.by * (1.0f / 448.0f);
+    float q[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        q[k] = x[k] * b.by;
+        q[k] = __builtin_copysignf(__builtin_fmaf(__builtin_fmaf(-q[k], b.top, x[k] * 448.0f), down, q[k]), x[k]);         // (zeros would lose their sign)
+    }
+    u32x2 t;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int p = __builtin_amdgcn_cvt_pk_fp8_f32(q[4 * h], q[4 * h + 1], 0, false);
+        t[h] = static_cast<u32>(__builtin_amdgcn_cvt_pk_fp8_f32(q[4 * h + 2], q[4 * h + 3], p, true));
+    }
+    return t;
+}
+__device__ inline bool plain_range(float top) { return top >= 0x1p-100f && top <= 0x1p100f; }
+
+// The same for longer significands: the product with the reciprocal decides where it is three units or more from the middle of two codes, which it nearly always is (of
+// what is below the smallest normal code that is not looked at); a wavefront that has another case takes the long way.
+__device__ inline u32x2 codes8_long(const float (&x)[8], const BlockBy& b) {
+    float q[8];
+    u32 near = ~0u, small = ~0u;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        q[k] = x[k] * b.by;
+        const u32 size = __float_as_uint(q[k]) & 0x7FFFFFFFu, from = (size - 0x7FFFDu) & 0xFFFFFu;         // a code keeps 20 bits less than binary32
+        near = near < from ? near : from;
+        small = small < size - 1 ? small : size - 1;          // zero is no case
+    }
+    if (__any(near <= 6u || small < 0x3C800000u - 1)) return codes8(x, b);
+    u32x2 t;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int p = __builtin_amdgcn_cvt_pk_fp8_f32(q[4 * h], q[4 * h + 1], 0, false);
+        t[h] = static_cast<u32>(__builtin_amdgcn_cvt_pk_fp8_f32(q[4 * h + 2], q[4 * h + 3], p, true));
+    }
+    return t;
+}
+// LONG: values have more than 21 bits and are what the quotient is of.
+template <bool LONG>
+__device__ inline u32x2 codes8_in_range(const float (&x)[8], const BlockBy& b) { return LONG ? codes8_long(x, b) : codes8_plain(x, b); }
+
+// Codes of the block that sixteen lanes hold, and its scale.
+template <bool LONG>
+__device__ inline u32x2 block_codes(const float (&x)[8], float* scale) {
+    const float top = largest_of16(largest8(x));
+    if (__all(plain_range(top) || top == 0.0f)) {
+        const BlockBy b = block_by(top);
+        *scale = b.scale;
+        return codes8_in_range<LONG>(x, b);
+    }
+    const BlockBy b = block_by(largest_of16(finite_largest8(x)));
+    *scale = b.scale;
+    return codes8(x, b);
+}
+
 // ---- the codec ------------------------------------------------------------------------------------------------------
 
 struct BlockArgs {
@@ -175,40 +259,44 @@ __global__ __launch_bounds__(256) void k_block_encode_rows(BlockArgs p) {
     const i64 k = static_cast<i64>(item % p.across) * kWaveCols + lane * kLaneCols;
     float v[8];
     R::template load<VEC>(static_cast<const typename R::elem*>(p.x) + static_cast<i64>(row) * p.ldx, k, p.cols, v);
-    const BlockBy b = block_by(largest_of16(largest8(v)));
-    store8_codes(p.q + static_cast<i64>(row) * p.ldq, k, p.cols, codes8(v, b));
-    if ((lane & 15u) == 0 && k < p.cols) p.scale[static_cast<i64>(row) * p.lds + k / kFp8Block] = b.scale;
+    float scale;
+    const u32x2 c = block_codes<sizeof(typename R::elem) == 4>(v, &scale);
+    store8_codes(p.q + static_cast<i64>(row) * p.ldq, k, p.cols, c);
+    if ((lane & 15u) == 0 && k < p.cols) p.scale[static_cast<i64>(row) * p.lds + k / kFp8Block] = scale;
 }
 
 // A workgroup takes a block of 128 x 128, sixteen rows at a time, and keeps it in registers between looking for its largest and making codes of it.
 template <typename R, bool VEC>
 __global__ __launch_bounds__(256) void k_block_encode_squares(BlockArgs p) {
-    __shared__ u32 s_top[4];
+    __shared__ float s_top[2][4];
     const u32 row0 = static_cast<u32>(blockIdx.x / p.across) * kFp8Block + (threadIdx.x >> 4);
     const u32 block = static_cast<u32>(blockIdx.x % p.across);
     const i64 k = static_cast<i64>(block) * kFp8Block + (threadIdx.x & 15u) * kLaneCols;
+    constexpr bool kLong = sizeof(typename R::elem) == 4;
     float v[8][8];
-    u32 top = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const u32 row = row0 + i * 16;
         R::template load<VEC>(static_cast<const typename R::elem*>(p.x) + static_cast<i64>(row < p.rows ? row : 0) * p.ldx, k, row < p.rows ? p.cols : 0, v[i]);
     }
+    auto largest = [&](auto of8, float* s) {
+        float top = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const u32 t = largest8(v[i]);
-        top = top > t ? top : t;
-    }
-    top = wave_most(top);
-    if ((threadIdx.x & 63u) == 0) s_top[threadIdx.x >> 6] = top;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 4; ++i) top = top > s_top[i] ? top : s_top[i];
+        for (int i = 0; i < 8; ++i) top = __builtin_fmaxf(top, of8(v[i]));
+        top = wave_largest(top);
+        if ((threadIdx.x & 63u) == 0) s[threadIdx.x >> 6] = top;
+        __syncthreads();
+        return __builtin_fmaxf(__builtin_fmaxf(s[0], s[1]), __builtin_fmaxf(s[2], s[3]));
+    };
+    float top = largest([](const float (&x)[8]) { return largest8(x); }, s_top[0]);
+    const bool in_range = plain_range(top) || top == 0.0f;    // the same in the workgroup
+    if (!in_range) top = largest([](const float (&x)[8]) { return finite_largest8(x); }, s_top[1]);
     const BlockBy b = block_by(top);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const u32 row = row0 + i * 16;
-        if (row < p.rows) store8_codes(p.q + static_cast<i64>(row) * p.ldq, k, p.cols, codes8(v[i], b));
+        const u32x2 c = in_range ? codes8_in_range<kLong>(v[i], b) : codes8(v[i], b);
+        if (row < p.rows) store8_codes(p.q + static_cast<i64>(row) * p.ldq, k, p.cols, c);
     }
     if (threadIdx.x == 0) p.scale[static_cast<i64>(row0 / kFp8Block) * p.lds + block] = b.scale;
 }
@@ -267,54 +355,65 @@ struct NormArgs {
     float eps;
 };
 
-__device__ inline float wave_sum(float x) {
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) x += __shfl_xor(x, d, 64);
-    return x;
-}
-
 constexpr u32 kNormWaves = 16;           // of a workgroup, at most
+constexpr u32 kNormSlots = 8;            // rows that a workgroup of the gradients has at once where a row is one wavefront
 
-// Sums of the wavefronts of a row: of the only one, or in the order of the wavefronts.
+// Sums of the wavefronts of a row: of the only one, or in the order of the wavefronts.  `s` is another piece of LDS in each call that follows without a barrier between.
 template <u32 N>
 __device__ inline void row_sums(float (&x)[N], u32 waves, float* s) {
 #pragma unroll
     for (u32 i = 0; i < N; ++i) x[i] = wave_sum(x[i]);
     if (waves == 1) return;                                   // the same in the whole workgroup
-    const u32 wave = threadIdx.x >> 6;
-    __syncthreads();                                          // what the call before this one left has been read
-    if ((threadIdx.x & 63u) == 0)
+    const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (lane == 0)
 #pragma unroll
-        for (u32 i = 0; i < N; ++i) s[wave * N + i] = x[i];
+        for (u32 i = 0; i < N; ++i) s[i * kNormWaves + wave] = x[i];
     __syncthreads();
 #pragma unroll
     for (u32 i = 0; i < N; ++i) {
-        x[i] = 0.0f;
-        for (u32 w = 0; w < waves; ++w) x[i] += s[w * N + i];
+        float t = (lane & 15u) < waves ? s[i * kNormWaves + (lane & 15u)] : 0.0f;
+        t += lane_of16<kNeighbour>(t);
+        t += lane_of16<kOtherPair>(t);
+        t += lane_of16<kOtherFour>(t);
+        x[i] = t + lane_of16<kOtherEight>(t);
     }
 }
 
-// 1 / sqrt(mean + eps), and the power of two that values are multiplied by before they are squared: 2^-64 where squares would leave binary32's range.
-struct RowNorm {
-    float by, r;                         // u = (h by) r
-};
+// A row's squares are of values times `by`, a power of two: 1, or 2^-64 where squares would leave binary32's range.  r = by / sqrt(mean + eps) then, for values times by.
 __device__ inline float norm_factor(float squares, u32 n, float eps) { return __fdiv_rn(1.0f, __fsqrt_rn(__fdiv_rn(squares, static_cast<float>(n)) + eps)); }
 
-// Rows of 512 CH columns a wavefront.
+// Codes of y r and their scale, from values y whose own range is in hand: r cancels in what a code is made of, so codes are those of products of h and the weight.
+__device__ inline u32x2 scaled_codes(const float (&y)[8], float r, float* scale) {
+    const float top = largest_of16(largest8(y)), top_r = top * r;
+    if (__all((plain_range(top) && plain_range(top_r)) || top == 0.0f)) {
+        *scale = __fdiv_rn(top_r, 448.0f);
+        return codes8_plain(y, block_by(top));
+    }
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = y[i] * r;
+    return block_codes<true>(v, scale);
+}
+
+// Rows of 512 CH columns a wavefront.  Reading x and the residual and writing their sum bounds it.
 template <typename R, typename W, u32 CH, bool VEC>
 __global__ __launch_bounds__(64 * kNormWaves) void k_rms_norm(NormArgs p) {
-    __shared__ float s[kNormWaves];
+    __shared__ float s[2][kNormWaves];
     const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6, per = (blockDim.x >> 6) / p.waves;        // rows of a workgroup: one where a row has several wavefronts
     const u32 row = blockIdx.x * per + wave / p.waves, part = wave % p.waves;
     if (row >= p.n_tokens) return;                            // then a row is one wavefront
     const i64 k0 = static_cast<i64>(part) * (CH * kWaveCols) + lane * kLaneCols;
-    u32x4 h[CH];
+    u32x4 h[CH], t[CH];
 #pragma unroll
     for (u32 c = 0; c < CH; ++c) h[c] = load8<VEC>(p.x + static_cast<i64>(row) * p.ldx, k0 + c * kWaveCols, p.n);
     if (p.res) {
-        u32x4 t[CH];
 #pragma unroll
         for (u32 c = 0; c < CH; ++c) t[c] = load8<VEC>(p.res + static_cast<i64>(row) * p.ldr, k0 + c * kWaveCols, p.n);
+    }
+    float w[CH][8];
+#pragma unroll
+    for (u32 c = 0; c < CH; ++c) W::template load<VEC>(static_cast<const typename W::elem*>(p.weight), k0 + c * kWaveCols, p.n, w[c]);
+    if (p.res) {
 #pragma unroll
         for (u32 c = 0; c < CH; ++c) {
             float a[8], b[8];
@@ -325,29 +424,27 @@ __global__ __launch_bounds__(64 * kNormWaves) void k_rms_norm(NormArgs p) {
             h[c] = pack8<R>(a);
         }
     }
-    float squares[1] = {0.0f};
-#pragma unroll
-    for (u32 c = 0; c < CH; ++c) {
-        float a[8];
-        R::unpack(h[c], a);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) squares[0] = __builtin_fmaf(a[i], a[i], squares[0]);
-    }
-    row_sums(squares, p.waves, s);
-    RowNorm m = {1.0f, norm_factor(squares[0], p.n, p.eps)};
-    if (!(squares[0] < __builtin_inff())) {                   // the same in the whole row
-        m.by = 0x1p-64f;
-        squares[0] = 0.0f;
+    auto squares_of = [&](float by) {
+        float q = 0.0f;
 #pragma unroll
         for (u32 c = 0; c < CH; ++c) {
             float a[8];
             R::unpack(h[c], a);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) squares[0] = __builtin_fmaf(a[i] * m.by, a[i] * m.by, squares[0]);
+            for (int i = 0; i < 8; ++i) q = __builtin_fmaf(a[i] * by, a[i] * by, q);
         }
-        row_sums(squares, p.waves, s);
-        m.r = norm_factor(squares[0], p.n, p.eps * 0x1p-128f);
+        return q;
+    };
+    float squares[1] = {squares_of(1.0f)};
+    row_sums(squares, p.waves, s[0]);
+    float by = 1.0f, eps = p.eps;
+    if (!(squares[0] < __builtin_inff())) {                   // the same in the whole row
+        by = 0x1p-64f;
+        eps *= 0x1p-128f;
+        squares[0] = squares_of(by);
+        row_sums(squares, p.waves, s[1]);
     }
+    const float r = norm_factor(squares[0], p.n, eps);
     if (p.sum) {
 #pragma unroll
         for (u32 c = 0; c < CH; ++c) store8<VEC>(p.sum + static_cast<i64>(row) * p.ldsum, k0 + c * kWaveCols, p.n, h[c]);
@@ -357,16 +454,19 @@ __global__ __launch_bounds__(64 * kNormWaves) void k_rms_norm(NormArgs p) {
     for (u32 c = 0; c < CH; ++c) {
         const i64 k = k0 + c * kWaveCols;
         if (k - lane * kLaneCols >= p.n) break;               // the same in the wavefront
-        float a[8], w[8];
+        float a[8];
         R::unpack(h[c], a);
-        W::template load<VEC>(static_cast<const typename W::elem*>(p.weight), k, p.n, w);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) a[i] = a[i] * m.by * m.r * w[i];
-        if (p.y) store8<VEC>(p.y + static_cast<i64>(row) * p.ldy, k, p.n, pack8<R>(a));
+        for (int i = 0; i < 8; ++i) a[i] = a[i] * by * w[c][i];
         if (p.q) {
-            const BlockBy b = block_by(largest_of16(largest8(a)));
-            store8_codes(p.q + static_cast<i64>(row) * p.ldq, k, p.n, codes8(a, b));
-            if ((lane & 15u) == 0 && k < p.n) p.scale[static_cast<i64>(row) * p.lds + k / kFp8Block] = b.scale;
+            float scale;
+            store8_codes(p.q + static_cast<i64>(row) * p.ldq, k, p.n, scaled_codes(a, r, &scale));
+            if ((lane & 15u) == 0 && k < p.n) p.scale[static_cast<i64>(row) * p.lds + k / kFp8Block] = scale;
+        }
+        if (p.y) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) a[i] *= r;
+            store8<VEC>(p.y + static_cast<i64>(row) * p.ldy, k, p.n, pack8<R>(a));
         }
     }
 }
@@ -387,80 +487,118 @@ struct NormGradArgs {
     float eps;
 };
 
-// A workgroup takes rows in turn and keeps its lanes' columns of the weight's gradient.
+// Where a row is one wavefront, a workgroup's wavefronts have rows of their own; else it takes rows in turn.  Its lanes keep their columns of the weight's gradient.  Where a wavefront
+// has 512 columns the next row's values are on their way while one row is worked on, and the weight stays in registers; with 1024 and more there are none left for that.
+// Reading three operands and writing dx bounds it, beside a barrier for each row.
 template <typename R, typename W, u32 CH, bool VEC>
 __global__ __launch_bounds__(64 * kNormWaves) void k_rms_norm_grad(NormGradArgs p) {
-    __shared__ float s[2 * kNormWaves];
-    const u32 lane = threadIdx.x & 63, part = threadIdx.x >> 6;
+    constexpr bool kKeep = CH == 1;
+    __shared__ float s[3][2 * kNormWaves];
+    __shared__ float s_dw[kNormSlots][kWaveCols];
+    const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const u32 slots = p.waves == 1 ? kNormSlots : 1, slot = p.waves == 1 ? wave : 0, part = p.waves == 1 ? 0 : wave;
+    const u32 first = blockIdx.x * slots + slot, stride = gridDim.x * slots;
     const i64 k0 = static_cast<i64>(part) * (CH * kWaveCols) + lane * kLaneCols;
-    float dw[CH][8] = {};
-    for (u32 row = blockIdx.x; row < p.n_tokens; row += gridDim.x) {
-        u32x4 h[CH], dy[CH];
+    float dw[CH][8] = {}, w_kept[8];
+    const typename W::elem* weight = static_cast<const typename W::elem*>(p.weight);
+    if (kKeep) W::template load<VEC>(weight, k0, p.n, w_kept);
+    auto weights = [&](u32 c, float (&w)[8]) {
+        if (kKeep) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = w_kept[i];
+        } else {
+            W::template load<VEC>(weight, k0 + c * kWaveCols, p.n, w);
+        }
+    };
+    u32x4 h[CH], dy[CH], ds[CH] = {}, next_h[CH], next_dy[CH], next_ds[CH] = {};
+    auto fetch = [&](u32 row) {
 #pragma unroll
         for (u32 c = 0; c < CH; ++c) {
-            h[c] = load8<VEC>(p.h + static_cast<i64>(row) * p.ldh, k0 + c * kWaveCols, p.n);
-            dy[c] = load8<VEC>(p.dy + static_cast<i64>(row) * p.lddy, k0 + c * kWaveCols, p.n);
+            next_h[c] = load8<VEC>(p.h + static_cast<i64>(row) * p.ldh, k0 + c * kWaveCols, p.n);
+            next_dy[c] = load8<VEC>(p.dy + static_cast<i64>(row) * p.lddy, k0 + c * kWaveCols, p.n);
         }
+        if (p.dsum) {
+#pragma unroll
+            for (u32 c = 0; c < CH; ++c) next_ds[c] = load8<VEC>(p.dsum + static_cast<i64>(row) * p.ldds, k0 + c * kWaveCols, p.n);
+        }
+    };
+    if (kKeep && first < p.n_tokens) fetch(first);
+    u32 turn = 0;
+    for (u32 row = first; row < p.n_tokens; row += stride, turn ^= 1) {
+        if (!kKeep) fetch(row);
+#pragma unroll
+        for (u32 c = 0; c < CH; ++c) { h[c] = next_h[c]; dy[c] = next_dy[c]; ds[c] = next_ds[c]; }
+        if (kKeep && row + stride < p.n_tokens) fetch(row + stride);
         float sums[2];
-        auto add = [&](float by) {
+        auto add = [&](float by, float* room) {
             sums[0] = sums[1] = 0.0f;
 #pragma unroll
             for (u32 c = 0; c < CH; ++c) {
                 float a[8], g[8], w[8];
                 R::unpack(h[c], a);
                 R::unpack(dy[c], g);
-                W::template load<VEC>(static_cast<const typename W::elem*>(p.weight), k0 + c * kWaveCols, p.n, w);
+                weights(c, w);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     sums[0] = __builtin_fmaf(a[i] * by, a[i] * by, sums[0]);
                     sums[1] = __builtin_fmaf(g[i] * w[i], a[i] * by, sums[1]);
                 }
             }
-            row_sums(sums, p.waves, s);
+            row_sums(sums, p.waves, room);
         };
-        RowNorm m = {1.0f, 0.0f};
-        add(1.0f);
-        m.r = norm_factor(sums[0], p.n, p.eps);
-        if (!(sums[0] < __builtin_inff())) {                  // the same in the workgroup
-            m.by = 0x1p-64f;
-            add(m.by);
-            m.r = norm_factor(sums[0], p.n, p.eps * 0x1p-128f);
+        add(1.0f, s[turn]);
+        float by = 1.0f, eps = p.eps;
+        if (!(sums[0] < __builtin_inff())) {                  // the same in the whole row
+            if (p.waves > 1) __syncthreads();                 // (for the third piece of LDS)
+            by = 0x1p-64f;
+            eps *= 0x1p-128f;
+            add(by, s[2]);
         }
-        const float mean = __fdiv_rn(sums[1], static_cast<float>(p.n)) * m.r;        // of g u
+        const float r = norm_factor(sums[0], p.n, eps), r_by = r * by;
+        const float mean = __fdiv_rn(sums[1], static_cast<float>(p.n)) * r;          // of g u
 #pragma unroll
         for (u32 c = 0; c < CH; ++c) {
             const i64 k = k0 + c * kWaveCols;
             if (k - lane * kLaneCols >= p.n) break;           // the same in the wavefront
-            float a[8], g[8], w[8], d[8] = {};
+            float a[8], g[8], w[8], d[8];
             R::unpack(h[c], a);
             R::unpack(dy[c], g);
-            W::template load<VEC>(static_cast<const typename W::elem*>(p.weight), k, p.n, w);
-            if (p.dsum) R::template load<VEC>(p.dsum + static_cast<i64>(row) * p.ldds, k, p.n, d);
+            R::unpack(ds[c], d);
+            weights(c, w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float u = a[i] * m.by * m.r;
+                const float u = a[i] * r_by;
                 dw[c][i] = __builtin_fmaf(g[i], u, dw[c][i]);
-                a[i] = __builtin_fmaf(__builtin_fmaf(-u, mean, g[i] * w[i]), m.r * m.by, d[i]);
+                a[i] = __builtin_fmaf(__builtin_fmaf(-u, mean, g[i] * w[i]), r_by, d[i]);
             }
             if (p.dx) store8<VEC>(p.dx + static_cast<i64>(row) * p.lddx, k, p.n, pack8<R>(a));
             if (p.q) {
-                const BlockBy b = block_by(largest_of16(largest8(a)));
-                store8_codes(p.q + static_cast<i64>(row) * p.ldq, k, p.n, codes8(a, b));
-                if ((lane & 15u) == 0 && k < p.n) p.scale[static_cast<i64>(row) * p.lds + k / kFp8Block] = b.scale;
+                float scale;
+                store8_codes(p.q + static_cast<i64>(row) * p.ldq, k, p.n, block_codes<false>(a, &scale));
+                if ((lane & 15u) == 0 && k < p.n) p.scale[static_cast<i64>(row) * p.lds + k / kFp8Block] = scale;
             }
         }
     }
     if (!p.part) return;
-    float* out = p.part + static_cast<u64>(blockIdx.x) * p.n;
+    if (p.waves == 1) {                                       // the wavefronts' sums, in order
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s_dw[slot][i * 64 + lane] = dw[0][i];
+        __syncthreads();
+        if (slot != 0) return;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            for (u32 k = 1; k < kNormSlots; ++k) dw[0][i] += s_dw[k][i * 64 + lane];
+    }
+    float* to = p.part + static_cast<u64>(blockIdx.x) * p.n;
 #pragma unroll
     for (u32 c = 0; c < CH; ++c) {
         const i64 k = k0 + c * kWaveCols;
         if (k + 8 <= p.n) {
-            *reinterpret_cast<f32x4_any*>(out + k) = f32x4{dw[c][0], dw[c][1], dw[c][2], dw[c][3]};
-            *reinterpret_cast<f32x4_any*>(out + k + 4) = f32x4{dw[c][4], dw[c][5], dw[c][6], dw[c][7]};
+            *reinterpret_cast<f32x4_any*>(to + k) = f32x4{dw[c][0], dw[c][1], dw[c][2], dw[c][3]};
+            *reinterpret_cast<f32x4_any*>(to + k + 4) = f32x4{dw[c][4], dw[c][5], dw[c][6], dw[c][7]};
         } else {
 #pragma unroll
-            for (int i = 0; i < 7; ++i) if (k + i < p.n) out[k + i] = dw[c][i];
+            for (int i = 0; i < 7; ++i) if (k + i < p.n) to[k + i] = dw[c][i];
         }
     }
 }
@@ -471,7 +609,13 @@ __global__ __launch_bounds__(1024) void k_rms_norm_join(const float* __restrict_
     const u32 col = blockIdx.x * 64 + (threadIdx.x & 63), wave = threadIdx.x >> 6;
     float x = 0.0f;
     if (col < n)
-        for (u32 i = wave; i < parts; i += 16) x += part[static_cast<u64>(i) * n + col];
+        for (u32 i = wave; i < parts; i += 16 * 8) {          // eight loads under way
+            float v[8];
+#pragma unroll
+            for (u32 k = 0; k < 8; ++k) v[k] = i + k * 16 < parts ? part[static_cast<u64>(i + k * 16) * n + col] : 0.0f;
+#pragma unroll
+            for (u32 k = 0; k < 8; ++k) x += v[k];
+        }
     s[wave][threadIdx.x & 63] = x;
     __syncthreads();
     if (wave != 0 || col >= n) return;
