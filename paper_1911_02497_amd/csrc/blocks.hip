@@ -6,7 +6,7 @@
 
 namespace condensa {
 
-constexpr u64 kMaxGroups = static_cast<u64>(1) << 24;        // workgroups of 256 threads that a launch holds
+constexpr u64 kMaxGroups = static_cast<u64>(1) << 24;        // workgroups of 256 threads that a launch holds; half as many of 512
 
 static bool type_ok(int type, bool f32) { return type == CONDENSA_TYPE_F16 || type == CONDENSA_TYPE_BF16 || (f32 && type == CONDENSA_TYPE_F32); }
 static u64 type_bytes(int type) { return type == CONDENSA_TYPE_F32 ? 4 : 2; }
@@ -21,8 +21,8 @@ static void launch_codec(int what, bool vec, const BlockArgs& a, unsigned groups
         if (vec) hipLaunchKernelGGL((k_block_encode_rows<R, true>), grid, threads, 0, st, a);
         else     hipLaunchKernelGGL((k_block_encode_rows<R, false>), grid, threads, 0, st, a);
     } else if (what == kEncodeSquares) {
-        if (vec) hipLaunchKernelGGL((k_block_encode_squares<R, true>), grid, threads, 0, st, a);
-        else     hipLaunchKernelGGL((k_block_encode_squares<R, false>), grid, threads, 0, st, a);
+        if (vec) hipLaunchKernelGGL((k_block_encode_squares<R, true>), grid, dim3(64 * kSquareWaves), 0, st, a);
+        else     hipLaunchKernelGGL((k_block_encode_squares<R, false>), grid, dim3(64 * kSquareWaves), 0, st, a);
     } else {
         if (vec) hipLaunchKernelGGL((k_block_decode<R, true>), grid, threads, 0, st, a);
         else     hipLaunchKernelGGL((k_block_decode<R, false>), grid, threads, 0, st, a);
@@ -44,7 +44,7 @@ static condensa_status codec(const condensa_fp8_matrix* m, void* x, int type, i6
     a.across = static_cast<u32>(squares ? blocks_of(m->cols) : (m->cols + kWaveCols - 1) / kWaveCols);
     a.items = static_cast<u64>(a.across) * (squares ? blocks_of(m->rows) : m->rows);
     const u64 groups = squares ? a.items : (a.items + 3) / 4;
-    if (groups >= kMaxGroups) return CONDENSA_ERR_SIZE;
+    if (groups >= (squares ? kMaxGroups / 2 : kMaxGroups)) return CONDENSA_ERR_SIZE;
     ByteRange r[] = {byte_range(x, rows_bytes(m->rows, stride, m->cols, type_bytes(type)), !encode), codes_range(m, encode), scales_range(m, encode)};
     if (ranges_conflict(r, sizeof(r) / sizeof(r[0]))) return CONDENSA_ERR_ARG;
     const int what = squares ? kEncodeSquares : (encode ? kEncodeRows : kDecode);

@@ -469,62 +469,72 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN <= 4 && product_lds(BM, BN, N
 
 constexpr u32 kFewTokens = 64, kFewWaves = 8;
 
-// Up to 16 TF tokens times sixteen rows of W a workgroup, whose wavefronts take steps of the sum in turn and add their sums up in LDS, in order.  Fragments come straight from memory: a
-// lane's 16-byte pieces of W are read once, x comes out of the caches.  Rows at any address.
+// Up to 16 TF tokens times sixteen rows of W a workgroup, whose wavefronts take steps of the sum in turn and add their sums up in LDS, in order.  W is read once, x comes out of
+// the caches.  Loads take whole cache lines, eight lanes to a line (a lane each from sixteen rows, as the operands want them, costs the address unit four times as long), and the
+// wavefront's own LDS turns them into fragments, without barriers.  Rows at any address.
 template <int TF>
 __global__ __launch_bounds__(64 * kFewWaves) void k_product_few(ProductArgs p) {
     __shared__ __align__(16) f32x4 sums[kFewWaves][TF][64];
-    const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, g = lane >> 4;
+    __shared__ __align__(16) u8 turns[kFewWaves][TF + 1][16 * kStep];
+    const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, line = lane >> 3, piece = lane & 7;
     const u32 n0 = blockIdx.x * 16, all = (p.n_sum + kStep - 1) / kStep, whole = p.n_sum / kStep;
     constexpr u32 kAhead = TF > 2 ? 2 : 4;                          // steps whose codes are under way
-    const u32 n = n0 + (lane & 15) < p.n_out ? n0 + (lane & 15) : p.n_out - 1;
-    const u8* w = p.w + static_cast<i64>(n) * p.ldw;
-    const i64 w_left = static_cast<i64>(p.n_out - 1 - n) * p.ldw + p.n_sum;
-    const u8* x[TF];
+    const u8 *w[2], *x[TF][2];
+    i64 w_left[2], x_left[TF][2];
+#pragma unroll
+    for (u32 h = 0; h < 2; ++h) {
+        const u32 n = n0 + h * 8 + line < p.n_out ? n0 + h * 8 + line : p.n_out - 1;
+        w[h] = p.w + static_cast<i64>(n) * p.ldw;
+        w_left[h] = static_cast<i64>(p.n_out - 1 - n) * p.ldw + p.n_sum;
+#pragma unroll
+        for (int f = 0; f < TF; ++f) {
+            const u32 t = f * 16 + h * 8 + line < p.n_tokens ? f * 16 + h * 8 + line : p.n_tokens - 1;
+            x[f][h] = p.x + static_cast<i64>(t) * p.ldx;
+            x_left[f][h] = static_cast<i64>(p.n_tokens - 1 - t) * p.ldx + p.n_sum;
+        }
+    }
     const float* xs[TF];
-    i64 x_left[TF];
 #pragma unroll
     for (int f = 0; f < TF; ++f) {
         const u32 t = f * 16 + (lane & 15) < p.n_tokens ? f * 16 + (lane & 15) : p.n_tokens - 1;
-        x[f] = p.x + static_cast<i64>(t) * p.ldx;
         xs[f] = p.xs + static_cast<i64>(t) * p.ldxs;
-        x_left[f] = static_cast<i64>(p.n_tokens - 1 - t) * p.ldx + p.n_sum;
     }
     const float* ws = p.ws + static_cast<i64>(n0 / kStep) * p.ldws;
     f32x4 acc[TF] = {};
     auto load = [&](const u8* row, i64 left, u32 s) {
-        const i64 a = static_cast<i64>(s) * kStep + g * 16, b = a + 64;
-        u32x4 lo, hi;
-        if (s < whole) {                                            // the same in the wavefront
-            lo = *reinterpret_cast<const u32x4_bytes*>(row + a);
-            hi = *reinterpret_cast<const u32x4_bytes*>(row + b);
-        } else {
-            lo = load16_codes(row, a, p.n_sum, left - a);
-            hi = load16_codes(row, b, p.n_sum, left - b);
-        }
-        return u32x8{lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+        const i64 k = static_cast<i64>(s) * kStep + piece * 16;
+        return s < whole ? *reinterpret_cast<const u32x4_bytes*>(row + k) : load16_codes(row, k, p.n_sum, left - k);         // the same way in the wavefront
+    };
+    auto turned = [&](const u32x4 (&v)[2], u32 f) {
+        u8* room = turns[wave][f];
+#pragma unroll
+        for (u32 h = 0; h < 2; ++h) *reinterpret_cast<u32x4*>(room + codes_along_at(h * 8 + line, piece)) = v[h];
+        return codes_along_frag(room, 0);
     };
     for (u32 s0 = wave; s0 < all; s0 += kAhead * waves) {
-        u32x8 fw[kAhead], fx[kAhead][TF];
+        u32x4 vw[kAhead][2], vx[kAhead][TF][2];
         float scale[kAhead][TF];
 #pragma unroll
         for (u32 q = 0; q < kAhead; ++q) {
             const u32 s = s0 + q * waves;
             if (s >= all) break;                                    // the same in the wavefront
-            fw[q] = load(w, w_left, s);
+#pragma unroll
+            for (u32 h = 0; h < 2; ++h) vw[q][h] = load(w[h], w_left[h], s);
             const float by = ws[s];
 #pragma unroll
             for (int f = 0; f < TF; ++f) {
-                fx[q][f] = load(x[f], x_left[f], s);
+#pragma unroll
+                for (u32 h = 0; h < 2; ++h) vx[q][f][h] = load(x[f][h], x_left[f][h], s);
                 scale[q][f] = xs[f][s] * by;
             }
         }
 #pragma unroll
         for (u32 q = 0; q < kAhead; ++q) {
             if (s0 + q * waves >= all) break;
+            const u32x8 fw = turned(vw[q], TF);
 #pragma unroll
             for (int f = 0; f < TF; ++f) {
-                const f32x4 v = mfma_codes(fw[q], fx[q][f]);
+                const f32x4 v = mfma_codes(fw, turned(vx[q][f], f));
 #pragma unroll
                 for (u32 k = 0; k < 4; ++k) acc[f][k] = __builtin_fmaf(v[k], scale[q][f], acc[f][k]);
             }
@@ -536,7 +546,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_product_few(ProductArgs p) {
     for (u32 f = wave; f < TF; f += waves) {
         f32x4 v = sums[0][f][lane];
         for (u32 k = 1; k < waves; ++k) v += sums[k][f][lane];
-        store_outputs(p, f * 16 + (lane & 15), n0 + g * 4, v);
+        store_outputs(p, f * 16 + (lane & 15), n0 + (lane >> 4) * 4, v);
     }
 }
 

@@ -7,29 +7,29 @@ namespace condensa {
 struct ProductPlan {
     bool few = false;
     u32 splits = 1, steps_each = 0;
-    size_t part = 0;                                          // bytes of the parts
 };
 
-constexpr u32 kMostSplits = 16;
-constexpr u64 kSplitTiles = 512;                              // tiles of parts that sums are split into, at most
+// Sums are split where tiles of 64 x 64 are few and steps many.  4608 -> 512, us whole and in four: 96 tokens (16 tiles, 36 steps) 13.1 and 9.0; 2600 -> 650, in two: 100 tokens
+// (22 tiles, 21 steps) 10.4 and 10.2; 2048 -> 512: 100 tokens (16 tiles, 16 steps) 7.7 and 7.6.
+constexpr u64 kSplitTiles = 64;
+constexpr u32 kSplitSteps = 20, kMostSplits = 4;
 
 static ProductPlan make_plan(i64 T, i64 n_out, i64 n_sum, bool along) {
     ProductPlan p;
     p.few = along && T <= kFewTokens;
-    if (p.few) return p;
     const u32 steps = static_cast<u32>(blocks_of(n_sum));
+    p.steps_each = steps;
+    if (p.few) return p;
     const u64 tiles = static_cast<u64>((T + 63) / 64) * ((n_out + 63) / 64);
-    u64 s = tiles ? kSplitTiles / tiles : 1;
-    s = std::min<u64>(s, std::min<u64>(kMostSplits, steps / 2));
-    s = s < 1 ? 1 : s;
-    p.steps_each = static_cast<u32>((steps + s - 1) / s);
+    if (tiles > kSplitTiles || steps < kSplitSteps) return p;
+    const u32 s = std::min(kMostSplits, steps / 8);
+    p.steps_each = (steps + s - 1) / s;
     p.splits = (steps + p.steps_each - 1) / p.steps_each;
-    if (p.splits > 1) p.part = align_up(static_cast<u64>(p.splits) * T * n_out * 4);
     return p;
 }
-// What a call with T tokens and every call with fewer can do with: parts of most splits, or of as many tiles as sums are split into at all.
+// What a call with T tokens and every call with fewer can do with: the most parts, of these tokens or of as many tiles as have any.
 static size_t workspace_for(i64 T, i64 n_out) {
-    const u64 b = std::min(static_cast<u64>(T) * n_out * 4 * kMostSplits, kSplitTiles * 64 * 64 * 4);
+    const u64 b = kMostSplits * std::min(static_cast<u64>(T) * n_out, kSplitTiles * 64 * 64) * 4;
     return b ? align_up(b) : 256;
 }
 
@@ -41,21 +41,30 @@ static void launch_tile(const ProductArgs& a, hipStream_t st) {
     hipLaunchKernelGGL((k_product<BM, BN, WM, WN, NB, ALONG>), dim3(static_cast<unsigned>(tiles)), dim3(64 * WM * WN), 0, st, a);
 }
 
+// Times in us below: 4608 -> 4096, 36 steps of the sum, and 512 -> 2048, 4 steps (long / short).
 template <bool ALONG>
 static void launch_product(const ProductArgs& a, bool rows16, hipStream_t st) {
     const auto tiles = [&](u64 m, u64 n) { return (a.n_tokens + m - 1) / m * ((a.n_out + n - 1) / n); };
+    const u64 t64 = tiles(64, 64), t128 = tiles(128, 128);
     if (!rows16) {
-        hipLaunchKernelGGL((k_product_any<ALONG>), dim3(static_cast<unsigned>(tiles(64, 64) * a.splits)), dim3(256), 0, st, a);
-    } else if (a.splits == 1 && tiles(256, 256) >= 192) {
-        // A tile of 256 rows fills a compute unit.  The one whose rounds over the 256 of them cost less is taken: 8192 x 4608 outputs are 2.25 rounds
-        // of 256 x 256, which take as long as three (193 us), and three of 256 x 192 (178 us).
-        const auto cost = [&](u64 n) { return (tiles(256, n) + 255) / 256 * n; };
-        if (cost(192) < cost(256)) launch_tile<256, 192, 2, 4, 2, ALONG>(a, st);
-        else                       launch_tile<256, 256, 2, 4, 2, ALONG>(a, st);
-    } else if (a.splits == 1 && tiles(128, 128) >= 192) {
-        launch_tile<128, 128, 2, 2, 2, ALONG>(a, st);
-    } else {
+        hipLaunchKernelGGL((k_product_any<ALONG>), dim3(static_cast<unsigned>(t64 * a.splits)), dim3(256), 0, st, a);
+    } else if (a.splits > 1 || t64 <= 256) {
+        // A tile a unit: 200 tokens 14.5 long, 4.7 short; with tiles of 128, four times fewer, 23.9 and 7.0.
         launch_tile<64, 64, 2, 2, 4, ALONG>(a, st);
+    } else if (t64 <= 512) {
+        // Two a unit, room for three: 400 tokens (448 tiles) 20.8 long, 800 (416) 6.1 short; with four steps in LDS 21.6 and 6.5, with tiles of 128 24.1 and 7.7.  832 tiles: 37.2 and, of 128, 24.8.
+        launch_tile<64, 64, 2, 2, 3, ALONG>(a, st);
+    } else if (t128 <= 256) {
+        // One a unit, eight wavefronts and four steps in LDS: 800 tokens 24.8; four wavefronts and two steps, which leave room for another workgroup, 37.7.
+        launch_tile<128, 128, 2, 4, 4, ALONG>(a, st);
+    } else {
+        // Rounds over the 256 units: a workgroup of 128 rows shares its unit with another (44 for two, 35 alone), one of 256 rows does not (66, or 60 with 192 outputs).  2048 tokens,
+        // 512 tiles of 128: 44, and 66 with 128 of 256 x 256.  4096 tokens: 96, and 74 with 256 of 256 x 256.  8192 x 4608 outputs, backward: 205, 193 and, with 768 of 256 x 192, 178.
+        const auto rounds = [](u64 n, u64 each) { return (n + each - 1) / each; };
+        const u64 c128 = t128 / 512 * 44 + (t128 % 512 == 0 ? 0 : (t128 % 512 <= 256 ? 35 : 44)), c192 = rounds(tiles(256, 192), 256) * 60, c256 = rounds(tiles(256, 256), 256) * 66;
+        if (c128 <= c192 && c128 <= c256) launch_tile<128, 128, 2, 2, 2, ALONG>(a, st);
+        else if (c192 < c256)             launch_tile<256, 192, 2, 4, 2, ALONG>(a, st);
+        else                              launch_tile<256, 256, 2, 4, 2, ALONG>(a, st);
     }
 }
 
@@ -76,9 +85,10 @@ static condensa_status product(const condensa_fp8_matrix* x, const condensa_fp8_
     if (T == 0) return CONDENSA_OK;
     if (!grid_fits(T, n_out)) return CONDENSA_ERR_SIZE;
     const ProductPlan p = make_plan(T, n_out, n_sum, along);
-    if (!workspace || !aligned_to(workspace, 256) || workspace_bytes < p.part) return CONDENSA_ERR_WORKSPACE;
+    const size_t need = workspace_for(T, n_out);
+    if (!workspace || !aligned_to(workspace, 256) || workspace_bytes < need) return CONDENSA_ERR_WORKSPACE;
     ByteRange r[] = {codes_range(x, false), scales_range(x, false), codes_range(w, false), scales_range(w, false),
-                     byte_range(y, rows_bytes(T, y_stride, n_out, 2), true), byte_range(p.part ? workspace : nullptr, p.part, true)};
+                     byte_range(y, rows_bytes(T, y_stride, n_out, 2), true), byte_range(workspace, need, true)};
     if (ranges_conflict(r, sizeof(r) / sizeof(r[0]))) return CONDENSA_ERR_ARG;
     ProductArgs a{};
     a.x = x->q; a.ldx = x->q_stride; a.xs = x->scale; a.ldxs = x->scale_stride;
@@ -86,7 +96,7 @@ static condensa_status product(const condensa_fp8_matrix* x, const condensa_fp8_
     a.y = y; a.ldy = y_stride;
     a.n_tokens = static_cast<u32>(T); a.n_out = static_cast<u32>(n_out); a.n_sum = static_cast<u32>(n_sum);
     a.splits = p.splits; a.steps_each = p.steps_each;
-    a.part = p.part ? static_cast<float*>(workspace) : nullptr;
+    a.part = p.splits > 1 ? static_cast<float*>(workspace) : nullptr;
     a.bf16 = type == CONDENSA_TYPE_BF16;
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (p.few) {
