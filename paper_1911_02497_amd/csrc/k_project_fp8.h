@@ -197,6 +197,26 @@ __global__ __launch_bounds__(256) void k_product_any(ProductArgs p) {
         }
 }
 
+// Rows at any address copied to rows that are 16-byte aligned, sixteen codes a thread: loads straight into LDS want those.
+struct CodesCopy {
+    const u8* src; i64 ld;
+    u8* dst;
+    u32 rows, cols, width;               // width: of a copied row, a multiple of sixteen
+    u32 blocks;                          // workgroups that copy it
+};
+struct CopyArgs { CodesCopy m[2]; };
+__global__ __launch_bounds__(256) void k_product_copy(CopyArgs a) {
+    const bool second = blockIdx.x >= a.m[0].blocks;
+    const CodesCopy& m = a.m[second];
+    const u32 pieces = m.width / 16;
+    const u64 at = static_cast<u64>(blockIdx.x - (second ? a.m[0].blocks : 0)) * 256 + threadIdx.x;
+    const u64 row = at / pieces;
+    if (row >= m.rows) return;
+    const i64 k = static_cast<i64>(at % pieces) * 16;
+    const u32x4 v = load16_codes(m.src + static_cast<i64>(row) * m.ld, k, m.cols, static_cast<i64>(m.rows - 1 - row) * m.ld + m.cols - k);
+    *reinterpret_cast<u32x4*>(m.dst + row * m.width + k) = v;
+}
+
 // Tiles of BM tokens by BN outputs of rows that are 16-byte aligned, NB steps in LDS.  Loads go straight into LDS, NB steps ahead of their use; a token's and W's scales of a step
 // come with it.  Sixteen tokens at a time meet the wavefront's fragments of W, their results are scaled and added while the next sixteen are multiplied, and the fragments of the
 // next step are read beside the last sixteen: wavefronts meet once a step, there, when the next step has come and the last read of this one is done.
