@@ -63,19 +63,19 @@ static void launch_product(const ProductArgs& a, bool rows16, hipStream_t st) {
     if (!rows16) {
         hipLaunchKernelGGL((k_product_any<ALONG>), dim3(static_cast<unsigned>(t64 * a.splits)), dim3(256), 0, st, a);
     } else if (a.splits > 1 || t64 <= 256) {
-        // A tile a unit: 200 tokens 14.5 long, 4.7 short; with tiles of 128, four times fewer, 23.9 and 7.0.
+        // A tile a unit: 200 tokens 13.5 long, 4.1 short; with tiles of 128, four times fewer, 23.0 and 6.0.
         launch_tile<64, 64, 2, 2, 4, ALONG>(a, st);
     } else if (t64 <= 512) {
-        // Two a unit, room for three: 400 tokens (448 tiles) 20.8 long, 800 (416) 6.1 short; with four steps in LDS 21.6 and 6.5, with tiles of 128 24.1 and 7.7.  832 tiles: 37.2 and, of 128, 24.8.
+        // Two a unit, room for three: 400 tokens (448 tiles) 20.5 long, 800 (416) 5.7 short; with four steps in LDS 21.1 and 6.0, with tiles of 128 23.3 and 6.8.  832 tiles: 36.7 and, of 128, 24.1.
         launch_tile<64, 64, 2, 2, 3, ALONG>(a, st);
     } else if (t128 <= 256) {
-        // One a unit, eight wavefronts and four steps in LDS: 800 tokens 24.8; four wavefronts and two steps, which leave room for another workgroup, 37.7.
+        // One a unit, eight wavefronts and four steps in LDS: 800 tokens 24.1; four wavefronts and two steps, which leave room for another workgroup, 35.8.
         launch_tile<128, 128, 2, 4, 4, ALONG>(a, st);
     } else {
-        // Rounds over the 256 units: a workgroup of 128 rows shares its unit with another (44 for two, 35 alone), one of 256 rows does not (66, or 60 with 192 outputs).  2048 tokens,
-        // 512 tiles of 128: 44, and 66 with 128 of 256 x 256.  4096 tokens: 96, and 74 with 256 of 256 x 256.  8192 x 4608 outputs, backward: 205, 193 and, with 768 of 256 x 192, 178.
+        // Rounds over the 256 units: a workgroup of 128 rows shares its unit with another (43 for two, 34 alone), one of 256 rows does not (70, or 59 with 192 outputs).  2048 tokens,
+        // 512 tiles of 128: 43, and 62 with 128 of 256 x 256.  4096 tokens: 94, and 71 with 256 of 256 x 256.  2900 tokens, backward: 71, 59 and, with 288 of 256 x 192, 112.
         const auto rounds = [](u64 n, u64 each) { return (n + each - 1) / each; };
-        const u64 c128 = t128 / 512 * 44 + (t128 % 512 == 0 ? 0 : (t128 % 512 <= 256 ? 35 : 44)), c192 = rounds(tiles(256, 192), 256) * 60, c256 = rounds(tiles(256, 256), 256) * 66;
+        const u64 c128 = t128 / 512 * 43 + (t128 % 512 == 0 ? 0 : (t128 % 512 <= 256 ? 34 : 43)), c192 = rounds(tiles(256, 192), 256) * 59, c256 = rounds(tiles(256, 256), 256) * 70;
         if (c128 <= c192 && c128 <= c256) launch_tile<128, 128, 2, 2, 2, ALONG>(a, st);
         else if (c192 < c256)             launch_tile<256, 192, 2, 4, 2, ALONG>(a, st);
         else                              launch_tile<256, 256, 2, 4, 2, ALONG>(a, st);
