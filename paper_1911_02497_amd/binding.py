@@ -1046,7 +1046,7 @@ def _operand(name, t, place, dtype, rows, cols):
 
 def _codes_for(codes, place, stream, rows, cols):
     """The matrix that a call writes codes into: the given one, or room for it; None for none."""
-    if codes is None or codes is False:
+    if not codes:
         return None
     if codes is True:
         return _made_matrix(place, stream, rows, cols, 1)
@@ -1069,6 +1069,11 @@ def _made_matrix(place, stream, rows, cols, block_rows):
 def _empty_like_rows(rows, cols, dtype, device):
     import torch
     return torch.empty((rows, cols), dtype=dtype, device=device)
+
+
+def _float_values(n, device):
+    import torch
+    return torch.empty(n, dtype=torch.float32, device=device)
 
 
 def condensa_quantize_fp8_blocks(x, out: Optional[Fp8Matrix] = None, block_rows=1, stream=None) -> Fp8Matrix:
@@ -1101,43 +1106,53 @@ def condensa_dequantize_fp8_blocks(m: Fp8Matrix, out=None, dtype=None, stream=No
 
 
 def _norm_weight(weight, place, dtype, width):
-    if not (weight.dim() == 1 and weight.shape[0] == width and weight.get_device() == place.index and weight.is_contiguous()
-            and (weight.dtype is dtype or _types().get(weight.dtype) == TYPE_F32)):
+    kind = weight.dtype
+    if not (weight.shape == (width,) and weight.get_device() == place.index and weight.is_contiguous() and (kind is dtype or _types().get(kind) == TYPE_F32)):
         raise TypeError(f"weight: {width} contiguous values of {dtype} or float32 on {place.device}")
-    return weight.data_ptr(), _types()[weight.dtype]
+    return weight.data_ptr(), _types()[kind]
 
 
-def _norm_rows(name, t, place):
-    if t.dim() != 2 or _types().get(t.dtype) not in (TYPE_F16, TYPE_BF16):
-        raise TypeError(f"{name}: a float16 or bfloat16 tensor [tokens, width]")
-    return t.shape[0], t.shape[1], t.dtype
+def _norm_rows(name, t):
+    """(shape, type, place) of what a norm is taken of."""
+    shape, dtype, index = t.shape, t.dtype, t.get_device()
+    if len(shape) != 2 or index < 0 or not _types().get(dtype):
+        raise TypeError(f"{name}: a float16 or bfloat16 tensor [tokens, width] on a device")
+    return shape, dtype, _place(index)
+
+
+def _like(name, t, shape, dtype, place):
+    """(address, row stride) of an operand of that shape, whose rows are contiguous; of none, where there is none."""
+    if t is None:
+        return 0, shape[1]
+    stride = t.stride()
+    if not (t.shape == shape and t.dtype is dtype and t.get_device() == place.index and (stride[1] == 1 or shape[1] == 1 or shape[0] == 0)
+            and (stride[0] >= shape[1] or shape[0] <= 1)):
+        raise TypeError(f"{name}: a {dtype} tensor {list(shape)} with contiguous rows on {place.device}")
+    return t.data_ptr(), (stride[0] if shape[0] > 1 else shape[1])           # the address of a tensor without elements is 0
 
 
 # condensa_rms_norm_call and _grad_call as bytes: filling a structure of ctypes takes two microseconds more
 _NORM_CALL, _NORM_GRAD_CALL = struct.Struct("6P6q2ifi"), struct.Struct("7P6q2ifi")
 
 
-def _optional(name, t, place, dtype, rows, cols):
-    return (0, cols) if t is None else _operand(name, t, place, dtype, rows, cols)
-
-
 def condensa_rms_norm(x, weight, residual=None, eps=1e-6, sum=None, y=None, codes=None, stream=None):
     """Marshals condensa_rms_norm.  ``sum`` (h = x + residual) is made where there is a residual and no tensor is given for it; False for none; it may be
     ``residual`` or ``x`` itself.  ``y`` and ``codes``: a tensor and an Fp8Matrix to write, True to make one.  With neither, y is made."""
-    place = _place_of(x, "x")
-    T, n, dtype = _norm_rows("x", x, place)
-    made = lambda: _made_for(place, stream, _empty_like_rows, T, n, dtype, place.device)  # noqa: E731
+    shape, dtype, place = _norm_rows("x", x)
+    T, n = shape
     if sum is True or (sum is None and residual is not None):
-        sum = made()
-    sum = None if sum is False else sum
-    if y is True or ((y is None or y is False) and (codes is None or codes is False)):
-        y = made()
-    y = None if y is False else y
+        sum = _made_for(place, stream, _empty_like_rows, T, n, dtype, place.device)
+    elif sum is False:
+        sum = None
+    if y is True or (not codes and (y is None or y is False)):
+        y = _made_for(place, stream, _empty_like_rows, T, n, dtype, place.device)
+    elif y is False:
+        y = None
     codes = _codes_for(codes, place, stream, T, n)
-    px, ldx = _operand("x", x, place, dtype, T, n)
-    pr, ldr = _optional("residual", residual, place, dtype, T, n)
-    ps, lds = _optional("sum", sum, place, dtype, T, n)
-    py, ldy = _optional("y", y, place, dtype, T, n)
+    px, ldx = _like("x", x, shape, dtype, place)
+    pr, ldr = _like("residual", residual, shape, dtype, place)
+    ps, lds = _like("sum", sum, shape, dtype, place)
+    py, ldy = _like("y", y, shape, dtype, place)
     pw, wt = _norm_weight(weight, place, dtype, n)
     call = _NORM_CALL.pack(px, pr, pw, ps, py, 0 if codes is None else codes.address, T, n, ldx, ldr, lds, ldy, _types()[dtype], wt, eps, 0)
     _run(place, stream, library().condensa_rms_norm, call)
@@ -1156,28 +1171,30 @@ def rms_norm_workspace(n_tokens, width, device="cuda"):
 def condensa_rms_norm_backward(dy, h, weight, dsum=None, eps=1e-6, dx=True, dweight=True, codes=None, workspace=None, stream=None):
     """Marshals condensa_rms_norm_backward.  ``h``: what the norm was taken of (``sum`` of the forward call, or its x); ``dsum``: the gradient that reaches h from
     elsewhere.  ``dx``, ``dweight`` and ``codes`` (dx in 8 bits): what to write, True to make one, False or None for none; ``dx`` may be ``dsum`` itself."""
-    place = _place_of(dy, "dy")
-    T, n, dtype = _norm_rows("dy", dy, place)
+    shape, dtype, place = _norm_rows("dy", dy)
+    T, n = shape
     if dx is True:
         dx = _made_for(place, stream, _empty_like_rows, T, n, dtype, place.device)
-    dx = None if dx is False else dx
+    elif dx is False:
+        dx = None
     if dweight is True:
-        import torch
-        dweight = _made_for(place, stream, torch.empty, n, dtype=torch.float32, device=place.device)
-    dweight = None if dweight is False else dweight
-    if dweight is not None and not (dweight.dim() == 1 and dweight.shape[0] == n and _types().get(dweight.dtype) == TYPE_F32 and dweight.get_device() == place.index
-                                    and dweight.is_contiguous()):
-        raise TypeError(f"dweight: {n} contiguous float32 on {place.device}")
+        dweight = _made_for(place, stream, _float_values, n, place.device)
+    elif dweight is False:
+        dweight = None
+    pdw = 0
+    if dweight is not None:
+        if not (dweight.shape == (n,) and _types().get(dweight.dtype) == TYPE_F32 and dweight.get_device() == place.index and dweight.is_contiguous()):
+            raise TypeError(f"dweight: {n} contiguous float32 on {place.device}")
+        if workspace is None:
+            workspace = _made_for(place, stream, rms_norm_workspace, T, n, place.device)
+        pdw = dweight.data_ptr()
     codes = _codes_for(codes, place, stream, T, n)
-    if dweight is not None and workspace is None:
-        workspace = _made_for(place, stream, rms_norm_workspace, T, n, place.device)
-    pdy, lddy = _operand("dy", dy, place, dtype, T, n)
-    ph, ldh = _operand("h", h, place, dtype, T, n)
-    ps, lds = _optional("dsum", dsum, place, dtype, T, n)
-    pdx, lddx = _optional("dx", dx, place, dtype, T, n)
+    pdy, lddy = _like("dy", dy, shape, dtype, place)
+    ph, ldh = _like("h", h, shape, dtype, place)
+    ps, lds = _like("dsum", dsum, shape, dtype, place)
+    pdx, lddx = _like("dx", dx, shape, dtype, place)
     pw, wt = _norm_weight(weight, place, dtype, n)
-    call = _NORM_GRAD_CALL.pack(pdy, ph, ps, pw, pdx, 0 if dweight is None else dweight.data_ptr(), 0 if codes is None else codes.address, T, n,
-                                lddy, ldh, lds, lddx, _types()[dtype], wt, eps, 0)
+    call = _NORM_GRAD_CALL.pack(pdy, ph, ps, pw, pdx, pdw, 0 if codes is None else codes.address, T, n, lddy, ldh, lds, lddx, _types()[dtype], wt, eps, 0)
     pws, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
     _run(place, stream, library().condensa_rms_norm_backward, call, pws, size)
     return {"dx": dx, "dweight": dweight, "codes": codes, "workspace": workspace}

@@ -225,7 +225,7 @@ condensa_status condensa_rms_norm_backward(const condensa_rms_norm_grad_call* c,
         CONDENSA_LAUNCH_CHECK();
     }
     if (c->dweight) {
-        hipLaunchKernelGGL(k_rms_norm_join, dim3((a.n + 63) / 64), dim3(1024), 0, st, static_cast<const float*>(workspace_dev), groups, a.n, c->dweight);
+        hipLaunchKernelGGL(k_rms_norm_join, dim3((a.n + kJoinCols - 1) / kJoinCols), dim3(kJoinCols * kJoinRows), 0, st, static_cast<const float*>(workspace_dev), groups, a.n, c->dweight);
         CONDENSA_LAUNCH_CHECK();
     }
     return CONDENSA_OK;
