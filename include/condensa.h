@@ -569,7 +569,7 @@ typedef struct {
  * Quantize for such matrices, and back.  scale = (largest finite magnitude of the block) / 448, or 0 where that magnitude is below 2^-100;
  * code = the nearest code to x * 448 / (that magnitude), ties to the even fraction, of the exact quotient.  Infinities saturate, a NaN stays the
  * element's own, a block of scale 0 has codes of zeros (NaN but for).  Zeros stay zeros.  x and dq have the type CONDENSA_TYPE_F32, _F16 or _BF16,
- * contiguous rows x_stride / dq_stride elements apart (up to 2^22); dq = code * scale in binary32, rounded to the type.  No workspace; q and scale of `m` are what the first call
+ * contiguous rows x_stride / dq_stride elements apart (up to 2^22; fewer than 2^26 pieces of 512 columns, or 2^23 blocks, in all: CONDENSA_ERR_SIZE); dq = code * scale in binary32, rounded to the type.  No workspace; q and scale of `m` are what the first call
  * writes and the second reads.
  */
 condensa_status condensa_quantize_fp8_blocks(const void* x_dev, int type, int64_t x_stride, const condensa_fp8_matrix* m, void* stream);
@@ -580,7 +580,7 @@ condensa_status condensa_dequantize_fp8_blocks(const condensa_fp8_matrix* m, voi
  *   h = x + residual, rounded to the 16-bit type (h = x without a residual);   y = h * weight / sqrt(mean of h^2 + eps)
  * and the codes are those of y in binary32, one scale for 128 columns.  Sums are binary32 in an order that depends on width and n_tokens alone.
  * Squares outside the range of binary32 do not matter.  `sum` receives h; it may be `residual` or `x` itself (the same address and stride).
- * n_tokens 0..2^24, width 1..CONDENSA_MAX_NORM_WIDTH, strides in elements, up to 2^22; x, residual, sum and y of `type` (CONDENSA_TYPE_F16 or
+ * n_tokens 0..2^24 (and fewer than 2^26 wavefronts of 1024 columns: CONDENSA_ERR_SIZE), width 1..CONDENSA_MAX_NORM_WIDTH, strides in elements, up to 2^22; x, residual, sum and y of `type` (CONDENSA_TYPE_F16 or
  * _BF16), weight of weight_type (that one, or CONDENSA_TYPE_F32).  One launch, no workspace.
  */
 #define CONDENSA_MAX_NORM_WIDTH 32768

@@ -168,6 +168,7 @@ condensa_status condensa_rms_norm(const condensa_rms_norm_call* c, void* stream)
     a.waves = share.waves;
     const u32 rows_each = share.waves == 1 ? 4 : 1;
     const dim3 grid((a.n_tokens + rows_each - 1) / rows_each), threads(64 * share.waves * rows_each);
+    if (static_cast<u64>(grid.x) * threads.x >= kMaxGroups * 256) return CONDENSA_ERR_SIZE;
     hipStream_t st = static_cast<hipStream_t>(stream);
     with_types(c->type, c->weight_type, [&](auto rows_type, auto weight_type) {
         with_share(share.each, vec, [&](auto each, auto v) {

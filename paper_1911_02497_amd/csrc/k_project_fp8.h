@@ -219,9 +219,13 @@ __global__ __launch_bounds__(256) void k_product_copy(CopyArgs a) {
     *reinterpret_cast<u32x4*>(m.dst + row * m.width + k) = v;
 }
 
-// Tiles of BM tokens by BN outputs of rows that are 16-byte aligned, NB steps in LDS.  Loads go straight into LDS, NB steps ahead of their use; a token's and W's scales of a step
-// come with it.  Sixteen tokens at a time meet the wavefront's fragments of W, their results are scaled and added while the next sixteen are multiplied, and the fragments of the
-// next step are read beside the last sixteen: wavefronts meet once a step, there, when the next step has come and the last read of this one is done.
+// Tiles of BM tokens by BN outputs of rows that are 16-byte aligned, NB steps in LDS.  Loads go straight into LDS, NB - 1 steps ahead of their use, a few of them beside each sixteen tokens
+// of a step; a token's and W's scales of a step come with it.  (A 16-byte piece may end past its row; it never leaves the sixteen bytes that hold the row's last code.)  Sixteen
+// tokens at a time meet the wavefront's fragments of W, their results are scaled and added while the next sixteen are multiplied, and the fragments of the next step are read beside
+// the last sixteen: wavefronts meet once a step, just before, when the next step has come and the last read of this one is done.
+// 8192 tokens, 4608 -> 4096: 143 us, 2.2 PFLOP/s; backward 179 us.  What the time of 256 x 256 goes to, parts left out (150 us on that card): without loads 129, without LDS reads 142,
+// with a quarter of the additions 139, without all three 109, of which 22 are two rounds of first loads and of outputs, and the rest the matrix instructions.  So none of them
+// bounds it alone: they share a wavefront's issue and meet at its barrier.  Two groups of wavefronts in turns, one multiplying while the other reads LDS, took 150 us where this took 144.
 constexpr u32 product_lds(u32 bm, u32 bn, u32 nb) { return nb * ((bm + bn) * kStep + bm * 4 + 256) + (bm == 256 ? 256 : 0); }
 template <int BM, int BN, int WM, int WN, int NB, bool ALONG>
 __device__ inline void product_tile(const ProductArgs& p, u32 block_id, u32 n_blocks, u8* lds) {
@@ -489,7 +493,9 @@ constexpr u32 kFewTokens = 64, kFewWaves = 8;
 
 // Up to 16 TF tokens times sixteen rows of W a workgroup, whose wavefronts take steps of the sum in turn and add their sums up in LDS, in order.  W is read once, x comes out of
 // the caches.  Loads take whole cache lines, eight lanes to a line (a lane each from sixteen rows, as the operands want them, costs the address unit four times as long), and the
-// wavefront's own LDS turns them into fragments, without barriers.  Rows at any address.
+// wavefront's own LDS turns them into fragments, without barriers.  Rows at any address.  us, with fragments loaded as they are, this way, and as split tiles of 64: 4608 -> 4096, 1 token 6.0,
+// 6.8 and 8.4, 32 tokens 10.2, 7.6 and 9.4, 64 tokens 15.3, 10.2 and 10.3; 2048 -> 512, 64 tokens 8.3, 6.0 and 7.4.  Three and five steps under way, or sixteen wavefronts, gain nothing or
+// half a microsecond.
 template <int TF>
 __global__ __launch_bounds__(64 * kFewWaves) void k_product_few(ProductArgs p) {
     __shared__ __align__(16) f32x4 sums[kFewWaves][TF][64];
