@@ -55,31 +55,66 @@ static void launch_tile(const ProductArgs& a, hipStream_t st) {
     hipLaunchKernelGGL((k_product<BM, BN, WM, WN, NB, ALONG>), dim3(static_cast<unsigned>(tiles)), dim3(64 * WM * WN), 0, st, a);
 }
 
-// Times in us below: 4608 -> 4096, 36 steps of the sum, and 512 -> 2048, 4 steps (long / short).
-template <bool ALONG>
-static void launch_product(const ProductArgs& a, bool rows16, hipStream_t st) {
-    const auto tiles = [&](u64 m, u64 n) { return (a.n_tokens + m - 1) / m * ((a.n_out + n - 1) / n); };
+// Forms of tiles, and what a call costs with each, in us of 36 steps of the sum.  Times below: 4608 -> 4096, 36 steps, and 512 -> 2048, 4 steps (long / short).
+enum Form { kTiles64Deep, kTiles64, kTiles128Deep, kTiles128, kTiles192, kTiles256 };
+struct FormCost {
+    Form form;
+    u64 cost;
+};
+static FormCost best_form(u64 n_tokens, u64 n_out) {
+    const auto tiles = [&](u64 m, u64 n) { return (n_tokens + m - 1) / m * ((n_out + n - 1) / n); };
     const u64 t64 = tiles(64, 64), t128 = tiles(128, 128);
+    // A tile a unit: 200 tokens 13.5 long, 4.1 short; with tiles of 128, four times fewer, 23.0 and 6.0.
+    if (t64 <= 256) return {kTiles64Deep, 14};
+    // Two a unit, room for three: 400 tokens (448 tiles) 20.5 long, 800 (416) 5.7 short; with four steps in LDS 21.1 and 6.0, with tiles of 128 23.3 and 6.8.  832 tiles: 36.7 and, of 128, 24.1.
+    if (t64 <= 512) return {kTiles64, 21};
+    // One a unit, eight wavefronts and four steps in LDS: 800 tokens 24.1; four wavefronts and two steps, which leave room for another workgroup, 35.8.
+    if (t128 <= 256) return {kTiles128Deep, 24};
+    // Rounds over the 256 units: a workgroup of 128 rows shares its unit with another (43 for two, 34 alone), one of 256 rows does not (70, or 59 with 192 outputs).  2048 tokens,
+    // 512 tiles of 128: 43, and 62 with 128 of 256 x 256.  4096 tokens: 94, and 71 with 256 of 256 x 256.  2900 tokens, backward: 71, 59 and, with 288 of 256 x 192, 112.
+    const auto rounds = [](u64 n, u64 each) { return (n + each - 1) / each; };
+    const u64 c128 = t128 / 512 * 43 + (t128 % 512 == 0 ? 0 : (t128 % 512 <= 256 ? 34 : 43)), c192 = rounds(tiles(256, 192), 256) * 59, c256 = rounds(tiles(256, 256), 256) * 70;
+    if (c128 <= c192 && c128 <= c256) return {kTiles128, c128};
+    return c192 < c256 ? FormCost{kTiles192, c192} : FormCost{kTiles256, c256};
+}
+
+// Outputs that whole rounds of tiles of 256 x 256 make, where what is left costs less in a form of its own than another round; else 0.  8192 x 4608 outputs,
+// backward: two rounds and 512 outputs in tiles of 128 161 us, three rounds of 256 x 192 176; 4096 x 4608 93 and 111; 4000 x 4400 forward 53 and 62.
+static u32 whole_rounds(const ProductArgs& a, u64 cost) {
+    const u64 rows = (a.n_tokens + 255) / 256, columns = a.n_out / 256, rounds = rows * columns / 256;
+    if (rounds == 0 || a.n_sum < 16 * kStep) return 0;
+    const u64 first = rounds * 256 / rows * 256;
+    return first < a.n_out && rounds * 70 + best_form(a.n_tokens, a.n_out - first).cost < cost ? static_cast<u32>(first) : 0;
+}
+
+template <bool ALONG>
+static condensa_status launch_product(const ProductArgs& a, bool rows16, hipStream_t st) {
+    const FormCost best = best_form(a.n_tokens, a.n_out);
     if (!rows16) {
-        hipLaunchKernelGGL((k_product_any<ALONG>), dim3(static_cast<unsigned>(t64 * a.splits)), dim3(256), 0, st, a);
-    } else if (a.splits > 1 || t64 <= 256) {
-        // A tile a unit: 200 tokens 13.5 long, 4.1 short; with tiles of 128, four times fewer, 23.0 and 6.0.
-        launch_tile<64, 64, 2, 2, 4, ALONG>(a, st);
-    } else if (t64 <= 512) {
-        // Two a unit, room for three: 400 tokens (448 tiles) 20.5 long, 800 (416) 5.7 short; with four steps in LDS 21.1 and 6.0, with tiles of 128 23.3 and 6.8.  832 tiles: 36.7 and, of 128, 24.1.
-        launch_tile<64, 64, 2, 2, 3, ALONG>(a, st);
-    } else if (t128 <= 256) {
-        // One a unit, eight wavefronts and four steps in LDS: 800 tokens 24.1; four wavefronts and two steps, which leave room for another workgroup, 35.8.
-        launch_tile<128, 128, 2, 4, 4, ALONG>(a, st);
+        const u64 tiles = static_cast<u64>((a.n_tokens + 63) / 64) * ((a.n_out + 63) / 64) * a.splits;
+        hipLaunchKernelGGL((k_product_any<ALONG>), dim3(static_cast<unsigned>(tiles)), dim3(256), 0, st, a);
+    } else if (const u32 first = a.splits > 1 ? 0 : whole_rounds(a, best.cost)) {
+        ProductArgs r = a;
+        r.n_out = first;
+        launch_tile<256, 256, 2, 4, 2, ALONG>(r, st);
+        CONDENSA_LAUNCH_CHECK();
+        r.n_out = a.n_out - first;
+        r.w += ALONG ? static_cast<i64>(first) * a.ldw : first;
+        r.ws += ALONG ? static_cast<i64>(first / kStep) * a.ldws : first / kStep;
+        r.y += first;
+        return launch_product<ALONG>(r, rows16, st);
     } else {
-        // Rounds over the 256 units: a workgroup of 128 rows shares its unit with another (43 for two, 34 alone), one of 256 rows does not (70, or 59 with 192 outputs).  2048 tokens,
-        // 512 tiles of 128: 43, and 62 with 128 of 256 x 256.  4096 tokens: 94, and 71 with 256 of 256 x 256.  2900 tokens, backward: 71, 59 and, with 288 of 256 x 192, 112.
-        const auto rounds = [](u64 n, u64 each) { return (n + each - 1) / each; };
-        const u64 c128 = t128 / 512 * 43 + (t128 % 512 == 0 ? 0 : (t128 % 512 <= 256 ? 34 : 43)), c192 = rounds(tiles(256, 192), 256) * 59, c256 = rounds(tiles(256, 256), 256) * 70;
-        if (c128 <= c192 && c128 <= c256) launch_tile<128, 128, 2, 2, 2, ALONG>(a, st);
-        else if (c192 < c256)             launch_tile<256, 192, 2, 4, 2, ALONG>(a, st);
-        else                              launch_tile<256, 256, 2, 4, 2, ALONG>(a, st);
+        switch (a.splits > 1 ? kTiles64Deep : best.form) {
+            case kTiles64Deep:  launch_tile<64, 64, 2, 2, 4, ALONG>(a, st); break;
+            case kTiles64:      launch_tile<64, 64, 2, 2, 3, ALONG>(a, st); break;
+            case kTiles128Deep: launch_tile<128, 128, 2, 4, 4, ALONG>(a, st); break;
+            case kTiles128:     launch_tile<128, 128, 2, 2, 2, ALONG>(a, st); break;
+            case kTiles192:     launch_tile<256, 192, 2, 4, 2, ALONG>(a, st); break;
+            case kTiles256:     launch_tile<256, 256, 2, 4, 2, ALONG>(a, st); break;
+        }
     }
+    CONDENSA_LAUNCH_CHECK();
+    return CONDENSA_OK;
 }
 
 // Names the copy of a matrix's rows and puts it in their place.
@@ -143,9 +178,8 @@ static condensa_status product(const condensa_fp8_matrix* x, const condensa_fp8_
         CONDENSA_LAUNCH_CHECK();
     }
     const bool fast = rows16(a.x, a.ldx) && rows16(a.w, a.ldw);
-    if (along) launch_product<true>(a, fast, st);
-    else       launch_product<false>(a, fast, st);
-    CONDENSA_LAUNCH_CHECK();
+    rc = along ? launch_product<true>(a, fast, st) : launch_product<false>(a, fast, st);
+    if (rc != CONDENSA_OK) return rc;
     if (a.part) {
         hipLaunchKernelGGL(k_product_join, dim3((a.n_out + 1023) / 1024, a.n_tokens), dim3(256), 0, st, a);
         CONDENSA_LAUNCH_CHECK();

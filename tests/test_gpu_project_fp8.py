@@ -49,7 +49,7 @@ def check(out, x, w, t, steps):
 
 SIZES = [(1, 512, 2048), (1, 1, 1), (1, 130, 70), (2, 128, 64), (5, 257, 129), (16, 4608, 256), (17, 1000, 333), (31, 64, 4096), (64, 4608, 1024), (65, 200, 65), (96, 2048, 512),
          (129, 650, 2600), (200, 640, 640), (257, 1024, 520), (300, 2600, 650), (1000, 384, 384), (1024, 1024, 1024), (2048, 520, 2048), (1333, 650, 1000), (3584, 200, 3520), (3500, 3584, 300), (400, 520, 4096), (1800, 4096, 333),
-         (100, 2700, 500), (70, 600, 2600), (1100, 1003, 1999)]
+         (100, 2700, 500), (70, 600, 2600), (1100, 1003, 1999), (4000, 2100, 4400), (4000, 4400, 2100)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
