@@ -121,7 +121,7 @@ def check_codes(m, y, slack):
 
 
 NORMS = [(1, 512, 0, 0), (1, 1, 0, 0), (2, 7, 0, 1), (3, 130, 3, 1), (33, 650, 0, 0), (5, 4608, 8, 0), (9, 4097, 0, 0), (4, 8192, 0, 0), (600, 129, 7, 0), (2, 16384, 0, 0), (2, 30001, 0, 0),
-         (1, 32768, 0, 0), (1537, 64, 0, 0), (700, 1030, 0, 0)]
+         (1, 32768, 0, 0), (1537, 64, 0, 0), (700, 1030, 0, 0), (3, 1500, 0, 0), (2, 19900, 0, 0), (4200, 4608, 0, 0)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
