@@ -1031,6 +1031,8 @@ class Fp8Matrix:
 def fp8_matrix(rows, cols, block_rows=1, device="cuda") -> Fp8Matrix:
     """Room for a matrix in 8 bits, in rows that begin at multiples of 128 bytes: products are fastest with those."""
     import torch
+    if block_rows not in (1, FP8_BLOCK):
+        raise ValueError(f"block_rows is 1 or {FP8_BLOCK}")
     q = torch.empty((rows, -(-cols // FP8_BLOCK) * FP8_BLOCK), dtype=torch.uint8, device=device)[:, :cols]
     return Fp8Matrix(q, torch.empty((-(-rows // block_rows), -(-cols // FP8_BLOCK)), dtype=torch.float32, device=device), block_rows)
 

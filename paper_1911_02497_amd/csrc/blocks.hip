@@ -189,7 +189,8 @@ condensa_status condensa_rms_norm_backward(const condensa_rms_norm_grad_call* c,
     if (!c) return CONDENSA_ERR_NULL;
     condensa_status rc = check_norm(c->n_tokens, c->width, c->type, c->weight_type, c->weight, c->codes, c->eps, c->reserved);
     if (rc != CONDENSA_OK) return rc;
-    if ((c->n_tokens > 0 && (!c->dy || !c->h)) || (!c->dx && !c->dweight && !c->codes)) return CONDENSA_ERR_NULL;
+    if (c->n_tokens == 0 && !c->dweight) return CONDENSA_OK;
+    if (c->n_tokens > 0 && (!c->dy || !c->h || (!c->dx && !c->dweight && !c->codes))) return CONDENSA_ERR_NULL;
     if (!aligned_to(c->dweight, 4)) return CONDENSA_ERR_ARG;
     const struct { const void* p; i64 stride; } rows[] = {{c->dy, c->dy_stride}, {c->h, c->h_stride}, {c->dsum, c->dsum_stride}, {c->dx, c->dx_stride}};
     bool vec = vec_rows(c->weight, 0, c->width, c->weight_type);

@@ -112,6 +112,7 @@ def test_norm_without_tokens():
     assert lib.condensa_rms_norm(None, None) == NULL and lib.condensa_rms_norm_backward(None, None, 0, None) == NULL
     assert norm(n_tokens=0, x=None, residual=None, sum=None, y=None) == 0
     assert norm_back(n_tokens=0, dy=None, h=None, dsum=None, dx=None, dweight=None, codes=matrix(6, rows=0, q=None, scale=None), ws=None, size=0) == 0
+    assert norm_back(n_tokens=0, dy=None, h=None, dsum=None, dx=None, dweight=None, ws=None, size=0) == 0           # dx of no tokens has no address
     size = lib.condensa_rms_norm_workspace_bytes
     assert size(-1, 64) == 0 and size((1 << 24) + 1, 64) == 0 and size(1, 0) == 0 and size(1, 32769) == 0
     sizes = [size(T, 1000) for T in (0, 1, 100, 511, 512, 513, 8192, 1 << 24)]
