@@ -105,3 +105,20 @@ def test_zero_tokens_and_a_kept_workspace():
         x, dy = matrix(T, 900, 1, g), matrix(T, 700, 1, g)
         assert torch.equal(P.condensa_project_fp8(x, w, dtype=torch.float16, workspace=ws[0])["y"], P.condensa_project_fp8(x, w, dtype=torch.float16)["y"])
         assert torch.equal(P.condensa_project_fp8_backward(dy, w, dtype=torch.float16, workspace=ws[1])["dx"], P.condensa_project_fp8_backward(dy, w, dtype=torch.float16)["dx"])
+
+
+@pytest.mark.parametrize("T", [1, 40, 100, 700])
+def test_scales_of_infinity_stay_in_their_rows_and_blocks(T):
+    K, N = 300, 400
+    g = torch.Generator(DEV).manual_seed(T)
+    w, x = matrix(N, K, 128, g, 20, 0), matrix(T, K, 1, g, 20, 0)
+    y = P.condensa_project_fp8(x, w, dtype=torch.bfloat16)["y"]
+    was = float(x.scale[T // 2, 1])
+    x.scale[T // 2, 1] = float("inf")
+    bad = P.condensa_project_fp8(x, w, dtype=torch.bfloat16)["y"]
+    rest = torch.arange(T, device=DEV) != T // 2
+    assert not bool(torch.isfinite(bad[T // 2]).any()) and torch.equal(bad[rest], y[rest])
+    x.scale[T // 2, 1] = was
+    w.scale[2, 0] = float("inf")                                          # rows 256 .. 383 of W
+    bad = P.condensa_project_fp8(x, w, dtype=torch.bfloat16)["y"]
+    assert not bool(torch.isfinite(bad[:, 256:384]).any()) and torch.equal(bad[:, :256], y[:, :256]) and torch.equal(bad[:, 384:], y[:, 384:])
