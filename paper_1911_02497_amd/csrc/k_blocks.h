@@ -512,8 +512,8 @@ struct NormGradArgs {
 
 // Where a row is one wavefront, a workgroup's wavefronts have rows of their own; else it takes rows in turn.  Its lanes keep their columns of the weight's gradient.  Where a wavefront
 // has 512 columns the next row's values are on their way while one row is worked on, and the weight stays in registers; with 1024 and more there are none left for that.
-// Reading three operands and writing dx bounds it, beside a barrier for each row: 8192 x 4608 with codes 72 us, 4.7 TB/s; without the next row's values under way 82, with 1024 columns
-// a wavefront 78.
+// Reading three operands and writing dx, twice with codes, bounds it: 8192 x 4608 with codes 72 us, 4.7 TB/s, as a copy; without the next row's values under way 82, with 1024 columns
+// a wavefront 78; two rows between barriers, which spill five registers, take 8 us more.
 template <typename R, typename W, u32 CH, bool VEC>
 __global__ __launch_bounds__(64 * kNormWaves) void k_rms_norm_grad(NormGradArgs p) {
     constexpr bool kKeep = CH == 1;
