@@ -401,7 +401,10 @@ __device__ inline void row_sums(float (&x)[N], u32 waves, float* s) {
     }
 }
 
-// A row's squares are of values times `by`, a power of two: 1, or 2^-64 where squares would leave binary32's range.  r = by / sqrt(mean + eps) then, for values times by.
+// A row whose squares leave binary32's range is taken again with values times half * half, a power of two, and eps times its square; what this answers is then 1 / sqrt(mean + eps) of
+// such values, and 1 / sqrt(mean of h^2 + eps) itself is that times half * half.  2^-72: 32768 squares of the largest value, 2^112 then, sum up to 2^127, and the mean of a row that needs
+// it is 2^-31 or more.  Half of the factor goes to the values and half to the rest where h is multiplied by the weight, so that neither leaves the range for the other's sake.
+constexpr float kLargeHalf = 0x1p-36f;
 __device__ inline float norm_factor(float squares, u32 n, float eps) { return __fdiv_rn(1.0f, __fsqrt_rn(__fdiv_rn(squares, static_cast<float>(n)) + eps)); }
 
 // Codes of y r and their scale, from values y whose own range is in hand: r cancels in what a code is made of, so codes are those of products of h and the weight.
@@ -460,14 +463,15 @@ __global__ __launch_bounds__(64 * kNormWaves) void k_rms_norm(NormArgs p) {
     };
     float squares[1] = {squares_of(1.0f)};
     row_sums(squares, p.waves, s[0]);
-    float by = 1.0f, eps = p.eps;
+    float half = 1.0f, eps = p.eps;
     if (!(squares[0] < __builtin_inff())) {                   // the same in the whole row
-        by = 0x1p-64f;
-        eps *= 0x1p-128f;
+        half = kLargeHalf;
+        const float by = half * half;
+        eps = eps * by * by;
         squares[0] = squares_of(by);
         row_sums(squares, p.waves, s[1]);
     }
-    const float r = norm_factor(squares[0], p.n, eps);
+    const float r = norm_factor(squares[0], p.n, eps) * half;
     if (p.sum) {
 #pragma unroll
         for (u32 c = 0; c < CH; ++c) store8<VEC>(p.sum + static_cast<i64>(row) * p.ldsum, k0 + c * kWaveCols, p.n, h[c]);
@@ -480,7 +484,7 @@ __global__ __launch_bounds__(64 * kNormWaves) void k_rms_norm(NormArgs p) {
         float a[8];
         R::unpack(h[c], a);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) a[i] = a[i] * by * w[c][i];
+        for (int i = 0; i < 8; ++i) a[i] = a[i] * half * w[c][i];
         if (p.q) {
             float scale;
             store8_codes(p.q + static_cast<i64>(row) * p.ldq, k, p.n, scaled_codes(a, r, &scale));
@@ -574,8 +578,8 @@ __global__ __launch_bounds__(64 * kNormWaves) void k_rms_norm_grad(NormGradArgs 
         float by = 1.0f, eps = p.eps;
         if (!(sums[0] < __builtin_inff())) {                  // the same in the whole row
             if (p.waves > 1) __syncthreads();                 // (for the third piece of LDS)
-            by = 0x1p-64f;
-            eps *= 0x1p-128f;
+            by = kLargeHalf * kLargeHalf;
+            eps = eps * by * by;
             add(by, s[2]);
         }
         const float r = norm_factor(sums[0], p.n, eps), r_by = r * by;
