@@ -405,6 +405,9 @@ __device__ inline void row_sums(float (&x)[N], u32 waves, float* s) {
 // such values, and 1 / sqrt(mean of h^2 + eps) itself is that times half * half.  2^-72: 32768 squares of the largest value, 2^112 then, sum up to 2^127, and the mean of a row that needs
 // it is 2^-31 or more.  Half of the factor goes to the values and half to the rest where h is multiplied by the weight, so that neither leaves the range for the other's sake.
 constexpr float kLargeHalf = 0x1p-36f;
+// The same for sums of (dy weight) h, whose mean is in range wherever the products dy weight are: those are taken times kLargeSlope^2 for the sum (2^48 at most beside values of up to
+// 2^64: 32768 products sum up to 2^127) and times kLargeSlope beside their mean, with the other half in the factor that follows.
+constexpr float kLargeSlope = 0x1p-40f;
 __device__ inline float norm_factor(float squares, u32 n, float eps) { return __fdiv_rn(1.0f, __fsqrt_rn(__fdiv_rn(squares, static_cast<float>(n)) + eps)); }
 
 // Codes of y r and their scale, from values y whose own range is in hand: r cancels in what a code is made of, so codes are those of products of h and the weight.
@@ -558,7 +561,7 @@ __global__ __launch_bounds__(64 * kNormWaves) void k_rms_norm_grad(NormGradArgs 
         for (u32 c = 0; c < CH; ++c) { h[c] = next_h[c]; dy[c] = next_dy[c]; ds[c] = next_ds[c]; }
         if (kKeep && row + stride < p.n_tokens) fetch(row + stride);
         float sums[2];
-        auto add = [&](float by, float* room) {
+        auto add = [&](float by, float slope, float* room) {
             sums[0] = sums[1] = 0.0f;
 #pragma unroll
             for (u32 c = 0; c < CH; ++c) {
@@ -569,43 +572,56 @@ __global__ __launch_bounds__(64 * kNormWaves) void k_rms_norm_grad(NormGradArgs 
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     sums[0] = __builtin_fmaf(a[i] * by, a[i] * by, sums[0]);
-                    sums[1] = __builtin_fmaf(g[i] * w[i], a[i] * by, sums[1]);
+                    sums[1] = __builtin_fmaf(g[i] * w[i] * slope, a[i] * by, sums[1]);
                 }
             }
             row_sums(sums, p.waves, room);
         };
-        add(1.0f, s[turn]);
-        float by = 1.0f, eps = p.eps;
-        if (!(sums[0] < __builtin_inff())) {                  // the same in the whole row
-            if (p.waves > 1) __syncthreads();                 // (for the third piece of LDS)
+        add(1.0f, 1.0f, s[turn]);
+        // The rest of a row from its sums; with `large`, the sum of products is times down^2, and those beside its mean are times down.
+        auto finish = [&](auto large, float by, float eps, float down) {
+            const float up = 1.0f / down, r = norm_factor(sums[0], p.n, eps), r_by = r * by, r_up = r * (by * up);
+            const float mean = __fdiv_rn(sums[1], static_cast<float>(p.n)) * r * up;          // of g u
+#pragma unroll
+            for (u32 c = 0; c < CH; ++c) {
+                const i64 k = k0 + c * kWaveCols;
+                if (k - lane * kLaneCols >= p.n) break;       // the same in the wavefront
+                float a[8], g[8], w[8], d[8];
+                R::unpack(h[c], a);
+                R::unpack(dy[c], g);
+                R::unpack(ds[c], d);
+                weights(c, w);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float u = a[i] * r_by, gw = g[i] * w[i];
+                    dw[c][i] = __builtin_fmaf(g[i], u, dw[c][i]);
+                    a[i] = __builtin_fmaf(__builtin_fmaf(-u, mean, decltype(large)::value ? gw * down : gw), r_up, d[i]);
+                }
+                if (p.dx) store8<VEC>(p.dx + static_cast<i64>(row) * p.lddx, k, p.n, pack8<R>(a));
+                if (p.q) {
+                    float scale;
+                    store8_codes(p.q + static_cast<i64>(row) * p.ldq, k, p.n, block_codes<false>(a, &scale));
+                    if ((lane & 15u) == 0 && k < p.n) p.scale[static_cast<i64>(row) * p.lds + k / kFp8Block] = scale;
+                }
+            }
+        };
+        if (sums[0] < __builtin_inff() && __builtin_fabsf(sums[1]) < __builtin_inff()) {          // the same in the whole row
+            finish(std::false_type{}, 1.0f, p.eps, 1.0f);
+            continue;
+        }
+        float by = 1.0f, eps = p.eps, down = 1.0f;
+        if (!(sums[0] < __builtin_inff())) {
             by = kLargeHalf * kLargeHalf;
             eps = eps * by * by;
-            add(by, s[2]);
+            if (p.waves > 1) __syncthreads();                 // (for the third piece of LDS)
+            add(by, 1.0f, s[2]);
         }
-        const float r = norm_factor(sums[0], p.n, eps), r_by = r * by;
-        const float mean = __fdiv_rn(sums[1], static_cast<float>(p.n)) * r;          // of g u
-#pragma unroll
-        for (u32 c = 0; c < CH; ++c) {
-            const i64 k = k0 + c * kWaveCols;
-            if (k - lane * kLaneCols >= p.n) break;           // the same in the wavefront
-            float a[8], g[8], w[8], d[8];
-            R::unpack(h[c], a);
-            R::unpack(dy[c], g);
-            R::unpack(ds[c], d);
-            weights(c, w);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float u = a[i] * r_by;
-                dw[c][i] = __builtin_fmaf(g[i], u, dw[c][i]);
-                a[i] = __builtin_fmaf(__builtin_fmaf(-u, mean, g[i] * w[i]), r_by, d[i]);
-            }
-            if (p.dx) store8<VEC>(p.dx + static_cast<i64>(row) * p.lddx, k, p.n, pack8<R>(a));
-            if (p.q) {
-                float scale;
-                store8_codes(p.q + static_cast<i64>(row) * p.ldq, k, p.n, block_codes<false>(a, &scale));
-                if ((lane & 15u) == 0 && k < p.n) p.scale[static_cast<i64>(row) * p.lds + k / kFp8Block] = scale;
-            }
+        if (!(__builtin_fabsf(sums[1]) < __builtin_inff())) {
+            down = kLargeSlope;
+            if (p.waves > 1) __syncthreads();
+            add(by, down * down, s[2]);
         }
+        finish(std::true_type{}, by, eps, down);
     }
     if (!p.part) return;
     if (p.waves == 1) {                                       // the wavefronts' sums, in order

@@ -81,3 +81,22 @@ def test_a_large_eps_beside_large_rows():
     for eps in (1e20, 3e38):
         check_forward(h, w, eps)
         check_backward(h, torch.randn(7, 1000, device=DEV, generator=g).to(B16), w, None, eps)
+
+
+@pytest.mark.parametrize("weight_type", [torch.float32, B16])
+@pytest.mark.parametrize("pad", [0, 3])
+@pytest.mark.parametrize("n", WIDTHS)
+def test_products_of_h_and_its_gradient_beyond_the_range(n, pad, weight_type):
+    """The sum of dy * weight * h leaves binary32 where neither the squares nor dy * weight do, and where the squares do as well."""
+    g = torch.Generator(DEV).manual_seed(n)
+    h = torch.randn(7, n, device=DEV, generator=g)
+    dy = torch.randn(7, n, device=DEV, generator=g)
+    # rows 1 and 2: products beyond the range; 3: their sum alone, since dy follows h; 4 and 5: squares too; 6: one product of many
+    dy[3] = h[3]
+    size = torch.tensor([[0, 0], [50, 86], [60, 100], [0, 115], [120, 70], [100, 110], [0, 60]], device=DEV)
+    h, dy = h * 2.0 ** size[:, :1], dy * 2.0 ** size[:, 1:]
+    h[6, n // 2], dy[6, n // 2] = 2.0 ** 62, 2.0 ** 80
+    h, dy = h.to(B16), dy.to(B16)
+    w = (1 + 0.3 * torch.randn(n, device=DEV, generator=g)).to(weight_type)
+    for dsum in (None, torch.randn(7, n, device=DEV, generator=g).to(B16)):
+        check_backward(rows_of(h, pad)[0], rows_of(dy, pad)[0], w, dsum, 1e-6)
