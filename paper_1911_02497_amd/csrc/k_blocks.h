@@ -405,6 +405,13 @@ __device__ inline void row_sums(float (&x)[N], u32 waves, float* s) {
 // such values, and 1 / sqrt(mean of h^2 + eps) itself is that times half * half.  2^-72: 32768 squares of the largest value, 2^112 then, sum up to 2^127, and the mean of a row that needs
 // it is 2^-31 or more.  Half of the factor goes to the values and half to the rest where h is multiplied by the weight, so that neither leaves the range for the other's sake.
 constexpr float kLargeHalf = 0x1p-36f;
+// Squares below binary32's normal range lose bits, up to 2^-150 each. That matters where both their sum and eps are below 2^-100; such values, of up to 2^-50, are taken times 2^64.
+constexpr float kSmall = 0x1p-100f, kSmallHalf = 0x1p32f;
+__device__ inline bool squares_in_range(float squares, float eps) {              // neither below what counts, nor infinite or NaN, in one comparison
+    const u32 least = eps < kSmall ? __float_as_uint(kSmall) : 0u;
+    return __float_as_uint(squares) - least < 0x7F800000u - least;
+}
+__device__ inline float half_for(float squares) { return squares < kSmall ? kSmallHalf : kLargeHalf; }          // (of NaN: any)
 // The same for sums of (dy weight) h, whose mean is in range wherever the products dy weight are: those are taken times kLargeSlope^2 for the sum (2^48 at most beside values of up to
 // 2^64: 32768 products sum up to 2^127) and times kLargeSlope beside their mean, with the other half in the factor that follows.
 constexpr float kLargeSlope = 0x1p-40f;
@@ -467,8 +474,8 @@ __global__ __launch_bounds__(64 * kNormWaves) void k_rms_norm(NormArgs p) {
     float squares[1] = {squares_of(1.0f)};
     row_sums(squares, p.waves, s[0]);
     float half = 1.0f, eps = p.eps;
-    if (!(squares[0] < __builtin_inff())) {                   // the same in the whole row
-        half = kLargeHalf;
+    if (!squares_in_range(squares[0], eps)) {                 // the same in the whole row
+        half = half_for(squares[0]);
         const float by = half * half;
         eps = eps * by * by;
         squares[0] = squares_of(by);
@@ -605,13 +612,13 @@ __global__ __launch_bounds__(64 * kNormWaves) void k_rms_norm_grad(NormGradArgs 
                 }
             }
         };
-        if (sums[0] < __builtin_inff() && __builtin_fabsf(sums[1]) < __builtin_inff()) {          // the same in the whole row
+        if (__builtin_expect(squares_in_range(sums[0], p.eps) && __builtin_fabsf(sums[1]) < __builtin_inff(), 1)) {          // the same in the whole row
             finish(std::false_type{}, 1.0f, p.eps, 1.0f);
             continue;
         }
         float by = 1.0f, eps = p.eps, down = 1.0f;
-        if (!(sums[0] < __builtin_inff())) {
-            by = kLargeHalf * kLargeHalf;
+        if (!squares_in_range(sums[0], eps)) {
+            by = half_for(sums[0]) * half_for(sums[0]);
             eps = eps * by * by;
             if (p.waves > 1) __syncthreads();                 // (for the third piece of LDS)
             add(by, 1.0f, s[2]);

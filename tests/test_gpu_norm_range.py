@@ -48,8 +48,10 @@ def check_forward(h, w, eps):
     out = P.condensa_rms_norm(h, w, eps=eps, y=True, codes=True)
     h, w = h.cpu().double(), w.cpu().double()
     want = h / factor(h, eps) * w
-    assert bool(((out["y"].cpu().double() - want).abs() <= (2.0 ** -8 + SUMS) * want.abs() + 2.0 ** -133).all())
-    check_codes(out["codes"], want, SUMS * want.abs())
+    # h * weight below 2^-126 is a multiple of 2^-149, so up to 2^-150 off before it is divided: of 2^-133, the least value, that is 2^-17, which is more than SUMS
+    slack = SUMS * want.abs() + 2.0 ** -150 / factor(h, eps)
+    assert bool(((out["y"].cpu().double() - want).abs() <= 2.0 ** -8 * want.abs() + slack + 2.0 ** -133).all())
+    check_codes(out["codes"], want, slack)
 
 
 def check_backward(h, dy, w, dsum, eps):
@@ -100,3 +102,18 @@ def test_products_of_h_and_its_gradient_beyond_the_range(n, pad, weight_type):
     w = (1 + 0.3 * torch.randn(n, device=DEV, generator=g)).to(weight_type)
     for dsum in (None, torch.randn(7, n, device=DEV, generator=g).to(B16)):
         check_backward(rows_of(h, pad)[0], rows_of(dy, pad)[0], w, dsum, 1e-6)
+
+
+@pytest.mark.parametrize("weight_type", [torch.float32, B16])
+@pytest.mark.parametrize("pad", [0, 3])
+@pytest.mark.parametrize("n", WIDTHS)
+def test_squares_below_the_range(n, pad, weight_type):
+    """h of 2^-74 and an eps of as little as a square of it: neither is lost."""
+    g = torch.Generator(DEV).manual_seed(n)
+    h = torch.randn(5, n, device=DEV, generator=g) * 2.0 ** torch.tensor([-74.0, -70.0, -60.0, -40.0, -133.0], device=DEV)[:, None]
+    h = rows_of(h.to(B16), pad)[0]
+    w = (1 + 0.3 * torch.randn(n, device=DEV, generator=g)).to(weight_type)
+    dy = torch.randn(5, n, device=DEV, generator=g).to(B16)
+    for eps in (1e-44, 1e-40, 1e-30):
+        check_forward(h, w, eps)
+        check_backward(h, dy, w, None, eps)
