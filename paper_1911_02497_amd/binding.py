@@ -315,11 +315,20 @@ def _cfg(config):
     return ctypes.byref(config)
 
 
+def _room(workspace, index):
+    """(address, bytes) of a workspace that the caller keeps, which has to lie on the device of that index: the library sees an address and a size alone."""
+    if not (workspace.get_device() == index and workspace.is_contiguous()):
+        raise TypeError(f"workspace: a contiguous tensor on cuda:{index}")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
 def _workspace(op, total, n_struct, n_tensors, n_dens, scope, device, workspace=None, config=None):
     import torch
     need = int(library().condensa_workspace_bytes(op, total, n_struct, n_tensors, n_dens, scope, _cfg(config)))
     if workspace is None:
         workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=device)
+    else:
+        _room(workspace, torch.cuda.current_device() if device.index is None else device.index)
     return workspace, need
 
 
@@ -954,8 +963,8 @@ def condensa_adapter_project(x, w, table: AdapterTable, token_adapter, y=None, z
     pz, ldz = (None, 0) if z is None else _kept_z(z, table, T)
     if workspace is None:
         workspace = _made_for(table, stream, adapter_workspace, table, T)
-    _run(table, table.keep_for(stream), library().condensa_adapter_project, table.ref, px, ldx, T, pw, ldw, ids, py, ldy, pz, ldz, workspace.data_ptr(),
-         workspace.numel())
+    pws, size = _room(workspace, table.index)
+    _run(table, table.keep_for(stream), library().condensa_adapter_project, table.ref, px, ldx, T, pw, ldw, ids, py, ldy, pz, ldz, pws, size)
     return {"y": y, "z": z, "workspace": workspace}
 
 
@@ -973,8 +982,9 @@ def condensa_adapter_project_backward(dy, x, w, table: AdapterTable, token_adapt
     pdx, lddx = (None, 0) if dx is False else _rows("dx", dx, table, T, table.n_in)
     if workspace is None:
         workspace = _made_for(table, stream, adapter_workspace, table, T, backward=True)
+    pws, size = _room(workspace, table.index)
     _run(table, table.keep_for(stream), library().condensa_adapter_project_backward, table.ref, pdy, lddy, px, ldx, T, pw, ldw, ids, pz, ldz, pdx, lddx,
-         workspace.data_ptr(), workspace.numel())
+         pws, size)
     return {"dx": None if dx is False else dx, "grads": table.grads, "workspace": workspace}
 
 
@@ -1183,13 +1193,13 @@ def condensa_rms_norm_backward(dy, h, weight, dsum=None, eps=1e-6, dx=True, dwei
         dweight = _made_for(place, stream, _float_values, n, place.device)
     elif dweight is False:
         dweight = None
-    pdw = 0
+    pdw, pws, size = 0, None, 0
     if dweight is not None:
         if not (dweight.shape == (n,) and _types().get(dweight.dtype) == TYPE_F32 and dweight.get_device() == place.index and dweight.is_contiguous()):
             raise TypeError(f"dweight: {n} contiguous float32 on {place.device}")
         if workspace is None:
             workspace = _made_for(place, stream, rms_norm_workspace, T, n, place.device)
-        pdw = dweight.data_ptr()
+        pdw, (pws, size) = dweight.data_ptr(), _room(workspace, place.index)
     codes = _codes_for(codes, place, stream, T, n)
     pdy, lddy = _like("dy", dy, shape, dtype, place)
     ph, ldh = _like("h", h, shape, dtype, place)
@@ -1197,7 +1207,6 @@ def condensa_rms_norm_backward(dy, h, weight, dsum=None, eps=1e-6, dx=True, dwei
     pdx, lddx = _like("dx", dx, shape, dtype, place)
     pw, wt = _norm_weight(weight, place, dtype, n)
     call = _NORM_GRAD_CALL.pack(pdy, ph, ps, pw, pdx, pdw, 0 if codes is None else codes.address, T, n, lddy, ldh, lds, lddx, _types()[dtype], wt, eps, 0)
-    pws, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
     _run(place, stream, library().condensa_rms_norm_backward, call, pws, size)
     return {"dx": dx, "dweight": dweight, "codes": codes, "workspace": workspace}
 
@@ -1225,7 +1234,7 @@ def _product(entry, x, w, out, width, dtype, workspace, stream, backward):
     p, ld = _operand("the product", out, place, out.dtype, x.rows, width)
     if workspace is None:
         workspace = _made_for(place, stream, project_fp8_workspace, w, x.rows, backward)
-    _run(place, stream, entry, x.ref, w.ref, p, ld, kind, workspace.data_ptr(), workspace.numel())
+    _run(place, stream, entry, x.ref, w.ref, p, ld, kind, *_room(workspace, w.index))
     return out, workspace
 
 
