@@ -27,8 +27,8 @@ static ProductPlan make_plan(i64 T, i64 n_out, i64 n_sum, bool along) {
     p.splits = (steps + p.steps_each - 1) / p.steps_each;
     return p;
 }
-// Rows that are 16-byte aligned.
-static bool rows16(const void* p, i64 stride) { return aligned_to(p, 16) && stride % 16 == 0; }
+// Rows that are 16-byte aligned; the distance to the next one does not matter where there is none.
+static bool rows16(const void* p, i64 stride, i64 rows) { return aligned_to(p, 16) && (stride % 16 == 0 || rows == 1); }
 // Rows of a length that is no multiple of sixteen, one behind the other, are copied to aligned ones where tiles are more than the units or sums are long: 1333 tokens 2600 -> 650 (231
 // tiles, 21 steps) 18.5 us with the copies and 24.6 as they are; 300 tokens 1003 -> 1999 (160 tiles, 8 steps), 12.8, gain nothing.  Rows of another length that lie at odd addresses
 // are read as they are.
@@ -36,7 +36,7 @@ static i64 copied_width(i64 cols) { return (cols + 15) / 16 * 16; }
 constexpr i64 kCopySum = 1024;
 constexpr u64 kCopyTiles = 256, kCopyBytes = static_cast<u64>(1) << 34;                 // a launch's worth of copies, at most
 static u64 bytes_of_copy(i64 rows, i64 cols) { return static_cast<u64>(rows) * copied_width(cols); }
-static bool copies(const condensa_fp8_matrix* m) { return m->cols % 16 != 0 && !rows16(m->q, m->q_stride) && bytes_of_copy(m->rows, m->cols) <= kCopyBytes; }
+static bool copies(const condensa_fp8_matrix* m) { return m->cols % 16 != 0 && !rows16(m->q, m->q_stride, m->rows) && bytes_of_copy(m->rows, m->cols) <= kCopyBytes; }
 
 // What a call with T tokens and every call with fewer can do with: the most parts, of these tokens or of as many tiles as have any, and copies of x and of W.
 static size_t part_bytes(i64 T, i64 n_out) { return align_up(kMostSplits * std::min(static_cast<u64>(T) * n_out, kSplitTiles * 64 * 64) * 4); }
@@ -165,7 +165,7 @@ static condensa_status product(const condensa_fp8_matrix* x, const condensa_fp8_
         CONDENSA_LAUNCH_CHECK();
         return CONDENSA_OK;
     }
-    const bool x16 = rows16(a.x, a.ldx), w16 = rows16(a.w, a.ldw);
+    const bool x16 = rows16(a.x, a.ldx, T), w16 = rows16(a.w, a.ldw, w->rows);
     if ((static_cast<u64>((T + 63) / 64) * ((n_out + 63) / 64) > kCopyTiles || n_sum > kCopySum) && !(x16 && w16) && (x16 || copies(x)) && (w16 || copies(w))) {
         CopyArgs c{};
         char* to = static_cast<char*>(workspace) + part_bytes(T, n_out);
@@ -177,7 +177,7 @@ static condensa_status product(const condensa_fp8_matrix* x, const condensa_fp8_
         hipLaunchKernelGGL(k_product_copy, dim3(c.m[0].blocks + c.m[1].blocks), dim3(256), 0, st, c);
         CONDENSA_LAUNCH_CHECK();
     }
-    const bool fast = rows16(a.x, a.ldx) && rows16(a.w, a.ldw);
+    const bool fast = rows16(a.x, a.ldx, T) && rows16(a.w, a.ldw, w->rows);
     rc = along ? launch_product<true>(a, fast, st) : launch_product<false>(a, fast, st);
     if (rc != CONDENSA_OK) return rc;
     if (a.part) {
