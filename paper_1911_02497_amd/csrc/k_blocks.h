@@ -180,9 +180,8 @@ __device__ inline u32 codes4(const float* x, const BlockBy& b) {
 }
 __device__ inline u32x2 codes8(const float (&x)[8], const BlockBy& b) { return u32x2{codes4(x, b), codes4(x + 4, b)}; }
 
-// The same for finite values (or NaN) whose largest is between 2^-100 and 2^100, without what then remains: exact where x 448 is, for significands of up to 21 bits, since a
-// quotient of two such values is the middle of two codes or not within a unit of it.  A third of the instructions.  Longer values are within a unit and a half of the
-// exact quotient before they become codes: no more than what a norm's sums leave open (8192 x 4608 gradients: 76 us with this, 82 with the next one).
+// The same for finite values (or NaN) whose largest is between 2^-100 and 2^100, without what then remains: exact for significands of up to 18 bits, where x 448 is exact and a quotient
+// is the middle of two codes (of five bits, so that its product with the largest has 23) or 2^-23 away from it.  A third of the instructions.
 __device__ inline u32x2 codes8_plain(const float (&x)[8], const BlockBy& b) {
     const float down = b.by * (1.0f / 448.0f);
     float q[8];
@@ -201,28 +200,23 @@ __device__ inline u32x2 codes8_plain(const float (&x)[8], const BlockBy& b) {
 }
 __device__ inline bool plain_range(float top) { return top >= 0x1p-100f && top <= 0x1p100f; }
 
-// The same for longer significands: the product with the reciprocal decides where it is three units or more from the middle of two codes, which it nearly always is (of
-// what is below the smallest normal code that is not looked at); a wavefront that has another case takes the long way.
+// The same for longer significands: products with the reciprocal 2^-22 down and up.  Reciprocal, border and product are each rounded, by 2^-24 at most, so the exact quotient lies between the
+// two products; where both have the same code, that is its code.  A wavefront that has another case, a quotient within a few units of the middle of two codes, takes the long way.
 __device__ inline u32x2 codes8_long(const float (&x)[8], const BlockBy& b) {
-    float q[8];
-    u32 near = ~0u, small = ~0u;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        q[k] = x[k] * b.by;
-        const u32 size = __float_as_uint(q[k]) & 0x7FFFFFFFu, from = (size - 0x7FFFDu) & 0xFFFFFu;         // a code keeps 20 bits less than binary32
-        near = near < from ? near : from;
-        small = small < size - 1 ? small : size - 1;          // zero is no case
-    }
-    if (__any(near <= 6u || small < 0x3C800000u - 1)) return codes8(x, b);
+    const float low = __builtin_fmaf(b.by, -0x1p-22f, b.by), high = __builtin_fmaf(b.by, 0x1p-22f, b.by);
     u32x2 t;
+    u32 differ = 0;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        const int p = __builtin_amdgcn_cvt_pk_fp8_f32(q[4 * h], q[4 * h + 1], 0, false);
-        t[h] = static_cast<u32>(__builtin_amdgcn_cvt_pk_fp8_f32(q[4 * h + 2], q[4 * h + 3], p, true));
+        const float* v = x + 4 * h;
+        const int p = __builtin_amdgcn_cvt_pk_fp8_f32(v[0] * low, v[1] * low, 0, false), q = __builtin_amdgcn_cvt_pk_fp8_f32(v[0] * high, v[1] * high, 0, false);
+        t[h] = static_cast<u32>(__builtin_amdgcn_cvt_pk_fp8_f32(v[2] * low, v[3] * low, p, true));
+        differ |= t[h] ^ static_cast<u32>(__builtin_amdgcn_cvt_pk_fp8_f32(v[2] * high, v[3] * high, q, true));
     }
+    if (__builtin_expect(__any(differ != 0), 0)) return codes8(x, b);
     return t;
 }
-// LONG: values have more than 21 bits and are themselves what is asked for.
+// LONG: values have more than 18 bits.
 template <bool LONG>
 __device__ inline u32x2 codes8_in_range(const float (&x)[8], const BlockBy& b) { return LONG ? codes8_long(x, b) : codes8_plain(x, b); }
 
@@ -418,11 +412,12 @@ constexpr float kLargeSlope = 0x1p-40f;
 __device__ inline float norm_factor(float squares, u32 n, float eps) { return __fdiv_rn(1.0f, __fsqrt_rn(__fdiv_rn(squares, static_cast<float>(n)) + eps)); }
 
 // Codes of y r and their scale, from values y whose own range is in hand: r cancels in what a code is made of, so codes are those of products of h and the weight.
+template <bool LONG>
 __device__ inline u32x2 scaled_codes(const float (&y)[8], float r, float* scale) {
     const float top = largest_of16(largest8(y)), top_r = top * r;
     if (__all((plain_range(top) && plain_range(top_r)) || (top == 0.0f && top_r == 0.0f))) {        // (a row of NaN goes the other way)
         *scale = __fdiv_rn(top_r, 448.0f);
-        return codes8_plain(y, block_by(top));
+        return codes8_in_range<LONG>(y, block_by(top));
     }
     float v[8];
 #pragma unroll
@@ -434,6 +429,7 @@ __device__ inline u32x2 scaled_codes(const float (&y)[8], float r, float* scale)
 // codes 50 us, 5.3 TB/s; 51.5 with half as many columns a wavefront, 88 with one wavefront a row, which has too few loads under way.
 template <typename R, typename W, u32 CH, bool VEC>
 __global__ __launch_bounds__(64 * kNormWaves) void k_rms_norm(NormArgs p) {
+    constexpr bool kLong = sizeof(typename W::elem) == 4 || std::is_same<R, RowsF16>::value;              // products of 16 bits where both are bfloat16, of 22 and more elsewhere
     __shared__ float s[2][kNormWaves];
     const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6, per = (blockDim.x >> 6) / p.waves;        // rows of a workgroup: one where a row has several wavefronts
     const u32 row = blockIdx.x * per + wave / p.waves, part = wave % p.waves;
@@ -497,7 +493,7 @@ __global__ __launch_bounds__(64 * kNormWaves) void k_rms_norm(NormArgs p) {
         for (int i = 0; i < 8; ++i) a[i] = a[i] * half * w[c][i];
         if (p.q) {
             float scale;
-            store8_codes(p.q + static_cast<i64>(row) * p.ldq, k, p.n, scaled_codes(a, r, &scale));
+            store8_codes(p.q + static_cast<i64>(row) * p.ldq, k, p.n, scaled_codes<kLong>(a, r, &scale));
             if ((lane & 15u) == 0 && k < p.n) p.scale[static_cast<i64>(row) * p.lds + k / kFp8Block] = scale;
         }
         if (p.y) {
@@ -607,7 +603,7 @@ __global__ __launch_bounds__(64 * kNormWaves) void k_rms_norm_grad(NormGradArgs 
                 if (p.dx) store8<VEC>(p.dx + static_cast<i64>(row) * p.lddx, k, p.n, pack8<R>(a));
                 if (p.q) {
                     float scale;
-                    store8_codes(p.q + static_cast<i64>(row) * p.ldq, k, p.n, block_codes<false>(a, &scale));
+                    store8_codes(p.q + static_cast<i64>(row) * p.ldq, k, p.n, block_codes<true>(a, &scale));
                     if ((lane & 15u) == 0 && k < p.n) p.scale[static_cast<i64>(row) * p.lds + k / kFp8Block] = scale;
                 }
             }

@@ -73,3 +73,55 @@ def test_weight_gradient_in_the_order_of_its_sums(T, n):
     got = P.condensa_rms_norm_backward(dy, h, w, eps=1e-5)["dweight"].cpu().double()
     _, _, want, size = norm_gradients(h, dy, w, None, float(torch.tensor(1e-5)))
     assert bool(((got - want).abs() <= 100 * H * size).all()), float(((got - want).abs() / size).max() / H)
+
+
+def blocks_of(top):
+    """Candidates in blocks of one row, the largest value first in each."""
+    x = candidates(top)
+    row = torch.zeros(-(-len(x) // 127), 128)
+    row[:, 0] = top
+    row[:, 1:] = torch.nn.functional.pad(x, (0, -len(x) % 127)).view(-1, 127)
+    return row.view(1, -1)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("top", [top for top, _ in TOPS])
+def test_ties_in_a_gradient(top, dtype):
+    """Where h is zero, dy and eps are one, the gradient is the weight."""
+    w = blocks_of(top)
+    n = w.shape[1]
+    for T in (1, 3):
+        dy, h = torch.ones(T, n, device=DEV, dtype=dtype), torch.zeros(T, n, device=DEV, dtype=dtype)
+        m = P.condensa_rms_norm_backward(dy, h, w[0].to(DEV), eps=1.0, dx=False, dweight=False, codes=True)["codes"]
+        code, scale = definition(w, 1)
+        assert same(values(m), code.expand(T, n)) and torch.equal(m.scale.cpu(), scale.expand(T, n // 128))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("top", [top for top, _ in TOPS if 2.0 ** -99 <= top <= 2.0 ** 100])
+def test_ties_in_a_norm(top, dtype):
+    """Where h is one, codes are those of the weight, whatever the row's factor is."""
+    w = blocks_of(top)
+    for T in (1, 5):
+        m = P.condensa_rms_norm(torch.ones(T, w.shape[1], device=DEV, dtype=dtype), w[0].to(DEV), eps=0.3, codes=True)["codes"]
+        assert same(values(m), definition(w, 1)[0].expand(T, w.shape[1]))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_products_of_16_bits_next_to_a_tie(dtype):
+    """Rows of h whose products with the weight have a quotient within 2^-24 of the middle of two codes, but not on it, or on it: found among many, since they cannot be made."""
+    g = torch.Generator(DEV).manual_seed(5)
+    w = (1 + 0.3 * torch.randn(128, device=DEV, generator=g)).to(dtype)
+    m = middles().to(DEV)
+    found = []
+    for _ in range(8):
+        h = torch.randn(100000, 128, device=DEV, generator=g).to(dtype)
+        y = h.double() * w.double()                                      # exact, and in binary32 as well
+        q = (y * 448 / y.abs().amax(1, keepdim=True)).abs()
+        at = torch.bucketize(q, m).clamp(max=len(m) - 1)
+        near = torch.minimum((m[at] - q).abs(), (m[(at - 1).clamp(min=0)] - q).abs()) <= q * 2.0 ** -24
+        found.append(h[near.any(1)])
+    h = torch.cat(found)[:20000]
+    assert len(h) >= 100
+    codes = P.condensa_rms_norm(h, w, codes=True)["codes"]
+    assert same(values(codes), definition(h.double() * w.double(), 1)[0])
