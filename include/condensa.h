@@ -578,8 +578,8 @@ condensa_status condensa_dequantize_fp8_blocks(const condensa_fp8_matrix* m, voi
 /*
  * Root-mean-square norm with the residual's addition, answered in 16 bits, in codes, or both.  For every token (row)
  *   h = x + residual, rounded to the 16-bit type (h = x without a residual);   y = h * weight / sqrt(mean of h^2 + eps)
- * and the codes are those of y in binary32, one scale for 128 columns.  Sums are binary32 in an order that depends on width and n_tokens alone.
- * Squares outside the range of binary32 do not matter; products h * weight (and dy * weight below) outside of it become infinite or zero.  `sum` receives h; it may be `residual` or `x` itself (the same address and stride).
+ * and the codes are those of y in binary32, one scale for 128 columns, made from products h * weight, in which the row's factor cancels.  Sums are binary32 in an order that depends on width and n_tokens alone.
+ * Squares outside the range of binary32, above it or below, do not matter, nor do sums of (dy * weight) * h above it; products h * weight (and dy * weight below) become infinite above it and lose bits below it.  `sum` receives h; it may be `residual` or `x` itself (the same address and stride).
  * n_tokens 0..2^24 (and fewer than 2^26 wavefronts of 1024 columns: CONDENSA_ERR_SIZE), width 1..CONDENSA_MAX_NORM_WIDTH, strides in elements, up to 2^22; x, residual, sum and y of `type` (CONDENSA_TYPE_F16 or
  * _BF16), weight of weight_type (that one, or CONDENSA_TYPE_F32).  One launch, no workspace.
  */
@@ -633,7 +633,7 @@ condensa_status condensa_rms_norm_backward(const condensa_rms_norm_grad_call* ca
  * after are binary32 (the product of two scales included, which overflows and underflows as such), in an order that depends on the sizes and on how rows lie alone: equal calls give equal bits.  (Of random codes that is a sixtieth of a rounding
  * to bfloat16, on the mean.)  NaN codes reach their own token's outputs and those of their own row or column of W alone.
  * n_tokens as the adapters' (CONDENSA_ERR_SIZE); row strides of y and dx up to 2^22.  Workspace for calls with n_tokens tokens or
- * fewer, 256-byte aligned; the two directions differ.
+ * fewer, 256-byte aligned; the two directions differ.  It has room for a copy of x where the summed axis is no multiple of 16, also for calls whose x turns out to be aligned.
  */
 size_t condensa_project_fp8_workspace_bytes(const condensa_fp8_matrix* w, int64_t n_tokens, int backward);        /* 0: invalid arguments */
 condensa_status condensa_project_fp8(const condensa_fp8_matrix* x, const condensa_fp8_matrix* w, uint16_t* y_dev, int64_t y_stride, int type,

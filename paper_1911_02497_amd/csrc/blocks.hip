@@ -69,8 +69,8 @@ static RowShare share_row(i64 width, u32 least_each) {
 }
 static_assert(CONDENSA_MAX_NORM_WIDTH == kNormWaves * kWaveCols * 4, "the widest row: four pieces a wavefront");
 
-// Workgroups that share the rows of a backward pass: one a unit for wide rows, more for narrow ones, and rows enough for each that its part of the weight's gradient
-// is small beside them.  8192 tokens of 4608, us with 256, 512 and 1024: 72, 77 and 78, and 2.7, 3.5 and 5.0 to add the parts up.
+// Workgroups that share the rows of a backward pass: 256, one a unit, for rows of eight wavefronts and more and for rows of one, of which a workgroup has eight at once; up to 1024 for those
+// between; fewer for few tokens, so that each has rows enough and its part of the weight's gradient is small beside them.  8192 tokens of 4608, us with 256, 512 and 1024: 72, 77 and 78, and 2.7, 3.5 and 5.0 to add the parts up.
 static u32 grad_groups(i64 n_tokens, i64 width) {
     const u32 waves = share_row(width, 1).waves;
     const u32 slots = waves == 1 ? kNormSlots : 1, most = 256 * (waves >= 8 || waves == 1 ? 1 : 8 / waves);

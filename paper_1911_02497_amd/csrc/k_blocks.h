@@ -245,7 +245,7 @@ struct BlockArgs {
     u32 block_rows;
 };
 
-// A wavefront takes 512 columns of a row.  4096 x 4608 of binary32: 17 us, 5.5 TB/s.
+// A wavefront takes 512 columns of a row.  4096 x 4608 of binary32: 18.7 us, 5.0 TB/s.
 template <typename R, bool VEC>
 __global__ __launch_bounds__(256) void k_block_encode_rows(BlockArgs p) {
     const u64 item = static_cast<u64>(blockIdx.x) * 4 + (threadIdx.x >> 6);
@@ -262,8 +262,8 @@ __global__ __launch_bounds__(256) void k_block_encode_rows(BlockArgs p) {
 
 constexpr u32 kSquareWaves = 8;
 
-// A workgroup takes a block of 128 x 128, 32 rows at a time, and keeps it in registers between looking for its largest and making codes of it.  4096 x 4608 of binary32: 18.7 us,
-// 5.0 TB/s; with half the wavefronts, which keep twice as much each, 19.9; with more of them a unit, whose registers spill, 29.
+// A workgroup takes a block of 128 x 128, 32 rows at a time, and keeps it in registers between looking for its largest and making codes of it.  4096 x 4608 of binary32: 19.0 to 19.8 us
+// by card, 4.9 TB/s; with half the wavefronts, which keep twice as much each, 1.2 us more; with more of them a unit, whose registers spill, 10 more.
 template <typename R, bool VEC>
 __global__ __launch_bounds__(64 * kSquareWaves, 4) void k_block_encode_squares(BlockArgs p) {
     __shared__ float s_top[2][kSquareWaves];
@@ -306,7 +306,7 @@ __device__ inline void decode4(u32 c, float s, float* v) {
 }
 
 // A wavefront takes 512 columns of a row: eight neighbours a lane, or, where they leave as binary32, twice four, so that each store is contiguous across the wavefront
-// and need not stay in the caches.  4096 x 4608 to binary32: 14.7 us, 6.4 TB/s; eight neighbours a lane 20.3, stores that are kept 17.9.
+// and need not stay in the caches.  4096 x 4608 to binary32: 14.9 us, 6.4 TB/s; eight neighbours a lane 20.3, stores that are kept 17.9.
 template <typename R, bool VEC>
 __global__ __launch_bounds__(256) void k_block_decode(BlockArgs p) {
     const u64 item = static_cast<u64>(blockIdx.x) * 4 + (threadIdx.x >> 6);
@@ -425,7 +425,8 @@ __device__ inline u32x2 scaled_codes(const float (&y)[8], float r, float* scale)
     return block_codes<true>(v, scale);
 }
 
-// Rows of 512 CH columns a wavefront; they stay in registers between the sum of squares and the outputs.  Reading x and the residual and writing their sum bounds it: 8192 x 4608 with
+// Rows of 512 CH columns a wavefront; they stay in registers between the sum of squares and the outputs.  Without VEC each piece waits for what is under way before it looks at the end of its row,
+// so x and the residual come one after the other: 1333 x 650 takes 6.4 us, its bytes 1.3.  Elsewhere reading x and the residual and writing their sum bounds it: 8192 x 4608 with
 // codes 50 us, 5.3 TB/s; 51.5 with half as many columns a wavefront, 88 with one wavefront a row, which has too few loads under way.
 template <typename R, typename W, u32 CH, bool VEC>
 __global__ __launch_bounds__(64 * kNormWaves) void k_rms_norm(NormArgs p) {
@@ -521,8 +522,9 @@ struct NormGradArgs {
 };
 
 // Where a row is one wavefront, a workgroup's wavefronts have rows of their own; else it takes rows in turn.  Its lanes keep their columns of the weight's gradient.  Where a wavefront
-// has 512 columns the next row's values are on their way while one row is worked on, and the weight stays in registers; with 1024 and more there are none left for that.
-// Reading three operands and writing dx, twice with codes, bounds it: 8192 x 4608 with codes 72 us, 4.7 TB/s, as a copy; without the next row's values under way 82, with 1024 columns
+// has 512 columns the next row's values are on their way while one row is worked on, and the weight stays in registers; with 1024 and more there are none left for that, and with 2048 (rows of more
+// than 16384) 190 to 380 bytes a lane spill: 2048 x 16384 with codes 72 us, 4.2 TB/s, 1024 x 32768 151 us, 2.0 TB/s.  Without VEC the loads of the next row are waited for where they are made, for
+// the ends of rows: 1333 x 650 takes 7.1 us.  Elsewhere reading three operands and writing dx, twice with codes, bounds it: 8192 x 4608 with codes 73 us, 4.7 TB/s, as a copy; without the next row's values under way 82, with 1024 columns
 // a wavefront 78; two rows between barriers, which spill five registers, take 8 us more.
 template <typename R, typename W, u32 CH, bool VEC>
 __global__ __launch_bounds__(64 * kNormWaves) void k_rms_norm_grad(NormGradArgs p) {

@@ -223,7 +223,7 @@ __global__ __launch_bounds__(256) void k_product_copy(CopyArgs a) {
 // of a step; a token's and W's scales of a step come with it.  (A 16-byte piece may end past its row; it never leaves the sixteen bytes that hold the row's last code.)  Sixteen
 // tokens at a time meet the wavefront's fragments of W, their results are scaled and added while the next sixteen are multiplied, and the fragments of the next step are read beside
 // the last sixteen: wavefronts meet once a step, just before, when the next step has come and the last read of this one is done.
-// 8192 tokens, 4608 -> 4096: 142 to 149 us by card, 2.2 PFLOP/s; backward, in two launches, 156 to 161.  What the time of 256 x 256 goes to, parts left out (150 us on that card): without loads 129, without LDS reads 142,
+// 8192 tokens, 4608 -> 4096: 142 to 152 us by card, 2.0 to 2.2 PFLOP/s; backward, in two launches, 154 to 162.  What the time of 256 x 256 goes to, parts left out (150 us on that card): without loads 129, without LDS reads 142,
 // with a quarter of the additions 139, without all three 109, of which 22 are two rounds of first loads and of outputs, and the rest the matrix instructions.  So none of them
 // bounds it alone: they share a wavefront's issue and meet at its barrier.  Two groups of wavefronts in turns, one multiplying while the other reads LDS, took 150 us where this took 144.
 constexpr u32 product_lds(u32 bm, u32 bn, u32 nb) { return nb * ((bm + bn) * kStep + bm * 4 + 256) + (bm == 256 ? 256 : 0); }
